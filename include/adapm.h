@@ -291,6 +291,136 @@ int adapm_group_meansq(const void* g, int32_t grad_dtype, int64_t n_groups, int6
 int adapm_group_meansq_static(const void* g, int32_t grad_dtype, int64_t n_groups, int64_t group_elems,
                               float* out, adapm_stream stream);
 
+/* ---- Operators around the step -------------------------------------------------------------------------
+ *
+ * What stands between a decoder's last layers and the gradients that adapm_step reads: the dropout of a
+ * branch, the RMS norm with the residual's addition, and the output head's loss over the vocabulary, each
+ * with its gradient.  Their weights are read where the step keeps them (the bf16 copy set by
+ * adapm_set_shadow_params, or params, at the block's offset), and the gradients of those weights are
+ * written, or added, where adapm_step reads them (grads, at the block's offset).
+ *
+ * They need no context.  Every call is asynchronous on `stream`, allocates nothing, never synchronises and
+ * may be captured into a graph.  `stream` must belong to the current device, and every buffer must be memory
+ * of that device: a host pointer or another device's memory is refused with ADAPM_EINVAL.  A `_ld` is the
+ * pitch of a matrix: elements from one row to the next, at least the row's length; what lies between two rows
+ * is neither read nor written.  A scratch buffer is 256-byte aligned, its contents need not be kept or
+ * cleared, and calls that may overlap on the GPU (captured graphs included) need one each.  Unless said
+ * otherwise an output must not overlap an input.  Results do not depend on the run: no sum is made by atomics.
+ */
+enum { ADAPM_TYPE_F32 = 0, ADAPM_TYPE_BF16 = 1 };    /* element types; the numbers of ADAPM_GRAD_*    */
+
+/*
+ * Dropout from a counter-based generator: y = drop(x), or y = residual + drop(x) where `residual` is not
+ * NULL.  x, residual, y: [rows, cols] of `dtype`; y may be x or residual (same pitch).
+ *   drop(x) at (row, col): the (col % 8)-th 16 bits of Philox4x32-10 with key `seed` and the 128-bit counter
+ *   {row * ceil(cols / 8) + col / 8, offset + *step}; below rint(65536 p) the element becomes 0, whatever it
+ *   held (NaN too), otherwise it is multiplied by 1 / (1 - rint(65536 p) / 65536).
+ * The mask is not stored: the gradient of x is the same call on dy (residual NULL) with the same seed, offset,
+ * step and shape.  Give every layer and step its own offset.
+ *   p: 0 <= p <= 1;  step: device word added to the offset, or NULL (a captured graph then draws anew with each
+ *   replay if the program changes the word in between).
+ * Errors: ADAPM_EINVAL, ADAPM_ERANGE (p), ADAPM_EALIGN (a pointer that is no multiple of its element), ADAPM_ECUDA.
+ */
+int adapm_dropout(const void* x, const void* residual, void* y, int32_t dtype, int64_t rows, int64_t cols,
+                  int64_t x_ld, int64_t residual_ld, int64_t y_ld, float p, uint64_t seed, uint64_t offset,
+                  const uint64_t* step, adapm_stream stream);
+
+/*
+ * RMS norm of a residual stream:
+ *   s = residual + drop(x)    rstd = 1 / sqrt(mean(s^2) + eps)    y = s rstd w
+ * Arithmetic in fp32; s enters the statistic and the output unrounded and is rounded where `sum` is stored.
+ */
+typedef struct {
+  int64_t rows, cols;      /* cols: 1 .. 32768                                                       */
+  int64_t x_ld;            /* pitch of x and of its gradient dx                                      */
+  int64_t residual_ld;     /* of residual and dresidual                                              */
+  int64_t sum_ld;          /* of sum and dsum                                                        */
+  int64_t y_ld;            /* of y and dy                                                            */
+  int64_t y8_ld;           /* of y8                                                                  */
+  int32_t dtype;           /* ADAPM_TYPE_*: x, residual, sum, y and their gradients                  */
+  int32_t weight_dtype;    /* ADAPM_TYPE_*: weight [cols]                                            */
+  int32_t q8_group;        /* columns per scale of y8: 0 = one scale per row, or 128                 */
+  float   eps;             /* >= 0                                                                   */
+  float   drop_p;          /* dropout of x as in adapm_dropout; 0 = none                             */
+  uint64_t seed, offset;
+  const uint64_t* step;    /* as in adapm_dropout                                                    */
+} adapm_rmsnorm;
+
+/*
+ *   residual: may be NULL (s = drop(x));  sum: s, may be NULL, may be `residual` or `x` (same pitch);
+ *   y, y8: outputs, either may be NULL.  y8 is y in 8 bits (e4m3): round(y * 448 / m) with m = max |y| over the
+ *   row, or over q8_group columns of it, and y8_scales [rows, ceil(cols / q8_group) or 1] = m / 448 (1 where m is 0);
+ *   rstd [rows]: may be NULL; the backward pass reads it.
+ * Errors: ADAPM_EINVAL, ADAPM_ERANGE, ADAPM_EALIGN, ADAPM_ECUDA.  rows = 0 does nothing.
+ */
+int adapm_rmsnorm_forward(const adapm_rmsnorm* d, const void* x, const void* residual, const void* weight,
+                          void* sum, void* y, void* y8, float* y8_scales, float* rstd, adapm_stream stream);
+
+/*
+ * Gradient of the same norm, from dy (gradient of y) and, where not NULL, dsum (gradient that reaches s by the
+ * residual stream itself).  sum, rstd: what the forward call stored (sum = x where that call had neither residual
+ * nor dropout).
+ *   xh = sum rstd    ds = rstd (dy w - xh mean(dy w xh)) + dsum
+ *   dresidual = ds;  dx = drop(ds), the forward's mask;  dweight = sum over rows of dy xh
+ * Any output may be NULL, but not all.  dx may be dy, dresidual may be dsum or sum (same pitch).  dweight [cols] of
+ * dweight_dtype; `accumulate`: added to what is there.  scratch: only where dweight is wanted.
+ * rows = 0: dweight = 0 (unless accumulate).  Errors as above, and ADAPM_ENOWORKSPACE.
+ */
+size_t adapm_rmsnorm_backward_scratch_bytes(const adapm_rmsnorm* d);
+int adapm_rmsnorm_backward(const adapm_rmsnorm* d, const void* dy, const void* dsum, const void* sum,
+                           const float* rstd, const void* weight, void* dresidual, void* dx, void* dweight,
+                           int32_t dweight_dtype, int32_t accumulate, void* scratch, size_t scratch_bytes,
+                           adapm_stream stream);
+
+/*
+ * Loss of a language model's output head: softmax cross entropy over the vocabulary, from the hidden states and
+ * the head's weight, in pieces of the vocabulary (the logits are never stored, their gradient one piece at a time):
+ *   z = hidden weight^T    lse_t = log sum_v exp z_tv
+ *   loss_t = lse_t - (1 - e) z_t,target - (e / vocab) sum_v z_tv + z_loss lse_t^2        e = label_smoothing
+ * bf16 products with fp32 sums on the tensor cores; the softmax in fp32.
+ */
+typedef struct {
+  int64_t tokens, vocab, hidden;   /* hidden [tokens, hidden], weight [vocab, hidden], both bf16; hidden % 8 == 0      */
+  int64_t hidden_ld;               /* pitch of hidden and dhidden, a multiple of 8                                     */
+  int64_t weight_ld;               /* pitch of weight and dweight, a multiple of 8 (the block's cols in params)        */
+  int64_t ignore_index;            /* target of tokens that are left out                                               */
+  float   label_smoothing;         /* 0 .. 1                                                                           */
+  float   z_loss;                  /* >= 0                                                                             */
+  int32_t dhidden_dtype, dweight_dtype;   /* ADAPM_TYPE_* of the gradients.  F32: the logits' gradient is carried as
+                                      three bf16 numbers (24 bits) into that product, at three times its cost; BF16: it is
+                                      rounded to bf16 once                                                             */
+  int32_t accumulate;              /* 1: dweight is added to what is there (a tied embedding, micro-batches)           */
+} adapm_head_loss;
+
+size_t adapm_head_loss_scratch_bytes(const adapm_head_loss* d, int32_t backward);
+
+/*
+ * targets [tokens]: int64 on the device.  loss, lse [tokens] fp32 outputs.  A token whose target is ignore_index has
+ * loss = lse = 0; one whose target is otherwise outside [0, vocab) has loss = lse = NaN.  The hidden states of both kinds
+ * are not read into any product.  tokens = 0 does nothing.
+ * Errors: ADAPM_EINVAL, ADAPM_EALIGN (16 bytes for matrices, pitches), ADAPM_ERANGE (tokens or vocab above 2^24, hidden above 2^16), ADAPM_EUNSUPPORTED
+ * (hidden % 8), ADAPM_ENOWORKSPACE, ADAPM_ECUDA.
+ */
+int adapm_head_loss_forward(const adapm_head_loss* d, const void* hidden, const void* weight, const int64_t* targets,
+                            float* loss, float* lse, void* scratch, size_t scratch_bytes, adapm_stream stream);
+
+/*
+ * Gradient of sum_t scale * dloss_t * loss_t (dloss NULL: all ones), with the lse of the forward call:
+ *   dhidden [tokens, hidden] (rows of tokens without a valid target are zero), dweight [vocab, hidden].
+ * Either may be NULL.  Needs nothing from the forward call's scratch.  tokens = 0, or no valid target: dweight = 0
+ * (unless accumulate).  Errors as above; ADAPM_EINVAL also where a gradient overlaps an input or the other gradient.
+ */
+int adapm_head_loss_backward(const adapm_head_loss* d, const void* hidden, const void* weight, const int64_t* targets,
+                             const float* lse, const float* dloss, float scale, void* dhidden, void* dweight,
+                             void* scratch, size_t scratch_bytes, adapm_stream stream);
+
+/*
+ * Every wait inside the two calls above is bounded (see the conventions at the top).  If one ran out, the later kernels of
+ * that call do nothing, a forward call leaves NaN in the losses, and this call, which synchronises `stream`, returns
+ * ADAPM_EDEVICE and the status word of the last call that used `scratch` (0: fine; bits 1 to 8 as in adapm_get_status).
+ */
+int adapm_head_loss_status(const void* scratch, adapm_stream stream, int32_t* status);
+
 #ifdef __cplusplus
 }
 #endif

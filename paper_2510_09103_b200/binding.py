@@ -15,6 +15,7 @@ from . import build as _build
 MOM_NONE, MOM_FULL, MOM_LOWRANK = 0, 1, 2
 V_ELEMENT, V_BLOCKMEAN = 0, 1
 GRAD_F32, GRAD_BF16 = 0, 1
+TYPE_F32, TYPE_BF16 = 0, 1
 PATH_AUTO, PATH_SIMT, PATH_TENSOR = 0, 1, 2
 STATE_M, STATE_L, STATE_R, STATE_V = 0, 1, 2, 3
 FLAG_NO_PANEL_TEAMS, FLAG_FORCE_PANEL_TEAMS, FLAG_NO_SUMSQ_FOLD, FLAG_CHECK_FINITE = 1, 2, 4, 8
@@ -28,6 +29,8 @@ EXPORTS = (
     "adapm_group_meansq_scratch_bytes", "adapm_group_meansq", "adapm_set_profiling", "adapm_get_launch_times",
     "adapm_launch_kind_name", "adapm_group_meansq_static", "adapm_state_changed", "adapm_selftest_expired_wait", "adapm_set_shadow_params",
     "adapm_init_omega_floats", "adapm_init_omega_layout", "adapm_state_init_from_grads",
+    "adapm_dropout", "adapm_rmsnorm_forward", "adapm_rmsnorm_backward_scratch_bytes", "adapm_rmsnorm_backward",
+    "adapm_head_loss_scratch_bytes", "adapm_head_loss_forward", "adapm_head_loss_backward", "adapm_head_loss_status",
 )
 
 
@@ -64,6 +67,34 @@ def hparams(lr=1e-3, beta1=0.9, beta2=0.95, eps=1e-8, clip=1.0, inner_iters=5, i
     return adapm_hparams(lr, beta1, beta2, eps, clip, inner_iters, inner_lr_scale, grad_dtype, adam_debias,
                          correction, lowrank_path, seed, flags, max_grad_norm, refresh_period, tune_panels,
                          tune_stage_k, inner_precond, precond_damping)
+
+
+class adapm_rmsnorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("x_ld", C.c_int64), ("residual_ld", C.c_int64),
+                ("sum_ld", C.c_int64), ("y_ld", C.c_int64), ("y8_ld", C.c_int64), ("dtype", C.c_int32),
+                ("weight_dtype", C.c_int32), ("q8_group", C.c_int32), ("eps", C.c_float), ("drop_p", C.c_float),
+                ("seed", C.c_uint64), ("offset", C.c_uint64), ("step", C.c_void_p)]
+
+
+def rmsnorm_desc(rows, cols, dtype=TYPE_BF16, weight_dtype=TYPE_BF16, eps=1e-5, drop_p=0.0, seed=0, offset=0, step=None,
+                 q8_group=0, x_ld=None, residual_ld=None, sum_ld=None, y_ld=None, y8_ld=None) -> adapm_rmsnorm:
+    """Pitches that are not given are `cols`.  `step`: a device tensor of one int64, which the caller keeps alive."""
+    ld = lambda x: cols if x is None else x  # noqa: E731
+    return adapm_rmsnorm(rows, cols, ld(x_ld), ld(residual_ld), ld(sum_ld), ld(y_ld), ld(y8_ld), dtype, weight_dtype, q8_group,
+                         eps, drop_p, seed, offset, _ptr(step))
+
+
+class adapm_head_loss(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("vocab", C.c_int64), ("hidden", C.c_int64), ("hidden_ld", C.c_int64),
+                ("weight_ld", C.c_int64), ("ignore_index", C.c_int64), ("label_smoothing", C.c_float), ("z_loss", C.c_float),
+                ("dhidden_dtype", C.c_int32), ("dweight_dtype", C.c_int32), ("accumulate", C.c_int32)]
+
+
+def head_loss_desc(tokens, vocab, hidden, hidden_ld=None, weight_ld=None, ignore_index=-100, label_smoothing=0.0, z_loss=0.0,
+                   dhidden_dtype=TYPE_BF16, dweight_dtype=TYPE_BF16, accumulate=0) -> adapm_head_loss:
+    """Pitches that are not given are `hidden`."""
+    return adapm_head_loss(tokens, vocab, hidden, hidden if hidden_ld is None else hidden_ld, hidden if weight_ld is None else weight_ld,
+                           ignore_index, label_smoothing, z_loss, dhidden_dtype, dweight_dtype, accumulate)
 
 
 class AdapmError(RuntimeError):
@@ -122,6 +153,14 @@ def load(build_if_missing: bool = True) -> C.CDLL:
         "adapm_init_omega_floats": (i64, [vp]),
         "adapm_init_omega_layout": (C.c_int, [vp, i64, C.POINTER(i64), C.POINTER(i64)]),
         "adapm_state_init_from_grads": (C.c_int, [vp, vp, vp, vp, vp]),
+        "adapm_dropout": (C.c_int, [vp, vp, vp, i32, i64, i64, i64, i64, i64, C.c_float, C.c_uint64, C.c_uint64, vp, vp]),
+        "adapm_rmsnorm_forward": (C.c_int, [C.POINTER(adapm_rmsnorm)] + [vp] * 9),
+        "adapm_rmsnorm_backward_scratch_bytes": (sz, [C.POINTER(adapm_rmsnorm)]),
+        "adapm_rmsnorm_backward": (C.c_int, [C.POINTER(adapm_rmsnorm)] + [vp] * 8 + [i32, i32, vp, sz, vp]),
+        "adapm_head_loss_scratch_bytes": (sz, [C.POINTER(adapm_head_loss), i32]),
+        "adapm_head_loss_forward": (C.c_int, [C.POINTER(adapm_head_loss)] + [vp] * 6 + [sz, vp]),
+        "adapm_head_loss_backward": (C.c_int, [C.POINTER(adapm_head_loss)] + [vp] * 5 + [C.c_float, vp, vp, vp, sz, vp]),
+        "adapm_head_loss_status": (C.c_int, [vp, vp, C.POINTER(i32)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -314,3 +353,55 @@ def adapm_group_meansq_static(g, grad_dtype: int, n_groups: int, group_elems: in
     on the GPU share the scratch and race; keep them on one stream."""
     _check(load().adapm_group_meansq_static(_ptr(g), grad_dtype, n_groups, group_elems, _ptr(out), _stream(stream)),
            "adapm_group_meansq_static")
+
+
+def _bytes(buf) -> int:
+    return 0 if buf is None else buf.numel() * buf.element_size()
+
+
+def adapm_dropout(x, residual, y, dtype: int, rows: int, cols: int, p: float, seed: int, offset: int, step=None,
+                  x_ld: Optional[int] = None, residual_ld: Optional[int] = None, y_ld: Optional[int] = None, stream=None) -> None:
+    """Pitches that are not given are `cols`."""
+    ld = lambda v: cols if v is None else v  # noqa: E731
+    _check(load().adapm_dropout(_ptr(x), _ptr(residual), _ptr(y), dtype, rows, cols, ld(x_ld), ld(residual_ld), ld(y_ld), p, seed,
+                                offset, _ptr(step), _stream(stream)), "adapm_dropout")
+
+
+def adapm_rmsnorm_forward(desc: adapm_rmsnorm, x, residual, weight, sum, y, y8, y8_scales, rstd, stream=None) -> None:
+    _check(load().adapm_rmsnorm_forward(C.byref(desc), _ptr(x), _ptr(residual), _ptr(weight), _ptr(sum), _ptr(y), _ptr(y8),
+                                        _ptr(y8_scales), _ptr(rstd), _stream(stream)), "adapm_rmsnorm_forward")
+
+
+def adapm_rmsnorm_backward_scratch_bytes(desc: adapm_rmsnorm) -> int:
+    return load().adapm_rmsnorm_backward_scratch_bytes(C.byref(desc))
+
+
+def adapm_rmsnorm_backward(desc: adapm_rmsnorm, dy, dsum, sum, rstd, weight, dresidual, dx, dweight, dweight_dtype: int,
+                           accumulate: bool, scratch, stream=None) -> None:
+    _check(load().adapm_rmsnorm_backward(C.byref(desc), _ptr(dy), _ptr(dsum), _ptr(sum), _ptr(rstd), _ptr(weight), _ptr(dresidual),
+                                         _ptr(dx), _ptr(dweight), dweight_dtype, 1 if accumulate else 0, _ptr(scratch),
+                                         _bytes(scratch), _stream(stream)), "adapm_rmsnorm_backward")
+
+
+def adapm_head_loss_scratch_bytes(desc: adapm_head_loss, backward: bool) -> int:
+    return load().adapm_head_loss_scratch_bytes(C.byref(desc), 1 if backward else 0)
+
+
+def adapm_head_loss_forward(desc: adapm_head_loss, hidden, weight, targets, loss, lse, scratch, stream=None) -> None:
+    _check(load().adapm_head_loss_forward(C.byref(desc), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(loss), _ptr(lse),
+                                          _ptr(scratch), _bytes(scratch), _stream(stream)), "adapm_head_loss_forward")
+
+
+def adapm_head_loss_backward(desc: adapm_head_loss, hidden, weight, targets, lse, dloss, scale: float, dhidden, dweight, scratch,
+                             stream=None) -> None:
+    _check(load().adapm_head_loss_backward(C.byref(desc), _ptr(hidden), _ptr(weight), _ptr(targets), _ptr(lse), _ptr(dloss), scale,
+                                           _ptr(dhidden), _ptr(dweight), _ptr(scratch), _bytes(scratch), _stream(stream)),
+           "adapm_head_loss_backward")
+
+
+def adapm_head_loss_status(scratch, stream=None) -> int:
+    st = C.c_int32(0)
+    rc = load().adapm_head_loss_status(_ptr(scratch), _stream(stream), C.byref(st))
+    if rc not in (0, -7):
+        _check(rc, "adapm_head_loss_status")
+    return st.value

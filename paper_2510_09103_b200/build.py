@@ -10,7 +10,8 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libadapm.so")
-SOURCES = ["planner.cpp", "ctx.cu", "stream_kernels.cu", "lowrank_simt.cu", "lowrank_fp32.cu", "lowrank_tc.cu", "static_scratch.cu"]
+SOURCES = ["planner.cpp", "ctx.cu", "stream_kernels.cu", "lowrank_simt.cu", "lowrank_fp32.cu", "lowrank_tc.cu", "static_scratch.cu",
+           "norm_dropout.cu", "head_loss.cu"]
 
 
 def _nvcc() -> str:

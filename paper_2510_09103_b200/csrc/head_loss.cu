@@ -1,0 +1,903 @@
+// Softmax cross entropy of a language model's output head, and its gradient, from the hidden states and the head's weight, in
+// pieces of the vocabulary: neither the logits nor their gradient exist as a whole.
+//
+//   z = h W^T    lse_t = log sum_v exp z_tv    loss_t = lse_t - (1-e) z_ty - (e/V) sum_v z_tv + zl lse_t^2
+//   g_tv = dloss_t [ p_tv (1 + 2 zl lse_t) - (1-e) [v = y_t] - e/V ],  p = exp(z - lse)
+//   dh_t = scale sum_v g_tv W_v        dW_v = scale sum_t g_tv h_t
+//
+// One kernel (head_items_kernel) does all the products, on pairs of CTAs (tcgen05, cta_group::2, 256 x 256 tiles of the
+// result, K = 64 per stage) with the softmax in its epilogue; its items are
+//   logits -> partial (max, sum) of a row over 128 columns         forward
+//   logits -> g, rounded, into one of two buffers of a piece       backward, piece i + 1
+//   g W and g^T h -> dh (summed over the pieces in fp32) and dW    backward, piece i, in the same launch
+// The three kinds of items of a launch do not depend on one another, so that the many short logits items fill what the long
+// ones of the two gradients leave at the end.  Tokens without a target are taken out first (head_prepare_kernel): they cost
+// nothing, and whatever their hidden states hold (a padded batch's may be NaN) reaches neither gradient.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <mutex>
+
+#include "op_checks.h"
+#include "tc_engine.cuh"
+#include "tc_host.h"
+
+namespace adapm {
+namespace {
+
+using namespace tc;
+
+constexpr int kHeadThreads = 384;            // warp 0 loads A, 2 loads B, 1 issues the MMAs, 4-11 drain the accumulators
+// Registers per thread: of the launch, and as the first four and the other eight warps divide them (the eight keep 128 values each).
+constexpr int kHeadRegs = 168, kIssueRegs = 72, kDrainRegs = 216;
+static_assert(4 * kIssueRegs + 8 * kDrainRegs <= 12 * kHeadRegs, "a block has the registers that it was launched with");
+constexpr int kTile = 256;
+constexpr int kStageK = 64;
+constexpr int kOperandBytes = 128 * kStageK * 2;        // of one CTA and stage: 128 rows or columns of A, as many of B
+constexpr int kHeadStages = 6;
+constexpr int kHeadSmem = kHeadStages * 2 * kOperandBytes + 1024;
+constexpr int kGroupM = 16;                  // row tiles that share the head's columns at a time
+constexpr float kLog2e = 1.4426950408889634f;
+// The tensor cores cut every partial sum off toward zero (a K step of 16 leaves an accumulator up to 2^-23 of itself too small),
+// so that a long sum shrinks with its length: with the whole K in one accumulator an fp32 gradient was off by 1.3e-5 at K = 12288
+// (three planes of 4096) and by 2e-3 at K = 234222.  An item's K is therefore cut into segments, which the epilogue adds up in
+// registers, rounded to nearest; the next segment runs meanwhile in the other accumulator.
+constexpr int kSegLogits = 8, kSegF32 = 4, kSegBf16 = 64;      // stages of 64
+
+enum : int32_t { CLS_LOGITS = 0, CLS_DH = 1, CLS_DW = 2 };
+
+// head of the scratch
+enum : int32_t { HD_STATUS = 0, HD_COUNT = 1 };
+
+struct HeadArgs {
+  CUtensorMap hk, hn, ck, cn, wk, wn, gk, gn;      // hidden, its compacted copy, weight, g; boxes of 64 x 128 (K-major use) and 64 x 64
+  int32_t* head;                 // HD_*
+  const int32_t* token;          // of a compacted row
+  const int32_t* target;         // of a compacted row
+  const float* lse;              // of a compacted row
+  const float* dloss;            // of a compacted row, or null: 1
+  float2* part;                  // forward: (exponent, sum) [2 n_tiles][t_pad]
+  float* part_sum;               // forward with smoothing: sum of the logits, same layout
+  float* z_target;               // forward: logit of the target of a compacted row
+  uint16_t* g;                   // [2 buffers][planes][t_pad][piece]
+  float* dh_acc;                 // [t_pad][hidden], between two pieces
+  void* dh;
+  void* dw;
+  int64_t hidden_ld, weight_ld;
+  int32_t tokens, vocab, hidden, t_pad, piece, planes, planes_dh, planes_dw;
+  int32_t g_begin, g_cols, g_buf;          // piece whose g this launch makes (g_cols = 0: none)
+  int32_t o_begin, o_cols, o_buf;          // piece whose gradients it makes (o_cols = 0: none)
+  int32_t first, last;                     // of the pieces, for dh
+  int32_t dh_f32, dw_f32, accumulate, dh_wide, dw_wide;      // wide: rows start on 32 bytes
+  int32_t seg_dh, seg_dw;                  // longest segments, in stages
+  float scale, smooth, z_loss;
+};
+
+struct __align__(8) HeadShared {
+  uint64_t full[kHeadStages], empty[kHeadStages], tfull[2], tempty[2];
+  uint32_t tmem_base;
+  int abort, skip;
+};
+
+// The items of a launch, as every warp of a pair walks through them.  Long items (gradients) first, dealt out in turn; then the
+// short ones (logits) in turn, where the pairs that got a long item more join `skip` rounds later.
+struct Walk {
+  int pairs, pair, n_dh, n_long, n_short, extra, skip, mine;
+  int m_tiles, nt_v, nt_d, units, k_logits, k_dh, k_dw;
+
+  __device__ __forceinline__ Walk(const HeadArgs& a, bool backward, int tv, int pair_, int pairs_) : pairs(pairs_), pair(pair_) {
+    m_tiles = (tv + kTile - 1) / kTile;
+    const int cols = backward ? a.g_cols : a.vocab;
+    nt_v = (cols + kTile - 1) / kTile;
+    units = (a.hidden + 31) / 32;
+    nt_d = (units + 7) / 8;
+    k_logits = (a.hidden + kStageK - 1) / kStageK;
+    k_dh = (a.o_cols + kStageK - 1) / kStageK;
+    k_dw = max(1, (tv + kStageK - 1) / kStageK);
+    n_short = m_tiles * nt_v;
+    n_dh = backward && a.o_cols > 0 && a.dh ? m_tiles * nt_d : 0;
+    const int n_dw = backward && a.o_cols > 0 && a.dw ? (a.o_cols + kTile - 1) / kTile * nt_d : 0;
+    n_long = n_dh + n_dw;
+    extra = n_long % pairs;
+    const int long_cost = n_dw > 0 ? k_dw * a.planes_dw : k_dh * a.planes_dh;
+    skip = extra ? (long_cost + k_logits / 2) / k_logits : 0;
+    mine = pair < n_long ? (n_long - pair + pairs - 1) / pairs : 0;
+  }
+  // Of this pair's item `seq`: class, first row, first column, columns, stages per plane; false past the last.
+  __device__ __forceinline__ bool item(const HeadArgs& a, int seq, int& cls, int& m0, int& n0, int& bn, int& k_stages, int& planes) const {
+    if (seq < mine) {
+      int k = pair + seq * pairs;
+      cls = k < n_dh ? CLS_DH : CLS_DW;
+      if (cls == CLS_DW) k -= n_dh;
+      const int n = k % nt_d, base = units / nt_d, more = units % nt_d;
+      m0 = k / nt_d * kTile;
+      n0 = 32 * (n * base + min(n, more));          // widths as even as multiples of 32 allow
+      bn = 32 * (base + (n < more ? 1 : 0));
+      k_stages = cls == CLS_DH ? k_dh : k_dw;
+      planes = cls == CLS_DH ? a.planes_dh : a.planes_dw;
+      return true;
+    }
+    const int j = seq - mine;
+    int k;
+    if (pair < extra) k = skip * (pairs - extra) + j * pairs + pair;
+    else if (j < skip) k = j * (pairs - extra) + pair - extra;
+    else k = skip * (pairs - extra) + (j - skip) * pairs + pair;
+    if (k >= n_short) return false;
+    const int per_group = kGroupM * nt_v, group = k / per_group, in_group = min(kGroupM, m_tiles - group * kGroupM);
+    k -= group * per_group;
+    cls = CLS_LOGITS;
+    m0 = (group * kGroupM + k % in_group) * kTile;
+    n0 = k / in_group * kTile;
+    bn = kTile;
+    k_stages = k_logits;
+    planes = 1;
+    return true;
+  }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ void st_b32x4(void* p, const uint32_t* v) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(v[0], v[1], v[2], v[3]);
+}
+
+// 16 values of one row of a gradient, of which those below n (a multiple of 8) exist: as fp32 or bf16, to addresses that are
+// multiples of 32 (wide) or 16 bytes.
+__device__ __forceinline__ void store_row16(void* base, int64_t at, const float* x, int n, bool f32, bool wide) {
+  if (f32) {
+    float* p = static_cast<float*>(base) + at;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (8 * h < n) {
+        if (wide) st_f32x8(p + 8 * h, x + 8 * h);
+        else {
+          *reinterpret_cast<float4*>(p + 8 * h) = make_float4(x[8 * h], x[8 * h + 1], x[8 * h + 2], x[8 * h + 3]);
+          *reinterpret_cast<float4*>(p + 8 * h + 4) = make_float4(x[8 * h + 4], x[8 * h + 5], x[8 * h + 6], x[8 * h + 7]);
+        }
+      }
+    }
+    return;
+  }
+  uint16_t* p = static_cast<uint16_t*>(base) + at;
+  uint32_t w[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2_rn(x[2 * e], x[2 * e + 1]);
+  if (wide && n >= 16) st_b32x8(p, w);
+  else {
+    if (n > 0) st_b32x4(p, w);
+    if (n > 8) st_b32x4(p + 8, w + 4);
+  }
+}
+__device__ __forceinline__ void load_row16(const void* base, int64_t at, float* x, int n, bool f32) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (8 * h >= n) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[8 * h + e] = 0.f;
+    } else if (f32) {
+      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at + 8 * h);
+      const float4 u = __ldcg(p), v = __ldcg(p + 1);
+      x[8 * h] = u.x; x[8 * h + 1] = u.y; x[8 * h + 2] = u.z; x[8 * h + 3] = u.w;
+      x[8 * h + 4] = v.x; x[8 * h + 5] = v.y; x[8 * h + 6] = v.z; x[8 * h + 7] = v.w;
+    } else {
+      const uint4 u = __ldcg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at + 8 * h));
+      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[8 * h + 2 * e] = __uint_as_float(w[e] << 16);
+        x[8 * h + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+      }
+    }
+  }
+}
+
+// An item's K in segments of even length: how many, and the stages of each but the last.
+__device__ __forceinline__ void segments(int stages, int most, int& n, int& each) {
+  n = (stages + most - 1) / most;
+  each = (stages + n - 1) / n;
+  n = (stages + each - 1) / each;
+}
+
+// v = (or +=) `half` columns of this thread's row of an accumulator.
+__device__ __forceinline__ void take(uint32_t taddr, int half, bool add, float* v) {
+  if (!add) {
+#pragma unroll
+    for (int c = 0; c < 128; c += 16)
+      if (c < half) tmem_ld16(taddr + c, v + c);
+    tmem_ld_wait();
+    return;
+  }
+#pragma unroll
+  for (int c = 0; c < 128; c += 32) {
+    if (c < half) {
+      float t[32];
+      tmem_ld16(taddr + c, t);
+      if (c + 16 < half) tmem_ld16(taddr + c + 16, t + 16);
+      tmem_ld_wait();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[c + e] += t[e];
+      if (c + 16 < half) {
+#pragma unroll
+        for (int e = 16; e < 32; ++e) v[c + e] += t[e];
+      }
+    }
+  }
+}
+
+// v[y] for a y that the compiler does not know.
+__device__ __forceinline__ float pick(const float* v, int y) {
+  float x = 0.f;
+#pragma unroll
+  for (int c = 0; c < 128; c += 16) {
+    if ((unsigned)(y - c) < 16u) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (y - c == e) x = v[c + e];
+    }
+  }
+  return x;
+}
+
+// Sum of exp over 128 logits of a row, `n` of which exist, as sum * 2^k.  k is the greatest logit in base 2, rounded to a
+// whole number, so that z log2(e) - k is one multiply-add with one rounding and the sums of different columns are scaled by
+// powers of two only.
+__device__ __forceinline__ void row_sums(float* z, int n, bool with_sum, float& k, float& sum, float& total) {
+  total = 0.f;
+  if (n < 128) {
+#pragma unroll
+    for (int e = 0; e < 128; ++e) {
+      if (e < n) total += z[e];
+      else z[e] = -INFINITY;
+    }
+  } else if (with_sum) {
+    float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 128; ++e) t[e & 3] += z[e];
+    total = (t[0] + t[1]) + (t[2] + t[3]);
+  }
+  float top[4] = {z[0], z[1], z[2], z[3]};
+#pragma unroll
+  for (int e = 4; e < 128; ++e) top[e & 3] = fmaxf(top[e & 3], z[e]);
+  k = fmaxf(-INFINITY, rintf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e));      // (all NaN: -inf)
+  const float shift = k == -INFINITY ? 0.f : k;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < 128; ++e) s[e & 3] += ex2(fmaf(z[e], kLog2e, -shift));
+  sum = (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+template <bool BACKWARD>
+__global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __grid_constant__ HeadArgs a) {
+  extern __shared__ uint8_t dyn_smem[];
+  __shared__ HeadShared sh;
+  wait_for_previous_kernel();
+  const uint32_t rank = cluster_rank();
+  uint8_t* const stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~(uintptr_t)1023);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* const abort = &sh.abort;
+  int32_t* const status = a.head + HD_STATUS;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kHeadStages; ++i) {
+      mbar_init(&sh.full[i], 2);                    // A and B, those of rank 0 for both CTAs
+      mbar_init(&sh.empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 16); }
+    sh.abort = 0;
+    sh.skip = *reinterpret_cast<volatile int32_t*>(status) != 0;
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    tmem_alloc<true>(&sh.tmem_base, 512);
+    tmem_relinquish<true>();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem_base = sh.tmem_base;
+  const bool skip = load_shared_of(&sh.skip, 0) != 0;       // an earlier launch gave up: the pair decides together
+  const int tv = uniform(*reinterpret_cast<volatile int32_t*>(a.head + HD_COUNT));
+  const bool compacted = tv != a.tokens;
+  const Walk walk(a, BACKWARD, tv, (int)(blockIdx.x >> 1), (int)(gridDim.x >> 1));
+  int cls, m0, n0, bn, k_stages, planes;
+
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
+  if (skip) {
+    // nothing
+  } else if (warp == 0 || warp == 2) {
+    // ------------------------------------------------------------------ producers (all lanes run, one issues)
+    const bool leader = elect_one(), is_a = warp == 0;
+    const uint32_t pair_full = uniform(shared_of(sh.full, 0));
+    int stage = 0;
+    uint32_t phase = 0, issued = 0;
+    bool ok = true;
+    for (int seq = 0; ok && walk.item(a, seq, cls, m0, n0, bn, k_stages, planes); ++seq) {
+      const CUtensorMap* map;
+      int x, y, n_box = 1;                 // K-major: one box of 128 rows, x runs; MN-major: boxes of 64 columns, y runs
+      const int half = bn / 2, o_row = a.o_buf * a.planes * a.t_pad;
+      if (is_a) {
+        if (cls == CLS_DW) { map = &a.gn; x = m0 + (int)rank * 128; y = o_row; n_box = 2; }
+        else if (cls == CLS_DH) { map = &a.gk; x = 0; y = o_row + m0 + (int)rank * 128; }
+        else { map = compacted ? &a.ck : &a.hk; x = 0; y = m0 + (int)rank * 128; }
+      } else {
+        if (cls == CLS_LOGITS) { map = &a.wk; x = 0; y = (BACKWARD ? a.g_begin : 0) + n0 + (int)rank * 128; }
+        else {
+          map = cls == CLS_DH ? &a.wn : (compacted ? &a.cn : &a.hn);
+          x = n0 + (int)rank * half; y = cls == CLS_DH ? a.o_begin : 0; n_box = half > 64 ? 2 : 1;
+        }
+      }
+      const bool along_y = is_a ? cls == CLS_DW : cls != CLS_LOGITS;
+      const uint32_t bytes = along_y ? (uint32_t)n_box * (kOperandBytes / 2) : kOperandBytes;
+      const int plane_step = is_a && cls != CLS_LOGITS ? a.t_pad : 0;
+      for (int p = 0; p < planes && ok; ++p) {
+        int xk = x, yk = y + p * plane_step;
+        for (int k = 0; k < k_stages; ++k) {
+          if (!mbar_wait_warp<WAIT_PAIR>(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+          uint8_t* const dst = stages + stage * (2 * kOperandBytes) + (is_a ? 0 : kOperandBytes);
+          if (leader) {
+            if (rank == 0) mbar_arrive_expect_tx(&sh.full[stage], 2 * bytes);
+            const uint32_t bar = pair_full + 8u * (uint32_t)stage;
+            tma_load_box_pair(dst, map, xk, yk, bar);
+            if (n_box == 2) tma_load_box_pair(dst + kOperandBytes / 2, map, xk + 64, yk, bar);
+          }
+          __syncwarp();
+          if (along_y) yk += kStageK; else xk += kStageK;
+          ++issued;
+          if (++stage == kHeadStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+    if (!ok) drain_ring<true>(sh.full, stage, phase, issued, kHeadStages, rank);
+  } else if (warp == 1 && rank == 0) {
+    // ------------------------------------------------------------------ MMA issuer (all lanes run, one issues)
+    const bool leader = elect_one();
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    const uint32_t ring = uniform(smem_u32(stages)), d0 = uniform(tmem_base), dhi = desc_hi();
+    uint32_t run = 0;                     // segments so far
+    for (int seq = 0; ok && walk.item(a, seq, cls, m0, n0, bn, k_stages, planes); ++seq) {
+      const bool a_mn = cls == CLS_DW, b_mn = cls != CLS_LOGITS;
+      const uint32_t idesc = uniform(make_idesc(bn, a_mn, b_mn, false, 256));
+      // per K step of 16: 32 bytes inside a K-major row, 16 rows of 128 bytes of an MN-major box (in 16-byte units)
+      const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
+      int left = k_stages * planes, n_seg, each;
+      segments(left, cls == CLS_LOGITS ? kSegLogits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
+      for (; left > 0 && ok; left -= each, ++run) {
+        const int acc = (int)(run & 1);
+        if (!mbar_wait_warp<WAIT_PAIR_TC>(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d = d0 + (uint32_t)(acc * kTile);
+        uint32_t accumulate = 0;
+        for (int i = min(each, left); i > 0; --i) {
+          if (!mbar_wait_warp<WAIT_PAIR>(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t slot = ring + (uint32_t)(stage * 2 * kOperandBytes);
+          const uint32_t alo = desc_lo(slot, a_mn ? kOperandBytes / 2 : 16u);
+          const uint32_t blo = desc_lo(slot + kOperandBytes, b_mn ? kOperandBytes / 2 : 16u);
+          if (leader) {
+#pragma unroll
+            for (int q = 0; q < kStageK / 16; ++q)
+              mma_bf16<true>(d, desc_join(alo + q * a_step, dhi), desc_join(blo + q * b_step, dhi), idesc, q ? 1u : accumulate);
+            mma_commit<true>(&sh.empty[stage]);
+          }
+          __syncwarp();
+          accumulate = 1;
+          if (++stage == kHeadStages) { stage = 0; phase ^= 1u; }
+        }
+        if (ok && leader) mma_commit<true>(&sh.tfull[acc]);
+        __syncwarp();
+      }
+    }
+  }
+  } else {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kDrainRegs));
+    // ------------------------------------------------------------------ epilogue: a thread has one row of the tile and, by its
+    // group of four warps, the lower or upper half of the columns, all of them in registers
+    const int q = 32 * (warp & 3) + lane, grp = (warp - 4) >> 2;
+    const uint32_t lane_addr = (uint32_t)(32 * (warp & 3)) << 16;
+    uint32_t run = 0;
+    bool ok = true;
+    for (int seq = 0; !skip && walk.item(a, seq, cls, m0, n0, bn, k_stages, planes); ++seq) {
+      const int row = m0 + (int)rank * 128 + q, half = bn / 2;
+      // what the row needs is asked for before the accumulator is waited for
+      int y = -1, token = 0;
+      float lse = 0.f, dl = 0.f;
+      if (cls == CLS_LOGITS && row < tv) {
+        y = a.target[row] - n0 - 128 * grp;
+        if (BACKWARD) {
+          y -= a.g_begin;
+          lse = a.lse[row];
+          dl = a.dloss ? a.dloss[row] : 1.f;
+        }
+      } else if (BACKWARD && cls == CLS_DH && a.last && row < tv) {
+        token = a.token[row];
+      }
+      float v[128];
+      int n_seg, each;
+      segments(k_stages * planes, cls == CLS_LOGITS ? kSegLogits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
+#pragma unroll 1
+      for (int i = 0; i < n_seg; ++i, ++run) {
+        const int acc = (int)(run & 1);
+        if (lane == 0) ok = mbar_wait<WAIT_PAIR_TC>(&sh.tfull[acc], (run >> 1) & 1u, abort, status, ST_WAIT_TMEM_FULL, kWaitSpinDefault);
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        tc_fence_after();
+        take(tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * half), half, i > 0, v);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_relaxed_at(shared_of(&sh.tempty[acc], 0));
+      }
+      if (!ok) break;
+      if (!BACKWARD) {
+        const int n = min(128, a.vocab - n0 - 128 * grp);
+        float k, sum, total;
+        if ((unsigned)y < 128u && y < n) a.z_target[row] = pick(v, y);
+        row_sums(v, n, a.smooth != 0.f, k, sum, total);
+        if (row < tv) {
+          const int64_t at = (int64_t)(n0 / 128 + grp) * a.t_pad + row;
+          a.part[at] = make_float2(k, sum);
+          if (a.smooth != 0.f) a.part_sum[at] = total;
+        }
+      } else if (cls == CLS_LOGITS) {
+        // p = exp(z - lse) = 2^(z log2(e) - k) 2^(k - lse log2(e)) with k whole: the first exponent is one multiply-add
+        // with one rounding, the second factor belongs to the row
+        const float k = rintf(lse * kLog2e);
+        const float rest = fmaf(lse, kLog2e, -k) + lse * 1.925963033500e-8f;       // log2(e) - fp32(log2(e))
+        const float up = dl * ex2(-rest) * fmaf(2.f * a.z_loss, lse, 1.f);
+        const float down = dl * (a.smooth / (float)a.vocab), at_y = dl * (1.f - a.smooth);
+        const int n = row < tv ? a.vocab - a.g_begin - n0 - 128 * grp : 0;            // columns that exist
+        uint16_t* const dst = a.g + ((int64_t)(a.g_buf * a.planes) * a.t_pad + row) * a.piece + n0 + 128 * grp;
+        const int64_t plane = (int64_t)a.t_pad * a.piece;
+#pragma unroll
+        for (int c = 0; c < 128; c += 16) {
+          float* const z = v + c;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) z[e] = fmaf(ex2(fmaf(z[e], kLog2e, -k)), up, -down);
+          if ((unsigned)(y - c) < 16u) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (y - c == e) z[e] -= at_y;
+          }
+          if (c + 16 > n) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (c + e >= n) z[e] = 0.f;
+          }
+          // g in bf16 (off by 2^-8 of itself at most, like the gradients it makes), or, where a gradient is wanted in fp32, as
+          // the sum of three bf16 numbers, which have its 24 bits
+          for (int p = 0; p < a.planes; ++p) {
+            uint32_t w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              w[e] = pack_bf16x2_rn(z[2 * e], z[2 * e + 1]);
+              z[2 * e] -= __uint_as_float(w[e] << 16);
+              z[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+            }
+            st_b32x8(dst + p * plane + c, w);
+          }
+        }
+      } else {
+        const int col0 = n0 + grp * half;
+        const bool is_dh = cls == CLS_DH;
+        const bool row_ok = row < (is_dh ? tv : a.o_cols), none = tv == 0;
+        const bool to_acc = is_dh && !a.last, from_acc = is_dh && !a.first, from_out = !is_dh && a.accumulate;
+        void* const out = is_dh ? a.dh : a.dw;
+        const int64_t out_row = is_dh ? (int64_t)token * a.hidden_ld : (int64_t)(a.o_begin + row) * a.weight_ld;
+        float* const acc_row = a.dh_acc + (int64_t)row * a.hidden;
+        const bool f32 = is_dh ? a.dh_f32 : a.dw_f32, wide = is_dh ? a.dh_wide : a.dw_wide;
+        const float scale = to_acc ? 1.f : a.scale;
+#pragma unroll
+        for (int c = 0; c < 128; c += 16) {
+          if (c < half) {
+            const int n = row_ok ? a.hidden - col0 - c : 0;
+            float* const x = v + c;
+            float old[16];
+            if (from_acc) load_row16(acc_row, col0 + c, old, n, true);
+            if (from_out) load_row16(out, out_row + col0 + c, old, n, f32);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              if (none) x[e] = 0.f;
+              if (from_acc) x[e] += old[e];
+              x[e] *= scale;
+              if (from_out) x[e] += old[e];
+            }
+            if (to_acc) store_row16(acc_row, col0 + c, x, n, true, true);
+            else store_row16(out, out_row + col0 + c, x, n, f32, wide);
+          }
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();      // neither CTA leaves while the other may still reach into it
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc<true>(tmem_base, 512);
+  }
+}
+
+// ---- tokens with a target ----------------------------------------------------------------------------
+
+struct PrepareArgs {
+  const int64_t* targets;
+  const uint16_t* hidden;
+  uint16_t* compact;             // [t_pad][width]
+  int32_t* head;
+  int32_t* token;
+  int32_t* target;
+  const float* lse_in; float* lse;          // backward
+  const float* dloss_in; float* dloss;      // backward, may be null
+  float* loss; float* lse_out;              // forward: what tokens without a target get
+  void* dh;                                 // backward: its rows of tokens without a target become zero; may be null
+  int64_t hidden_ld, ignore;
+  int32_t tokens, vocab, width, per_cta, dh_f32;
+};
+
+// Every CTA counts the targets of all tokens (8 bytes each, from L2; cheaper than a second launch), then writes what belongs to
+// its own ones: the row number among those with a target, the copies that the products read, the answers of the others.
+__global__ void __launch_bounds__(256) head_prepare_kernel(const PrepareArgs a) {
+  __shared__ int counts[2][8];
+  __shared__ int at[256];
+  wait_for_previous_kernel();
+  const int begin = (int)blockIdx.x * a.per_cta, end = min(a.tokens, begin + a.per_cta);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto has_target = [&](int64_t y) { return y != a.ignore && y >= 0 && y < a.vocab; };
+  int before = 0, all = 0;
+#pragma unroll 4
+  for (int t = threadIdx.x; t < a.tokens; t += 256) {
+    const int v = has_target(a.targets[t]) ? 1 : 0;
+    all += v;
+    before += t < begin ? v : 0;
+  }
+  before = __reduce_add_sync(0xffffffffu, before);
+  all = __reduce_add_sync(0xffffffffu, all);
+  if (lane == 0) { counts[0][warp] = before; counts[1][warp] = all; }
+  __syncthreads();
+  before = all = 0;
+  for (int w = 0; w < 8; ++w) { before += counts[0][w]; all += counts[1][w]; }
+  if (blockIdx.x == 0 && threadIdx.x == 0) { a.head[HD_STATUS] = 0; a.head[HD_COUNT] = all; }
+  const bool copy = all != a.tokens;
+  const int vec = a.width >> 3;
+  for (int t0 = begin; t0 < end; t0 += 256) {
+    const int t = t0 + (int)threadIdx.x;
+    const int64_t y = t < end ? a.targets[t] : a.ignore;
+    const bool valid = t < end && has_target(y);
+    const unsigned votes = __ballot_sync(0xffffffffu, valid);
+    __syncthreads();                              // (counts and at of the round before have been read)
+    if (lane == 0) counts[0][warp] = __popc(votes);
+    __syncthreads();
+    int row = before + __popc(votes & ((1u << lane) - 1));
+    for (int w = 0; w < 8; ++w) {
+      if (w < warp) row += counts[0][w];
+      before += counts[0][w];
+    }
+    at[threadIdx.x] = valid ? row : -1;
+    if (valid) {
+      a.token[row] = t;
+      a.target[row] = (int32_t)y;
+      if (a.lse_in) a.lse[row] = a.lse_in[t];
+      if (a.dloss_in) a.dloss[row] = a.dloss_in[t];
+    } else if (t < end && a.loss) {
+      const float x = y == a.ignore ? 0.f : __int_as_float(0x7fffffff);
+      a.loss[t] = x;
+      a.lse_out[t] = x;
+    }
+    __syncthreads();
+    for (int i = warp; i < min(256, end - t0); i += 8) {
+      const int r = at[i];
+      const int64_t src_row = (int64_t)(t0 + i) * a.hidden_ld;
+      if (r >= 0 && copy) {
+        const uint4* src = reinterpret_cast<const uint4*>(a.hidden + src_row);
+        uint4* dst = reinterpret_cast<uint4*>(a.compact + (int64_t)r * a.width);
+#pragma unroll 4
+        for (int v = lane; v < vec; v += 32) dst[v] = src[v];
+      } else if (r < 0 && a.dh) {
+        uint4* dst = reinterpret_cast<uint4*>(a.dh_f32 ? (void*)(static_cast<float*>(a.dh) + src_row) : (void*)(static_cast<uint16_t*>(a.dh) + src_row));
+        for (int v = lane; v < (a.dh_f32 ? 2 * vec : vec); v += 32) dst[v] = make_uint4(0, 0, 0, 0);
+      }
+    }
+  }
+  // the last stage of a product over the tokens reads whole groups of 64 rows
+  if (copy && blockIdx.x == gridDim.x - 1) {
+    const int64_t stop = ((int64_t)max(all, 1) + 63) / 64 * 64 * vec;
+    for (int64_t v = (int64_t)all * vec + threadIdx.x; v < stop; v += 256) reinterpret_cast<uint4*>(a.compact)[v] = make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ---- what the forward items left of a row, put together ------------------------------------------------
+
+struct FinalArgs {
+  const int32_t* head;
+  const int32_t* token;
+  const float2* part;
+  const float* part_sum;
+  const float* z_target;
+  float* loss;
+  float* lse;
+  int32_t n_parts, t_pad, vocab;
+  float smooth, z_loss;
+};
+
+// A CTA has 32 rows (its lanes), eight warps share the parts of each.
+__global__ void __launch_bounds__(256) head_final_kernel(const FinalArgs a) {
+  __shared__ float ks[8][32], sums[8][32], totals[8][32];
+  wait_for_previous_kernel();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = (int)blockIdx.x * 32 + lane, tv = a.head[HD_COUNT];
+  float k = -INFINITY, sum = 0.f, total = 0.f;
+  auto add = [&](float pk, float ps) {
+    const float top = fmaxf(k, pk);
+    sum = (k == top ? sum : sum * ex2(k - top)) + (pk == top || pk == -INFINITY ? ps : ps * ex2(pk - top));
+    k = top;
+  };
+  if (row < tv) {
+#pragma unroll 4
+    for (int i = warp; i < a.n_parts; i += 8) {
+      const int64_t at = (int64_t)i * a.t_pad + row;
+      const float2 p = a.part[at];
+      add(p.x, p.y);
+      if (a.smooth != 0.f) total += a.part_sum[at];
+    }
+  }
+  ks[warp][lane] = k; sums[warp][lane] = sum; totals[warp][lane] = total;
+  __syncthreads();
+  if (warp != 0 || row >= tv) return;
+  for (int w = 1; w < 8; ++w) { add(ks[w][lane], sums[w][lane]); total += totals[w][lane]; }
+  const int t = a.token[row];
+  double lse = ((double)k + log2((double)sum)) * 0.69314718055994530942;
+  if (a.head[HD_STATUS] != 0) lse = __longlong_as_double(0x7ff8000000000000ll);       // a wait ran out: nothing of this call holds
+  const double loss = lse - (1.0 - (double)a.smooth) * (double)a.z_target[row] - (double)a.smooth * (double)total / a.vocab +
+                      (double)a.z_loss * lse * lse;
+  a.loss[t] = (float)loss;
+  a.lse[t] = (float)lse;
+}
+
+// ---- host ----------------------------------------------------------------------------------------------
+
+struct Layout {
+  int64_t t_pad, n_tiles, piece, n_pieces, n_buf, planes;
+  int64_t token, target, compact, lse, dloss, part, part_sum, z_target, g, dh_acc, bytes;      // byte offsets
+};
+
+// A piece of the vocabulary: as many columns as make g of one piece and plane about 64 M elements (128 MB: what the two
+// gradient products read is then mostly still in L2), of even sizes, and at least 2048 (the sum of dh goes through
+// memory once per piece).
+constexpr int64_t kPieceElems = (int64_t)64 << 20, kPieceMin = 2048;
+
+int plan(const adapm_head_loss& d, bool backward, Layout& l) {
+  if (d.tokens < 0 || d.vocab <= 0 || d.hidden <= 0) return ADAPM_EINVAL;
+  if (d.tokens > (1 << 24) || d.vocab > (1 << 24) || d.hidden > (1 << 16)) return ADAPM_ERANGE;
+  if (d.hidden % 8) return ADAPM_EUNSUPPORTED;
+  if (d.hidden_ld < d.hidden || d.weight_ld < d.hidden) return ADAPM_EINVAL;
+  if (d.hidden_ld % 8 || d.weight_ld % 8) return ADAPM_EALIGN;
+  if (d.hidden_ld >= ((int64_t)1 << 38) || d.weight_ld >= ((int64_t)1 << 38)) return ADAPM_ERANGE;      // (a tensor map's pitch has 40 bits)
+  if (!(d.label_smoothing >= 0.f && d.label_smoothing <= 1.f) || !(d.z_loss >= 0.f) || !std::isfinite(d.z_loss)) return ADAPM_ERANGE;
+  if (backward && (!known_type(d.dhidden_dtype) || !known_type(d.dweight_dtype))) return ADAPM_EINVAL;
+  l.t_pad = round_up(d.tokens < 1 ? 1 : d.tokens, kTile);
+  l.n_tiles = (d.vocab + kTile - 1) / kTile;
+  l.planes = backward && (d.dhidden_dtype == ADAPM_TYPE_F32 || d.dweight_dtype == ADAPM_TYPE_F32) ? 3 : 1;
+  const int64_t most = std::max(kPieceMin, kPieceElems / l.t_pad / kTile * kTile);
+  l.n_pieces = (d.vocab + most - 1) / most;
+  l.piece = round_up((d.vocab + l.n_pieces - 1) / l.n_pieces, kTile);
+  l.n_pieces = (d.vocab + l.piece - 1) / l.piece;
+  l.n_buf = l.n_pieces > 1 ? 2 : 1;
+  if (l.t_pad / kTile * l.n_tiles > (1 << 30) || l.n_buf * l.planes * l.t_pad >= ((int64_t)1 << 31)) return ADAPM_ERANGE;
+  int64_t at = 256;
+  auto take = [&](int64_t bytes) { const int64_t o = at; at += round_up(bytes, 256); return o; };
+  l.token = take(l.t_pad * 4);
+  l.target = take(l.t_pad * 4);
+  l.compact = take(l.t_pad * d.hidden * 2);
+  l.lse = l.dloss = l.part = l.part_sum = l.z_target = l.g = l.dh_acc = 0;
+  if (backward) {
+    l.lse = take(l.t_pad * 4);
+    l.dloss = take(l.t_pad * 4);
+    l.g = take(l.n_buf * l.planes * l.t_pad * l.piece * 2);
+    if (l.n_pieces > 1) l.dh_acc = take(l.t_pad * d.hidden * 4);
+  } else {
+    l.part = take(2 * l.n_tiles * l.t_pad * 8);
+    l.part_sum = take(d.label_smoothing != 0.f ? 2 * l.n_tiles * l.t_pad * 4 : 0);
+    l.z_target = take(l.t_pad * 4);
+  }
+  l.bytes = at;
+  return ADAPM_OK;
+}
+
+// Pairs of CTAs that run at the same time on this device; the kernels' shared memory is allowed on the way.  (Once per device.)
+int pairs_of(int device, int* pairs) {
+  static std::mutex mu;
+  static int known[64] = {};
+  if (device < 0 || device >= 64) return ADAPM_ERANGE;
+  std::lock_guard<std::mutex> lock(mu);
+  if (!known[device]) {
+    int sms = 0;
+    ADAPM_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    for (const void* kernel : {(const void*)head_items_kernel<false>, (const void*)head_items_kernel<true>}) {
+      cudaFuncAttributes fa;                  // (with fewer registers at launch the split above would wait for ever)
+      ADAPM_CUDA(cudaFuncGetAttributes(&fa, kernel));
+      if (fa.numRegs < kHeadRegs) {
+        set_error_text("head_items_kernel was built with fewer registers than it divides among its warps");
+        return ADAPM_EUNSUPPORTED;
+      }
+    }
+    ADAPM_CUDA(cudaFuncSetAttribute(head_items_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem));
+    ADAPM_CUDA(cudaFuncSetAttribute(head_items_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeadSmem));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(sms / 2 * 2); cfg.blockDim = dim3(kHeadThreads); cfg.dynamicSmemBytes = kHeadSmem;
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = 2; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    int resident = 0;
+    ADAPM_CUDA(cudaOccupancyMaxActiveClusters(&resident, head_items_kernel<true>, &cfg));
+    known[device] = std::max(1, std::min(resident, sms / 2));
+  }
+  *pairs = known[device];
+  return ADAPM_OK;
+}
+
+bool maps_of_operands(HeadArgs& a, const adapm_head_loss& d, const void* hidden, const void* weight, const void* compact, int64_t t_pad) {
+  return encode_bf16_matrix(&a.hk, hidden, d.tokens, d.hidden, d.hidden_ld, 128) && encode_bf16_matrix(&a.hn, hidden, d.tokens, d.hidden, d.hidden_ld, 64) &&
+         encode_bf16_matrix(&a.ck, compact, t_pad, d.hidden, d.hidden, 128) && encode_bf16_matrix(&a.cn, compact, t_pad, d.hidden, d.hidden, 64) &&
+         encode_bf16_matrix(&a.wk, weight, d.vocab, d.hidden, d.weight_ld, 128) && encode_bf16_matrix(&a.wn, weight, d.vocab, d.hidden, d.weight_ld, 64);
+}
+
+int launch_prepare(const adapm_head_loss& d, PrepareArgs p, cudaStream_t s) {
+  p.ignore = d.ignore_index;
+  p.hidden_ld = d.hidden_ld;
+  p.tokens = (int32_t)d.tokens; p.vocab = (int32_t)d.vocab; p.width = (int32_t)d.hidden;
+  p.per_cta = (int32_t)std::max<int64_t>(8, (d.tokens + 295) / 296);
+  const unsigned grid = (unsigned)((d.tokens + p.per_cta - 1) / p.per_cta);
+  ADAPM_CUDA(launch_chained(true, head_prepare_kernel, grid, 256, 0, s, p));
+  return ADAPM_OK;
+}
+
+}  // namespace
+}  // namespace adapm
+
+using namespace adapm;
+
+extern "C" size_t adapm_head_loss_scratch_bytes(const adapm_head_loss* d, int32_t backward) {
+  Layout l;
+  return d && plan(*d, backward != 0, l) == ADAPM_OK ? (size_t)l.bytes : 0;
+}
+
+extern "C" int adapm_head_loss_forward(const adapm_head_loss* d, const void* hidden, const void* weight, const int64_t* targets, float* loss,
+                                       float* lse, void* scratch, size_t scratch_bytes, adapm_stream stream) {
+  if (!d) return ADAPM_EINVAL;
+  Layout l;
+  int rc = plan(*d, false, l);
+  if (rc != ADAPM_OK || d->tokens == 0) return rc;
+  if (!hidden || !weight || !targets || !loss || !lse || !scratch) return ADAPM_EINVAL;
+  if ((uintptr_t)hidden % 16 || (uintptr_t)weight % 16 || (uintptr_t)targets % 8 || (uintptr_t)loss % 4 || (uintptr_t)lse % 4 || (uintptr_t)scratch % 256) return ADAPM_EALIGN;
+  if (scratch_bytes < (size_t)l.bytes) return ADAPM_ENOWORKSPACE;
+  int device, pairs;
+  rc = check_on_this_device({hidden, weight, targets, loss, lse, scratch}, &device);
+  if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
+  if (rc != ADAPM_OK) return rc;
+  cudaStream_t s = (cudaStream_t)stream;
+  char* const base = static_cast<char*>(scratch);
+
+  HeadArgs a;
+  std::memset(&a, 0, sizeof(a));
+  if (!maps_of_operands(a, *d, hidden, weight, base + l.compact, l.t_pad)) {
+    set_error_text("cuTensorMapEncodeTiled failed for the head");
+    return ADAPM_ECUDA;
+  }
+  a.head = (int32_t*)base;
+  a.token = (int32_t*)(base + l.token); a.target = (int32_t*)(base + l.target);
+  a.part = (float2*)(base + l.part); a.part_sum = (float*)(base + l.part_sum); a.z_target = (float*)(base + l.z_target);
+  a.tokens = (int32_t)d->tokens; a.vocab = (int32_t)d->vocab; a.hidden = (int32_t)d->hidden; a.t_pad = (int32_t)l.t_pad;
+  a.planes = a.planes_dh = a.planes_dw = 1;
+  a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
+
+  PrepareArgs p;
+  std::memset(&p, 0, sizeof(p));
+  p.targets = targets; p.hidden = (const uint16_t*)hidden; p.compact = (uint16_t*)(base + l.compact);
+  p.head = a.head; p.token = (int32_t*)(base + l.token); p.target = (int32_t*)(base + l.target); p.loss = loss; p.lse_out = lse;
+  rc = launch_prepare(*d, p, s);
+  if (rc != ADAPM_OK) return rc;
+  const int64_t items = l.t_pad / kTile * l.n_tiles;
+  ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<false>, 2 * (unsigned)std::min<int64_t>(pairs, items), kHeadThreads, kHeadSmem, s, a));
+  FinalArgs f;
+  f.head = a.head; f.token = a.token; f.part = a.part; f.part_sum = a.part_sum; f.z_target = a.z_target; f.loss = loss; f.lse = lse;
+  f.n_parts = (int32_t)(2 * l.n_tiles); f.t_pad = (int32_t)l.t_pad; f.vocab = (int32_t)d->vocab; f.smooth = d->label_smoothing; f.z_loss = d->z_loss;
+  ADAPM_CUDA(launch_chained(true, head_final_kernel, (unsigned)((d->tokens + 31) / 32), 256, 0, s, f));
+  return ADAPM_OK;
+}
+
+extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hidden, const void* weight, const int64_t* targets, const float* lse,
+                                        const float* dloss, float scale, void* dhidden, void* dweight, void* scratch, size_t scratch_bytes,
+                                        adapm_stream stream) {
+  if (!d) return ADAPM_EINVAL;
+  Layout l;
+  int rc = plan(*d, true, l);
+  if (rc != ADAPM_OK) return rc;
+  if (!dhidden && !dweight) return ADAPM_EINVAL;
+  cudaStream_t s = (cudaStream_t)stream;
+  if ((uintptr_t)hidden % 16 || (uintptr_t)weight % 16 || (uintptr_t)targets % 8 || (uintptr_t)lse % 4 || (uintptr_t)dloss % 4 ||
+      (uintptr_t)dhidden % 16 || (uintptr_t)dweight % 16 || (uintptr_t)scratch % 256) return ADAPM_EALIGN;
+  const int64_t dw_row = d->weight_ld * type_bytes(d->dweight_dtype);
+  int device, pairs;
+  if (d->tokens == 0) {                        // no token: the gradient of the weight is zero
+    if (!dweight || d->accumulate) return ADAPM_OK;
+    rc = check_on_this_device({dweight}, &device);
+    if (rc != ADAPM_OK) return rc;
+    ADAPM_CUDA(cudaMemset2DAsync(dweight, (size_t)dw_row, 0, (size_t)(d->hidden * type_bytes(d->dweight_dtype)), (size_t)d->vocab, s));
+    return ADAPM_OK;
+  }
+  if (!hidden || !weight || !targets || !lse || !scratch) return ADAPM_EINVAL;
+  if (scratch_bytes < (size_t)l.bytes) return ADAPM_ENOWORKSPACE;
+  const int64_t h_bytes = d->tokens * d->hidden_ld * 2, w_bytes = d->vocab * d->weight_ld * 2;
+  const int64_t dh_bytes = d->tokens * d->hidden_ld * type_bytes(d->dhidden_dtype), dw_bytes = d->vocab * dw_row;
+  if (overlap(hidden, h_bytes, dhidden, dh_bytes) || overlap(hidden, h_bytes, dweight, dw_bytes) || overlap(weight, w_bytes, dhidden, dh_bytes) ||
+      overlap(weight, w_bytes, dweight, dw_bytes) || overlap(dhidden, dh_bytes, dweight, dw_bytes)) {
+    set_error_text("adapm_head_loss_backward: a gradient overlaps an input or the other gradient");
+    return ADAPM_EINVAL;
+  }
+  rc = check_on_this_device({hidden, weight, targets, lse, dloss, dhidden, dweight, scratch}, &device);
+  if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
+  if (rc != ADAPM_OK) return rc;
+  char* const base = static_cast<char*>(scratch);
+
+  HeadArgs a;
+  std::memset(&a, 0, sizeof(a));
+  uint16_t* const g = (uint16_t*)(base + l.g);
+  const int64_t g_rows = l.n_buf * l.planes * l.t_pad;
+  if (!maps_of_operands(a, *d, hidden, weight, base + l.compact, l.t_pad) || !encode_bf16_matrix(&a.gk, g, g_rows, l.piece, l.piece, 128) ||
+      !encode_bf16_matrix(&a.gn, g, g_rows, l.piece, l.piece, 64)) {
+    set_error_text("cuTensorMapEncodeTiled failed for the head");
+    return ADAPM_ECUDA;
+  }
+  a.head = (int32_t*)base;
+  a.token = (int32_t*)(base + l.token); a.target = (int32_t*)(base + l.target);
+  a.lse = (float*)(base + l.lse); a.dloss = dloss ? (float*)(base + l.dloss) : nullptr;
+  a.g = g; a.dh_acc = (float*)(base + l.dh_acc); a.dh = dhidden; a.dw = dweight;
+  a.hidden_ld = d->hidden_ld; a.weight_ld = d->weight_ld;
+  a.tokens = (int32_t)d->tokens; a.vocab = (int32_t)d->vocab; a.hidden = (int32_t)d->hidden; a.t_pad = (int32_t)l.t_pad; a.piece = (int32_t)l.piece;
+  a.planes = (int32_t)l.planes;
+  a.dh_f32 = d->dhidden_dtype == ADAPM_TYPE_F32; a.dw_f32 = d->dweight_dtype == ADAPM_TYPE_F32;
+  a.planes_dh = a.dh_f32 ? 3 : 1; a.planes_dw = a.dw_f32 ? 3 : 1;
+  a.dh_wide = (uintptr_t)dhidden % 32 == 0 && (a.dh_f32 || d->hidden_ld % 16 == 0);
+  a.dw_wide = (uintptr_t)dweight % 32 == 0 && (a.dw_f32 || d->weight_ld % 16 == 0);
+  a.accumulate = d->accumulate != 0;
+  a.seg_dh = a.dh_f32 ? kSegF32 : kSegBf16; a.seg_dw = a.dw_f32 ? kSegF32 : kSegBf16;
+  a.scale = scale; a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
+
+  PrepareArgs p;
+  std::memset(&p, 0, sizeof(p));
+  p.targets = targets; p.hidden = (const uint16_t*)hidden; p.compact = (uint16_t*)(base + l.compact);
+  p.head = a.head; p.token = (int32_t*)(base + l.token); p.target = (int32_t*)(base + l.target);
+  p.lse_in = lse; p.lse = (float*)(base + l.lse); p.dloss_in = dloss; p.dloss = (float*)(base + l.dloss);
+  p.dh = dhidden; p.dh_f32 = a.dh_f32;
+  rc = launch_prepare(*d, p, s);
+  if (rc != ADAPM_OK) return rc;
+
+  const int64_t m_tiles = l.t_pad / kTile, nt_d = (d->hidden + kTile - 1) / kTile;
+  for (int64_t i = 0; i <= l.n_pieces; ++i) {
+    a.g_begin = (int32_t)(i * l.piece); a.g_buf = (int32_t)(i & 1);
+    a.g_cols = i < l.n_pieces ? (int32_t)std::min(l.piece, d->vocab - i * l.piece) : 0;
+    a.o_begin = (int32_t)((i - 1) * l.piece); a.o_buf = (int32_t)((i + 1) & 1);
+    a.o_cols = i > 0 ? (int32_t)std::min(l.piece, d->vocab - (i - 1) * l.piece) : 0;
+    a.first = i == 1; a.last = i == l.n_pieces;
+    const int64_t items = m_tiles * ((a.g_cols + kTile - 1) / kTile) + (a.o_cols ? (m_tiles + (a.o_cols + kTile - 1) / kTile) * nt_d : 0);
+    ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<true>, 2 * (unsigned)std::min<int64_t>(pairs, items), kHeadThreads, kHeadSmem, s, a));
+  }
+  return ADAPM_OK;
+}
+
+extern "C" int adapm_head_loss_status(const void* scratch, adapm_stream stream, int32_t* status) {
+  if (!scratch || !status) return ADAPM_EINVAL;
+  int32_t word = 0;
+  ADAPM_CUDA(cudaMemcpyAsync(&word, static_cast<const int32_t*>(scratch) + HD_STATUS, sizeof(word), cudaMemcpyDeviceToHost, (cudaStream_t)stream));
+  ADAPM_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
+  *status = word;
+  return word == 0 ? ADAPM_OK : ADAPM_EDEVICE;
+}
