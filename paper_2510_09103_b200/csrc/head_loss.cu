@@ -42,7 +42,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 // so that a long sum shrinks with its length: with the whole K in one accumulator an fp32 gradient was off by 1.3e-5 at K = 12288
 // (three planes of 4096) and by 2e-3 at K = 234222.  An item's K is therefore cut into segments, which the epilogue adds up in
 // registers, rounded to nearest; the next segment runs meanwhile in the other accumulator.
-constexpr int kSegLogits = 8, kSegF32 = 4, kSegBf16 = 64;      // stages of 64
+constexpr int kSegForward = 16, kSegLogits = 8, kSegF32 = 4, kSegBf16 = 64;      // stages of 64
 
 enum : int32_t { CLS_LOGITS = 0, CLS_DH = 1, CLS_DW = 2 };
 
@@ -69,7 +69,7 @@ struct HeadArgs {
   int32_t o_begin, o_cols, o_buf;          // piece whose gradients it makes (o_cols = 0: none)
   int32_t first, last;                     // of the pieces, for dh
   int32_t dh_f32, dw_f32, accumulate, dh_wide, dw_wide;      // wide: rows start on 32 bytes
-  int32_t seg_dh, seg_dw;                  // longest segments, in stages
+  int32_t seg_logits, seg_dh, seg_dw;      // longest segments, in stages
   float scale, smooth, z_loss;
 };
 
@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
       // per K step of 16: 32 bytes inside a K-major row, 16 rows of 128 bytes of an MN-major box (in 16-byte units)
       const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
       int left = k_stages * planes, n_seg, each;
-      segments(left, cls == CLS_LOGITS ? kSegLogits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
+      segments(left, cls == CLS_LOGITS ? a.seg_logits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
       for (; left > 0 && ok; left -= each, ++run) {
         const int acc = (int)(run & 1);
         if (!mbar_wait_warp<WAIT_PAIR_TC>(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
@@ -421,7 +421,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
       }
       float v[128];
       int n_seg, each;
-      segments(k_stages * planes, cls == CLS_LOGITS ? kSegLogits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
+      segments(k_stages * planes, cls == CLS_LOGITS ? a.seg_logits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
 #pragma unroll 1
       for (int i = 0; i < n_seg; ++i, ++run) {
         const int acc = (int)(run & 1);
@@ -796,6 +796,7 @@ extern "C" int adapm_head_loss_forward(const adapm_head_loss* d, const void* hid
   a.part = (float2*)(base + l.part); a.part_sum = (float*)(base + l.part_sum); a.z_target = (float*)(base + l.z_target);
   a.tokens = (int32_t)d->tokens; a.vocab = (int32_t)d->vocab; a.hidden = (int32_t)d->hidden; a.t_pad = (int32_t)l.t_pad;
   a.planes = a.planes_dh = a.planes_dw = 1;
+  a.seg_logits = kSegForward;
   a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
 
   PrepareArgs p;
@@ -868,6 +869,7 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   a.dh_wide = (uintptr_t)dhidden % 32 == 0 && (a.dh_f32 || d->hidden_ld % 16 == 0);
   a.dw_wide = (uintptr_t)dweight % 32 == 0 && (a.dw_f32 || d->weight_ld % 16 == 0);
   a.accumulate = d->accumulate != 0;
+  a.seg_logits = l.planes > 1 ? kSegLogits : kSegBf16;
   a.seg_dh = a.dh_f32 ? kSegF32 : kSegBf16; a.seg_dw = a.dw_f32 ? kSegF32 : kSegBf16;
   a.scale = scale; a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
 
