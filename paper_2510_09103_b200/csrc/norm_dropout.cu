@@ -21,30 +21,54 @@ constexpr int64_t kMaxCols = 32768;
 // ---- eight elements of a row -------------------------------------------------------------------------
 // VEC: the chunk starts on 16 bytes; a chunk cut by the end of the row goes element by element.  (Plain loads: an output may
 // lie on an input, and what an earlier launch wrote must not be asked for before this one may start.)
+// A chunk is held as it was read until it is used: in bf16 that is half the registers.
 template <typename T> struct Elem;
 template <> struct Elem<float> {
+  struct raw8 { float4 a, b; };
   static __device__ __forceinline__ float get(const float* p) { return *p; }
   static __device__ __forceinline__ void put(float* p, float x) { *p = x; }
-  static __device__ __forceinline__ void get8(const float* p, float* x) { load8f(p, x); }
+  static __device__ __forceinline__ raw8 load(const float* p) { return raw8{*reinterpret_cast<const float4*>(p), *(reinterpret_cast<const float4*>(p) + 1)}; }
+  static __device__ __forceinline__ raw8 zero() { return raw8{make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)}; }
+  static __device__ __forceinline__ void set(raw8& r, int e, float x) { (e < 4 ? (&r.a.x)[e] : (&r.b.x)[e - 4]) = x; }
+  static __device__ __forceinline__ void unpack(const raw8& r, float* x) {
+    x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w; x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
+  }
   static __device__ __forceinline__ void put8(float* p, const float* x) { store8f(p, x); }
 };
 template <> struct Elem<uint16_t> {
+  using raw8 = uint4;
   static __device__ __forceinline__ float get(const uint16_t* p) { return bf16_bits_to_float(*p); }
   static __device__ __forceinline__ void put(uint16_t* p, float x) { *p = (uint16_t)pack_bf16x2(x, 0.f); }
-  static __device__ __forceinline__ void get8(const uint16_t* p, float* x) { GradBF16::unpack(*reinterpret_cast<const uint4*>(p), x); }
+  static __device__ __forceinline__ raw8 load(const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); }
+  static __device__ __forceinline__ raw8 zero() { return make_uint4(0, 0, 0, 0); }
+  static __device__ __forceinline__ void set(raw8& r, int e, float x) {      // (x is a bf16 number)
+    uint32_t& w = (&r.x)[e >> 1];
+    w |= e & 1 ? __float_as_uint(x) & 0xffff0000u : __float_as_uint(x) >> 16;
+  }
+  static __device__ __forceinline__ void unpack(const raw8& r, float* x) { GradBF16::unpack(r, x); }
   static __device__ __forceinline__ void put8(uint16_t* p, const float* x) {
     *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
   }
 };
 
+// Up to eight elements, of which n exist (n <= 0: none); the others are zero.
+template <bool VEC, typename T>
+__device__ __forceinline__ typename Elem<T>::raw8 fetch8(const T* p, int n) {
+  if (VEC && n >= 8) return Elem<T>::load(p);
+  typename Elem<T>::raw8 r = Elem<T>::zero();
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) Elem<T>::set(r, e, Elem<T>::get(p + e));
+  return r;
+}
 template <bool VEC, typename T>
 __device__ __forceinline__ void load8(const T* p, int n, float* x) {
-  if (VEC && n >= 8) {
-    Elem<T>::get8(p, x);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < n ? Elem<T>::get(p + e) : 0.f;
-  }
+  Elem<T>::unpack(fetch8<VEC>(p, n), x);
+}
+template <bool VEC>
+__device__ __forceinline__ void load_weight8(const void* w, int f32, int at, int n, float* x) {
+  if (f32) load8<VEC>(static_cast<const float*>(w) + at, n, x);
+  else load8<VEC>(static_cast<const uint16_t*>(w) + at, n, x);
 }
 template <bool VEC, typename T>
 __device__ __forceinline__ void store8(T* p, int n, const float* x) {
@@ -59,46 +83,57 @@ __device__ __forceinline__ void store8(T* p, int n, const float* x) {
 
 // ---- dropout -------------------------------------------------------------------------------------------
 
+constexpr int kDropUnits = 2;      // groups of eight per thread
+
 struct DropArgs {
   const void* x;
   const void* residual;
   void* y;
-  int64_t x_ld, r_ld, y_ld, rows, cols, groups, total;     // groups of eight columns per row, and in all
+  int64_t x_ld, r_ld, y_ld, cols, groups, total;     // groups of eight columns per row, and in all
   DropRule drop;
 };
 
-template <typename T, bool VEC>
+// DENSE: the rows lie one behind the other and hold whole groups, so that group i is at element 8 i.
+template <typename T, bool VEC, bool DENSE>
 __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a) {
   wait_for_previous_kernel();
   const DropKey key = drop_key(a.drop);
   const T* const x = static_cast<const T*>(a.x);
   const T* const res = static_cast<const T*>(a.residual);
   T* const y = static_cast<T*>(a.y);
-  const int64_t stride = (int64_t)gridDim.x * 256;
-  for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < a.total; i0 += 2 * stride) {
-    float v[2][8], r[2][8];
-    int64_t row[2], col[2];
+  typename Elem<T>::raw8 xs[kDropUnits], rs[kDropUnits];
+  int64_t out[kDropUnits];
+  int n[kDropUnits];
+  const int64_t i0 = (int64_t)blockIdx.x * (256 * kDropUnits) + threadIdx.x;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t i = i0 + u * stride;
-      if (i >= a.total) continue;
-      row[u] = a.total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)a.groups) : i / a.groups;
-      col[u] = (i - row[u] * a.groups) * 8;
-      const int n = (int)min((int64_t)8, a.cols - col[u]);
-      load8<VEC>(x + row[u] * a.x_ld + col[u], n, v[u]);
-      if (res) load8<VEC>(res + row[u] * a.r_ld + col[u], n, r[u]);
+  for (int u = 0; u < kDropUnits; ++u) {
+    const int64_t i = i0 + u * 256;
+    n[u] = 0;
+    if (i >= a.total) continue;
+    int64_t row = 0, col = i * 8;
+    n[u] = 8;
+    if (!DENSE) {
+      row = a.total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)a.groups) : i / a.groups;
+      col = (i - row * a.groups) * 8;
+      n[u] = (int)min((int64_t)8, a.cols - col);
     }
+    xs[u] = fetch8<VEC>(x + row * a.x_ld + col, n[u]);
+    if (res) rs[u] = fetch8<VEC>(res + row * a.r_ld + col, n[u]);
+    out[u] = row * a.y_ld + col;
+  }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t i = i0 + u * stride;
-      if (i >= a.total) continue;
-      if (a.drop.least) drop8(a.drop, key, (uint64_t)i, v[u]);
-      if (res) {
+  for (int u = 0; u < kDropUnits; ++u) {
+    if (n[u] == 0) continue;
+    float v[8];
+    Elem<T>::unpack(xs[u], v);
+    if (a.drop.mode) drop8(a.drop, key, (uint64_t)(i0 + u * 256), v);
+    if (res) {
+      float r[8];
+      Elem<T>::unpack(rs[u], r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] += r[u][e];
-      }
-      store8<VEC>(y + row[u] * a.y_ld + col[u], (int)min((int64_t)8, a.cols - col[u]), v[u]);
+      for (int e = 0; e < 8; ++e) v[e] += r[e];
     }
+    store8<VEC>(y + out[u], n[u], v);
   }
 }
 
@@ -144,7 +179,7 @@ struct NormArgs {
   float* scales;
   float* rstd;
   int64_t x_ld, r_ld, s_ld, y_ld, y8_ld, rows;
-  int32_t cols, groups, q8_group, n_scales;
+  int32_t cols, groups, q8_group, n_scales, weight_f32;
   float eps;
   DropRule drop;
 };
@@ -157,7 +192,7 @@ __device__ __forceinline__ uint32_t pack_e4m3x4(const float* x) {
 }
 
 // s stays in 32 bits for the statistic and the output and is rounded only where it is stored.
-template <typename T, typename W, int NC, bool WARP, bool VEC>
+template <typename T, int NC, bool WARP, bool VEC, bool DROP>
 __global__ void __launch_bounds__(WARP ? 128 : NC == 4 ? 1024 : 512) rmsnorm_forward_kernel(const NormArgs a) {
   __shared__ float red[2][32];
   wait_for_previous_kernel();
@@ -168,29 +203,29 @@ __global__ void __launch_bounds__(WARP ? 128 : NC == 4 ? 1024 : 512) rmsnorm_for
   const T* const res = a.residual ? static_cast<const T*>(a.residual) + row * a.r_ld : nullptr;
   T* const sum = a.sum ? static_cast<T*>(a.sum) + row * a.s_ld : nullptr;
   T* const y = a.y ? static_cast<T*>(a.y) + row * a.y_ld : nullptr;
-  const W* const weight = static_cast<const W*>(a.weight);
-  float s[NC][8], r[NC][8];
+  typename Elem<T>::raw8 xs[NC], rs[NC];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const int g = me + i * team;
+    xs[i] = rs[i] = Elem<T>::zero();
     if (g < a.groups) {
-      load8<VEC>(x + 8 * g, a.cols - 8 * g, s[i]);
-      if (res) load8<VEC>(res + 8 * g, a.cols - 8 * g, r[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[i][e] = 0.f;
+      xs[i] = fetch8<VEC>(x + 8 * g, a.cols - 8 * g);
+      if (res) rs[i] = fetch8<VEC>(res + 8 * g, a.cols - 8 * g);
     }
   }
-  float sq = 0.f;
-  const DropKey key = drop_key(a.drop);
+  float s[NC][8], sq = 0.f;
+  const DropKey key = DROP ? drop_key(a.drop) : DropKey{0, 0};
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const int g = me + i * team;
+    Elem<T>::unpack(xs[i], s[i]);
     if (g < a.groups) {
-      if (a.drop.least) drop8(a.drop, key, (uint64_t)row * a.groups + g, s[i]);
+      if (DROP) drop8(a.drop, key, (uint64_t)row * a.groups + g, s[i]);
       if (res) {
+        float r[8];
+        Elem<T>::unpack(rs[i], r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[i][e] += r[i][e];
+        for (int e = 0; e < 8; ++e) s[i][e] += r[e];
       }
       if (sum) store8<VEC>(sum + 8 * g, a.cols - 8 * g, s[i]);
 #pragma unroll
@@ -205,14 +240,15 @@ __global__ void __launch_bounds__(WARP ? 128 : NC == 4 ? 1024 : 512) rmsnorm_for
     const int g = me + i * team;
     if (g < a.groups) {
       float w[8];
-      load8<VEC>(weight + 8 * g, a.cols - 8 * g, w);
+      load_weight8<VEC>(a.weight, a.weight_f32, 8 * g, a.cols - 8 * g, w);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[i][e] = s[i][e] * rstd * w[e];
       if (y) store8<VEC>(y + 8 * g, a.cols - 8 * g, s[i]);
     }
+    if (!a.y8) continue;
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(s[i][e]));
-    if (a.y8 && a.q8_group) {                      // a group of 128 columns: sixteen neighbouring lanes
+    if (a.q8_group) {                              // a group of 128 columns: sixteen neighbouring lanes
       float m = top;
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -263,78 +299,119 @@ struct NormGradArgs {
   void* dx;
   float* partial;                // [CTAs][cols], or null: no gradient of the weight
   int64_t dy_ld, s_ld, r_ld, x_ld, rows;
-  int32_t cols, groups;
+  int32_t cols, groups, weight_f32;
   DropRule drop;
 };
 
-// A CTA takes rows blockIdx, blockIdx + grid, ...; a thread has the same columns in each, whose share of dw it keeps.  NC = 4
-// (rows above 8192 columns): dw alone fills the registers, so the row is read a second time, out of L2.
-template <typename T, typename W, int NC, bool VEC>
+// Two fp32 operations per instruction (the same roundings as one at a time).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+
+// A CTA takes row after row; a thread has the same columns in each, whose share of dw it keeps.  The next row's elements are
+// on their way while a row is worked on.  NC = 4 (rows above 8192 columns): dw alone fills the registers, so a row is read a
+// second time, out of L2.
+template <typename T, int NC, bool VEC, bool DROP>
 __global__ void __launch_bounds__(NC == 1 ? 256 : NC == 2 ? 512 : 1024) rmsnorm_backward_kernel(const NormGradArgs a) {
+  using E = Elem<T>;
   constexpr bool kTwice = NC == 4;
   constexpr int kHeld = kTwice ? 1 : NC;
   __shared__ float red[2][32];
   wait_for_previous_kernel();
   const int team = (int)blockDim.x, me = (int)threadIdx.x;
-  const W* const weight = static_cast<const W*>(a.weight);
-  const DropKey key = drop_key(a.drop);
-  float w[kHeld][8], dw[NC][8];
+  const DropKey key = DROP ? drop_key(a.drop) : DropKey{0, 0};
+  typename E::raw8 dys[kHeld], ss[kHeld], more[kHeld];
+  float w[kHeld][8];
+  float2 dw[NC][4];
+  auto fetch = [&](int i, int64_t row, bool with_more) {
+    const int g = me + i * team, n = g < a.groups ? a.cols - 8 * g : 0;
+    dys[i % kHeld] = fetch8<VEC>(static_cast<const T*>(a.dy) + row * a.dy_ld + 8 * g, n);
+    ss[i % kHeld] = fetch8<VEC>(static_cast<const T*>(a.sum) + row * a.s_ld + 8 * g, n);
+    if (kTwice) load_weight8<VEC>(a.weight, a.weight_f32, 8 * g, n, w[0]);
+    if (with_more) more[i % kHeld] = a.dsum ? fetch8<VEC>(static_cast<const T*>(a.dsum) + row * a.s_ld + 8 * g, n) : E::zero();
+  };
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const int g = me + i * team;
-    if (!kTwice) load8<VEC>(weight + 8 * g, g < a.groups ? a.cols - 8 * g : 0, w[i % kHeld]);
+    if (!kTwice) {
+      load_weight8<VEC>(a.weight, a.weight_f32, 8 * g, g < a.groups ? a.cols - 8 * g : 0, w[i % kHeld]);
+      fetch(i, blockIdx.x, true);
+    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) dw[i][e] = 0.f;
+    for (int e = 0; e < 4; ++e) dw[i][e] = make_float2(0.f, 0.f);
   }
+  float rstd_next = a.rstd[blockIdx.x];
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-    const T* const dy = static_cast<const T*>(a.dy) + row * a.dy_ld;
-    const T* const s = static_cast<const T*>(a.sum) + row * a.s_ld;
-    const T* const ds_in = a.dsum ? static_cast<const T*>(a.dsum) + row * a.s_ld : nullptr;
-    const float rstd = a.rstd[row];
-    float g8[kHeld][8], xh[kHeld][8], more[kHeld][8], c = 0.f;
-    auto fetch = [&](int i, bool with_more) {
-      const int g = me + i * team, n = g < a.groups ? a.cols - 8 * g : 0;
-      load8<VEC>(dy + 8 * g, n, g8[i % kHeld]);
-      load8<VEC>(s + 8 * g, n, xh[i % kHeld]);
-      if (kTwice) load8<VEC>(weight + 8 * g, n, w[0]);
-      if (with_more && ds_in) load8<VEC>(ds_in + 8 * g, n, more[i % kHeld]);
-    };
-    if (!kTwice) {
-#pragma unroll
-      for (int i = 0; i < NC; ++i) fetch(i, true);
-    }
+    const int64_t next = row + gridDim.x;
+    const float rstd = rstd_next;
+    const float2 rstd2 = make_float2(rstd, rstd);
+    // with g = rstd dy w: mean(dy w xh) = sum(g s) / cols, ds = g - s (rstd^2 sum(g s) / cols) + dsum
+    float2 g8[kHeld][4], s8[kHeld][4], extra[kHeld][4], c2 = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      if (kTwice) fetch(i, false);
+      if (kTwice) fetch(i, row, false);
+      const int h = i % kHeld;
+      float dy[8], sv[8], ev[8];
+      E::unpack(dys[h], dy);
+      E::unpack(ss[h], sv);
+      if (!kTwice) E::unpack(more[h], ev);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float &g = g8[i % kHeld][e], &x = xh[i % kHeld][e];
-        x *= rstd;
-        dw[i][e] = fmaf(g, x, dw[i][e]);
-        g *= w[i % kHeld][e];
-        c = fmaf(g, x, c);
+      for (int e = 0; e < 4; ++e) {
+        const float2 d = mul2(make_float2(dy[2 * e], dy[2 * e + 1]), rstd2);
+        s8[h][e] = make_float2(sv[2 * e], sv[2 * e + 1]);
+        if (!kTwice) extra[h][e] = make_float2(ev[2 * e], ev[2 * e + 1]);
+        dw[i][e] = fma2(d, s8[h][e], dw[i][e]);
+        g8[h][e] = mul2(d, make_float2(w[h][2 * e], w[h][2 * e + 1]));
+        c2 = fma2(g8[h][e], s8[h][e], c2);
       }
     }
-    c = row_sum<false>(c, red[turn]) / (float)a.cols;
+    if (next < a.rows) {
+      rstd_next = a.rstd[next];
+      if (!kTwice) {
+#pragma unroll
+        for (int i = 0; i < NC; ++i) fetch(i, next, true);
+      }
+    }
+    const float c = row_sum<false>(c2.x + c2.y, red[turn]) * (rstd * rstd) / (float)a.cols;
+    const float2 minus = make_float2(-c, -c);
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int g = me + i * team, n = a.cols - 8 * g, h = i % kHeld;
       if (g >= a.groups) continue;
       if (kTwice) {
-        fetch(i, true);
+        fetch(i, row, true);
+        float dy[8], sv[8], ev[8];
+        E::unpack(dys[h], dy);
+        E::unpack(ss[h], sv);
+        E::unpack(more[h], ev);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) { xh[h][e] *= rstd; g8[h][e] *= w[h][e]; }
+        for (int e = 0; e < 4; ++e) {
+          s8[h][e] = make_float2(sv[2 * e], sv[2 * e + 1]);
+          extra[h][e] = make_float2(ev[2 * e], ev[2 * e + 1]);
+          g8[h][e] = mul2(mul2(make_float2(dy[2 * e], dy[2 * e + 1]), rstd2), make_float2(w[h][2 * e], w[h][2 * e + 1]));
+        }
       }
+      float ds[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        g8[h][e] = rstd * fmaf(-xh[h][e], c, g8[h][e]);
-        if (ds_in) g8[h][e] += more[h][e];
+      for (int e = 0; e < 4; ++e) {
+        const float2 d = fma2(s8[h][e], minus, g8[h][e]);
+        ds[2 * e] = d.x + extra[h][e].x;
+        ds[2 * e + 1] = d.y + extra[h][e].y;
       }
-      if (a.dres) store8<VEC>(static_cast<T*>(a.dres) + row * a.r_ld + 8 * g, n, g8[h]);
+      if (a.dres) store8<VEC>(static_cast<T*>(a.dres) + row * a.r_ld + 8 * g, n, ds);
       if (a.dx) {
-        if (a.drop.least) drop8(a.drop, key, (uint64_t)row * a.groups + g, g8[h]);
-        store8<VEC>(static_cast<T*>(a.dx) + row * a.x_ld + 8 * g, n, g8[h]);
+        if (DROP) drop8(a.drop, key, (uint64_t)row * a.groups + g, ds);
+        store8<VEC>(static_cast<T*>(a.dx) + row * a.x_ld + 8 * g, n, ds);
       }
     }
   }
@@ -342,7 +419,10 @@ __global__ void __launch_bounds__(NC == 1 ? 256 : NC == 2 ? 512 : 1024) rmsnorm_
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const int g = me + i * team;
-    if (g < a.groups) store8<false>(a.partial + (int64_t)blockIdx.x * a.cols + 8 * g, a.cols - 8 * g, dw[i]);
+    float out[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { out[2 * e] = dw[i][e].x; out[2 * e + 1] = dw[i][e].y; }
+    if (g < a.groups) store8<false>(a.partial + (int64_t)blockIdx.x * a.cols + 8 * g, a.cols - 8 * g, out);
   }
 }
 
@@ -373,8 +453,10 @@ __global__ void __launch_bounds__(1024) column_sum_kernel(const float* partial, 
 
 int drop_rule(float p, uint64_t seed, uint64_t offset, const uint64_t* step, DropRule& d) {
   if (!(p >= 0.f && p <= 1.f)) return ADAPM_ERANGE;
-  d.least = (uint32_t)std::lrint((double)p * 65536.0);
-  d.factor = d.least >= 65536u ? 0.f : (float)(65536.0 / (65536.0 - d.least));
+  const uint32_t least = (uint32_t)std::lrint((double)p * 65536.0);
+  d.cut = least << 16;
+  d.mode = least == 0 ? 0u : least < 65536u ? 1u : 2u;
+  d.factor = d.mode == 2 ? 0.f : (float)(65536.0 / (65536.0 - least));
   d.seed_lo = (uint32_t)seed; d.seed_hi = (uint32_t)(seed >> 32);
   d.offset = offset; d.step = step;
   return ADAPM_OK;
@@ -413,46 +495,49 @@ int sm_count(int device, int* sms) {
 // Threads of a CTA that has `groups` chunks of a row, nc at most per thread.
 unsigned threads_for(int64_t groups, int nc) { return (unsigned)(((groups + nc - 1) / nc + 31) / 32 * 32); }
 
-template <typename T, typename W, bool VEC>
+template <typename T, int NC, bool WARP, bool VEC, bool DROP>
+cudaError_t forward_launch(const NormArgs& a, cudaStream_t s) {
+  return launch_chained(true, rmsnorm_forward_kernel<T, NC, WARP, VEC, DROP>, (unsigned)(WARP ? (a.rows + 3) / 4 : a.rows),
+                        WARP ? 128u : threads_for(a.groups, NC), 0, s, a);
+}
+
+// A warp per row up to 512 columns, else a CTA, with two chunks of eight per thread, where there are rows for all SMs; one chunk
+// per thread where there are few (a row then takes less time).  Two reads and two writes of 67 MB each, bf16: 65536 x 512 42 us
+// (a CTA per row: 69), 32768 x 1024 43 (warp 44, one chunk 45), 16384 x 2048 42 (one chunk 46), 8192 x 4096 43 (one chunk 48):
+// 0.95 of the copy rate.  CTAs that take row after row with the next row's elements on their way: 45 to 48.
+template <typename T, bool VEC, bool DROP>
 cudaError_t forward_form(const NormArgs& a, int sms, cudaStream_t s) {
-#define ADAPM_WARP(NC) return launch_chained(true, rmsnorm_forward_kernel<T, W, NC, true, VEC>, (unsigned)((a.rows + 3) / 4), 128, 0, s, a)
-#define ADAPM_CTA(NC) return launch_chained(true, rmsnorm_forward_kernel<T, W, NC, false, VEC>, (unsigned)a.rows, threads_for(a.groups, NC), 0, s, a)
-  // a warp per row where that keeps all SMs busy, else as many threads per row as there are chunks
-  if (a.groups <= 256 && a.rows >= 16 * (int64_t)sms) {
-    if (a.groups <= 32) ADAPM_WARP(1);
-    if (a.groups <= 64) ADAPM_WARP(2);
-    if (a.groups <= 128) ADAPM_WARP(4);
-    ADAPM_WARP(8);
+  if (VEC) {
+    const bool many = a.rows >= 8 * (int64_t)sms;
+    if (many && a.groups <= 32) return forward_launch<T, 1, true, VEC, DROP>(a, s);
+    if (many && a.groups <= 64) return forward_launch<T, 2, true, VEC, DROP>(a, s);
+    if (!many && a.groups <= 512) return forward_launch<T, 1, false, VEC, DROP>(a, s);
+    if (a.groups <= 1024) return forward_launch<T, 2, false, VEC, DROP>(a, s);
+  } else if (a.groups <= 512) {
+    return forward_launch<T, 1, false, VEC, DROP>(a, s);
   }
-  if (a.groups <= 512) ADAPM_CTA(1);
-  if (a.groups <= 1024) ADAPM_CTA(2);
-  ADAPM_CTA(4);
-#undef ADAPM_WARP
-#undef ADAPM_CTA
+  return forward_launch<T, 4, false, VEC, DROP>(a, s);
 }
 
 struct GradForm { int nc; unsigned threads; int ctas; };
-// One chunk per thread up to 256 threads, then two, then four; as many CTAs as fit.
+// Two chunks of eight per thread where there are rows for all SMs (16384 rows of 1600 in bf16 with dropout 63 us, one chunk per
+// thread 69), one where there are few (a row then takes less time), four above 8192 columns.  As many CTAs as the registers of
+// an SM hold at once: with four of 128 threads 63 us, three 80, five 84 (the fifth waits for one of the four to end).
 GradForm grad_form(int64_t rows, int64_t groups, int sms) {
   GradForm f;
-  f.nc = groups <= 256 ? 1 : groups <= 1024 ? 2 : 4;
+  f.nc = groups > 1024 ? 4 : groups > 256 || rows >= 4 * (int64_t)sms ? 2 : 1;
   f.threads = threads_for(groups, f.nc);
-  f.ctas = (int)std::min<int64_t>(rows, (int64_t)sms * std::max(1, 1024 / (int)f.threads));
+  const int per = std::max(1, (f.nc == 4 ? 1024 : 512) / (int)f.threads);
+  f.ctas = (int)std::min<int64_t>(rows, (int64_t)sms * per);
   return f;
 }
 
-template <typename T, typename W, bool VEC>
+template <typename T, bool VEC, bool DROP>
 cudaError_t backward_form(const NormGradArgs& a, const GradForm& f, cudaStream_t s) {
-  if (f.nc == 1) return launch_chained(true, rmsnorm_backward_kernel<T, W, 1, VEC>, (unsigned)f.ctas, f.threads, 0, s, a);
-  if (f.nc == 2) return launch_chained(true, rmsnorm_backward_kernel<T, W, 2, VEC>, (unsigned)f.ctas, f.threads, 0, s, a);
-  return launch_chained(true, rmsnorm_backward_kernel<T, W, 4, VEC>, (unsigned)f.ctas, f.threads, 0, s, a);
+  if (f.nc == 1) return launch_chained(true, rmsnorm_backward_kernel<T, 1, VEC, DROP>, (unsigned)f.ctas, f.threads, 0, s, a);
+  if (f.nc == 2) return launch_chained(true, rmsnorm_backward_kernel<T, 2, VEC, DROP>, (unsigned)f.ctas, f.threads, 0, s, a);
+  return launch_chained(true, rmsnorm_backward_kernel<T, 4, VEC, DROP>, (unsigned)f.ctas, f.threads, 0, s, a);
 }
-
-#define ADAPM_FORMS(F, vec, t, w, ...)                                                                          \
-  ((vec) ? ((t) == ADAPM_TYPE_F32 ? ((w) == ADAPM_TYPE_F32 ? F<float, float, true>(__VA_ARGS__) : F<float, uint16_t, true>(__VA_ARGS__))          \
-                                  : ((w) == ADAPM_TYPE_F32 ? F<uint16_t, float, true>(__VA_ARGS__) : F<uint16_t, uint16_t, true>(__VA_ARGS__)))   \
-         : ((t) == ADAPM_TYPE_F32 ? ((w) == ADAPM_TYPE_F32 ? F<float, float, false>(__VA_ARGS__) : F<float, uint16_t, false>(__VA_ARGS__))        \
-                                  : ((w) == ADAPM_TYPE_F32 ? F<uint16_t, float, false>(__VA_ARGS__) : F<uint16_t, uint16_t, false>(__VA_ARGS__))))
 
 }  // namespace
 }  // namespace adapm
@@ -473,18 +558,22 @@ extern "C" int adapm_dropout(const void* x, const void* residual, void* y, int32
   rc = check_rows({{x, x_ld, eb}, {residual, residual_ld, eb}, {y, y_ld, eb}}, rows, cols, vec);
   if (rc != ADAPM_OK) return rc;
   if ((uintptr_t)step % 8) return ADAPM_EALIGN;
-  int device, sms;
+  int device;
   rc = check_on_this_device({x, residual, y, step}, &device);
-  if (rc == ADAPM_OK) rc = sm_count(device, &sms);
   if (rc != ADAPM_OK) return rc;
   a.x = x; a.residual = residual; a.y = y;
-  a.x_ld = x_ld; a.r_ld = residual_ld; a.y_ld = y_ld; a.rows = rows; a.cols = cols;
+  a.x_ld = x_ld; a.r_ld = residual_ld; a.y_ld = y_ld; a.cols = cols;
   a.groups = (cols + 7) / 8; a.total = rows * a.groups;
   cudaStream_t s = (cudaStream_t)stream;
-  const unsigned grid = (unsigned)std::min<int64_t>((a.total + 511) / 512, (int64_t)sms * 64);
-  const bool f32 = dtype == ADAPM_TYPE_F32;
-  ADAPM_CUDA(f32 ? (vec ? launch_chained(true, dropout_kernel<float, true>, grid, 256, 0, s, a) : launch_chained(true, dropout_kernel<float, false>, grid, 256, 0, s, a))
-                 : (vec ? launch_chained(true, dropout_kernel<uint16_t, true>, grid, 256, 0, s, a) : launch_chained(true, dropout_kernel<uint16_t, false>, grid, 256, 0, s, a)));
+  if (a.total > (int64_t)INT32_MAX * (256 * kDropUnits)) return ADAPM_ERANGE;
+  const unsigned grid = (unsigned)((a.total + 256 * kDropUnits - 1) / (256 * kDropUnits));
+  const bool dense = vec && cols % 8 == 0 && x_ld == cols && y_ld == cols && (!residual || residual_ld == cols);
+#define ADAPM_DROP(T)                                                                                                \
+  (dense ? launch_chained(true, dropout_kernel<T, true, true>, grid, 256, 0, s, a)                                   \
+         : vec ? launch_chained(true, dropout_kernel<T, true, false>, grid, 256, 0, s, a)                            \
+               : launch_chained(true, dropout_kernel<T, false, false>, grid, 256, 0, s, a))
+  ADAPM_CUDA(dtype == ADAPM_TYPE_F32 ? ADAPM_DROP(float) : ADAPM_DROP(uint16_t));
+#undef ADAPM_DROP
   return ADAPM_OK;
 }
 
@@ -515,7 +604,14 @@ extern "C" int adapm_rmsnorm_forward(const adapm_rmsnorm* d, const void* x, cons
   a.cols = (int32_t)d->cols; a.groups = (int32_t)((d->cols + 7) / 8); a.q8_group = d->q8_group;
   a.n_scales = d->q8_group ? (int32_t)((d->cols + 127) / 128) : 1;
   a.eps = d->eps;
-  ADAPM_CUDA(ADAPM_FORMS(forward_form, vec, d->dtype, d->weight_dtype, a, sms, (cudaStream_t)stream));
+  a.weight_f32 = d->weight_dtype == ADAPM_TYPE_F32;
+  const bool f32 = d->dtype == ADAPM_TYPE_F32;
+  cudaStream_t s = (cudaStream_t)stream;
+#define ADAPM_NORM(DROP)                                                                                             \
+  (vec ? (f32 ? forward_form<float, true, DROP>(a, sms, s) : forward_form<uint16_t, true, DROP>(a, sms, s))          \
+       : (f32 ? forward_form<float, false, DROP>(a, sms, s) : forward_form<uint16_t, false, DROP>(a, sms, s)))
+  ADAPM_CUDA(a.drop.mode ? ADAPM_NORM(true) : ADAPM_NORM(false));
+#undef ADAPM_NORM
   return ADAPM_OK;
 }
 
@@ -523,8 +619,11 @@ extern "C" size_t adapm_rmsnorm_backward_scratch_bytes(const adapm_rmsnorm* d) {
   DropRule drop;
   if (!d || check_desc(*d, drop) != ADAPM_OK) return 0;
   // the largest grid of any row length, on a device of up to 256 SMs
-  const GradForm f = grad_form(std::max<int64_t>(d->rows, 1), (d->cols + 7) / 8, 256);
-  return (size_t)round_up((int64_t)f.ctas * d->cols * 4, 256);
+  // The number of SMs is not known here.  256 at most are used, and there are never more CTAs than this many or than rows.
+  const int64_t groups = (d->cols + 7) / 8;
+  const int64_t per = groups > 1024 ? 1024 / threads_for(groups, 4) : std::max<int64_t>(1, 512 / threads_for(groups, 2));
+  const int64_t ctas = std::min<int64_t>(std::max<int64_t>(d->rows, 1), 256 * per);
+  return (size_t)round_up(ctas * d->cols * 4, 256);
 }
 
 extern "C" int adapm_rmsnorm_backward(const adapm_rmsnorm* d, const void* dy, const void* dsum, const void* sum, const float* rstd,
@@ -572,7 +671,13 @@ extern "C" int adapm_rmsnorm_backward(const adapm_rmsnorm* d, const void* dy, co
   a.dy_ld = d->y_ld; a.s_ld = d->sum_ld; a.r_ld = d->residual_ld; a.x_ld = d->x_ld; a.rows = d->rows;
   a.cols = (int32_t)d->cols; a.groups = (int32_t)((d->cols + 7) / 8);
   const GradForm f = grad_form(d->rows, a.groups, std::min(sms, 256));
-  ADAPM_CUDA(ADAPM_FORMS(backward_form, vec, d->dtype, d->weight_dtype, a, f, s));
+  a.weight_f32 = d->weight_dtype == ADAPM_TYPE_F32;
+  const bool f32 = d->dtype == ADAPM_TYPE_F32;
+#define ADAPM_NORM(DROP)                                                                                             \
+  (vec ? (f32 ? backward_form<float, true, DROP>(a, f, s) : backward_form<uint16_t, true, DROP>(a, f, s))            \
+       : (f32 ? backward_form<float, false, DROP>(a, f, s) : backward_form<uint16_t, false, DROP>(a, f, s)))
+  ADAPM_CUDA(a.drop.mode ? ADAPM_NORM(true) : ADAPM_NORM(false));
+#undef ADAPM_NORM
   if (!dweight) return ADAPM_OK;
   const unsigned grid = (unsigned)((d->cols + 31) / 32);
   ADAPM_CUDA(dweight_dtype == ADAPM_TYPE_F32

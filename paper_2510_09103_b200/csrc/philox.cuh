@@ -23,11 +23,12 @@ __host__ __device__ __forceinline__ Philox4 philox4x32_10(uint32_t c0, uint32_t 
   return Philox4{{c0, c1, c2, c3}};
 }
 
-// Dropout of one call: elements whose 16 bits are below `least` become zero, the others are multiplied by `factor`.
-// 16 bits: p is taken to the nearest multiple of 2^-16 (1.5e-5 at p = 0.1 in the worst case, relative), and the factor is the
-// one that belongs to that multiple, so that the expectation is kept.
+// Dropout of one call: elements whose 16 bits are below `least` = rint(65536 p) become zero, the others are multiplied by `factor`.
+// 16 bits: p is taken to the nearest multiple of 2^-16 (7.6e-6 at most), and the factor is the one that belongs to that
+// multiple, so that the expectation is kept.
 struct DropRule {
-  uint32_t least;              // 0: nothing is dropped; 65536: everything
+  uint32_t cut;                // least << 16
+  uint32_t mode;               // 0: nothing is dropped, 1: by the generator, 2: everything (least = 65536)
   float factor;
   uint32_t seed_lo, seed_hi;
   uint64_t offset;
@@ -41,12 +42,17 @@ __device__ __forceinline__ DropKey drop_key(const DropRule& d) {
   return DropKey{(uint32_t)off, (uint32_t)(off >> 32)};
 }
 // Eight elements of group `q` = row * ceil(cols / 8) + column / 8.  Dropped elements are zero whatever they held.
+// (The upper 16 bits are compared in place, below the cut's zeros; the lower ones after a shift.)
 __device__ __forceinline__ void drop8(const DropRule& d, const DropKey& k, uint64_t q, float* x) {
   const Philox4 r = philox4x32_10((uint32_t)q, (uint32_t)(q >> 32), k.off_lo, k.off_hi, d.seed_lo, d.seed_hi);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    x[2 * e] = (r.w[e] & 0xffffu) >= d.least ? x[2 * e] * d.factor : 0.f;
-    x[2 * e + 1] = (r.w[e] >> 16) >= d.least ? x[2 * e + 1] * d.factor : 0.f;
+    x[2 * e] = (r.w[e] << 16) >= d.cut ? x[2 * e] * d.factor : 0.f;
+    x[2 * e + 1] = r.w[e] >= d.cut ? x[2 * e + 1] * d.factor : 0.f;
+  }
+  if (d.mode == 2) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
   }
 }
 #endif
