@@ -29,7 +29,7 @@ using namespace tc;
 
 constexpr int kHeadThreads = 384;            // warp 0 loads A, 2 loads B, 1 issues the MMAs, 4-11 drain the accumulators
 // Registers per thread: of the launch, and as the first four and the other eight warps divide them (the eight keep 128 values each).
-constexpr int kHeadRegs = 168, kIssueRegs = 72, kDrainRegs = 216;
+constexpr int kHeadRegs = 168, kIssueRegs = 88, kDrainRegs = 208;
 static_assert(4 * kIssueRegs + 8 * kDrainRegs <= 12 * kHeadRegs, "a block has the registers that it was launched with");
 constexpr int kTile = 256;
 constexpr int kStageK = 64;
@@ -46,21 +46,24 @@ constexpr int kSegForward = 16, kSegLogits = 8, kSegF32 = 4, kSegBf16 = 64;     
 
 enum : int32_t { CLS_LOGITS = 0, CLS_DH = 1, CLS_DW = 2 };
 
-// head of the scratch
-enum : int32_t { HD_STATUS = 0, HD_COUNT = 1 };
+// head of the scratch: status word, number of tokens with a target, and (forward) a status word of every pair of CTAs
+enum : int32_t { HD_STATUS = 0, HD_COUNT = 1, HD_PAIRS = 64 };
+constexpr int kMostPairs = 128, kHeadBytes = 4 * (HD_PAIRS + kMostPairs);
 
 struct HeadArgs {
   CUtensorMap hk, hn, ck, cn, wk, wn, gk, gn;      // hidden, its compacted copy, weight, g; boxes of 64 x 128 (K-major use) and 64 x 64
   int32_t* head;                 // HD_*
   const int32_t* token;          // of a compacted row
   const int32_t* target;         // of a compacted row
+  const int64_t* targets;        // forward over at most a tile of tokens, which are not compacted: the caller's (else null)
   const float* lse;              // of a compacted row
   const float* dloss;            // of a compacted row, or null: 1
   float2* part;                  // forward: (exponent, sum) [2 n_tiles][t_pad]
   float* part_sum;               // forward with smoothing: sum of the logits, same layout
   float* z_target;               // forward: logit of the target of a compacted row
   uint16_t* g;                   // [2 buffers][planes][t_pad][piece]
-  float* dh_acc;                 // [t_pad][hidden], between two pieces
+  float* dh_acc;                 // [split_dh][t_pad][hidden], between two pieces and before the splits are added up
+  float* dw_acc;                 // [split_dw][vocab][hidden], before the splits are added up
   void* dh;
   void* dw;
   int64_t hidden_ld, weight_ld;
@@ -68,53 +71,81 @@ struct HeadArgs {
   int32_t g_begin, g_cols, g_buf;          // piece whose g this launch makes (g_cols = 0: none)
   int32_t o_begin, o_cols, o_buf;          // piece whose gradients it makes (o_cols = 0: none)
   int32_t first, last;                     // of the pieces, for dh
+  int32_t split_dh, split_dw;              // parts that K is cut into, at most; 1: not cut
   int32_t dh_f32, dw_f32, accumulate, dh_wide, dw_wide;      // wide: rows start on 32 bytes
   int32_t seg_logits, seg_dh, seg_dw;      // longest segments, in stages
   float scale, smooth, z_loss;
 };
 
-struct __align__(8) HeadShared {
-  uint64_t full[kHeadStages], empty[kHeadStages], tfull[2], tempty[2];
-  uint32_t tmem_base;
-  int abort, skip;
-};
+// `stages` in at most `most` parts of even length: how many, and the stages of each but the last.
+__device__ __host__ __forceinline__ void parts_of(int stages, int most, int& n, int& each) {
+  each = (stages + most - 1) / most;
+  n = (stages + each - 1) / each;
+}
+
+// One tile of a result: its first row and column, its columns, and its share of K, `count` stages from stage k0 of
+// `planes` planes of per_plane stages laid end to end.
+struct Item { int cls, m0, n0, bn, k0, count, per_plane, split; };
 
 // The items of a launch, as every warp of a pair walks through them.  Long items (gradients) first, dealt out in turn; then the
 // short ones (logits) in turn, where the pairs that got a long item more join `skip` rounds later.
 struct Walk {
   int pairs, pair, n_dh, n_long, n_short, extra, skip, mine;
-  int m_tiles, nt_v, nt_d, units, k_logits, k_dh, k_dw;
+  int m_tiles, nt_v, nt_d, units, k_logits, k_dh, k_dw, each_dh, each_dw;
 
-  __device__ __forceinline__ Walk(const HeadArgs& a, bool backward, int tv, int pair_, int pairs_) : pairs(pairs_), pair(pair_) {
+  __device__ __forceinline__ void start(const HeadArgs& a, bool backward, int tv, int pair_, int pairs_) {
+    pairs = pairs_; pair = pair_;
     m_tiles = (tv + kTile - 1) / kTile;
     const int cols = backward ? a.g_cols : a.vocab;
     nt_v = (cols + kTile - 1) / kTile;
     units = (a.hidden + 31) / 32;
     nt_d = (units + 7) / 8;
     k_logits = (a.hidden + kStageK - 1) / kStageK;
+    n_short = m_tiles * nt_v;
+    n_dh = n_long = extra = skip = mine = 0;
+    if (!backward || a.o_cols == 0) return;
     k_dh = (a.o_cols + kStageK - 1) / kStageK;
     k_dw = max(1, (tv + kStageK - 1) / kStageK);
-    n_short = m_tiles * nt_v;
-    n_dh = backward && a.o_cols > 0 && a.dh ? m_tiles * nt_d : 0;
-    const int n_dw = backward && a.o_cols > 0 && a.dw ? (a.o_cols + kTile - 1) / kTile * nt_d : 0;
-    n_long = n_dh + n_dw;
+    int split_dh, split_dw;
+    parts_of(k_dh * a.planes_dh, a.split_dh, split_dh, each_dh);
+    parts_of(k_dw * a.planes_dw, a.split_dw, split_dw, each_dw);
+    n_dh = a.dh ? m_tiles * nt_d * split_dh : 0;
+    n_long = n_dh + (a.dw ? (a.o_cols + kTile - 1) / kTile * nt_d * split_dw : 0);
     extra = n_long % pairs;
-    const int long_cost = n_dw > 0 ? k_dw * a.planes_dw : k_dh * a.planes_dh;
-    skip = extra ? (long_cost + k_logits / 2) / k_logits : 0;
-    mine = pair < n_long ? (n_long - pair + pairs - 1) / pairs : 0;
+    const int surplus = load(0) - load(pairs - 1);
+    skip = extra && surplus > 0 ? (surplus + k_logits / 2) / k_logits : 0;
+    mine = dealt(n_long, pair);
   }
-  // Of this pair's item `seq`: class, first row, first column, columns, stages per plane; false past the last.
-  __device__ __forceinline__ bool item(const HeadArgs& a, int seq, int& cls, int& m0, int& n0, int& bn, int& k_stages, int& planes) const {
+  __device__ __forceinline__ int dealt(int n, int p) const { return p < n ? (n - p + pairs - 1) / pairs : 0; }
+  __device__ __forceinline__ int load(int p) const {
+    const int dh = dealt(n_dh, p);
+    return dh * each_dh + (dealt(n_long, p) - dh) * each_dw;
+  }
+  // This pair's item `seq`; false past the last.
+  // (Read from shared memory: `uniform` tells the compiler that all lanes have the same.)
+  __device__ __forceinline__ bool item_uniform(const HeadArgs& a, int seq, Item& t) const {
+    if (!uniform((int)item(a, seq, t))) return false;
+    t.cls = uniform(t.cls); t.m0 = uniform(t.m0); t.n0 = uniform(t.n0); t.bn = uniform(t.bn);
+    t.k0 = uniform(t.k0); t.count = uniform(t.count); t.per_plane = uniform(t.per_plane);
+    return true;
+  }
+  __device__ __forceinline__ bool item(const HeadArgs& a, int seq, Item& t) const {
+    t.split = t.k0 = 0;
     if (seq < mine) {
       int k = pair + seq * pairs;
-      cls = k < n_dh ? CLS_DH : CLS_DW;
-      if (cls == CLS_DW) k -= n_dh;
+      t.cls = k < n_dh ? CLS_DH : CLS_DW;
+      if (t.cls == CLS_DW) k -= n_dh;
       const int n = k % nt_d, base = units / nt_d, more = units % nt_d;
-      m0 = k / nt_d * kTile;
-      n0 = 32 * (n * base + min(n, more));          // widths as even as multiples of 32 allow
-      bn = 32 * (base + (n < more ? 1 : 0));
-      k_stages = cls == CLS_DH ? k_dh : k_dw;
-      planes = cls == CLS_DH ? a.planes_dh : a.planes_dw;
+      k /= nt_d;
+      const int m = t.cls == CLS_DH ? m_tiles : (a.o_cols + kTile - 1) / kTile;
+      t.split = k / m;
+      t.m0 = (k - t.split * m) * kTile;
+      t.n0 = 32 * (n * base + min(n, more));          // widths as even as multiples of 32 allow
+      t.bn = 32 * (base + (n < more ? 1 : 0));
+      t.per_plane = t.cls == CLS_DH ? k_dh : k_dw;
+      const int each = t.cls == CLS_DH ? each_dh : each_dw, all = t.per_plane * (t.cls == CLS_DH ? a.planes_dh : a.planes_dw);
+      t.k0 = t.split * each;
+      t.count = min(each, all - t.k0);
       return true;
     }
     const int j = seq - mine;
@@ -125,14 +156,20 @@ struct Walk {
     if (k >= n_short) return false;
     const int per_group = kGroupM * nt_v, group = k / per_group, in_group = min(kGroupM, m_tiles - group * kGroupM);
     k -= group * per_group;
-    cls = CLS_LOGITS;
-    m0 = (group * kGroupM + k % in_group) * kTile;
-    n0 = k / in_group * kTile;
-    bn = kTile;
-    k_stages = k_logits;
-    planes = 1;
+    t.cls = CLS_LOGITS;
+    t.m0 = (group * kGroupM + k % in_group) * kTile;
+    t.n0 = k / in_group * kTile;
+    t.bn = kTile;
+    t.per_plane = t.count = k_logits;
     return true;
   }
+};
+
+struct __align__(8) HeadShared {
+  uint64_t full[kHeadStages], empty[kHeadStages], tfull[2], tempty[2];
+  uint32_t tmem_base;
+  int abort, skip, tv;
+  Walk walk;                     // here and not in every thread's registers
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -279,7 +316,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
   uint8_t* const stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* const abort = &sh.abort;
-  int32_t* const status = a.head + HD_STATUS;
+  // forward: a word of this pair's own, so that nothing has to be cleared before the launch
+  int32_t* const status = a.head + (BACKWARD ? HD_STATUS : HD_PAIRS + (int)(blockIdx.x >> 1));
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kHeadStages; ++i) {
@@ -288,8 +326,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 16); }
     sh.abort = 0;
-    sh.skip = *reinterpret_cast<volatile int32_t*>(status) != 0;
+    if (!BACKWARD && rank == 0) *status = 0;          // (the cluster barrier below orders it before what either CTA adds)
+    sh.skip = BACKWARD && *reinterpret_cast<volatile int32_t*>(status) != 0;
     mbar_fence_init();
+    sh.tv = !BACKWARD && a.targets ? a.tokens : *reinterpret_cast<volatile int32_t*>(a.head + HD_COUNT);
+    sh.walk.start(a, BACKWARD, sh.tv, (int)(blockIdx.x >> 1), (int)(gridDim.x >> 1));
   }
   if (warp == 1) {
     tmem_alloc<true>(&sh.tmem_base, 512);
@@ -301,10 +342,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
   tc_fence_after();
   const uint32_t tmem_base = sh.tmem_base;
   const bool skip = load_shared_of(&sh.skip, 0) != 0;       // an earlier launch gave up: the pair decides together
-  const int tv = uniform(*reinterpret_cast<volatile int32_t*>(a.head + HD_COUNT));
+  const int tv = uniform(sh.tv);
   const bool compacted = tv != a.tokens;
-  const Walk walk(a, BACKWARD, tv, (int)(blockIdx.x >> 1), (int)(gridDim.x >> 1));
-  int cls, m0, n0, bn, k_stages, planes;
+  const Walk& walk = sh.walk;
+  Item t;
 
   if (warp < 4) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
@@ -317,40 +358,47 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     int stage = 0;
     uint32_t phase = 0, issued = 0;
     bool ok = true;
-    for (int seq = 0; ok && walk.item(a, seq, cls, m0, n0, bn, k_stages, planes); ++seq) {
+    for (int seq = 0; ok && walk.item_uniform(a, seq, t); ++seq) {
       const CUtensorMap* map;
       int x, y, n_box = 1;                 // K-major: one box of 128 rows, x runs; MN-major: boxes of 64 columns, y runs
-      const int half = bn / 2, o_row = a.o_buf * a.planes * a.t_pad;
+      const int half = t.bn / 2, o_row = a.o_buf * a.planes * a.t_pad;
       if (is_a) {
-        if (cls == CLS_DW) { map = &a.gn; x = m0 + (int)rank * 128; y = o_row; n_box = 2; }
-        else if (cls == CLS_DH) { map = &a.gk; x = 0; y = o_row + m0 + (int)rank * 128; }
-        else { map = compacted ? &a.ck : &a.hk; x = 0; y = m0 + (int)rank * 128; }
+        if (t.cls == CLS_DW) { map = &a.gn; x = t.m0 + (int)rank * 128; y = o_row; n_box = 2; }
+        else if (t.cls == CLS_DH) { map = &a.gk; x = 0; y = o_row + t.m0 + (int)rank * 128; }
+        else { map = compacted ? &a.ck : &a.hk; x = 0; y = t.m0 + (int)rank * 128; }
       } else {
-        if (cls == CLS_LOGITS) { map = &a.wk; x = 0; y = (BACKWARD ? a.g_begin : 0) + n0 + (int)rank * 128; }
+        if (t.cls == CLS_LOGITS) { map = &a.wk; x = 0; y = (BACKWARD ? a.g_begin : 0) + t.n0 + (int)rank * 128; }
         else {
-          map = cls == CLS_DH ? &a.wn : (compacted ? &a.cn : &a.hn);
-          x = n0 + (int)rank * half; y = cls == CLS_DH ? a.o_begin : 0; n_box = half > 64 ? 2 : 1;
+          map = t.cls == CLS_DH ? &a.wn : (compacted ? &a.cn : &a.hn);
+          x = t.n0 + (int)rank * half; y = t.cls == CLS_DH ? a.o_begin : 0; n_box = half > 64 ? 2 : 1;
         }
       }
-      const bool along_y = is_a ? cls == CLS_DW : cls != CLS_LOGITS;
+      const bool along_y = is_a ? t.cls == CLS_DW : t.cls != CLS_LOGITS;
       const uint32_t bytes = along_y ? (uint32_t)n_box * (kOperandBytes / 2) : kOperandBytes;
-      const int plane_step = is_a && cls != CLS_LOGITS ? a.t_pad : 0;
-      for (int p = 0; p < planes && ok; ++p) {
-        int xk = x, yk = y + p * plane_step;
-        for (int k = 0; k < k_stages; ++k) {
-          if (!mbar_wait_warp<WAIT_PAIR>(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
-          uint8_t* const dst = stages + stage * (2 * kOperandBytes) + (is_a ? 0 : kOperandBytes);
-          if (leader) {
-            if (rank == 0) mbar_arrive_expect_tx(&sh.full[stage], 2 * bytes);
-            const uint32_t bar = pair_full + 8u * (uint32_t)stage;
-            tma_load_box_pair(dst, map, xk, yk, bar);
-            if (n_box == 2) tma_load_box_pair(dst + kOperandBytes / 2, map, xk + 64, yk, bar);
-          }
-          __syncwarp();
-          if (along_y) yk += kStageK; else xk += kStageK;
-          ++issued;
-          if (++stage == kHeadStages) { stage = 0; phase ^= 1u; }
+      const int plane_step = is_a && t.cls != CLS_LOGITS ? a.t_pad : 0;
+      const int plane0 = t.k0 / t.per_plane, kx = along_y ? 0 : kStageK, ky = along_y ? kStageK : 0;
+      int k = t.k0 - plane0 * t.per_plane;
+      y += plane0 * plane_step + k * ky;
+      x += k * kx;
+      for (int left = t.count; left > 0; --left) {
+        if (!mbar_wait_warp<WAIT_PAIR>(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+        uint8_t* const dst = stages + stage * (2 * kOperandBytes) + (is_a ? 0 : kOperandBytes);
+        if (leader) {
+          if (rank == 0) mbar_arrive_expect_tx(&sh.full[stage], 2 * bytes);
+          const uint32_t bar = pair_full + 8u * (uint32_t)stage;
+          tma_load_box_pair(dst, map, x, y, bar);
+          if (n_box == 2) tma_load_box_pair(dst + kOperandBytes / 2, map, x + 64, y, bar);
         }
+        __syncwarp();
+        x += kx;
+        y += ky;
+        if (++k == t.per_plane) {                 // the next plane of A, the same B again
+          k = 0;
+          x -= kx * t.per_plane;
+          y += plane_step - ky * t.per_plane;
+        }
+        ++issued;
+        if (++stage == kHeadStages) { stage = 0; phase ^= 1u; }
       }
     }
     if (!ok) drain_ring<true>(sh.full, stage, phase, issued, kHeadStages, rank);
@@ -362,13 +410,13 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     bool ok = true;
     const uint32_t ring = uniform(smem_u32(stages)), d0 = uniform(tmem_base), dhi = desc_hi();
     uint32_t run = 0;                     // segments so far
-    for (int seq = 0; ok && walk.item(a, seq, cls, m0, n0, bn, k_stages, planes); ++seq) {
-      const bool a_mn = cls == CLS_DW, b_mn = cls != CLS_LOGITS;
-      const uint32_t idesc = uniform(make_idesc(bn, a_mn, b_mn, false, 256));
+    for (int seq = 0; ok && walk.item_uniform(a, seq, t); ++seq) {
+      const bool a_mn = t.cls == CLS_DW, b_mn = t.cls != CLS_LOGITS;
+      const uint32_t idesc = uniform(make_idesc(t.bn, a_mn, b_mn, false, 256));
       // per K step of 16: 32 bytes inside a K-major row, 16 rows of 128 bytes of an MN-major box (in 16-byte units)
       const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
-      int left = k_stages * planes, n_seg, each;
-      segments(left, cls == CLS_LOGITS ? a.seg_logits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
+      int left = t.count, n_seg, each;
+      segments(left, t.cls == CLS_LOGITS ? a.seg_logits : t.cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
       for (; left > 0 && ok; left -= each, ++run) {
         const int acc = (int)(run & 1);
         if (!mbar_wait_warp<WAIT_PAIR_TC>(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
@@ -404,24 +452,31 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     const uint32_t lane_addr = (uint32_t)(32 * (warp & 3)) << 16;
     uint32_t run = 0;
     bool ok = true;
-    for (int seq = 0; !skip && walk.item(a, seq, cls, m0, n0, bn, k_stages, planes); ++seq) {
-      const int row = m0 + (int)rank * 128 + q, half = bn / 2;
+    for (int seq = 0; !skip && walk.item(a, seq, t); ++seq) {
+      const int cls = t.cls, m0 = t.m0, n0 = t.n0;
+      const int row = m0 + (int)rank * 128 + q, half = t.bn / 2;
       // what the row needs is asked for before the accumulator is waited for
       int y = -1, token = 0;
       float lse = 0.f, dl = 0.f;
       if (cls == CLS_LOGITS && row < tv) {
-        y = a.target[row] - n0 - 128 * grp;
+        if (!BACKWARD && a.targets) {
+          const int64_t wide_y = a.targets[row];
+          y = wide_y >= 0 && wide_y < a.vocab ? (int)wide_y : -(1 << 30);
+        } else {
+          y = a.target[row];
+        }
+        y -= n0 + 128 * grp;
         if (BACKWARD) {
           y -= a.g_begin;
           lse = a.lse[row];
           dl = a.dloss ? a.dloss[row] : 1.f;
         }
-      } else if (BACKWARD && cls == CLS_DH && a.last && row < tv) {
+      } else if (BACKWARD && cls == CLS_DH && a.last && a.split_dh == 1 && row < tv) {
         token = a.token[row];
       }
       float v[128];
       int n_seg, each;
-      segments(k_stages * planes, cls == CLS_LOGITS ? a.seg_logits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
+      segments(t.count, cls == CLS_LOGITS ? a.seg_logits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
 #pragma unroll 1
       for (int i = 0; i < n_seg; ++i, ++run) {
         const int acc = (int)(run & 1);
@@ -487,10 +542,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         const int col0 = n0 + grp * half;
         const bool is_dh = cls == CLS_DH;
         const bool row_ok = row < (is_dh ? tv : a.o_cols), none = tv == 0;
-        const bool to_acc = is_dh && !a.last, from_acc = is_dh && !a.first, from_out = !is_dh && a.accumulate;
+        const bool cut = is_dh ? a.split_dh > 1 : a.split_dw > 1;
+        const bool to_acc = cut || (is_dh && !a.last), from_acc = is_dh && !a.first, from_out = !to_acc && !is_dh && a.accumulate;
         void* const out = is_dh ? a.dh : a.dw;
         const int64_t out_row = is_dh ? (int64_t)token * a.hidden_ld : (int64_t)(a.o_begin + row) * a.weight_ld;
-        float* const acc_row = a.dh_acc + (int64_t)row * a.hidden;
+        float* const acc_row = is_dh ? a.dh_acc + ((int64_t)t.split * a.t_pad + row) * a.hidden : a.dw_acc + ((int64_t)t.split * a.vocab + row) * a.hidden;
         const bool f32 = is_dh ? a.dh_f32 : a.dw_f32, wide = is_dh ? a.dh_wide : a.dw_wide;
         const float scale = to_acc ? 1.f : a.scale;
 #pragma unroll
@@ -616,60 +672,135 @@ __global__ void __launch_bounds__(256) head_prepare_kernel(const PrepareArgs a) 
 // ---- what the forward items left of a row, put together ------------------------------------------------
 
 struct FinalArgs {
-  const int32_t* head;
+  int32_t* head;
   const int32_t* token;
+  const int64_t* targets;        // tokens that were not compacted: the caller's (else null)
   const float2* part;
   const float* part_sum;
   const float* z_target;
   float* loss;
   float* lse;
-  int32_t n_parts, t_pad, vocab;
+  int64_t ignore;
+  int32_t n_parts, t_pad, tokens, vocab, pairs;
   float smooth, z_loss;
 };
 
-// A CTA has 32 rows (its lanes), eight warps share the parts of each.
+// A CTA has 32 rows (its lanes), eight warps share the parts of each, eight at a time.
 __global__ void __launch_bounds__(256) head_final_kernel(const FinalArgs a) {
   __shared__ float ks[8][32], sums[8][32], totals[8][32];
   wait_for_previous_kernel();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = (int)blockIdx.x * 32 + lane, tv = a.head[HD_COUNT];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, row = (int)blockIdx.x * 32 + lane;
+  const int tv = a.targets ? a.tokens : a.head[HD_COUNT];
+  const bool gave_up = __syncthreads_or((int)threadIdx.x < a.pairs ? a.head[HD_PAIRS + threadIdx.x] : 0) != 0;
+  if (blockIdx.x == 0 && threadIdx.x < 32) {
+    int word = 0;
+    for (int p = lane; p < a.pairs; p += 32) word |= a.head[HD_PAIRS + p];
+    word = __reduce_or_sync(0xffffffffu, (unsigned)word);
+    if (lane == 0) a.head[HD_STATUS] = word;
+  }
   float k = -INFINITY, sum = 0.f, total = 0.f;
-  auto add = [&](float pk, float ps) {
+  auto add = [&](float pk, float ps) {             // (a part whose logits are all -inf or NaN has k = -inf and counts as it is)
     const float top = fmaxf(k, pk);
     sum = (k == top ? sum : sum * ex2(k - top)) + (pk == top || pk == -INFINITY ? ps : ps * ex2(pk - top));
     k = top;
   };
   if (row < tv) {
-#pragma unroll 4
-    for (int i = warp; i < a.n_parts; i += 8) {
-      const int64_t at = (int64_t)i * a.t_pad + row;
-      const float2 p = a.part[at];
-      add(p.x, p.y);
-      if (a.smooth != 0.f) total += a.part_sum[at];
+    for (int i0 = warp; i0 < a.n_parts; i0 += 64) {
+      float2 p[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) p[u] = i0 + 8 * u < a.n_parts ? a.part[(int64_t)(i0 + 8 * u) * a.t_pad + row] : make_float2(-INFINITY, 0.f);
+      float top = p[0].x, ps = 0.f;
+#pragma unroll
+      for (int u = 1; u < 8; ++u) top = fmaxf(top, p[u].x);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) ps += p[u].x == -INFINITY ? p[u].y : p[u].y * ex2(p[u].x - top);
+      add(top, ps);
+      if (a.smooth != 0.f) {
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (i0 + 8 * u < a.n_parts) total += a.part_sum[(int64_t)(i0 + 8 * u) * a.t_pad + row];
+      }
     }
   }
   ks[warp][lane] = k; sums[warp][lane] = sum; totals[warp][lane] = total;
   __syncthreads();
   if (warp != 0 || row >= tv) return;
   for (int w = 1; w < 8; ++w) { add(ks[w][lane], sums[w][lane]); total += totals[w][lane]; }
-  const int t = a.token[row];
-  double lse = ((double)k + log2((double)sum)) * 0.69314718055994530942;
-  if (a.head[HD_STATUS] != 0) lse = __longlong_as_double(0x7ff8000000000000ll);       // a wait ran out: nothing of this call holds
+  int t = row;
+  float none = 0.f;
+  bool left_out = false;
+  if (a.targets) {
+    const int64_t y = a.targets[row];
+    left_out = y == a.ignore || y < 0 || y >= a.vocab;
+    none = y == a.ignore ? 0.f : __int_as_float(0x7fffffff);
+  } else {
+    t = a.token[row];
+  }
+  // the sum of k and the logarithm in 64 bits: what is rounded is the result
+  double lse = ((double)k + (double)log2f(sum)) * 0.69314718055994530942;
+  if (gave_up) lse = __longlong_as_double(0x7ff8000000000000ll);       // a wait ran out: nothing of this call holds
   const double loss = lse - (1.0 - (double)a.smooth) * (double)a.z_target[row] - (double)a.smooth * (double)total / a.vocab +
                       (double)a.z_loss * lse * lse;
-  a.loss[t] = (float)loss;
-  a.lse[t] = (float)lse;
+  a.loss[t] = left_out ? none : (float)loss;
+  a.lse[t] = left_out ? none : (float)lse;
+}
+
+// ---- a gradient whose K was cut: its parts, put together ------------------------------------------------
+
+struct SumArgs {
+  const int32_t* head;
+  const int32_t* token;
+  struct Job {
+    const float* acc;            // [parts][pitch of a part in rows][hidden]
+    void* out;
+    int64_t ld, part_rows;
+    int32_t rows;                // < 0: the tokens with a target, whose places in `out` are `token`
+    int32_t most, stages, planes_of_tokens;      // K in stages, or (planes > 0) as many planes of the tokens with a target
+    int32_t f32, wide, accumulate;
+  } job[2];
+  int32_t hidden, jobs;
+  float scale;
+};
+
+__global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
+  wait_for_previous_kernel();
+  if (a.head[HD_STATUS] != 0) return;
+  const SumArgs::Job& j = a.job[blockIdx.x % a.jobs];
+  const int tv = a.head[HD_COUNT], rows = j.rows < 0 ? tv : j.rows, vec = (a.hidden + 15) / 16;
+  int n, each;
+  parts_of(j.planes_of_tokens ? max(1, (tv + kStageK - 1) / kStageK) * j.planes_of_tokens : j.stages, j.most, n, each);
+  const int64_t part = j.part_rows * a.hidden, stride = (int64_t)(gridDim.x / a.jobs) * 256;
+  for (int64_t i = (int64_t)(blockIdx.x / a.jobs) * 256 + threadIdx.x; i < (int64_t)rows * vec; i += stride) {
+    const int64_t row = i / vec;
+    const int c = (int)(i - row * vec) * 16, live = a.hidden - c;
+    float x[16], more[16];
+    load_row16(j.acc, row * a.hidden + c, x, live, true);
+#pragma unroll 4
+    for (int p = 1; p < n; ++p) {
+      load_row16(j.acc, p * part + row * a.hidden + c, more, live, true);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] += more[e];
+    }
+    const int64_t at = (j.rows < 0 ? (int64_t)a.token[row] : row) * j.ld + c;
+    if (j.accumulate) load_row16(j.out, at, more, live, j.f32);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], a.scale, j.accumulate ? more[e] : 0.f);
+    store_row16(j.out, at, x, live, j.f32, j.wide);
+  }
 }
 
 // ---- host ----------------------------------------------------------------------------------------------
 
 struct Layout {
-  int64_t t_pad, n_tiles, piece, n_pieces, n_buf, planes;
-  int64_t token, target, compact, lse, dloss, part, part_sum, z_target, g, dh_acc, bytes;      // byte offsets
+  int64_t t_pad, n_tiles, piece, n_pieces, n_buf, planes, split_dh, split_dw;
+  bool direct;                   // forward over at most a tile of tokens: they are not compacted
+  int64_t token, target, compact, lse, dloss, part, part_sum, z_target, g, dh_acc, dw_acc, bytes;      // byte offsets
 };
 
 // A piece of the vocabulary: as many columns as make g of one piece and plane about 64 M elements (128 MB: what the two
 // gradient products read is then mostly still in L2), of even sizes, and at least 2048 (the sum of dh goes through
 // memory once per piece).
+constexpr int64_t kPlanPairs = 74;       // what the scratch is planned for (148 SMs)
 constexpr int64_t kPieceElems = (int64_t)64 << 20, kPieceMin = 2048;
 
 int plan(const adapm_head_loss& d, bool backward, Layout& l) {
@@ -690,17 +821,32 @@ int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   l.n_pieces = (d.vocab + l.piece - 1) / l.piece;
   l.n_buf = l.n_pieces > 1 ? 2 : 1;
   if (l.t_pad / kTile * l.n_tiles > (1 << 30) || l.n_buf * l.planes * l.t_pad >= ((int64_t)1 << 31)) return ADAPM_ERANGE;
-  int64_t at = 256;
+  // A gradient's K is cut into parts where one of its items would take longer than all items divided over the pairs: few tokens
+  // leave dh a handful of tiles with the whole vocabulary as their K, a small vocabulary does the same to dw.  (512 tokens of
+  // 4096 x 256 in fp32: 77 us without.)  A part is at least four stages.
+  l.split_dh = l.split_dw = 1;
+  if (backward) {
+    const int64_t mt = l.t_pad / kTile, nt_d = (d.hidden + kTile - 1) / kTile, tiles = l.piece / kTile;
+    const int64_t k_dh = (std::min(l.piece, d.vocab) + kStageK - 1) / kStageK * (d.dhidden_dtype == ADAPM_TYPE_F32 ? 3 : 1);
+    const int64_t k_dw = l.t_pad / kStageK * (d.dweight_dtype == ADAPM_TYPE_F32 ? 3 : 1);
+    const int64_t logits = l.n_pieces > 1 ? mt * tiles * ((d.hidden + kStageK - 1) / kStageK) : 0;
+    const int64_t share = std::max<int64_t>(4, (nt_d * (mt * k_dh + tiles * k_dw) + logits) / kPlanPairs);
+    l.split_dh = std::min<int64_t>((k_dh + share - 1) / share, 256);
+    if (l.n_pieces == 1) l.split_dw = std::min<int64_t>((k_dw + share - 1) / share, 256);
+  }
+  int64_t at = kHeadBytes;
   auto take = [&](int64_t bytes) { const int64_t o = at; at += round_up(bytes, 256); return o; };
+  l.direct = !backward && d.tokens <= kTile;
   l.token = take(l.t_pad * 4);
   l.target = take(l.t_pad * 4);
-  l.compact = take(l.t_pad * d.hidden * 2);
-  l.lse = l.dloss = l.part = l.part_sum = l.z_target = l.g = l.dh_acc = 0;
+  l.compact = take(l.direct ? 0 : l.t_pad * d.hidden * 2);
+  l.lse = l.dloss = l.part = l.part_sum = l.z_target = l.g = l.dh_acc = l.dw_acc = 0;
   if (backward) {
     l.lse = take(l.t_pad * 4);
     l.dloss = take(l.t_pad * 4);
     l.g = take(l.n_buf * l.planes * l.t_pad * l.piece * 2);
-    if (l.n_pieces > 1) l.dh_acc = take(l.t_pad * d.hidden * 4);
+    if (l.n_pieces > 1 || l.split_dh > 1) l.dh_acc = take(l.split_dh * l.t_pad * d.hidden * 4);
+    if (l.split_dw > 1) l.dw_acc = take(l.split_dw * d.vocab * d.hidden * 4);
   } else {
     l.part = take(2 * l.n_tiles * l.t_pad * 8);
     l.part_sum = take(d.label_smoothing != 0.f ? 2 * l.n_tiles * l.t_pad * 4 : 0);
@@ -737,16 +883,21 @@ int pairs_of(int device, int* pairs) {
     cfg.attrs = &at; cfg.numAttrs = 1;
     int resident = 0;
     ADAPM_CUDA(cudaOccupancyMaxActiveClusters(&resident, head_items_kernel<true>, &cfg));
-    known[device] = std::max(1, std::min(resident, sms / 2));
+    known[device] = std::max(1, std::min({resident, sms / 2, kMostPairs}));
   }
   *pairs = known[device];
   return ADAPM_OK;
 }
 
-bool maps_of_operands(HeadArgs& a, const adapm_head_loss& d, const void* hidden, const void* weight, const void* compact, int64_t t_pad) {
-  return encode_bf16_matrix(&a.hk, hidden, d.tokens, d.hidden, d.hidden_ld, 128) && encode_bf16_matrix(&a.hn, hidden, d.tokens, d.hidden, d.hidden_ld, 64) &&
-         encode_bf16_matrix(&a.ck, compact, t_pad, d.hidden, d.hidden, 128) && encode_bf16_matrix(&a.cn, compact, t_pad, d.hidden, d.hidden, 64) &&
-         encode_bf16_matrix(&a.wk, weight, d.vocab, d.hidden, d.weight_ld, 128) && encode_bf16_matrix(&a.wn, weight, d.vocab, d.hidden, d.weight_ld, 64);
+// Tensor maps of the operands.  (Half a microsecond of the host's time each: only those that the call reads.)
+bool maps_of_operands(HeadArgs& a, const adapm_head_loss& d, const void* hidden, const void* weight, const void* compact, int64_t t_pad,
+                      bool direct, bool backward) {
+  bool ok = encode_bf16_matrix(&a.hk, hidden, d.tokens, d.hidden, d.hidden_ld, 128) && encode_bf16_matrix(&a.wk, weight, d.vocab, d.hidden, d.weight_ld, 128);
+  if (!direct) ok = ok && encode_bf16_matrix(&a.ck, compact, t_pad, d.hidden, d.hidden, 128);
+  if (backward)
+    ok = ok && encode_bf16_matrix(&a.hn, hidden, d.tokens, d.hidden, d.hidden_ld, 64) && encode_bf16_matrix(&a.cn, compact, t_pad, d.hidden, d.hidden, 64) &&
+         encode_bf16_matrix(&a.wn, weight, d.vocab, d.hidden, d.weight_ld, 64);
+  return ok;
 }
 
 int launch_prepare(const adapm_head_loss& d, PrepareArgs p, cudaStream_t s) {
@@ -787,29 +938,33 @@ extern "C" int adapm_head_loss_forward(const adapm_head_loss* d, const void* hid
 
   HeadArgs a;
   std::memset(&a, 0, sizeof(a));
-  if (!maps_of_operands(a, *d, hidden, weight, base + l.compact, l.t_pad)) {
+  if (!maps_of_operands(a, *d, hidden, weight, base + l.compact, l.t_pad, l.direct, false)) {
     set_error_text("cuTensorMapEncodeTiled failed for the head");
     return ADAPM_ECUDA;
   }
   a.head = (int32_t*)base;
   a.token = (int32_t*)(base + l.token); a.target = (int32_t*)(base + l.target);
+  a.targets = l.direct ? targets : nullptr;
   a.part = (float2*)(base + l.part); a.part_sum = (float*)(base + l.part_sum); a.z_target = (float*)(base + l.z_target);
   a.tokens = (int32_t)d->tokens; a.vocab = (int32_t)d->vocab; a.hidden = (int32_t)d->hidden; a.t_pad = (int32_t)l.t_pad;
-  a.planes = a.planes_dh = a.planes_dw = 1;
+  a.planes = a.planes_dh = a.planes_dw = a.split_dh = a.split_dw = 1;
   a.seg_logits = kSegForward;
   a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
 
-  PrepareArgs p;
-  std::memset(&p, 0, sizeof(p));
-  p.targets = targets; p.hidden = (const uint16_t*)hidden; p.compact = (uint16_t*)(base + l.compact);
-  p.head = a.head; p.token = (int32_t*)(base + l.token); p.target = (int32_t*)(base + l.target); p.loss = loss; p.lse_out = lse;
-  rc = launch_prepare(*d, p, s);
-  if (rc != ADAPM_OK) return rc;
-  const int64_t items = l.t_pad / kTile * l.n_tiles;
-  ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<false>, 2 * (unsigned)std::min<int64_t>(pairs, items), kHeadThreads, kHeadSmem, s, a));
+  if (!l.direct) {
+    PrepareArgs p;
+    std::memset(&p, 0, sizeof(p));
+    p.targets = targets; p.hidden = (const uint16_t*)hidden; p.compact = (uint16_t*)(base + l.compact);
+    p.head = a.head; p.token = (int32_t*)(base + l.token); p.target = (int32_t*)(base + l.target); p.loss = loss; p.lse_out = lse;
+    rc = launch_prepare(*d, p, s);
+    if (rc != ADAPM_OK) return rc;
+  }
+  const int used = (int)std::min<int64_t>(pairs, l.t_pad / kTile * l.n_tiles);
+  ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<false>, 2 * (unsigned)used, kHeadThreads, kHeadSmem, s, a));
   FinalArgs f;
-  f.head = a.head; f.token = a.token; f.part = a.part; f.part_sum = a.part_sum; f.z_target = a.z_target; f.loss = loss; f.lse = lse;
-  f.n_parts = (int32_t)(2 * l.n_tiles); f.t_pad = (int32_t)l.t_pad; f.vocab = (int32_t)d->vocab; f.smooth = d->label_smoothing; f.z_loss = d->z_loss;
+  f.head = a.head; f.token = a.token; f.targets = a.targets; f.part = a.part; f.part_sum = a.part_sum; f.z_target = a.z_target; f.loss = loss; f.lse = lse;
+  f.ignore = d->ignore_index; f.n_parts = (int32_t)(2 * l.n_tiles); f.t_pad = (int32_t)l.t_pad; f.tokens = a.tokens; f.vocab = a.vocab; f.pairs = used;
+  f.smooth = d->label_smoothing; f.z_loss = d->z_loss;
   ADAPM_CUDA(launch_chained(true, head_final_kernel, (unsigned)((d->tokens + 31) / 32), 256, 0, s, f));
   return ADAPM_OK;
 }
@@ -852,7 +1007,7 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   std::memset(&a, 0, sizeof(a));
   uint16_t* const g = (uint16_t*)(base + l.g);
   const int64_t g_rows = l.n_buf * l.planes * l.t_pad;
-  if (!maps_of_operands(a, *d, hidden, weight, base + l.compact, l.t_pad) || !encode_bf16_matrix(&a.gk, g, g_rows, l.piece, l.piece, 128) ||
+  if (!maps_of_operands(a, *d, hidden, weight, base + l.compact, l.t_pad, false, true) || !encode_bf16_matrix(&a.gk, g, g_rows, l.piece, l.piece, 128) ||
       !encode_bf16_matrix(&a.gn, g, g_rows, l.piece, l.piece, 64)) {
     set_error_text("cuTensorMapEncodeTiled failed for the head");
     return ADAPM_ECUDA;
@@ -860,10 +1015,11 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   a.head = (int32_t*)base;
   a.token = (int32_t*)(base + l.token); a.target = (int32_t*)(base + l.target);
   a.lse = (float*)(base + l.lse); a.dloss = dloss ? (float*)(base + l.dloss) : nullptr;
-  a.g = g; a.dh_acc = (float*)(base + l.dh_acc); a.dh = dhidden; a.dw = dweight;
+  a.g = g; a.dh_acc = (float*)(base + l.dh_acc); a.dw_acc = (float*)(base + l.dw_acc); a.dh = dhidden; a.dw = dweight;
   a.hidden_ld = d->hidden_ld; a.weight_ld = d->weight_ld;
   a.tokens = (int32_t)d->tokens; a.vocab = (int32_t)d->vocab; a.hidden = (int32_t)d->hidden; a.t_pad = (int32_t)l.t_pad; a.piece = (int32_t)l.piece;
   a.planes = (int32_t)l.planes;
+  a.split_dh = (int32_t)l.split_dh; a.split_dw = (int32_t)l.split_dw;
   a.dh_f32 = d->dhidden_dtype == ADAPM_TYPE_F32; a.dw_f32 = d->dweight_dtype == ADAPM_TYPE_F32;
   a.planes_dh = a.dh_f32 ? 3 : 1; a.planes_dw = a.dw_f32 ? 3 : 1;
   a.dh_wide = (uintptr_t)dhidden % 32 == 0 && (a.dh_f32 || d->hidden_ld % 16 == 0);
@@ -889,9 +1045,24 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
     a.o_begin = (int32_t)((i - 1) * l.piece); a.o_buf = (int32_t)((i + 1) & 1);
     a.o_cols = i > 0 ? (int32_t)std::min(l.piece, d->vocab - (i - 1) * l.piece) : 0;
     a.first = i == 1; a.last = i == l.n_pieces;
-    const int64_t items = m_tiles * ((a.g_cols + kTile - 1) / kTile) + (a.o_cols ? (m_tiles + (a.o_cols + kTile - 1) / kTile) * nt_d : 0);
+    const int64_t items = m_tiles * ((a.g_cols + kTile - 1) / kTile) +
+                          (a.o_cols ? (m_tiles * l.split_dh + (a.o_cols + kTile - 1) / kTile * l.split_dw) * nt_d : 0);
     ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<true>, 2 * (unsigned)std::min<int64_t>(pairs, items), kHeadThreads, kHeadSmem, s, a));
   }
+  const bool sum_dh = dhidden && l.split_dh > 1, sum_dw = dweight && l.split_dw > 1;
+  if (!sum_dh && !sum_dw) return ADAPM_OK;
+  SumArgs u;
+  std::memset(&u, 0, sizeof(u));
+  u.head = a.head; u.token = a.token; u.hidden = a.hidden; u.scale = scale;
+  int jobs = 0;
+  if (sum_dh)
+    u.job[jobs++] = {a.dh_acc, dhidden, d->hidden_ld, l.t_pad, -1, a.split_dh,
+                     (int32_t)((std::min(l.piece, d->vocab) + kStageK - 1) / kStageK) * a.planes_dh, 0, a.dh_f32, a.dh_wide, 0};
+  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, 0, a.planes_dw, a.dw_f32, a.dw_wide, a.accumulate};
+  u.jobs = jobs;
+  const int64_t rows = std::max(sum_dh ? d->tokens : 0, sum_dw ? d->vocab : 0);
+  const unsigned grid = (unsigned)std::min<int64_t>((rows * ((d->hidden + 15) / 16) + 255) / 256, 4096);
+  ADAPM_CUDA(launch_chained(true, head_sum_kernel, grid * (unsigned)jobs, 256, 0, s, u));
   return ADAPM_OK;
 }
 
