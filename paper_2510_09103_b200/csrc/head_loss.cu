@@ -83,6 +83,20 @@ __device__ __host__ __forceinline__ void parts_of(int stages, int most, int& n, 
   n = (stages + each - 1) / each;
 }
 
+// n / d for 0 <= n < 2^31 by a multiplication: with 2^(s-1) < d <= 2^s and m = floor(2^(31+s) / d) + 1 the quotient is
+// n m >> (31 + s) (Granlund and Montgomery, PLDI 1994).  Every warp divides a few times per item.
+struct Divisor {
+  uint32_t d, m;
+  int shift;
+  __device__ __forceinline__ void set(int x) {
+    d = (uint32_t)x;
+    const int s = x > 1 ? 32 - __clz(x - 1) : 0;
+    shift = s - 1;
+    m = x > 1 ? (uint32_t)((1ull << (31 + s)) / d + 1) : 0;
+  }
+  __device__ __forceinline__ int of(int n) const { return m ? (int)(__umulhi((uint32_t)n, m) >> shift) : n; }
+};
+
 // One tile of a result: its first row and column, its columns, and its share of K, `count` stages from stage k0 of
 // `planes` planes of per_plane stages laid end to end.
 struct Item { int cls, m0, n0, bn, k0, count, per_plane, split; };
@@ -91,15 +105,17 @@ struct Item { int cls, m0, n0, bn, k0, count, per_plane, split; };
 // short ones (logits) in turn, where the pairs that got a long item more join `skip` rounds later.
 struct Walk {
   int pairs, pair, n_dh, n_long, n_short, extra, skip, mine;
-  int m_tiles, nt_v, nt_d, units, k_logits, k_dh, k_dw, each_dh, each_dw;
+  int m_tiles, tiles_dw, base_d, more_d, k_logits, k_dh, k_dw, each_dh, each_dw, all_dh, all_dw, last_group;
+  Divisor by_group, by_last, by_d, by_m, by_dw;
 
   __device__ __forceinline__ void start(const HeadArgs& a, bool backward, int tv, int pair_, int pairs_) {
     pairs = pairs_; pair = pair_;
     m_tiles = (tv + kTile - 1) / kTile;
-    const int cols = backward ? a.g_cols : a.vocab;
-    nt_v = (cols + kTile - 1) / kTile;
-    units = (a.hidden + 31) / 32;
-    nt_d = (units + 7) / 8;
+    const int cols = backward ? a.g_cols : a.vocab, nt_v = (cols + kTile - 1) / kTile;
+    const int units = (a.hidden + 31) / 32, nt_d = (units + 7) / 8;
+    base_d = units / nt_d; more_d = units % nt_d;
+    last_group = m_tiles / kGroupM;
+    by_group.set(max(1, kGroupM * nt_v)); by_last.set(max(1, m_tiles % kGroupM)); by_d.set(nt_d); by_m.set(max(1, m_tiles));
     k_logits = (a.hidden + kStageK - 1) / kStageK;
     n_short = m_tiles * nt_v;
     n_dh = n_long = extra = skip = mine = 0;
@@ -107,10 +123,13 @@ struct Walk {
     k_dh = (a.o_cols + kStageK - 1) / kStageK;
     k_dw = max(1, (tv + kStageK - 1) / kStageK);
     int split_dh, split_dw;
-    parts_of(k_dh * a.planes_dh, a.split_dh, split_dh, each_dh);
-    parts_of(k_dw * a.planes_dw, a.split_dw, split_dw, each_dw);
+    all_dh = k_dh * a.planes_dh; all_dw = k_dw * a.planes_dw;
+    parts_of(all_dh, a.split_dh, split_dh, each_dh);
+    parts_of(all_dw, a.split_dw, split_dw, each_dw);
+    tiles_dw = (a.o_cols + kTile - 1) / kTile;
+    by_dw.set(tiles_dw);
     n_dh = a.dh ? m_tiles * nt_d * split_dh : 0;
-    n_long = n_dh + (a.dw ? (a.o_cols + kTile - 1) / kTile * nt_d * split_dw : 0);
+    n_long = n_dh + (a.dw ? tiles_dw * nt_d * split_dw : 0);
     extra = n_long % pairs;
     const int surplus = load(0) - load(pairs - 1);
     skip = extra && surplus > 0 ? (surplus + k_logits / 2) / k_logits : 0;
@@ -123,42 +142,44 @@ struct Walk {
   }
   // This pair's item `seq`; false past the last.
   // (Read from shared memory: `uniform` tells the compiler that all lanes have the same.)
+  template <bool BACKWARD>
   __device__ __forceinline__ bool item_uniform(const HeadArgs& a, int seq, Item& t) const {
-    if (!uniform((int)item(a, seq, t))) return false;
+    if (!uniform((int)item<BACKWARD>(a, seq, t))) return false;
     t.cls = uniform(t.cls); t.m0 = uniform(t.m0); t.n0 = uniform(t.n0); t.bn = uniform(t.bn);
     t.k0 = uniform(t.k0); t.count = uniform(t.count); t.per_plane = uniform(t.per_plane);
     return true;
   }
+  template <bool BACKWARD>
   __device__ __forceinline__ bool item(const HeadArgs& a, int seq, Item& t) const {
     t.split = t.k0 = 0;
-    if (seq < mine) {
+    if (BACKWARD && seq < mine) {
       int k = pair + seq * pairs;
-      t.cls = k < n_dh ? CLS_DH : CLS_DW;
-      if (t.cls == CLS_DW) k -= n_dh;
-      const int n = k % nt_d, base = units / nt_d, more = units % nt_d;
-      k /= nt_d;
-      const int m = t.cls == CLS_DH ? m_tiles : (a.o_cols + kTile - 1) / kTile;
-      t.split = k / m;
-      t.m0 = (k - t.split * m) * kTile;
-      t.n0 = 32 * (n * base + min(n, more));          // widths as even as multiples of 32 allow
-      t.bn = 32 * (base + (n < more ? 1 : 0));
-      t.per_plane = t.cls == CLS_DH ? k_dh : k_dw;
-      const int each = t.cls == CLS_DH ? each_dh : each_dw, all = t.per_plane * (t.cls == CLS_DH ? a.planes_dh : a.planes_dw);
-      t.k0 = t.split * each;
-      t.count = min(each, all - t.k0);
+      const bool dh = k < n_dh;
+      t.cls = dh ? CLS_DH : CLS_DW;
+      if (!dh) k -= n_dh;
+      const int q = by_d.of(k), n = k - q * (int)by_d.d;
+      t.split = dh ? by_m.of(q) : by_dw.of(q);
+      t.m0 = (q - t.split * (dh ? m_tiles : tiles_dw)) * kTile;
+      t.n0 = 32 * (n * base_d + min(n, more_d));      // widths as even as multiples of 32 allow
+      t.bn = 32 * (base_d + (n < more_d ? 1 : 0));
+      t.per_plane = dh ? k_dh : k_dw;
+      t.k0 = t.split * (dh ? each_dh : each_dw);
+      t.count = min(dh ? each_dh : each_dw, (dh ? all_dh : all_dw) - t.k0);
       return true;
     }
     const int j = seq - mine;
     int k;
-    if (pair < extra) k = skip * (pairs - extra) + j * pairs + pair;
+    if (!BACKWARD) k = seq * pairs + pair;
+    else if (pair < extra) k = skip * (pairs - extra) + j * pairs + pair;
     else if (j < skip) k = j * (pairs - extra) + pair - extra;
     else k = skip * (pairs - extra) + (j - skip) * pairs + pair;
     if (k >= n_short) return false;
-    const int per_group = kGroupM * nt_v, group = k / per_group, in_group = min(kGroupM, m_tiles - group * kGroupM);
-    k -= group * per_group;
+    const int group = by_group.of(k);
+    k -= group * (int)by_group.d;
+    const int n = group < last_group ? k / kGroupM : by_last.of(k);
     t.cls = CLS_LOGITS;
-    t.m0 = (group * kGroupM + k % in_group) * kTile;
-    t.n0 = k / in_group * kTile;
+    t.m0 = (group * kGroupM + k - n * (group < last_group ? kGroupM : (int)by_last.d)) * kTile;
+    t.n0 = n * kTile;
     t.bn = kTile;
     t.per_plane = t.count = k_logits;
     return true;
@@ -171,6 +192,16 @@ struct __align__(8) HeadShared {
   int abort, skip, tv;
   Walk walk;                     // here and not in every thread's registers
 };
+
+// Two fp32 operations per instruction (the same roundings as one at a time).
+__device__ __forceinline__ void fma2(float& d0, float& d1, float a0, float a1, float b, float c) {
+  asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %4};\nmov.b64 z, {%5, %5};\nfma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}"
+      : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b), "f"(c));
+}
+__device__ __forceinline__ void add2(float& d0, float& d1, float a0, float a1) {
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%0, %1};\nmov.b64 y, {%2, %3};\nadd.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+      : "+f"(d0), "+f"(d1) : "f"(a0), "f"(a1));
+}
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -239,27 +270,27 @@ __device__ __forceinline__ void segments(int stages, int most, int& n, int& each
   n = (stages + each - 1) / each;
 }
 
-// v = (or +=) `half` columns of this thread's row of an accumulator.
-__device__ __forceinline__ void take(uint32_t taddr, int half, bool add, float* v) {
-  if (!add) {
+// Columns FROM to TO of `half` of this thread's row of an accumulator: v = them (tmem_ld_wait is the caller's) or v += them.
+template <int FROM, int TO>
+__device__ __forceinline__ void take(uint32_t taddr, int half, float* v) {
 #pragma unroll
-    for (int c = 0; c < 128; c += 16)
-      if (c < half) tmem_ld16(taddr + c, v + c);
-    tmem_ld_wait();
-    return;
-  }
+  for (int c = FROM; c < TO; c += 16)
+    if (c < half) tmem_ld16(taddr + c, v + c);
+}
+template <int FROM, int TO>
+__device__ __forceinline__ void take_add(uint32_t taddr, int half, float* v) {
 #pragma unroll
-  for (int c = 0; c < 128; c += 32) {
+  for (int c = FROM; c < TO; c += 32) {
     if (c < half) {
       float t[32];
       tmem_ld16(taddr + c, t);
       if (c + 16 < half) tmem_ld16(taddr + c + 16, t + 16);
       tmem_ld_wait();
 #pragma unroll
-      for (int e = 0; e < 16; ++e) v[c + e] += t[e];
+      for (int e = 0; e < 16; e += 2) add2(v[c + e], v[c + e + 1], t[e], t[e + 1]);
       if (c + 16 < half) {
 #pragma unroll
-        for (int e = 16; e < 32; ++e) v[c + e] += t[e];
+        for (int e = 16; e < 32; e += 2) add2(v[c + e], v[c + e + 1], t[e], t[e + 1]);
       }
     }
   }
@@ -279,32 +310,36 @@ __device__ __forceinline__ float pick(const float* v, int y) {
   return x;
 }
 
-// Sum of exp over 128 logits of a row, `n` of which exist, as sum * 2^k.  k is the greatest logit in base 2, rounded to a
-// whole number, so that z log2(e) - k is one multiply-add with one rounding and the sums of different columns are scaled by
-// powers of two only.
-__device__ __forceinline__ void row_sums(float* z, int n, bool with_sum, float& k, float& sum, float& total) {
-  total = 0.f;
-  if (n < 128) {
+// Sum of exp over 128 logits of a row as sum * 2^k, k a whole number: z log2(e) - k is then one multiply-add with one rounding,
+// and the sums of different columns are scaled by powers of two only.  k is the greatest of the first 16 logits in base 2: any
+// k near the greatest one does, and one that is known early lets the maxima be found beside the exponentials.  Where a logit is over 2^64 times exp of it after all, or all 16 are -inf, the sum is made again with
+// the greatest of all.  NaN and +inf logits make the sum NaN.
+__device__ __forceinline__ float exponent_of(float top) { return fmaxf(-INFINITY, rintf(top * kLog2e)); }      // (NaN: -inf)
+template <int FROM, int TO>
+__device__ __forceinline__ void add_exponentials(const float* z, float shift, float* s) {
 #pragma unroll
-    for (int e = 0; e < 128; ++e) {
-      if (e < n) total += z[e];
-      else z[e] = -INFINITY;
-    }
-  } else if (with_sum) {
-    float t[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < 128; ++e) t[e & 3] += z[e];
-    total = (t[0] + t[1]) + (t[2] + t[3]);
+  for (int e = FROM; e < TO; e += 2) {
+    float p0, p1;
+    fma2(p0, p1, z[e], z[e + 1], kLog2e, -shift);
+    add2(s[e & 2], s[(e & 2) + 1], ex2(p0), ex2(p1));
   }
-  float top[4] = {z[0], z[1], z[2], z[3]};
+}
+template <int FROM, int TO>
+__device__ __forceinline__ float greatest(const float* z) {
+  float top[4] = {z[FROM], z[FROM + 1], z[FROM + 2], z[FROM + 3]};
 #pragma unroll
-  for (int e = 4; e < 128; ++e) top[e & 3] = fmaxf(top[e & 3], z[e]);
-  k = fmaxf(-INFINITY, rintf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * kLog2e));      // (all NaN: -inf)
-  const float shift = k == -INFINITY ? 0.f : k;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int e = FROM + 4; e < TO; ++e) top[e & 3] = fmaxf(top[e & 3], z[e]);
+  return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+}
+// Columns from n on count as -inf; returns the sum of the others.
+__device__ __forceinline__ float cut_row(float* z, int n) {
+  float t = 0.f;
 #pragma unroll
-  for (int e = 0; e < 128; ++e) s[e & 3] += ex2(fmaf(z[e], kLog2e, -shift));
-  sum = (s[0] + s[1]) + (s[2] + s[3]);
+  for (int e = 0; e < 128; ++e) {
+    if (e < n) t += z[e];
+    else z[e] = -INFINITY;
+  }
+  return t;
 }
 
 template <bool BACKWARD>
@@ -358,7 +393,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     int stage = 0;
     uint32_t phase = 0, issued = 0;
     bool ok = true;
-    for (int seq = 0; ok && walk.item_uniform(a, seq, t); ++seq) {
+    for (int seq = 0; ok && walk.item_uniform<BACKWARD>(a, seq, t); ++seq) {
       const CUtensorMap* map;
       int x, y, n_box = 1;                 // K-major: one box of 128 rows, x runs; MN-major: boxes of 64 columns, y runs
       const int half = t.bn / 2, o_row = a.o_buf * a.planes * a.t_pad;
@@ -410,7 +445,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     bool ok = true;
     const uint32_t ring = uniform(smem_u32(stages)), d0 = uniform(tmem_base), dhi = desc_hi();
     uint32_t run = 0;                     // segments so far
-    for (int seq = 0; ok && walk.item_uniform(a, seq, t); ++seq) {
+    for (int seq = 0; ok && walk.item_uniform<BACKWARD>(a, seq, t); ++seq) {
       const bool a_mn = t.cls == CLS_DW, b_mn = t.cls != CLS_LOGITS;
       const uint32_t idesc = uniform(make_idesc(t.bn, a_mn, b_mn, false, 256));
       // per K step of 16: 32 bytes inside a K-major row, 16 rows of 128 bytes of an MN-major box (in 16-byte units)
@@ -452,31 +487,42 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     const uint32_t lane_addr = (uint32_t)(32 * (warp & 3)) << 16;
     uint32_t run = 0;
     bool ok = true;
-    for (int seq = 0; !skip && walk.item(a, seq, t); ++seq) {
-      const int cls = t.cls, m0 = t.m0, n0 = t.n0;
-      const int row = m0 + (int)rank * 128 + q, half = t.bn / 2;
-      // what the row needs is asked for before the accumulator is waited for
-      int y = -1, token = 0;
-      float lse = 0.f, dl = 0.f;
-      if (cls == CLS_LOGITS && row < tv) {
+    // what a row needs is asked for an item ahead
+    struct Row { int y, token; float lse, dl; };
+    auto fetch = [&](const Item& t) {
+      Row r = {-1, 0, 0.f, 0.f};
+      const int row = t.m0 + (int)rank * 128 + q;
+      if (row >= tv) return r;
+      if (t.cls == CLS_LOGITS) {
         if (!BACKWARD && a.targets) {
           const int64_t wide_y = a.targets[row];
-          y = wide_y >= 0 && wide_y < a.vocab ? (int)wide_y : -(1 << 30);
+          r.y = wide_y >= 0 && wide_y < a.vocab ? (int)wide_y : -(1 << 30);
         } else {
-          y = a.target[row];
+          r.y = a.target[row];
         }
-        y -= n0 + 128 * grp;
         if (BACKWARD) {
-          y -= a.g_begin;
-          lse = a.lse[row];
-          dl = a.dloss ? a.dloss[row] : 1.f;
+          r.lse = a.lse[row];
+          r.dl = a.dloss ? a.dloss[row] : 1.f;
         }
-      } else if (BACKWARD && cls == CLS_DH && a.last && a.split_dh == 1 && row < tv) {
-        token = a.token[row];
+      } else if (BACKWARD && t.cls == CLS_DH && a.last && a.split_dh == 1) {
+        r.token = a.token[row];
       }
+      return r;
+    };
+    bool more = !skip && walk.item<BACKWARD>(a, 0, t);
+    Row here = {-1, 0, 0.f, 0.f};
+    if (more) here = fetch(t);
+    for (int seq = 1; more; ++seq) {
+      const int cls = t.cls, m0 = t.m0, n0 = t.n0, split = t.split, count = t.count;
+      const int row = m0 + (int)rank * 128 + q, half = t.bn / 2;
+      const Row now = here;
+      more = walk.item<BACKWARD>(a, seq, t);
+      if (more) here = fetch(t);
+      const int y = row < tv ? now.y - (BACKWARD ? a.g_begin : 0) - n0 - 128 * grp : -1, token = now.token;
+      const float lse = now.lse, dl = now.dl;
       float v[128];
       int n_seg, each;
-      segments(t.count, cls == CLS_LOGITS ? a.seg_logits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
+      segments(count, cls == CLS_LOGITS ? a.seg_logits : cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
 #pragma unroll 1
       for (int i = 0; i < n_seg; ++i, ++run) {
         const int acc = (int)(run & 1);
@@ -484,7 +530,13 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
         tc_fence_after();
-        take(tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * half), half, i > 0, v);
+        const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * half);
+        if (i > 0) {
+          take_add<0, 128>(at, half, v);
+        } else {
+          take<0, 128>(at, half, v);
+          tmem_ld_wait();
+        }
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_relaxed_at(shared_of(&sh.tempty[acc], 0));
@@ -492,9 +544,25 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
       if (!ok) break;
       if (!BACKWARD) {
         const int n = min(128, a.vocab - n0 - 128 * grp);
-        float k, sum, total;
         if ((unsigned)y < 128u && y < n) a.z_target[row] = pick(v, y);
-        row_sums(v, n, a.smooth != 0.f, k, sum, total);
+        float total = 0.f, s[4] = {0.f, 0.f, 0.f, 0.f};
+        if (n < 128) {
+          total = cut_row(v, n);
+        } else if (a.smooth != 0.f) {
+          float t[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < 128; e += 2) add2(t[e & 2], t[(e & 2) + 1], v[e], v[e + 1]);
+          total = (t[0] + t[1]) + (t[2] + t[3]);
+        }
+        float k = exponent_of(greatest<0, 16>(v));
+        add_exponentials<0, 128>(v, k == -INFINITY ? 0.f : k, s);
+        const float all = exponent_of(greatest<16, 128>(v));
+        if (all > k && (all > k + 64.f || k == -INFINITY)) {
+          k = all;
+          s[0] = s[1] = s[2] = s[3] = 0.f;
+          add_exponentials<0, 128>(v, k, s);
+        }
+        const float sum = (s[0] + s[1]) + (s[2] + s[3]);
         if (row < tv) {
           const int64_t at = (int64_t)(n0 / 128 + grp) * a.t_pad + row;
           a.part[at] = make_float2(k, sum);
@@ -514,7 +582,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         for (int c = 0; c < 128; c += 16) {
           float* const z = v + c;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) z[e] = fmaf(ex2(fmaf(z[e], kLog2e, -k)), up, -down);
+          for (int e = 0; e < 16; e += 2) {
+            float p0, p1;
+            fma2(p0, p1, z[e], z[e + 1], kLog2e, -k);
+            fma2(z[e], z[e + 1], ex2(p0), ex2(p1), up, -down);
+          }
           if ((unsigned)(y - c) < 16u) {
 #pragma unroll
             for (int e = 0; e < 16; ++e)
@@ -546,7 +618,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         const bool to_acc = cut || (is_dh && !a.last), from_acc = is_dh && !a.first, from_out = !to_acc && !is_dh && a.accumulate;
         void* const out = is_dh ? a.dh : a.dw;
         const int64_t out_row = is_dh ? (int64_t)token * a.hidden_ld : (int64_t)(a.o_begin + row) * a.weight_ld;
-        float* const acc_row = is_dh ? a.dh_acc + ((int64_t)t.split * a.t_pad + row) * a.hidden : a.dw_acc + ((int64_t)t.split * a.vocab + row) * a.hidden;
+        float* const acc_row = is_dh ? a.dh_acc + ((int64_t)split * a.t_pad + row) * a.hidden : a.dw_acc + ((int64_t)split * a.vocab + row) * a.hidden;
         const bool f32 = is_dh ? a.dh_f32 : a.dw_f32, wide = is_dh ? a.dh_wide : a.dw_wide;
         const float scale = to_acc ? 1.f : a.scale;
 #pragma unroll
@@ -766,26 +838,39 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
   wait_for_previous_kernel();
   if (a.head[HD_STATUS] != 0) return;
   const SumArgs::Job& j = a.job[blockIdx.x % a.jobs];
-  const int tv = a.head[HD_COUNT], rows = j.rows < 0 ? tv : j.rows, vec = (a.hidden + 15) / 16;
+  const int tv = a.head[HD_COUNT], rows = j.rows < 0 ? tv : j.rows, vec = a.hidden / 8;
   int n, each;
   parts_of(j.planes_of_tokens ? max(1, (tv + kStageK - 1) / kStageK) * j.planes_of_tokens : j.stages, j.most, n, each);
   const int64_t part = j.part_rows * a.hidden, stride = (int64_t)(gridDim.x / a.jobs) * 256;
   for (int64_t i = (int64_t)(blockIdx.x / a.jobs) * 256 + threadIdx.x; i < (int64_t)rows * vec; i += stride) {
     const int64_t row = i / vec;
-    const int c = (int)(i - row * vec) * 16, live = a.hidden - c;
-    float x[16], more[16];
-    load_row16(j.acc, row * a.hidden + c, x, live, true);
-#pragma unroll 4
-    for (int p = 1; p < n; ++p) {
-      load_row16(j.acc, p * part + row * a.hidden + c, more, live, true);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[e] += more[e];
-    }
+    const int c = (int)(i - row * vec) * 8;
     const int64_t at = (j.rows < 0 ? (int64_t)a.token[row] : row) * j.ld + c;
-    if (j.accumulate) load_row16(j.out, at, more, live, j.f32);
+    float x[8], old[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) x[e] = fmaf(x[e], a.scale, j.accumulate ? more[e] : 0.f);
-    store_row16(j.out, at, x, live, j.f32, j.wide);
+    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+    if (j.accumulate) load_row16(j.out, at, old, 8, j.f32);
+    const float* p = j.acc + row * a.hidden + c;
+    for (int left = n; left > 0; left -= 8, p += 8 * part) {         // eight parts on their way at a time
+      float4 v[8][2];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        v[u][0] = v[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (u < left) {
+          const float4* const q = reinterpret_cast<const float4*>(p + u * part);
+          v[u][0] = __ldcg(q); v[u][1] = __ldcg(q + 1);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        x[0] += v[u][0].x; x[1] += v[u][0].y; x[2] += v[u][0].z; x[3] += v[u][0].w;
+        x[4] += v[u][1].x; x[5] += v[u][1].y; x[6] += v[u][1].z; x[7] += v[u][1].w;
+      }
+    }
+    float out[16];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = fmaf(x[e], a.scale, j.accumulate ? old[e] : 0.f);
+    store_row16(j.out, at, out, 8, j.f32, j.wide);
   }
 }
 
@@ -809,7 +894,7 @@ int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   if (d.hidden % 8) return ADAPM_EUNSUPPORTED;
   if (d.hidden_ld < d.hidden || d.weight_ld < d.hidden) return ADAPM_EINVAL;
   if (d.hidden_ld % 8 || d.weight_ld % 8) return ADAPM_EALIGN;
-  if (d.hidden_ld >= ((int64_t)1 << 38) || d.weight_ld >= ((int64_t)1 << 38)) return ADAPM_ERANGE;      // (a tensor map's pitch has 40 bits)
+  if (d.hidden_ld >= ((int64_t)1 << 32) || d.weight_ld >= ((int64_t)1 << 32)) return ADAPM_ERANGE;      // (sizes in bytes fit 64 bits, pitches a tensor map's 40)
   if (!(d.label_smoothing >= 0.f && d.label_smoothing <= 1.f) || !(d.z_loss >= 0.f) || !std::isfinite(d.z_loss)) return ADAPM_ERANGE;
   if (backward && (!known_type(d.dhidden_dtype) || !known_type(d.dweight_dtype))) return ADAPM_EINVAL;
   l.t_pad = round_up(d.tokens < 1 ? 1 : d.tokens, kTile);
@@ -821,18 +906,20 @@ int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   l.n_pieces = (d.vocab + l.piece - 1) / l.piece;
   l.n_buf = l.n_pieces > 1 ? 2 : 1;
   if (l.t_pad / kTile * l.n_tiles > (1 << 30) || l.n_buf * l.planes * l.t_pad >= ((int64_t)1 << 31)) return ADAPM_ERANGE;
-  // A gradient's K is cut into parts where one of its items would take longer than all items divided over the pairs: few tokens
-  // leave dh a handful of tiles with the whole vocabulary as their K, a small vocabulary does the same to dw.  (512 tokens of
-  // 4096 x 256 in fp32: 77 us without.)  A part is at least four stages.
+  // A gradient's K is cut into parts where an item of it would take more than half of what all items take divided over the
+  // pairs: few tokens leave dh a handful of tiles with the whole vocabulary as their K, a small vocabulary does the same to dw.
+  // A part is at least 16 stages (5 us), because the parts cost a launch and their way through memory.  512 tokens of 4096 x 256
+  // in fp32, both gradients: 78 us without; parts of at least 4 stages 56, of 16 44.
   l.split_dh = l.split_dw = 1;
   if (backward) {
     const int64_t mt = l.t_pad / kTile, nt_d = (d.hidden + kTile - 1) / kTile, tiles = l.piece / kTile;
     const int64_t k_dh = (std::min(l.piece, d.vocab) + kStageK - 1) / kStageK * (d.dhidden_dtype == ADAPM_TYPE_F32 ? 3 : 1);
     const int64_t k_dw = l.t_pad / kStageK * (d.dweight_dtype == ADAPM_TYPE_F32 ? 3 : 1);
     const int64_t logits = l.n_pieces > 1 ? mt * tiles * ((d.hidden + kStageK - 1) / kStageK) : 0;
-    const int64_t share = std::max<int64_t>(4, (nt_d * (mt * k_dh + tiles * k_dw) + logits) / kPlanPairs);
-    l.split_dh = std::min<int64_t>((k_dh + share - 1) / share, 256);
-    if (l.n_pieces == 1) l.split_dw = std::min<int64_t>((k_dw + share - 1) / share, 256);
+    const int64_t share = std::max<int64_t>(1, (nt_d * (mt * k_dh + tiles * k_dw) + logits) / kPlanPairs);
+    auto parts = [&](int64_t k) { return std::max<int64_t>(1, std::min({(2 * k + share - 1) / share, k / 16, (int64_t)256})); };
+    l.split_dh = parts(k_dh);
+    if (l.n_pieces == 1) l.split_dw = parts(k_dw);
   }
   int64_t at = kHeadBytes;
   auto take = [&](int64_t bytes) { const int64_t o = at; at += round_up(bytes, 256); return o; };
@@ -1061,7 +1148,7 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, 0, a.planes_dw, a.dw_f32, a.dw_wide, a.accumulate};
   u.jobs = jobs;
   const int64_t rows = std::max(sum_dh ? d->tokens : 0, sum_dw ? d->vocab : 0);
-  const unsigned grid = (unsigned)std::min<int64_t>((rows * ((d->hidden + 15) / 16) + 255) / 256, 4096);
+  const unsigned grid = (unsigned)std::min<int64_t>((rows * (d->hidden / 8) + 255) / 256, 4096);
   ADAPM_CUDA(launch_chained(true, head_sum_kernel, grid * (unsigned)jobs, 256, 0, s, u));
   return ADAPM_OK;
 }

@@ -475,6 +475,20 @@ def test_head_loss_backward_over_several_pieces_of_the_vocabulary(dht, dwt):
     _check_backward(hidden, weight, targets, lse, dh, dw, None, 1.0 / tokens, into=into)
 
 
+@pytest.mark.parametrize("dht,dwt", [(BF16, BF16), (F32, F32)])
+@pytest.mark.parametrize("tokens,vocab,width,ignored", [(2000, 40000, 72, 0.1), (5000, 700, 136, 0.3), (5000, 700, 136, 0.99), (40, 9000, 264, 0.0)])
+def test_head_loss_backward_where_the_long_side_of_a_product_is_cut(tokens, vocab, width, ignored, dht, dwt):
+    """Few tiles with a long K: dhidden over two pieces in several parts each, dweight in parts (with fewer tokens than they were
+    planned for, too), and both added to what is there."""
+    hidden, _, weight, _, targets = _head_case(tokens, vocab, width, ignored=ignored, std=0.3)
+    lse = R.head_loss(hidden, weight, targets)[1].float()
+    into = torch.randn(vocab, width, device="cuda").to(dwt)
+    dh, dw = _backward(hidden, weight, targets, lse, None, 0.25, dht, dwt, into=into)
+    _check_backward(hidden, weight, targets, lse, dh, dw, None, 0.25, into=into)
+    assert torch.equal(_backward(hidden, weight, targets, lse, None, 0.25, dht, dwt, want_dw=False)[0], dh)
+    assert torch.equal(_backward(hidden, weight, targets, lse, None, 0.25, dht, dwt, want_dh=False, into=into)[1], dw)
+
+
 def test_head_loss_one_gradient_alone_and_the_same_bits_twice():
     hidden, _, weight, _, targets = _head_case(600, 3001, 96, ignored=0.2)
     lse = R.head_loss(hidden, weight, targets)[1].float()
