@@ -50,33 +50,6 @@ enum : int32_t { CLS_LOGITS = 0, CLS_DH = 1, CLS_DW = 2 };
 enum : int32_t { HD_STATUS = 0, HD_COUNT = 1, HD_PAIRS = 64 };
 constexpr int kMostPairs = 128, kHeadBytes = 4 * (HD_PAIRS + kMostPairs);
 
-struct HeadArgs {
-  CUtensorMap hk, hn, ck, cn, wk, wn, gk, gn;      // hidden, its compacted copy, weight, g; boxes of 64 x 128 (K-major use) and 64 x 64
-  int32_t* head;                 // HD_*
-  const int32_t* token;          // of a compacted row
-  const int32_t* target;         // of a compacted row
-  const int64_t* targets;        // forward over at most a tile of tokens, which are not compacted: the caller's (else null)
-  const float* lse;              // of a compacted row
-  const float* dloss;            // of a compacted row, or null: 1
-  float2* part;                  // forward: (exponent, sum) [2 n_tiles][t_pad]
-  float* part_sum;               // forward with smoothing: sum of the logits, same layout
-  float* z_target;               // forward: logit of the target of a compacted row
-  uint16_t* g;                   // [2 buffers][planes][t_pad][piece]
-  float* dh_acc;                 // [split_dh][t_pad][hidden], between two pieces and before the splits are added up
-  float* dw_acc;                 // [split_dw][vocab][hidden], before the splits are added up
-  void* dh;
-  void* dw;
-  int64_t hidden_ld, weight_ld;
-  int32_t tokens, vocab, hidden, t_pad, piece, planes, planes_dh, planes_dw;
-  int32_t g_begin, g_cols, g_buf;          // piece whose g this launch makes (g_cols = 0: none)
-  int32_t o_begin, o_cols, o_buf;          // piece whose gradients it makes (o_cols = 0: none)
-  int32_t first, last;                     // of the pieces, for dh
-  int32_t split_dh, split_dw;              // parts that K is cut into, at most; 1: not cut
-  int32_t dh_f32, dw_f32, accumulate, dh_wide, dw_wide;      // wide: rows start on 32 bytes
-  int32_t seg_logits, seg_dh, seg_dw;      // longest segments, in stages
-  float scale, smooth, z_loss;
-};
-
 // `stages` in at most `most` parts of even length: how many, and the stages of each but the last.
 __device__ __host__ __forceinline__ void parts_of(int stages, int most, int& n, int& each) {
   each = (stages + most - 1) / most;
@@ -88,70 +61,92 @@ __device__ __host__ __forceinline__ void parts_of(int stages, int most, int& n, 
 struct Divisor {
   uint32_t d, m;
   int shift;
-  __device__ __forceinline__ void set(int x) {
+  __host__ __device__ void set(int x) {
     d = (uint32_t)x;
-    const int s = x > 1 ? 32 - __clz(x - 1) : 0;
+    int s = 0;
+    while ((1ll << s) < x) ++s;
     shift = s - 1;
     m = x > 1 ? (uint32_t)((1ull << (31 + s)) / d + 1) : 0;
   }
-  __device__ __forceinline__ int of(int n) const { return m ? (int)(__umulhi((uint32_t)n, m) >> shift) : n; }
+  __host__ __device__ __forceinline__ int of(int n) const { return m ? (int)((uint32_t)(((uint64_t)(uint32_t)n * m) >> 32) >> shift) : n; }
 };
 
 // One tile of a result: its first row and column, its columns, and its share of K, `count` stages from stage k0 of
 // `planes` planes of per_plane stages laid end to end.
-struct Item { int cls, m0, n0, bn, k0, count, per_plane, split; };
+struct HeadItem { int cls, m0, n0, bn, k0, count, per_plane, split; };
 
-// The items of a launch, as every warp of a pair walks through them.  Long items (gradients) first, dealt out in turn; then the
-// short ones (logits) in turn, where the pairs that got a long item more join `skip` rounds later.
+// What the items of a call follow from, beside the number of tokens with a target.
+struct Plan {
+  int32_t tokens, vocab, hidden, piece, n_pieces, planes_dh, planes_dw, split_dh, split_dw, dh, dw, backward, pairs;
+  __host__ __device__ int cols(int i) const {               // of piece i of the vocabulary
+    const int left = vocab - i * piece;
+    return i < 0 || i >= n_pieces ? 0 : left < piece ? left : piece;
+  }
+  // Pairs of CTAs of launch i (with every token counted: the host does not know better).
+  __host__ __device__ int used(int i) const {
+    const int64_t m = (tokens + kTile - 1) / kTile, tiles = (cols(i) + kTile - 1) / kTile, o = backward ? (cols(i - 1) + kTile - 1) / kTile : 0;
+    const int64_t items = m * tiles + (o ? (m * split_dh + o * split_dw) * ((hidden + kTile - 1) / kTile) : 0);
+    return items < pairs ? (int)items : pairs;
+  }
+};
+
+// The items of launch i of a call, as every warp of a pair walks through them: in the backward call those of the logits of piece i
+// and of the gradients of piece i - 1.  Long items (gradients) first, dealt out in turn; then the short ones (logits) in turn,
+// where the pairs that got a long item more join `skip` rounds later.  Made once per call, by the host or by the kernel that
+// counts the tokens; a launch that made it anew spent two microseconds on its divisions.
 struct Walk {
-  int pairs, pair, n_dh, n_long, n_short, extra, skip, mine;
+  int tv, pairs, n_dh, n_long, n_short, extra, skip, rounds;
   int m_tiles, tiles_dw, base_d, more_d, k_logits, k_dh, k_dw, each_dh, each_dw, all_dh, all_dw, last_group;
   Divisor by_group, by_last, by_d, by_m, by_dw;
 
-  __device__ __forceinline__ void start(const HeadArgs& a, bool backward, int tv, int pair_, int pairs_) {
-    pairs = pairs_; pair = pair_;
+  __host__ __device__ void make(const Plan& p, int i, int tv_) {
+    tv = tv_;
+    pairs = p.used(i);
     m_tiles = (tv + kTile - 1) / kTile;
-    const int cols = backward ? a.g_cols : a.vocab, nt_v = (cols + kTile - 1) / kTile;
-    const int units = (a.hidden + 31) / 32, nt_d = (units + 7) / 8;
+    const int nt_v = (p.cols(i) + kTile - 1) / kTile, units = (p.hidden + 31) / 32, nt_d = (units + 7) / 8;
     base_d = units / nt_d; more_d = units % nt_d;
     last_group = m_tiles / kGroupM;
-    by_group.set(max(1, kGroupM * nt_v)); by_last.set(max(1, m_tiles % kGroupM)); by_d.set(nt_d); by_m.set(max(1, m_tiles));
-    k_logits = (a.hidden + kStageK - 1) / kStageK;
+    by_group.set(nt_v ? kGroupM * nt_v : 1); by_last.set(m_tiles % kGroupM ? m_tiles % kGroupM : 1);
+    by_d.set(nt_d); by_m.set(m_tiles ? m_tiles : 1);
+    k_logits = (p.hidden + kStageK - 1) / kStageK;
     n_short = m_tiles * nt_v;
-    n_dh = n_long = extra = skip = mine = 0;
-    if (!backward || a.o_cols == 0) return;
-    k_dh = (a.o_cols + kStageK - 1) / kStageK;
-    k_dw = max(1, (tv + kStageK - 1) / kStageK);
+    n_dh = n_long = extra = skip = rounds = k_dh = k_dw = each_dh = each_dw = all_dh = all_dw = tiles_dw = 0;
+    const int o_cols = p.backward ? p.cols(i - 1) : 0;
+    by_dw.set(1);
+    if (o_cols == 0) return;
+    k_dh = (o_cols + kStageK - 1) / kStageK;
+    k_dw = tv > 0 ? (tv + kStageK - 1) / kStageK : 1;
     int split_dh, split_dw;
-    all_dh = k_dh * a.planes_dh; all_dw = k_dw * a.planes_dw;
-    parts_of(all_dh, a.split_dh, split_dh, each_dh);
-    parts_of(all_dw, a.split_dw, split_dw, each_dw);
-    tiles_dw = (a.o_cols + kTile - 1) / kTile;
+    all_dh = k_dh * p.planes_dh; all_dw = k_dw * p.planes_dw;
+    parts_of(all_dh, p.split_dh, split_dh, each_dh);
+    parts_of(all_dw, p.split_dw, split_dw, each_dw);
+    tiles_dw = (o_cols + kTile - 1) / kTile;
     by_dw.set(tiles_dw);
-    n_dh = a.dh ? m_tiles * nt_d * split_dh : 0;
-    n_long = n_dh + (a.dw ? tiles_dw * nt_d * split_dw : 0);
+    n_dh = p.dh ? m_tiles * nt_d * split_dh : 0;
+    n_long = n_dh + (p.dw ? tiles_dw * nt_d * split_dw : 0);
+    rounds = n_long / pairs;
     extra = n_long % pairs;
     const int surplus = load(0) - load(pairs - 1);
     skip = extra && surplus > 0 ? (surplus + k_logits / 2) / k_logits : 0;
-    mine = dealt(n_long, pair);
   }
-  __device__ __forceinline__ int dealt(int n, int p) const { return p < n ? (n - p + pairs - 1) / pairs : 0; }
-  __device__ __forceinline__ int load(int p) const {
+  __host__ __device__ int dealt(int n, int p) const { return n / pairs + (p < n % pairs ? 1 : 0); }
+  __host__ __device__ int load(int p) const {
     const int dh = dealt(n_dh, p);
     return dh * each_dh + (dealt(n_long, p) - dh) * each_dw;
   }
   // This pair's item `seq`; false past the last.
   // (Read from shared memory: `uniform` tells the compiler that all lanes have the same.)
   template <bool BACKWARD>
-  __device__ __forceinline__ bool item_uniform(const HeadArgs& a, int seq, Item& t) const {
-    if (!uniform((int)item<BACKWARD>(a, seq, t))) return false;
+  __device__ __forceinline__ bool item_uniform(int pair, int seq, HeadItem& t) const {
+    if (!uniform((int)item<BACKWARD>(pair, seq, t))) return false;
     t.cls = uniform(t.cls); t.m0 = uniform(t.m0); t.n0 = uniform(t.n0); t.bn = uniform(t.bn);
     t.k0 = uniform(t.k0); t.count = uniform(t.count); t.per_plane = uniform(t.per_plane);
     return true;
   }
   template <bool BACKWARD>
-  __device__ __forceinline__ bool item(const HeadArgs& a, int seq, Item& t) const {
+  __host__ __device__ __forceinline__ bool item(int pair, int seq, HeadItem& t) const {
     t.split = t.k0 = 0;
+    const int mine = BACKWARD ? rounds + (pair < extra ? 1 : 0) : 0;
     if (BACKWARD && seq < mine) {
       int k = pair + seq * pairs;
       const bool dh = k < n_dh;
@@ -160,11 +155,12 @@ struct Walk {
       const int q = by_d.of(k), n = k - q * (int)by_d.d;
       t.split = dh ? by_m.of(q) : by_dw.of(q);
       t.m0 = (q - t.split * (dh ? m_tiles : tiles_dw)) * kTile;
-      t.n0 = 32 * (n * base_d + min(n, more_d));      // widths as even as multiples of 32 allow
+      t.n0 = 32 * (n * base_d + (n < more_d ? n : more_d));      // widths as even as multiples of 32 allow
       t.bn = 32 * (base_d + (n < more_d ? 1 : 0));
       t.per_plane = dh ? k_dh : k_dw;
       t.k0 = t.split * (dh ? each_dh : each_dw);
-      t.count = min(dh ? each_dh : each_dw, (dh ? all_dh : all_dw) - t.k0);
+      const int each = dh ? each_dh : each_dw, left = (dh ? all_dh : all_dw) - t.k0;
+      t.count = each < left ? each : left;
       return true;
     }
     const int j = seq - mine;
@@ -186,10 +182,39 @@ struct Walk {
   }
 };
 
+struct HeadArgs {
+  CUtensorMap hk, hn, ck, cn, wk, wn, gk, gn;      // hidden, its compacted copy, weight, g; boxes of 64 x 128 (K-major use) and 64 x 64
+  int32_t* head;                 // HD_*
+  const Walk* walk;              // of this launch, on the device; null: own_walk
+  Walk own_walk;
+  const int32_t* token;          // of a compacted row
+  const int32_t* target;         // of a compacted row
+  const int64_t* targets;        // forward over at most a tile of tokens, which are not compacted: the caller's (else null)
+  const float* lse;              // of a compacted row
+  const float* dloss;            // of a compacted row, or null: 1
+  float2* part;                  // forward: (exponent, sum) [2 n_tiles][t_pad]
+  float* part_sum;               // forward with smoothing: sum of the logits, same layout
+  float* z_target;               // forward: logit of the target of a compacted row
+  uint16_t* g;                   // [2 buffers][planes][t_pad][piece]
+  float* dh_acc;                 // [split_dh][t_pad][hidden], between two pieces and before the splits are added up
+  float* dw_acc;                 // [split_dw][vocab][hidden], before the splits are added up
+  void* dh;
+  void* dw;
+  int64_t hidden_ld, weight_ld;
+  int32_t tokens, vocab, hidden, t_pad, piece, planes;
+  int32_t g_begin, g_cols, g_buf;          // piece whose g this launch makes (g_cols = 0: none)
+  int32_t o_begin, o_cols, o_buf;          // piece whose gradients it makes (o_cols = 0: none)
+  int32_t first, last;                     // of the pieces, for dh
+  int32_t split_dh, split_dw;              // parts that K is cut into, at most; 1: not cut
+  int32_t dh_f32, dw_f32, accumulate, dh_wide, dw_wide;      // wide: rows start on 32 bytes
+  int32_t seg_logits, seg_dh, seg_dw;      // longest segments, in stages
+  float scale, smooth, z_loss;
+};
+
 struct __align__(8) HeadShared {
   uint64_t full[kHeadStages], empty[kHeadStages], tfull[2], tempty[2];
   uint32_t tmem_base;
-  int abort, skip, tv;
+  int abort, skip;
   Walk walk;                     // here and not in every thread's registers
 };
 
@@ -364,9 +389,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     if (!BACKWARD && rank == 0) *status = 0;          // (the cluster barrier below orders it before what either CTA adds)
     sh.skip = BACKWARD && *reinterpret_cast<volatile int32_t*>(status) != 0;
     mbar_fence_init();
-    sh.tv = !BACKWARD && a.targets ? a.tokens : *reinterpret_cast<volatile int32_t*>(a.head + HD_COUNT);
-    sh.walk.start(a, BACKWARD, sh.tv, (int)(blockIdx.x >> 1), (int)(gridDim.x >> 1));
   }
+  if (threadIdx.x >= 64 && threadIdx.x < 64 + sizeof(Walk) / 4)
+    reinterpret_cast<int*>(&sh.walk)[threadIdx.x - 64] = reinterpret_cast<const int*>(a.walk ? a.walk : &a.own_walk)[threadIdx.x - 64];
   if (warp == 1) {
     tmem_alloc<true>(&sh.tmem_base, 512);
     tmem_relinquish<true>();
@@ -377,10 +402,10 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
   tc_fence_after();
   const uint32_t tmem_base = sh.tmem_base;
   const bool skip = load_shared_of(&sh.skip, 0) != 0;       // an earlier launch gave up: the pair decides together
-  const int tv = uniform(sh.tv);
+  const int tv = uniform(sh.walk.tv), pair = (int)(blockIdx.x >> 1);
   const bool compacted = tv != a.tokens;
   const Walk& walk = sh.walk;
-  Item t;
+  HeadItem t;
 
   if (warp < 4) {
   asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
@@ -393,7 +418,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     int stage = 0;
     uint32_t phase = 0, issued = 0;
     bool ok = true;
-    for (int seq = 0; ok && walk.item_uniform<BACKWARD>(a, seq, t); ++seq) {
+    for (int seq = 0; ok && walk.item_uniform<BACKWARD>(pair, seq, t); ++seq) {
       const CUtensorMap* map;
       int x, y, n_box = 1;                 // K-major: one box of 128 rows, x runs; MN-major: boxes of 64 columns, y runs
       const int half = t.bn / 2, o_row = a.o_buf * a.planes * a.t_pad;
@@ -445,7 +470,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     bool ok = true;
     const uint32_t ring = uniform(smem_u32(stages)), d0 = uniform(tmem_base), dhi = desc_hi();
     uint32_t run = 0;                     // segments so far
-    for (int seq = 0; ok && walk.item_uniform<BACKWARD>(a, seq, t); ++seq) {
+    for (int seq = 0; ok && walk.item_uniform<BACKWARD>(pair, seq, t); ++seq) {
       const bool a_mn = t.cls == CLS_DW, b_mn = t.cls != CLS_LOGITS;
       const uint32_t idesc = uniform(make_idesc(t.bn, a_mn, b_mn, false, 256));
       // per K step of 16: 32 bytes inside a K-major row, 16 rows of 128 bytes of an MN-major box (in 16-byte units)
@@ -489,7 +514,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
     bool ok = true;
     // what a row needs is asked for an item ahead
     struct Row { int y, token; float lse, dl; };
-    auto fetch = [&](const Item& t) {
+    auto fetch = [&](const HeadItem& t) {
       Row r = {-1, 0, 0.f, 0.f};
       const int row = t.m0 + (int)rank * 128 + q;
       if (row >= tv) return r;
@@ -509,14 +534,14 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
       }
       return r;
     };
-    bool more = !skip && walk.item<BACKWARD>(a, 0, t);
+    bool more = !skip && walk.item<BACKWARD>(pair, 0, t);
     Row here = {-1, 0, 0.f, 0.f};
     if (more) here = fetch(t);
     for (int seq = 1; more; ++seq) {
       const int cls = t.cls, m0 = t.m0, n0 = t.n0, split = t.split, count = t.count;
       const int row = m0 + (int)rank * 128 + q, half = t.bn / 2;
       const Row now = here;
-      more = walk.item<BACKWARD>(a, seq, t);
+      more = walk.item<BACKWARD>(pair, seq, t);
       if (more) here = fetch(t);
       const int y = row < tv ? now.y - (BACKWARD ? a.g_begin : 0) - n0 - 128 * grp : -1, token = now.token;
       const float lse = now.lse, dl = now.dl;
@@ -569,6 +594,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
           if (a.smooth != 0.f) a.part_sum[at] = total;
         }
       } else if (cls == CLS_LOGITS) {
+        if (m0 + (int)rank * 128 + 32 * (warp & 3) >= ((tv + kStageK - 1) & -kStageK)) continue;      // rows that nothing reads
         // p = exp(z - lse) = 2^(z log2(e) - k) 2^(k - lse log2(e)) with k whole: the first exponent is one multiply-add
         // with one rounding, the second factor belongs to the row
         const float k = rintf(lse * kLog2e);
@@ -666,8 +692,10 @@ struct PrepareArgs {
   const float* dloss_in; float* dloss;      // backward, may be null
   float* loss; float* lse_out;              // forward: what tokens without a target get
   void* dh;                                 // backward: its rows of tokens without a target become zero; may be null
+  Walk* walks;                   // of the launches that follow
+  Plan plan;
   int64_t hidden_ld, ignore;
-  int32_t tokens, vocab, width, per_cta, dh_f32;
+  int32_t tokens, vocab, width, per_cta, dh_f32, n_walks;
 };
 
 // Every CTA counts the targets of all tokens (8 bytes each, from L2; cheaper than a second launch), then writes what belongs to
@@ -693,6 +721,7 @@ __global__ void __launch_bounds__(256) head_prepare_kernel(const PrepareArgs a) 
   before = all = 0;
   for (int w = 0; w < 8; ++w) { before += counts[0][w]; all += counts[1][w]; }
   if (blockIdx.x == 0 && threadIdx.x == 0) { a.head[HD_STATUS] = 0; a.head[HD_COUNT] = all; }
+  for (int i = (int)(gridDim.x - 1 - blockIdx.x) * 256 + (int)threadIdx.x; i < a.n_walks; i += (int)gridDim.x * 256) a.walks[i].make(a.plan, i, all);
   const bool copy = all != a.tokens;
   const int vec = a.width >> 3;
   for (int t0 = begin; t0 < end; t0 += 256) {
@@ -855,14 +884,12 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
       float4 v[8][2];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        v[u][0] = v[u][1] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (u < left) {
-          const float4* const q = reinterpret_cast<const float4*>(p + u * part);
-          v[u][0] = __ldcg(q); v[u][1] = __ldcg(q + 1);
-        }
+        const float4* const q = reinterpret_cast<const float4*>(p + min(u, left - 1) * part);      // (the last one again past the end)
+        v[u][0] = __ldcg(q); v[u][1] = __ldcg(q + 1);
       }
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
+        if (u >= left) break;
         x[0] += v[u][0].x; x[1] += v[u][0].y; x[2] += v[u][0].z; x[3] += v[u][0].w;
         x[4] += v[u][1].x; x[5] += v[u][1].y; x[6] += v[u][1].z; x[7] += v[u][1].w;
       }
@@ -879,7 +906,7 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
 struct Layout {
   int64_t t_pad, n_tiles, piece, n_pieces, n_buf, planes, split_dh, split_dw;
   bool direct;                   // forward over at most a tile of tokens: they are not compacted
-  int64_t token, target, compact, lse, dloss, part, part_sum, z_target, g, dh_acc, dw_acc, bytes;      // byte offsets
+  int64_t token, target, compact, lse, dloss, part, part_sum, z_target, g, dh_acc, dw_acc, walks, bytes;      // byte offsets
 };
 
 // A piece of the vocabulary: as many columns as make g of one piece and plane about 64 M elements (128 MB: what the two
@@ -924,6 +951,7 @@ int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   int64_t at = kHeadBytes;
   auto take = [&](int64_t bytes) { const int64_t o = at; at += round_up(bytes, 256); return o; };
   l.direct = !backward && d.tokens <= kTile;
+  l.walks = take(l.direct ? 0 : (backward ? l.n_pieces + 1 : 1) * (int64_t)sizeof(Walk));
   l.token = take(l.t_pad * 4);
   l.target = take(l.t_pad * 4);
   l.compact = take(l.direct ? 0 : l.t_pad * d.hidden * 2);
@@ -987,10 +1015,21 @@ bool maps_of_operands(HeadArgs& a, const adapm_head_loss& d, const void* hidden,
   return ok;
 }
 
+Plan plan_of(const adapm_head_loss& d, const Layout& l, bool backward, bool dh, bool dw, int pairs) {
+  Plan p;
+  p.tokens = (int32_t)d.tokens; p.vocab = (int32_t)d.vocab; p.hidden = (int32_t)d.hidden;
+  p.piece = (int32_t)(backward ? l.piece : d.vocab); p.n_pieces = (int32_t)(backward ? l.n_pieces : 1);
+  p.planes_dh = backward && d.dhidden_dtype == ADAPM_TYPE_F32 ? 3 : 1; p.planes_dw = backward && d.dweight_dtype == ADAPM_TYPE_F32 ? 3 : 1;
+  p.split_dh = (int32_t)l.split_dh; p.split_dw = (int32_t)l.split_dw;
+  p.dh = dh; p.dw = dw; p.backward = backward; p.pairs = pairs;
+  return p;
+}
+
 int launch_prepare(const adapm_head_loss& d, PrepareArgs p, cudaStream_t s) {
   p.ignore = d.ignore_index;
   p.hidden_ld = d.hidden_ld;
   p.tokens = (int32_t)d.tokens; p.vocab = (int32_t)d.vocab; p.width = (int32_t)d.hidden;
+  p.n_walks = p.plan.backward ? p.plan.n_pieces + 1 : 1;
   p.per_cta = (int32_t)std::max<int64_t>(8, (d.tokens + 295) / 296);
   const unsigned grid = (unsigned)((d.tokens + p.per_cta - 1) / p.per_cta);
   ADAPM_CUDA(launch_chained(true, head_prepare_kernel, grid, 256, 0, s, p));
@@ -1034,19 +1073,24 @@ extern "C" int adapm_head_loss_forward(const adapm_head_loss* d, const void* hid
   a.targets = l.direct ? targets : nullptr;
   a.part = (float2*)(base + l.part); a.part_sum = (float*)(base + l.part_sum); a.z_target = (float*)(base + l.z_target);
   a.tokens = (int32_t)d->tokens; a.vocab = (int32_t)d->vocab; a.hidden = (int32_t)d->hidden; a.t_pad = (int32_t)l.t_pad;
-  a.planes = a.planes_dh = a.planes_dw = a.split_dh = a.split_dw = 1;
+  a.planes = a.split_dh = a.split_dw = 1;
   a.seg_logits = kSegForward;
   a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
 
-  if (!l.direct) {
+  const Plan plan = plan_of(*d, l, false, false, false, pairs);
+  if (l.direct) {
+    a.own_walk.make(plan, 0, a.tokens);
+  } else {
+    a.walk = (const Walk*)(base + l.walks);
     PrepareArgs p;
     std::memset(&p, 0, sizeof(p));
+    p.walks = (Walk*)(base + l.walks); p.plan = plan;
     p.targets = targets; p.hidden = (const uint16_t*)hidden; p.compact = (uint16_t*)(base + l.compact);
     p.head = a.head; p.token = (int32_t*)(base + l.token); p.target = (int32_t*)(base + l.target); p.loss = loss; p.lse_out = lse;
     rc = launch_prepare(*d, p, s);
     if (rc != ADAPM_OK) return rc;
   }
-  const int used = (int)std::min<int64_t>(pairs, l.t_pad / kTile * l.n_tiles);
+  const int used = plan.used(0);
   ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<false>, 2 * (unsigned)used, kHeadThreads, kHeadSmem, s, a));
   FinalArgs f;
   f.head = a.head; f.token = a.token; f.targets = a.targets; f.part = a.part; f.part_sum = a.part_sum; f.z_target = a.z_target; f.loss = loss; f.lse = lse;
@@ -1108,7 +1152,6 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   a.planes = (int32_t)l.planes;
   a.split_dh = (int32_t)l.split_dh; a.split_dw = (int32_t)l.split_dw;
   a.dh_f32 = d->dhidden_dtype == ADAPM_TYPE_F32; a.dw_f32 = d->dweight_dtype == ADAPM_TYPE_F32;
-  a.planes_dh = a.dh_f32 ? 3 : 1; a.planes_dw = a.dw_f32 ? 3 : 1;
   a.dh_wide = (uintptr_t)dhidden % 32 == 0 && (a.dh_f32 || d->hidden_ld % 16 == 0);
   a.dw_wide = (uintptr_t)dweight % 32 == 0 && (a.dw_f32 || d->weight_ld % 16 == 0);
   a.accumulate = d->accumulate != 0;
@@ -1116,8 +1159,10 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   a.seg_dh = a.dh_f32 ? kSegF32 : kSegBf16; a.seg_dw = a.dw_f32 ? kSegF32 : kSegBf16;
   a.scale = scale; a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
 
+  const Plan plan = plan_of(*d, l, true, dhidden != nullptr, dweight != nullptr, pairs);
   PrepareArgs p;
   std::memset(&p, 0, sizeof(p));
+  p.walks = (Walk*)(base + l.walks); p.plan = plan;
   p.targets = targets; p.hidden = (const uint16_t*)hidden; p.compact = (uint16_t*)(base + l.compact);
   p.head = a.head; p.token = (int32_t*)(base + l.token); p.target = (int32_t*)(base + l.target);
   p.lse_in = lse; p.lse = (float*)(base + l.lse); p.dloss_in = dloss; p.dloss = (float*)(base + l.dloss);
@@ -1125,16 +1170,12 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   rc = launch_prepare(*d, p, s);
   if (rc != ADAPM_OK) return rc;
 
-  const int64_t m_tiles = l.t_pad / kTile, nt_d = (d->hidden + kTile - 1) / kTile;
-  for (int64_t i = 0; i <= l.n_pieces; ++i) {
-    a.g_begin = (int32_t)(i * l.piece); a.g_buf = (int32_t)(i & 1);
-    a.g_cols = i < l.n_pieces ? (int32_t)std::min(l.piece, d->vocab - i * l.piece) : 0;
-    a.o_begin = (int32_t)((i - 1) * l.piece); a.o_buf = (int32_t)((i + 1) & 1);
-    a.o_cols = i > 0 ? (int32_t)std::min(l.piece, d->vocab - (i - 1) * l.piece) : 0;
-    a.first = i == 1; a.last = i == l.n_pieces;
-    const int64_t items = m_tiles * ((a.g_cols + kTile - 1) / kTile) +
-                          (a.o_cols ? (m_tiles * l.split_dh + (a.o_cols + kTile - 1) / kTile * l.split_dw) * nt_d : 0);
-    ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<true>, 2 * (unsigned)std::min<int64_t>(pairs, items), kHeadThreads, kHeadSmem, s, a));
+  for (int i = 0; i <= plan.n_pieces; ++i) {
+    a.walk = (const Walk*)(base + l.walks) + i;
+    a.g_begin = i * plan.piece; a.g_buf = i & 1; a.g_cols = plan.cols(i);
+    a.o_begin = (i - 1) * plan.piece; a.o_buf = (i + 1) & 1; a.o_cols = plan.cols(i - 1);
+    a.first = i == 1; a.last = i == plan.n_pieces;
+    ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<true>, 2 * (unsigned)plan.used(i), kHeadThreads, kHeadSmem, s, a));
   }
   const bool sum_dh = dhidden && l.split_dh > 1, sum_dw = dweight && l.split_dw > 1;
   if (!sum_dh && !sum_dw) return ADAPM_OK;
@@ -1144,8 +1185,8 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   int jobs = 0;
   if (sum_dh)
     u.job[jobs++] = {a.dh_acc, dhidden, d->hidden_ld, l.t_pad, -1, a.split_dh,
-                     (int32_t)((std::min(l.piece, d->vocab) + kStageK - 1) / kStageK) * a.planes_dh, 0, a.dh_f32, a.dh_wide, 0};
-  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, 0, a.planes_dw, a.dw_f32, a.dw_wide, a.accumulate};
+                     (int32_t)((std::min(l.piece, d->vocab) + kStageK - 1) / kStageK) * plan.planes_dh, 0, a.dh_f32, a.dh_wide, 0};
+  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, 0, plan.planes_dw, a.dw_f32, a.dw_wide, a.accumulate};
   u.jobs = jobs;
   const int64_t rows = std::max(sum_dh ? d->tokens : 0, sum_dw ? d->vocab : 0);
   const unsigned grid = (unsigned)std::min<int64_t>((rows * (d->hidden / 8) + 255) / 256, 4096);
