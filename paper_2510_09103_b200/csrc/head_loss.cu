@@ -625,15 +625,17 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
           }
           // g in bf16 (off by 2^-8 of itself at most, like the gradients it makes), or, where a gradient is wanted in fp32, as
           // the sum of three bf16 numbers, which have its 24 bits
-          for (int p = 0; p < a.planes; ++p) {
+          for (int p = 0;;) {
             uint32_t w[8];
 #pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2_rn(z[2 * e], z[2 * e + 1]);
+            st_b32x8(dst + p * plane + c, w);
+            if (++p == a.planes) break;
+#pragma unroll
             for (int e = 0; e < 8; ++e) {
-              w[e] = pack_bf16x2_rn(z[2 * e], z[2 * e + 1]);
               z[2 * e] -= __uint_as_float(w[e] << 16);
               z[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
             }
-            st_b32x8(dst + p * plane + c, w);
           }
         }
       } else {
@@ -642,28 +644,28 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         const bool row_ok = row < (is_dh ? tv : a.o_cols), none = tv == 0;
         const bool cut = is_dh ? a.split_dh > 1 : a.split_dw > 1;
         const bool to_acc = cut || (is_dh && !a.last), from_acc = is_dh && !a.first, from_out = !to_acc && !is_dh && a.accumulate;
-        void* const out = is_dh ? a.dh : a.dw;
         const int64_t out_row = is_dh ? (int64_t)token * a.hidden_ld : (int64_t)(a.o_begin + row) * a.weight_ld;
         float* const acc_row = is_dh ? a.dh_acc + ((int64_t)split * a.t_pad + row) * a.hidden : a.dw_acc + ((int64_t)split * a.vocab + row) * a.hidden;
-        const bool f32 = is_dh ? a.dh_f32 : a.dw_f32, wide = is_dh ? a.dh_wide : a.dw_wide;
-        const float scale = to_acc ? 1.f : a.scale;
+        // where the result goes, and where what it is added to comes from
+        const bool to_f32 = to_acc || (is_dh ? a.dh_f32 : a.dw_f32), with_old = from_acc || from_out;
+        void* const to = to_acc ? (void*)acc_row : to_f32 ? (void*)(static_cast<float*>(is_dh ? a.dh : a.dw) + out_row)
+                                                          : (void*)(static_cast<uint16_t*>(is_dh ? a.dh : a.dw) + out_row);
+        const bool wide = to_acc || (is_dh ? a.dh_wide : a.dw_wide);
+        const float scale = to_acc ? 1.f : a.scale, old_scale = from_acc ? scale : 1.f;
 #pragma unroll
         for (int c = 0; c < 128; c += 16) {
           if (c < half) {
             const int n = row_ok ? a.hidden - col0 - c : 0;
             float* const x = v + c;
-            float old[16];
-            if (from_acc) load_row16(acc_row, col0 + c, old, n, true);
-            if (from_out) load_row16(out, out_row + col0 + c, old, n, f32);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              if (none) x[e] = 0.f;
-              if (from_acc) x[e] += old[e];
-              x[e] *= scale;
-              if (from_out) x[e] += old[e];
+            for (int e = 0; e < 16; ++e) x[e] = none ? 0.f : x[e] * scale;
+            if (with_old) {
+              float old[16];
+              load_row16(from_acc ? acc_row : to, col0 + c, old, n, from_acc || to_f32);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) x[e] = fmaf(old[e], old_scale, x[e]);
             }
-            if (to_acc) store_row16(acc_row, col0 + c, x, n, true, true);
-            else store_row16(out, out_row + col0 + c, x, n, f32, wide);
+            store_row16(to, col0 + c, x, n, to_f32, wide);
           }
         }
       }
@@ -857,47 +859,65 @@ struct SumArgs {
     int64_t ld, part_rows;
     int32_t rows;                // < 0: the tokens with a target, whose places in `out` are `token`
     int32_t most, stages, planes_of_tokens;      // K in stages, or (planes > 0) as many planes of the tokens with a target
-    int32_t f32, wide, accumulate;
+    int32_t f32, accumulate;
   } job[2];
-  int32_t hidden, jobs;
+  int32_t hidden, ctas[2];       // ... of each job
   float scale;
 };
 
 __global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
+  __shared__ float4 sums[8][32];
   wait_for_previous_kernel();
   if (a.head[HD_STATUS] != 0) return;
-  const SumArgs::Job& j = a.job[blockIdx.x % a.jobs];
-  const int tv = a.head[HD_COUNT], rows = j.rows < 0 ? tv : j.rows, vec = a.hidden / 8;
+  const int job = (int)blockIdx.x < a.ctas[0] ? 0 : 1, cta = (int)blockIdx.x - (job ? a.ctas[0] : 0);
+  const SumArgs::Job& j = a.job[job];
+  const int tv = a.head[HD_COUNT], rows = j.rows < 0 ? tv : j.rows, vec = a.hidden / 4;
   int n, each;
   parts_of(j.planes_of_tokens ? max(1, (tv + kStageK - 1) / kStageK) * j.planes_of_tokens : j.stages, j.most, n, each);
-  const int64_t part = j.part_rows * a.hidden, stride = (int64_t)(gridDim.x / a.jobs) * 256;
-  for (int64_t i = (int64_t)(blockIdx.x / a.jobs) * 256 + threadIdx.x; i < (int64_t)rows * vec; i += stride) {
-    const int64_t row = i / vec;
-    const int c = (int)(i - row * vec) * 8;
-    const int64_t at = (j.rows < 0 ? (int64_t)a.token[row] : row) * j.ld + c;
-    float x[8], old[16];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = 0.f;
-    if (j.accumulate) load_row16(j.out, at, old, 8, j.f32);
+  const int64_t part = j.part_rows * a.hidden, total = (int64_t)rows * vec;
+  // many parts: the eight warps of a CTA share those of 32 places; few: a thread has a place to itself
+  const bool shared = n >= 8;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, each_cta = shared ? 32 : 256;
+  const int64_t stride = (int64_t)a.ctas[job] * each_cta;
+  for (int64_t i0 = (int64_t)cta * each_cta; i0 < total; i0 += stride) {
+    const int64_t i = i0 + (shared ? lane : (int)threadIdx.x);
+    const bool live = i < total;
+    const int64_t row = !live ? 0 : total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)vec) : i / vec;
+    const int c = live ? (int)(i - row * vec) * 4 : 0, step = shared ? 8 : 1;
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
     const float* p = j.acc + row * a.hidden + c;
-    for (int left = n; left > 0; left -= 8, p += 8 * part) {         // eight parts on their way at a time
-      float4 v[8][2];
+    for (int u = shared ? warp : 0; u < n; u += 4 * step) {
+      float4 v[4];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float4* const q = reinterpret_cast<const float4*>(p + min(u, left - 1) * part);      // (the last one again past the end)
-        v[u][0] = __ldcg(q); v[u][1] = __ldcg(q + 1);
-      }
+      for (int k = 0; k < 4; ++k) v[k] = __ldcg(reinterpret_cast<const float4*>(p + min(u + k * step, n - 1) * part));      // (the last one again past the end)
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        if (u >= left) break;
-        x[0] += v[u][0].x; x[1] += v[u][0].y; x[2] += v[u][0].z; x[3] += v[u][0].w;
-        x[4] += v[u][1].x; x[5] += v[u][1].y; x[6] += v[u][1].z; x[7] += v[u][1].w;
+      for (int k = 0; k < 4; ++k) {
+        const bool counts = u + k * step < n;
+        x[0] += counts ? v[k].x : 0.f; x[1] += counts ? v[k].y : 0.f; x[2] += counts ? v[k].z : 0.f; x[3] += counts ? v[k].w : 0.f;
       }
     }
-    float out[16];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = fmaf(x[e], a.scale, j.accumulate ? old[e] : 0.f);
-    store_row16(j.out, at, out, 8, j.f32, j.wide);
+    if (shared) {
+      __syncthreads();
+      sums[warp][lane] = make_float4(x[0], x[1], x[2], x[3]);
+      __syncthreads();
+      if (warp != 0) continue;
+      for (int w = 1; w < 8; ++w) {
+        const float4 o = sums[w][lane];
+        x[0] += o.x; x[1] += o.y; x[2] += o.z; x[3] += o.w;
+      }
+    }
+    if (!live) continue;
+    const int64_t at = (j.rows < 0 ? (int64_t)a.token[row] : row) * j.ld + c;
+    if (j.f32) {
+      float4* const to = reinterpret_cast<float4*>(static_cast<float*>(j.out) + at);
+      const float4 o = j.accumulate ? *to : make_float4(0.f, 0.f, 0.f, 0.f);
+      *to = make_float4(fmaf(x[0], a.scale, o.x), fmaf(x[1], a.scale, o.y), fmaf(x[2], a.scale, o.z), fmaf(x[3], a.scale, o.w));
+    } else {
+      uint2* const to = reinterpret_cast<uint2*>(static_cast<uint16_t*>(j.out) + at);
+      const uint2 o = j.accumulate ? *to : make_uint2(0, 0);
+      *to = make_uint2(pack_bf16x2_rn(fmaf(x[0], a.scale, __uint_as_float(o.x << 16)), fmaf(x[1], a.scale, __uint_as_float(o.x & 0xffff0000u))),
+                       pack_bf16x2_rn(fmaf(x[2], a.scale, __uint_as_float(o.y << 16)), fmaf(x[3], a.scale, __uint_as_float(o.y & 0xffff0000u))));
+    }
   }
 }
 
@@ -1185,12 +1205,13 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   int jobs = 0;
   if (sum_dh)
     u.job[jobs++] = {a.dh_acc, dhidden, d->hidden_ld, l.t_pad, -1, a.split_dh,
-                     (int32_t)((std::min(l.piece, d->vocab) + kStageK - 1) / kStageK) * plan.planes_dh, 0, a.dh_f32, a.dh_wide, 0};
-  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, 0, plan.planes_dw, a.dw_f32, a.dw_wide, a.accumulate};
-  u.jobs = jobs;
-  const int64_t rows = std::max(sum_dh ? d->tokens : 0, sum_dw ? d->vocab : 0);
-  const unsigned grid = (unsigned)std::min<int64_t>((rows * (d->hidden / 8) + 255) / 256, 4096);
-  ADAPM_CUDA(launch_chained(true, head_sum_kernel, grid * (unsigned)jobs, 256, 0, s, u));
+                     (int32_t)((std::min(l.piece, d->vocab) + kStageK - 1) / kStageK) * plan.planes_dh, 0, a.dh_f32, 0};
+  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, 0, plan.planes_dw, a.dw_f32, a.accumulate};
+  for (int i = 0; i < jobs; ++i) {
+    const int64_t places = (u.job[i].rows < 0 ? d->tokens : d->vocab) * (d->hidden / 4), each = u.job[i].most >= 8 ? 32 : 256;
+    u.ctas[i] = (int32_t)std::min<int64_t>((places + each - 1) / each, 4096);
+  }
+  ADAPM_CUDA(launch_chained(true, head_sum_kernel, (unsigned)(u.ctas[0] + u.ctas[1]), 256, 0, s, u));
   return ADAPM_OK;
 }
 
