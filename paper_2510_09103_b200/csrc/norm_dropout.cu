@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a) {
   int64_t out[kDropUnits];
   int n[kDropUnits];
   const int64_t i0 = (int64_t)blockIdx.x * (256 * kDropUnits) + threadIdx.x;
+  Philox4 bits[kDropUnits];
 #pragma unroll
   for (int u = 0; u < kDropUnits; ++u) {
     const int64_t i = i0 + u * 256;
@@ -122,11 +123,13 @@ __global__ void __launch_bounds__(256) dropout_kernel(const DropArgs a) {
     out[u] = row * a.y_ld + col;
   }
 #pragma unroll
+  for (int u = 0; u < kDropUnits; ++u) bits[u] = drop_bits(a.drop, key, (uint64_t)(i0 + u * 256));
+#pragma unroll
   for (int u = 0; u < kDropUnits; ++u) {
     if (n[u] == 0) continue;
     float v[8];
     Elem<T>::unpack(xs[u], v);
-    if (a.drop.mode) drop8(a.drop, key, (uint64_t)(i0 + u * 256), v);
+    if (a.drop.mode) drop8(a.drop, bits[u], v);
     if (res) {
       float r[8];
       Elem<T>::unpack(rs[u], r);
@@ -191,6 +194,22 @@ __device__ __forceinline__ uint32_t pack_e4m3x4(const float* x) {
   return (uint32_t)lo | ((uint32_t)hi << 16);
 }
 
+// The scale of values whose greatest magnitude is m, and what they are multiplied by: m / 448 and 448 / m, one where m is 0.  The
+// quotient by the hardware's reciprocal (an ulp off) where that has a normal result, else by the division, and at most the
+// greatest float (zeros stay zeros).
+__device__ __forceinline__ float scale_of(float m) { return m > 0.f ? m * (1.f / 448.f) : 1.f; }
+__device__ __forceinline__ float inverse_scale_of(float m) {
+  if (m >= 1e-30f && m <= 1e30f) return __fdividef(448.f, m);
+  return m > 0.f ? fminf(448.f / m, 3.402823466e38f) : 1.f;
+}
+__device__ __forceinline__ void times(float* x, float f) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const float2 t = mul2(make_float2(x[e], x[e + 1]), make_float2(f, f));
+    x[e] = t.x; x[e + 1] = t.y;
+  }
+}
+
 // s stays in 32 bits for the statistic and the output and is rounded only where it is stored.
 template <typename T, int NC, bool WARP, bool VEC, bool DROP>
 __global__ void __launch_bounds__(WARP ? 128 : NC == 4 ? 1024 : 512) rmsnorm_forward_kernel(const NormArgs a) {
@@ -213,26 +232,41 @@ __global__ void __launch_bounds__(WARP ? 128 : NC == 4 ? 1024 : 512) rmsnorm_for
       if (res) rs[i] = fetch8<VEC>(res + 8 * g, a.cols - 8 * g);
     }
   }
-  float s[NC][8], sq = 0.f;
+  float s[NC][8];
+  float2 sq = make_float2(0.f, 0.f);
+  // (with four chunks there are no registers for their bits too)
+  constexpr bool kAhead = DROP && NC < 4;
+  constexpr int kBits = kAhead ? NC : 1;
+  Philox4 bits[kBits];
   const DropKey key = DROP ? drop_key(a.drop) : DropKey{0, 0};
+  if (kAhead) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) bits[i % kBits] = drop_bits(a.drop, key, (uint64_t)row * a.groups + me + i * team);
+  }
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
     const int g = me + i * team;
     Elem<T>::unpack(xs[i], s[i]);
     if (g < a.groups) {
-      if (DROP) drop8(a.drop, key, (uint64_t)row * a.groups + g, s[i]);
+      if (DROP) drop8(a.drop, kAhead ? bits[i % kBits] : drop_bits(a.drop, key, (uint64_t)row * a.groups + g), s[i]);
       if (res) {
         float r[8];
         Elem<T>::unpack(rs[i], r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[i][e] += r[e];
+        for (int e = 0; e < 8; e += 2) {
+          const float2 t = add2(make_float2(s[i][e], s[i][e + 1]), make_float2(r[e], r[e + 1]));
+          s[i][e] = t.x; s[i][e + 1] = t.y;
+        }
       }
       if (sum) store8<VEC>(sum + 8 * g, a.cols - 8 * g, s[i]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sq = fmaf(s[i][e], s[i][e], sq);
+      for (int e = 0; e < 8; e += 2) {
+        const float2 t = make_float2(s[i][e], s[i][e + 1]);
+        sq = fma2(t, t, sq);
+      }
     }
   }
-  const float rstd = 1.f / sqrtf(row_sum<WARP>(sq, red[0]) / (float)a.cols + a.eps);
+  const float rstd = 1.f / sqrtf(row_sum<WARP>(sq.x + sq.y, red[0]) / (float)a.cols + a.eps);
   if (a.rstd && me == 0) a.rstd[row] = rstd;
   float top = 0.f;
 #pragma unroll
@@ -242,7 +276,10 @@ __global__ void __launch_bounds__(WARP ? 128 : NC == 4 ? 1024 : 512) rmsnorm_for
       float w[8];
       load_weight8<VEC>(a.weight, a.weight_f32, 8 * g, a.cols - 8 * g, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[i][e] = s[i][e] * rstd * w[e];
+      for (int e = 0; e < 8; e += 2) {
+        const float2 t = mul2(mul2(make_float2(s[i][e], s[i][e + 1]), make_float2(rstd, rstd)), make_float2(w[e], w[e + 1]));
+        s[i][e] = t.x; s[i][e + 1] = t.y;
+      }
       if (y) store8<VEC>(y + 8 * g, a.cols - 8 * g, s[i]);
     }
     if (!a.y8) continue;
@@ -254,22 +291,17 @@ __global__ void __launch_bounds__(WARP ? 128 : NC == 4 ? 1024 : 512) rmsnorm_for
       for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
       top = 0.f;
       if (g < a.groups) {
-        const float inv = m > 0.f ? 448.f / m : 1.f;
-        if ((g & 15) == 0) a.scales[row * a.n_scales + (g >> 4)] = m > 0.f ? m / 448.f : 1.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s[i][e] *= inv;
+        if ((g & 15) == 0) a.scales[row * a.n_scales + (g >> 4)] = scale_of(m);
+        times(s[i], inverse_scale_of(m));
       }
     }
   }
   if (!a.y8) return;
   if (!a.q8_group) {
-    const float m = row_max<WARP>(top, red[1]);
-    const float inv = m > 0.f ? 448.f / m : 1.f;
-    if (me == 0) a.scales[row] = m > 0.f ? m / 448.f : 1.f;
+    const float m = row_max<WARP>(top, red[1]), inv = inverse_scale_of(m);
+    if (me == 0) a.scales[row] = scale_of(m);
 #pragma unroll
-    for (int i = 0; i < NC; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[i][e] *= inv;
+    for (int i = 0; i < NC; ++i) times(s[i], inv);
   }
   uint8_t* const q = a.y8 + row * a.y8_ld;
 #pragma unroll
@@ -302,20 +334,6 @@ struct NormGradArgs {
   int32_t cols, groups, weight_f32;
   DropRule drop;
 };
-
-// Two fp32 operations per instruction (the same roundings as one at a time).
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  float2 d;
-  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-  return d;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 d;
-  asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}"
-      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-  return d;
-}
 
 // A CTA takes row after row; a thread has the same columns in each, whose share of dw it keeps.  The next row's elements are
 // on their way while a row is worked on.  NC = 4 (rows above 8192 columns): dw alone fills the registers, so a row is read a
@@ -410,7 +428,7 @@ __global__ void __launch_bounds__(NC == 1 ? 256 : NC == 2 ? 512 : 1024) rmsnorm_
       }
       if (a.dres) store8<VEC>(static_cast<T*>(a.dres) + row * a.r_ld + 8 * g, n, ds);
       if (a.dx) {
-        if (DROP) drop8(a.drop, key, (uint64_t)row * a.groups + g, ds);
+        if (DROP) drop8(a.drop, drop_bits(a.drop, key, (uint64_t)row * a.groups + g), ds);
         store8<VEC>(static_cast<T*>(a.dx) + row * a.x_ld + 8 * g, n, ds);
       }
     }

@@ -36,15 +36,39 @@ struct DropRule {
 };
 
 #ifdef __CUDACC__
+// Two fp32 operations per instruction (the same roundings as one at a time).
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmul.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 x, y, z;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nadd.rn.f32x2 z, x, y;\nmov.b64 {%0, %1}, z;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n.reg .b64 x, y, z, w;\nmov.b64 x, {%2, %3};\nmov.b64 y, {%4, %5};\nmov.b64 z, {%6, %7};\nfma.rn.f32x2 w, x, y, z;\nmov.b64 {%0, %1}, w;\n}"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+
 struct DropKey { uint32_t off_lo, off_hi; };
 __device__ __forceinline__ DropKey drop_key(const DropRule& d) {
   const uint64_t off = d.offset + (d.step ? *d.step : 0);
   return DropKey{(uint32_t)off, (uint32_t)(off >> 32)};
 }
-// Eight elements of group `q` = row * ceil(cols / 8) + column / 8.  Dropped elements are zero whatever they held.
-// (The upper 16 bits are compared in place, below the cut's zeros; the lower ones after a shift.)
-__device__ __forceinline__ void drop8(const DropRule& d, const DropKey& k, uint64_t q, float* x) {
-  const Philox4 r = philox4x32_10((uint32_t)q, (uint32_t)(q >> 32), k.off_lo, k.off_hi, d.seed_lo, d.seed_hi);
+// The 128 bits of group `q` = row * ceil(cols / 8) + column / 8.  They follow from the place alone: a kernel makes them while
+// its elements are on their way.
+__device__ __forceinline__ Philox4 drop_bits(const DropRule& d, const DropKey& k, uint64_t q) {
+  return philox4x32_10((uint32_t)q, (uint32_t)(q >> 32), k.off_lo, k.off_hi, d.seed_lo, d.seed_hi);
+}
+// Its eight elements.  Dropped ones are zero whatever they held.  (The upper 16 bits are compared in place, below the cut's
+// zeros; the lower ones after a shift.)
+__device__ __forceinline__ void drop8(const DropRule& d, const Philox4& r, float* x) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[2 * e] = (r.w[e] << 16) >= d.cut ? x[2 * e] * d.factor : 0.f;
