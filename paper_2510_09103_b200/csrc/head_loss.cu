@@ -42,7 +42,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 // so that a long sum shrinks with its length: with the whole K in one accumulator an fp32 gradient was off by 1.3e-5 at K = 12288
 // (three planes of 4096) and by 2e-3 at K = 234222.  An item's K is therefore cut into segments, which the epilogue adds up in
 // registers, rounded to nearest; the next segment runs meanwhile in the other accumulator.
-constexpr int kSegForward = 16, kSegLogits = 8, kSegF32 = 4, kSegBf16 = 64;      // stages of 64
+constexpr int kSegForward = 8, kSegF32 = 4, kSegBf16 = 64;      // stages of 64 K: for the losses, for gradients in fp32 and in bf16
 
 enum : int32_t { CLS_LOGITS = 0, CLS_DH = 1, CLS_DW = 2 };
 
@@ -367,6 +367,16 @@ __device__ __forceinline__ float cut_row(float* z, int n) {
   return t;
 }
 
+// What bounds it: the tensor cores, and with them the power cap, where there are a few hundred tokens or more.  8192 x 50257 x 1600
+// forward 0.95 ms = 1.38 PFLOP/s (cuBLAS sustains 1.38 on this card, 1.62 in a burst), both gradients 3.25 to 3.4 ms = 1.16 to
+// 1.22, with half the tokens of 8192 x 128256 x 4096 10.0 to 10.3 ms = 1.25 to 1.29; tensor pipe 83 % active in the forward
+// launch, 76 to 80 % in those of the gradients, DRAM 10 and 30 %.  With few tokens the weight's way from memory and back (100 tokens of
+// 128256 x 4096: both gradients 0.98 ms for 3.2 GB), and below a few ten microseconds the launches themselves.  With D = 256 the
+// exponentials: a tile of 256 x 256 is multiplied in 2 thousand cycles, and its epilogue takes 4 (2 of them the pipe that
+// makes 16 exponentials a cycle).
+// Not kept: an epilogue that reads the accumulator column by column as it goes (smaller code, but its multiply-segment form
+// spilled: 1150 us forward against 955); rows turned in shared memory so that stores cover 64 bytes of a row (no change for
+// bf16, 49 against 43 us on 512 tokens in fp32).
 template <bool BACKWARD>
 __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __grid_constant__ HeadArgs a) {
   extern __shared__ uint8_t dyn_smem[];
@@ -700,7 +710,8 @@ struct PrepareArgs {
   int32_t tokens, vocab, width, per_cta, dh_f32, n_walks;
 };
 
-// Every CTA counts the targets of all tokens (8 bytes each, from L2; cheaper than a second launch), then writes what belongs to
+// Every CTA counts the targets of all tokens (8 bytes each, from L2; cheaper than a second launch: 4 us for 8192 tokens, all of it
+// latency), then writes what belongs to
 // its own ones: the row number among those with a target, the copies that the products read, the answers of the others.
 __global__ void __launch_bounds__(256) head_prepare_kernel(const PrepareArgs a) {
   __shared__ int counts[2][8];
@@ -788,7 +799,8 @@ struct FinalArgs {
   float smooth, z_loss;
 };
 
-// A CTA has 32 rows (its lanes), eight warps share the parts of each, eight at a time.
+// A CTA has 32 rows (its lanes), eight warps share the parts of each, eight at a time (one after the other, each with its own
+// rescaling: 20 us for 8192 tokens of 50257 columns, 8 now; 8 bytes per 128 columns are read).
 __global__ void __launch_bounds__(256) head_final_kernel(const FinalArgs a) {
   __shared__ float ks[8][32], sums[8][32], totals[8][32];
   wait_for_previous_kernel();
@@ -924,7 +936,7 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
 // ---- host ----------------------------------------------------------------------------------------------
 
 struct Layout {
-  int64_t t_pad, n_tiles, piece, n_pieces, n_buf, planes, split_dh, split_dw;
+  int64_t t_pad, n_tiles, piece, n_pieces, n_buf, planes, planes_dh, planes_dw, split_dh, split_dw;
   bool direct;                   // forward over at most a tile of tokens: they are not compacted
   int64_t token, target, compact, lse, dloss, part, part_sum, z_target, g, dh_acc, dw_acc, walks, bytes;      // byte offsets
 };
@@ -934,6 +946,13 @@ struct Layout {
 // memory once per piece).
 constexpr int64_t kPlanPairs = 74;       // what the scratch is planned for (148 SMs)
 constexpr int64_t kPieceElems = (int64_t)64 << 20, kPieceMin = 2048;
+
+// bf16 numbers that g is carried as into the product of a gradient of type `t`.  One for bf16, but two where there are few tokens:
+// a token's gradient is mostly its target's element of g, whose rounding is averaged out over the tokens only (a norm's error of
+// one token's gradients was up to 2.4 times that of their own rounding, of 64 tokens 1.4 times), and with so few of them the
+// weight's way through memory takes the time.
+constexpr int64_t kFewTokens = 64;
+int64_t planes_of(const adapm_head_loss& d, int32_t t) { return t == ADAPM_TYPE_F32 ? 3 : d.tokens <= kFewTokens ? 2 : 1; }
 
 int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   if (d.tokens < 0 || d.vocab <= 0 || d.hidden <= 0) return ADAPM_EINVAL;
@@ -946,7 +965,9 @@ int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   if (backward && (!known_type(d.dhidden_dtype) || !known_type(d.dweight_dtype))) return ADAPM_EINVAL;
   l.t_pad = round_up(d.tokens < 1 ? 1 : d.tokens, kTile);
   l.n_tiles = (d.vocab + kTile - 1) / kTile;
-  l.planes = backward && (d.dhidden_dtype == ADAPM_TYPE_F32 || d.dweight_dtype == ADAPM_TYPE_F32) ? 3 : 1;
+  l.planes_dh = backward ? planes_of(d, d.dhidden_dtype) : 1;
+  l.planes_dw = backward ? planes_of(d, d.dweight_dtype) : 1;
+  l.planes = std::max(l.planes_dh, l.planes_dw);
   const int64_t most = std::max(kPieceMin, kPieceElems / l.t_pad / kTile * kTile);
   l.n_pieces = (d.vocab + most - 1) / most;
   l.piece = round_up((d.vocab + l.n_pieces - 1) / l.n_pieces, kTile);
@@ -960,8 +981,8 @@ int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   l.split_dh = l.split_dw = 1;
   if (backward) {
     const int64_t mt = l.t_pad / kTile, nt_d = (d.hidden + kTile - 1) / kTile, tiles = l.piece / kTile;
-    const int64_t k_dh = (std::min(l.piece, d.vocab) + kStageK - 1) / kStageK * (d.dhidden_dtype == ADAPM_TYPE_F32 ? 3 : 1);
-    const int64_t k_dw = l.t_pad / kStageK * (d.dweight_dtype == ADAPM_TYPE_F32 ? 3 : 1);
+    const int64_t k_dh = (std::min(l.piece, d.vocab) + kStageK - 1) / kStageK * l.planes_dh;
+    const int64_t k_dw = l.t_pad / kStageK * l.planes_dw;
     const int64_t logits = l.n_pieces > 1 ? mt * tiles * ((d.hidden + kStageK - 1) / kStageK) : 0;
     const int64_t share = std::max<int64_t>(1, (nt_d * (mt * k_dh + tiles * k_dw) + logits) / kPlanPairs);
     auto parts = [&](int64_t k) { return std::max<int64_t>(1, std::min({(2 * k + share - 1) / share, k / 16, (int64_t)256})); };
@@ -1039,7 +1060,7 @@ Plan plan_of(const adapm_head_loss& d, const Layout& l, bool backward, bool dh, 
   Plan p;
   p.tokens = (int32_t)d.tokens; p.vocab = (int32_t)d.vocab; p.hidden = (int32_t)d.hidden;
   p.piece = (int32_t)(backward ? l.piece : d.vocab); p.n_pieces = (int32_t)(backward ? l.n_pieces : 1);
-  p.planes_dh = backward && d.dhidden_dtype == ADAPM_TYPE_F32 ? 3 : 1; p.planes_dw = backward && d.dweight_dtype == ADAPM_TYPE_F32 ? 3 : 1;
+  p.planes_dh = (int32_t)l.planes_dh; p.planes_dw = (int32_t)l.planes_dw;
   p.split_dh = (int32_t)l.split_dh; p.split_dw = (int32_t)l.split_dw;
   p.dh = dh; p.dw = dw; p.backward = backward; p.pairs = pairs;
   return p;
@@ -1175,7 +1196,7 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   a.dh_wide = (uintptr_t)dhidden % 32 == 0 && (a.dh_f32 || d->hidden_ld % 16 == 0);
   a.dw_wide = (uintptr_t)dweight % 32 == 0 && (a.dw_f32 || d->weight_ld % 16 == 0);
   a.accumulate = d->accumulate != 0;
-  a.seg_logits = l.planes > 1 ? kSegLogits : kSegBf16;
+  a.seg_logits = l.planes > 2 ? kSegF32 : kSegBf16;
   a.seg_dh = a.dh_f32 ? kSegF32 : kSegBf16; a.seg_dw = a.dw_f32 ? kSegF32 : kSegBf16;
   a.scale = scale; a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
 
