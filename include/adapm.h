@@ -348,7 +348,7 @@ typedef struct {
 
 /*
  *   residual: may be NULL (s = drop(x));  sum: s, may be NULL, may be `residual` or `x` (same pitch);
- *   y, y8: outputs, either may be NULL.  y8 is y in 8 bits (e4m3): round(y * 448 / m) with m = max |y| over the
+ *   y, y8: outputs, either may be NULL; y may be `residual` or `x` (same pitch) where sum is not.  y8 is y in 8 bits (e4m3): round(y * 448 / m) with m = max |y| over the
  *   row, or over q8_group columns of it, and y8_scales [rows, ceil(cols / q8_group) or 1] = m / 448 (1 where m is 0);
  *   rstd [rows]: may be NULL; the backward pass reads it.
  * Errors: ADAPM_EINVAL, ADAPM_ERANGE, ADAPM_EALIGN, ADAPM_ECUDA.  rows = 0 does nothing.
@@ -362,7 +362,7 @@ int adapm_rmsnorm_forward(const adapm_rmsnorm* d, const void* x, const void* res
  * nor dropout).
  *   xh = sum rstd    ds = rstd (dy w - xh mean(dy w xh)) + dsum
  *   dresidual = ds;  dx = drop(ds), the forward's mask;  dweight = sum over rows of dy xh
- * Any output may be NULL, but not all.  dx may be dy, dresidual may be dsum or sum (same pitch).  dweight [cols] of
+ * Any output may be NULL, but not all.  dx and dresidual may each be dy, dsum or sum (same pitch).  dweight [cols] of
  * dweight_dtype; `accumulate`: added to what is there.  scratch: only where dweight is wanted.
  * rows = 0: dweight = 0 (unless accumulate).  Errors as above, and ADAPM_ENOWORKSPACE.
  */

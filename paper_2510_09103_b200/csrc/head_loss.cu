@@ -1096,6 +1096,10 @@ extern "C" int adapm_head_loss_forward(const adapm_head_loss* d, const void* hid
   if (!hidden || !weight || !targets || !loss || !lse || !scratch) return ADAPM_EINVAL;
   if ((uintptr_t)hidden % 16 || (uintptr_t)weight % 16 || (uintptr_t)targets % 8 || (uintptr_t)loss % 4 || (uintptr_t)lse % 4 || (uintptr_t)scratch % 256) return ADAPM_EALIGN;
   if (scratch_bytes < (size_t)l.bytes) return ADAPM_ENOWORKSPACE;
+  if (overlap(loss, d->tokens * 4, lse, d->tokens * 4) || overlap(loss, d->tokens * 4, targets, d->tokens * 8) || overlap(lse, d->tokens * 4, targets, d->tokens * 8)) {
+    set_error_text("adapm_head_loss_forward: the losses, their lse and the targets overlap");
+    return ADAPM_EINVAL;
+  }
   int device, pairs;
   rc = check_on_this_device({hidden, weight, targets, loss, lse, scratch}, &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
@@ -1166,7 +1170,9 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   const int64_t h_bytes = d->tokens * d->hidden_ld * 2, w_bytes = d->vocab * d->weight_ld * 2;
   const int64_t dh_bytes = d->tokens * d->hidden_ld * type_bytes(d->dhidden_dtype), dw_bytes = d->vocab * dw_row;
   if (overlap(hidden, h_bytes, dhidden, dh_bytes) || overlap(hidden, h_bytes, dweight, dw_bytes) || overlap(weight, w_bytes, dhidden, dh_bytes) ||
-      overlap(weight, w_bytes, dweight, dw_bytes) || overlap(dhidden, dh_bytes, dweight, dw_bytes)) {
+      overlap(weight, w_bytes, dweight, dw_bytes) || overlap(dhidden, dh_bytes, dweight, dw_bytes) || overlap(lse, d->tokens * 4, dhidden, dh_bytes) ||
+      overlap(lse, d->tokens * 4, dweight, dw_bytes) || overlap(targets, d->tokens * 8, dhidden, dh_bytes) || overlap(targets, d->tokens * 8, dweight, dw_bytes) ||
+      overlap(dloss, d->tokens * 4, dhidden, dh_bytes) || overlap(dloss, d->tokens * 4, dweight, dw_bytes)) {
     set_error_text("adapm_head_loss_backward: a gradient overlaps an input or the other gradient");
     return ADAPM_EINVAL;
   }

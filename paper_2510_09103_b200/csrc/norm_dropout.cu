@@ -584,6 +584,10 @@ extern "C" int adapm_dropout(const void* x, const void* residual, void* y, int32
   rc = check_rows({{x, x_ld, eb}, {residual, residual_ld, eb}, {y, y_ld, eb}}, rows, cols, vec);
   if (rc != ADAPM_OK) return rc;
   if ((uintptr_t)step % 8) return ADAPM_EALIGN;
+  if (!apart_or_same(y, y_ld, x, x_ld, rows, cols, eb) || !apart_or_same(y, y_ld, residual, residual_ld, rows, cols, eb)) {
+    set_error_text("adapm_dropout: the output lies over an input, but not element on element");
+    return ADAPM_EINVAL;
+  }
   int device;
   rc = check_on_this_device({x, residual, y, step}, &device);
   if (rc != ADAPM_OK) return rc;
@@ -617,8 +621,16 @@ extern "C" int adapm_rmsnorm_forward(const adapm_rmsnorm* d, const void* x, cons
   if (rc != ADAPM_OK) return rc;
   vec = vec && (uintptr_t)weight % 16 == 0;
   if ((uintptr_t)weight % (uintptr_t)type_bytes(d->weight_dtype) || (uintptr_t)y8_scales % 4 || (uintptr_t)rstd % 4 || (uintptr_t)d->step % 8) return ADAPM_EALIGN;
-  if (overlap(sum, ((d->rows - 1) * d->sum_ld + d->cols) * eb, y, ((d->rows - 1) * d->y_ld + d->cols) * eb)) {
-    set_error_text("adapm_rmsnorm_forward: the sum and the output overlap");
+  auto extent = [&](int64_t ld, int64_t bytes) { return ((d->rows - 1) * ld + d->cols) * bytes; };
+  const int64_t wb = d->cols * type_bytes(d->weight_dtype);
+  bool apart = !overlap(sum, extent(d->sum_ld, eb), y, extent(d->y_ld, eb)) && !overlap(y8, extent(d->y8_ld, 1), x, extent(d->x_ld, eb)) &&
+               !overlap(y8, extent(d->y8_ld, 1), residual, extent(d->residual_ld, eb)) && !overlap(y8, extent(d->y8_ld, 1), sum, extent(d->sum_ld, eb)) &&
+               !overlap(y8, extent(d->y8_ld, 1), y, extent(d->y_ld, eb)) && !overlap(sum, extent(d->sum_ld, eb), weight, wb) &&
+               !overlap(y, extent(d->y_ld, eb), weight, wb) && !overlap(y8, extent(d->y8_ld, 1), weight, wb);
+  apart = apart && apart_or_same(sum, d->sum_ld, x, d->x_ld, d->rows, d->cols, eb) && apart_or_same(sum, d->sum_ld, residual, d->residual_ld, d->rows, d->cols, eb) &&
+          apart_or_same(y, d->y_ld, x, d->x_ld, d->rows, d->cols, eb) && apart_or_same(y, d->y_ld, residual, d->residual_ld, d->rows, d->cols, eb);
+  if (!apart) {
+    set_error_text("adapm_rmsnorm_forward: an output lies over an input, but not element on element, or over another output");
     return ADAPM_EINVAL;
   }
   int device, sms;
@@ -680,8 +692,17 @@ extern "C" int adapm_rmsnorm_backward(const adapm_rmsnorm* d, const void* dy, co
   if (rc != ADAPM_OK) return rc;
   vec = vec && (uintptr_t)weight % 16 == 0;
   if ((uintptr_t)weight % (uintptr_t)type_bytes(d->weight_dtype) || (uintptr_t)rstd % 4 || (uintptr_t)d->step % 8) return ADAPM_EALIGN;
-  if (overlap(dresidual, ((d->rows - 1) * d->residual_ld + d->cols) * eb, dx, ((d->rows - 1) * d->x_ld + d->cols) * eb)) {
-    set_error_text("adapm_rmsnorm_backward: the two gradients overlap");
+  auto extent = [&](int64_t ld) { return ((d->rows - 1) * ld + d->cols) * eb; };
+  bool apart = !overlap(dresidual, extent(d->residual_ld), dx, extent(d->x_ld));
+  for (int o = 0; o < 2; ++o) {
+    const void* const out = o ? dx : dresidual;
+    const int64_t ld = o ? d->x_ld : d->residual_ld;
+    apart = apart && apart_or_same(out, ld, dy, d->y_ld, d->rows, d->cols, eb) && apart_or_same(out, ld, dsum, d->sum_ld, d->rows, d->cols, eb) &&
+            apart_or_same(out, ld, sum, d->sum_ld, d->rows, d->cols, eb) && !overlap(out, extent(ld), weight, d->cols * type_bytes(d->weight_dtype)) &&
+            !overlap(out, extent(ld), dweight, d->cols * gb) && !overlap(out, extent(ld), rstd, d->rows * 4);
+  }
+  if (!apart) {
+    set_error_text("adapm_rmsnorm_backward: an output lies over an input, but not element on element, or over another output");
     return ADAPM_EINVAL;
   }
   if (dweight) {

@@ -39,4 +39,10 @@ inline bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
   return x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
 }
 
+// Whether an output [rows, cols] may lie where an input does: apart, or element on element.
+inline bool apart_or_same(const void* out, int64_t out_ld, const void* in, int64_t in_ld, int64_t rows, int64_t cols, int64_t bytes) {
+  if (out == in && (out_ld == in_ld || rows <= 1)) return true;
+  return !overlap(out, ((rows - 1) * out_ld + cols) * bytes, in, ((rows - 1) * in_ld + cols) * bytes);
+}
+
 }  // namespace adapm

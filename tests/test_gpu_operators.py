@@ -177,6 +177,11 @@ def test_rmsnorm_forward(dtype, wtype, rows, cols, pad, shift):
     assert torch.equal(x, before[0]) and torch.equal(residual, before[1])
     for m, b in ((x, xb), (residual, rb), *out):
         _guards_stand(m, b)
+    # the output over the input
+    if pad == 0:
+        over = x.clone(memory_format=torch.contiguous_format)
+        A.adapm_rmsnorm_forward(A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[wtype], 1e-5, residual_ld=ld + 8), over, residual, w, None, over, None, None, None)
+        assert torch.equal(over, y)
     # the residual updated in place, no norm of it kept
     A.adapm_rmsnorm_forward(A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[wtype], 1e-5, x_ld=ld, residual_ld=ld + 8, sum_ld=ld + 8),
                             x, residual, w, residual, None, None, None, None)
@@ -585,6 +590,115 @@ def test_head_loss_on_another_stream_and_in_a_graph():
         assert torch.equal(out[2], dh) and torch.equal(out[3], dw)
 
 
+def test_head_loss_twice_at_once():
+    """Two calls on two streams, each with a scratch of its own, again and again."""
+    cases = [_head_case(700, 5003, 520, ignored=0.3), _head_case(300, 9001, 264, seed=1)]
+    want = [(_forward(h, w, t)[0], _backward(h, w, t, R.head_loss(h, w, t)[1].float())) for h, _, w, _, t in cases]
+    lses = [R.head_loss(h, w, t)[1].float() for h, _, w, _, t in cases]
+    streams, out = [torch.cuda.Stream() for _ in cases], [[], []]
+    held = []
+    for i, (h, _, w, _, t) in enumerate(cases):
+        d = A.head_loss_desc(h.shape[0], w.shape[0], h.shape[1])
+        held.append((d, torch.empty(A.adapm_head_loss_scratch_bytes(d, False), dtype=torch.uint8, device="cuda"),
+                     torch.empty(A.adapm_head_loss_scratch_bytes(d, True), dtype=torch.uint8, device="cuda")))
+        out[i] = [[torch.empty(h.shape[0], device="cuda"), torch.empty(h.shape[0], device="cuda"), torch.empty_like(h.contiguous()), torch.empty_like(w.contiguous())] for _ in range(6)]
+    torch.cuda.synchronize()
+    for k in range(6):
+        for i, (h, _, w, _, t) in enumerate(cases):
+            d, sf, sb = held[i]
+            o = out[i][k]
+            A.adapm_head_loss_forward(d, h, w, t, o[0], o[1], sf, stream=streams[i])
+            A.adapm_head_loss_backward(d, h, w, t, lses[i], None, 1.0, o[2], o[3], sb, stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o in out[i]:
+            assert torch.equal(o[0], want[i][0]) and torch.equal(o[2], want[i][1][0]) and torch.equal(o[3], want[i][1][1])
+
+
+def test_head_loss_past_32_bits_of_weight_elements():
+    """2.2e9 elements of weight: the last rows' addresses need more than 32 bits."""
+    tokens, vocab, width = 5, 540000, 4096
+    g = _gen(8)
+    weight = torch.empty(vocab, width, dtype=BF16, device="cuda")
+    for part in weight.split(20000):
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda") * 0.02)
+    hidden = torch.randn(tokens, width, generator=g, device="cuda").to(BF16)
+    targets = torch.tensor([vocab - 1, 0, 524288, vocab - 2, 300000], device="cuda")
+    loss, lse = _forward(hidden, weight, targets)
+    z = torch.cat([hidden.double() @ part.double().T for part in weight.split(20000)], 1)
+    want = torch.logsumexp(z, 1)
+    err = _tensor_sum(width, 512) * 4096 * 0.02 * 5 * 5 + 600 * 2.0**-24 + 2.0**-20      # (no product above 25 times its mean size)
+    assert ((lse.double() - want).abs() < err).all()
+    assert ((loss.double() - want + z.gather(1, targets[:, None])[:, 0]).abs() < 2 * err).all()
+    d = A.head_loss_desc(tokens, vocab, width)
+    scratch = torch.empty(A.adapm_head_loss_scratch_bytes(d, True), dtype=torch.uint8, device="cuda")
+    dw, dh = torch.full_like(weight, 7.0), torch.empty_like(hidden)
+    A.adapm_head_loss_backward(d, hidden, weight, targets, lse, None, 1.0, dh, dw, scratch)
+    grad = torch.exp(z - lse.double()[:, None])
+    grad[torch.arange(tokens, device="cuda"), targets] -= 1
+    for rows in (slice(0, 300), slice(524200, 524400), slice(vocab - 300, vocab)):
+        ref = grad[:, rows].T @ hidden.double()
+        assert (dw[rows].double() - ref).norm() < 4e-3 * ref.norm()          # two roundings of 2^-8 at most, 1.7e-3 in the norm each
+    ref = sum(grad[:, i:i + 20000] @ weight[i:i + 20000].double() for i in range(0, vocab, 20000))
+    assert (dh.double() - ref).norm() < 4e-3 * ref.norm()
+    assert dw.isfinite().all() and (dw[::1013] != 7.0).any(1).all()
+
+
+def test_rmsnorm_past_32_bits_of_elements():
+    """The last rows of 2.3e9 elements are what the same rows give by themselves."""
+    rows, cols = 70000, 32768
+    x = torch.empty(rows, cols, dtype=BF16, device="cuda")
+    x.normal_(generator=_gen(9))
+    w = torch.ones(cols, dtype=BF16, device="cuda")
+    rstd, y = torch.empty(rows, device="cuda"), torch.empty_like(x)
+    A.adapm_rmsnorm_forward(A.rmsnorm_desc(rows, cols), x, None, w, None, y, None, None, rstd)
+    tail = x[-8:].clone()
+    alone, r = torch.empty_like(tail), torch.empty(8, device="cuda")
+    A.adapm_rmsnorm_forward(A.rmsnorm_desc(8, cols), tail, None, w, None, alone, None, None, r)
+    assert torch.equal(y[-8:], alone) and torch.equal(rstd[-8:], r) and y[65536 + 1].isfinite().all()
+    A.adapm_rmsnorm_backward(A.rmsnorm_desc(rows, cols), y, None, x, rstd, w, y, None, None, A.TYPE_F32, False, None)
+    A.adapm_rmsnorm_backward(A.rmsnorm_desc(8, cols), alone, None, tail, r, w, alone, None, None, A.TYPE_F32, False, None)
+    assert torch.equal(y[-8:], alone)
+
+
+FIRST_CALL_IN_A_CAPTURE = """
+import torch, paper_2510_09103_b200 as A
+b = torch.bfloat16
+x, w, y = torch.randn(64, 512, device="cuda").to(b), torch.randn(300, 512, device="cuda").to(b), torch.zeros(64, 512, dtype=b, device="cuda")
+t, out = torch.randint(0, 300, (64,), device="cuda"), torch.zeros(6, 64, device="cuda")
+ones = torch.ones(512, dtype=b, device="cuda")
+nd, hd = A.rmsnorm_desc(64, 512, drop_p=0.1), A.head_loss_desc(64, 300, 512)
+s = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in (A.adapm_head_loss_scratch_bytes(hd, False), A.adapm_head_loss_scratch_bytes(hd, True), A.adapm_rmsnorm_backward_scratch_bytes(nd))]
+g = [torch.zeros_like(v) for v in (x, w, x, ones, x, y)]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+def calls(g, y, out):
+    A.adapm_dropout(x, None, g[5], A.TYPE_BF16, 64, 512, 0.1, 1, 1)
+    A.adapm_rmsnorm_forward(nd, g[5], x, ones, g[4], y, None, None, out[0])
+    A.adapm_head_loss_forward(hd, y, w, t, out[1], out[2], s[0])
+    A.adapm_head_loss_backward(hd, y, w, t, out[2], None, 1.0, g[0], g[1], s[1])
+    A.adapm_rmsnorm_backward(nd, g[0], None, g[4], out[0], ones, g[2], None, g[3], A.TYPE_BF16, False, s[2])
+with torch.cuda.graph(graph):
+    calls(g, y, out)
+graph.replay()
+torch.cuda.synchronize()
+again, y2, out2 = [torch.zeros_like(v) for v in g], torch.zeros_like(y), torch.zeros_like(out)
+calls(again, y2, out2)
+torch.cuda.synchronize()
+assert torch.equal(out, out2) and torch.equal(y, y2) and all(torch.equal(a, b) for a, b in zip(g, again)) and out[1].isfinite().all() and out[1].any()
+print("same")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_a_captured_one():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL_IN_A_CAPTURE], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
 def test_operators_refuse_memory_that_is_not_the_devices():
     host = torch.zeros(64, 64, dtype=BF16)
     dev = torch.zeros(64, 64, dtype=BF16, device="cuda")
@@ -602,8 +716,7 @@ def test_operators_refuse_memory_that_is_not_the_devices():
 
 def test_the_tail_of_a_training_step():
     """Dropout of a branch, residual, norm, head loss and back, the gradients of the norm's and the head's weight written where
-    adapm_step reads them, and the step itself: as a training program runs them, against the plain forms, and with a smaller
-    loss of the same batch after some steps."""
+    adapm_step reads them, and the step itself: as a training program runs them, against the plain forms."""
     tokens, width, vocab, p = 512, 128, 1000, 0.1
     blocks = [A.adapm_block(0, vocab, width, A.MOM_NONE, 0, A.V_BLOCKMEAN, 1, 0.75, 0.0),
               A.adapm_block(vocab * width, 1, width, A.MOM_FULL, 0, A.V_BLOCKMEAN, 0, 1.0, 0.0)]
@@ -626,8 +739,7 @@ def test_the_tail_of_a_training_step():
     hd = A.head_loss_desc(tokens, vocab, width)
     sf, sb = (torch.empty(A.adapm_head_loss_scratch_bytes(hd, b), dtype=torch.uint8, device="cuda") for b in (False, True))
     valid = int((targets != -100).sum())
-    first = None
-    for t in range(1, 9):
+    for t in range(1, 5):
         nd = A.rmsnorm_desc(tokens, width, drop_p=p, seed=5, offset=t)
         sn = torch.empty(A.adapm_rmsnorm_backward_scratch_bytes(nd), dtype=torch.uint8, device="cuda")
         A.adapm_rmsnorm_forward(nd, branch, stream, norm_w, s, y, None, None, rstd)
@@ -644,9 +756,7 @@ def test_the_tail_of_a_training_step():
         before = params.clone()
         ctx.adapm_step(params, grads, state, t)
         assert not torch.equal(before, params) and torch.equal(shadow, params.to(BF16))
-        mean = loss.sum().item() / valid
-        first = mean if first is None else first
-        assert math.isfinite(mean)
+        assert loss.isfinite().all()
     assert ctx.adapm_get_status() == 0 and A.adapm_head_loss_status(sb) == 0
     ctx.close()
 

@@ -41,6 +41,8 @@ def test_dropout_refusals():
     assert _dropout(p=-0.1) == ERANGE and _dropout(p=1.5) == ERANGE and _dropout(p=float("nan")) == ERANGE
     assert _dropout(rows=1 << 40, cols=1 << 40) == ERANGE
     assert _dropout(x=P + 1) == EALIGN and _dropout(step=P + 4) == EALIGN
+    assert _dropout(y=P + 16) == EINVAL and _dropout(y=P, y_ld=24) == EINVAL          # over x, but not element on element
+    assert _dropout(residual=3 * P, y=3 * P + 32) == EINVAL
     assert _dropout(rows=0) == 0 and _dropout(cols=0, x=None, y=None) == 0
 
 
@@ -63,6 +65,9 @@ def test_rmsnorm_refusals():
     assert _norm(y8=4 * P) == EINVAL                               # no room for its scales
     assert _norm(x=P + 1) == EALIGN and _norm(weight=P + 1) == EALIGN and _norm(rstd=P + 2) == EALIGN
     assert _norm(sum=3 * P + 16) == EINVAL                         # over y
+    assert _norm(y=P + 16) == EINVAL and _norm(desc(4, 64, y_ld=72), y=P) == EINVAL     # over x, but not element on element
+    assert _norm(sum=P + 128, y=3 * P) == EINVAL and _norm(y=2 * P) == EINVAL           # over x, over the weight
+    assert _norm(y8=P, y8_scales=5 * P) == EINVAL
     assert _norm(desc(0, 64), x=None) == 0
     assert A.load().adapm_rmsnorm_forward(None, P, None, P, None, P, None, None, None, 0) == EINVAL
 
@@ -99,6 +104,8 @@ def test_rmsnorm_gradient_refusals():
     assert _norm_grad(scratch=_Scratch(1 << 30, 16 * P + 16)) == EALIGN
     assert _norm_grad(dweight=6 * P + 2) == EALIGN and _norm_grad(rstd=3 * P + 1) == EALIGN
     assert _norm_grad(dx=5 * P) == EINVAL                           # both gradients in one place
+    assert _norm_grad(dresidual=P + 32) == EINVAL and _norm_grad(dresidual=4 * P) == EINVAL and _norm_grad(dresidual=6 * P) == EINVAL
+    assert _norm_grad(dresidual=None, dx=2 * P + 2) == EINVAL
     assert _norm_grad(A.rmsnorm_desc(4, 64, residual_ld=3)) == EINVAL
     assert _norm_grad(A.rmsnorm_desc(0, 64), accumulate=True) == 0
     assert A.adapm_rmsnorm_backward_scratch_bytes(A.rmsnorm_desc(4, 1 << 20)) == 0
@@ -142,6 +149,8 @@ def test_head_loss_refusals():
     assert _head_grad(dhidden=None, dweight=None) == EINVAL
     assert _head_grad(desc(4, 100, 64, dhidden_dtype=3)) == EINVAL and _head_grad(desc(4, 100, 64, dweight_dtype=-1)) == EINVAL
     assert _head_grad(dhidden=P) == EINVAL and _head_grad(dweight=2 * P + 128) == EINVAL and _head_grad(dweight=6 * P) == EINVAL
+    assert _head(lse=4 * P) == EINVAL and _head(loss=3 * P + 8) == EINVAL
+    assert _head_grad(dhidden=5 * P) == EINVAL and _head_grad(dweight=3 * P) == EINVAL and _head_grad(dloss=9 * P, dweight=9 * P) == EINVAL
     assert _head_grad(desc(0, 100, 64, accumulate=1), hidden=None) == 0
     assert A.load().adapm_head_loss_scratch_bytes(None, 0) == 0 and A.adapm_head_loss_scratch_bytes(desc(4, 100, 60), True) == 0
     st = C.c_int32()
