@@ -53,7 +53,8 @@ def _close(got, want, bound, what):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("rows,cols,ld,shift,residual", [(1, 1, 1, 0, False), (1, 8, 8, 0, True), (3, 7, 9, 1, True), (5, 40, 48, 0, False),
-                                                          (4, 33, 40, 0, True), (17, 64, 64, 1, False), (2, 300, 304, 8, True)])
+                                                          (4, 33, 40, 0, True), (17, 64, 64, 1, False), (2, 300, 304, 8, True),
+                                                          (17, 33, 33, 0, True), (16, 63, 63, 0, False), (9, 6, 6, 0, True), (11, 64, 65, 8, False), (40, 95, 95, 0, True)])
 def test_dropout_against_the_generator(dtype, rows, cols, ld, shift, residual):
     g = _gen(rows * cols)
     x, xb = _rows(g, rows, cols, dtype, ld, shift)
@@ -151,6 +152,7 @@ NORM_SIZES = [  # rows, cols, pitch added, shift of the buffers in elements
     (1, 1, 0, 0), (1, 8, 0, 0), (3, 5, 3, 1), (2, 129, 7, 0), (5, 256, 0, 0), (1, 4096, 0, 0), (7, 1000, 8, 8), (4, 1001, 0, 0),
     (2400, 64, 0, 0), (2500, 248, 8, 0), (2400, 512, 0, 0), (2371, 1024, 0, 0), (2369, 2048, 0, 0), (2400, 333, 0, 1),
     (3, 4104, 0, 0), (2, 8192, 0, 0), (2, 8200, 0, 0), (2, 32768, 0, 0), (2, 20001, 0, 0),
+    (2400, 1001, 0, 0), (2400, 255, 0, 8), (9, 2, 0, 0), (1300, 2056, 3, 0), (17, 8192, 5, 0), (9, 32761, 0, 0), (9, 32767, 0, 0), (20, 8191, 0, 0),
 ]
 
 
@@ -190,7 +192,7 @@ def test_rmsnorm_forward(dtype, wtype, rows, cols, pad, shift):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("group", [0, 128])
-@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 128), (2, 130), (5, 1000), (4, 1001), (2400, 264), (2369, 1600), (2, 4096), (3, 9000)])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 128), (2, 130), (5, 1000), (4, 1001), (2400, 264), (2369, 1600), (2, 4096), (3, 9000), (2400, 1003)])
 def test_rmsnorm_in_8_bits(dtype, group, rows, cols):
     g = _gen(rows * 3 + cols)
     x, _ = _rows(g, rows, cols, dtype)
@@ -214,13 +216,20 @@ def test_rmsnorm_in_8_bits(dtype, group, rows, cols):
     _close(q * per, wy, wy.abs() * (2.0**-4 + 2 * fp) + per * 2.0**-10, "y8")
     assert (q.abs().amax(1) == 448).sum() == rows - 1 or group
     assert (scales[rows // 2] == 1).all() and (q[rows // 2] == 0).all()
+    tight = torch.full((rows * cols + 8,), 0x5A, dtype=torch.uint8, device="cuda")       # rows one behind the other
+    s3 = torch.empty_like(scales)
+    A.adapm_rmsnorm_forward(A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[dtype], 1e-5, q8_group=group), x, None, w, None, None, tight, s3, None)
+    q3 = tight[:rows * cols].view(rows, cols).view(torch.float8_e4m3fn).double()
+    _close(s3, ws, ws * fp, "scales")
+    _close(q3 * s3.double().repeat_interleave(group or cols, 1)[:, :cols], wy, wy.abs() * (2.0**-4 + 2 * fp) + per * 2.0**-10, "y8, rows one behind the other")
+    assert (tight[rows * cols:] == 0x5A).all()
     alone, s2 = torch.empty_like(buf), torch.empty_like(scales)     # 8 bits only: the same numbers
     A.adapm_rmsnorm_forward(d, x, None, w, None, None, alone, s2, None)
     assert torch.equal(alone[:, :cols], buf[:, :cols]) and torch.equal(s2, scales)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("rows,cols", [(3, 7), (5, 96), (2, 1001)])
+@pytest.mark.parametrize("rows,cols", [(3, 7), (5, 96), (2, 1001), (17, 61), (9, 30)])
 def test_rmsnorm_with_the_branchs_dropout(dtype, rows, cols):
     g = _gen(cols)
     x, _ = _rows(g, rows, cols, dtype)
@@ -257,7 +266,7 @@ def test_rmsnorm_rows_of_extreme_values():
 
 
 @pytest.mark.parametrize("dtype,gtype", [(BF16, BF16), (BF16, F32), (F32, F32)])
-@pytest.mark.parametrize("rows,cols,pad,shift", NORM_SIZES + [(5000, 40, 0, 0), (1300, 4096, 0, 0)])
+@pytest.mark.parametrize("rows,cols,pad,shift", NORM_SIZES + [(5000, 40, 0, 0), (1300, 4096, 0, 0), (5000, 41, 0, 0), (1500, 4099, 0, 0), (1200, 8195, 0, 0)])
 def test_rmsnorm_backward(dtype, gtype, rows, cols, pad, shift):
     g = _gen(rows + 2 * cols)
     ld = cols + pad
@@ -297,7 +306,7 @@ def test_rmsnorm_backward(dtype, gtype, rows, cols, pad, shift):
     assert torch.equal(again, dw[8:8 + cols])
 
 
-@pytest.mark.parametrize("rows,cols", [(3, 7), (6, 96), (2, 9001)])
+@pytest.mark.parametrize("rows,cols", [(3, 7), (6, 96), (2, 9001), (19, 61), (9, 30)])
 def test_rmsnorm_backward_with_dropout_and_in_place(rows, cols):
     g = _gen(cols + 1)
     dy, dsum, s = (_rows(g, rows, cols, F32)[0] for _ in range(3))
