@@ -295,17 +295,16 @@ __device__ __forceinline__ void segments(int stages, int most, int& n, int& each
   n = (stages + each - 1) / each;
 }
 
-// Columns FROM to TO of `half` of this thread's row of an accumulator: v = them (tmem_ld_wait is the caller's) or v += them.
-template <int FROM, int TO>
+// `half` columns of this thread's row of an accumulator: v = them, or v += them.
 __device__ __forceinline__ void take(uint32_t taddr, int half, float* v) {
 #pragma unroll
-  for (int c = FROM; c < TO; c += 16)
+  for (int c = 0; c < 128; c += 16)
     if (c < half) tmem_ld16(taddr + c, v + c);
+  tmem_ld_wait();
 }
-template <int FROM, int TO>
 __device__ __forceinline__ void take_add(uint32_t taddr, int half, float* v) {
 #pragma unroll
-  for (int c = FROM; c < TO; c += 32) {
+  for (int c = 0; c < 128; c += 32) {
     if (c < half) {
       float t[32];
       tmem_ld16(taddr + c, t);
@@ -335,15 +334,16 @@ __device__ __forceinline__ float pick(const float* v, int y) {
   return x;
 }
 
-// Sum of exp over 128 logits of a row as sum * 2^k, k a whole number: z log2(e) - k is then one multiply-add with one rounding,
-// and the sums of different columns are scaled by powers of two only.  k is the greatest of the first 16 logits in base 2: any
-// k near the greatest one does, and one that is known early lets the maxima be found beside the exponentials.  Where a logit is over 2^64 times exp of it after all, or all 16 are -inf, the sum is made again with
-// the greatest of all.  NaN and +inf logits make the sum NaN.
+// The sum of exp over 128 logits of a row is made as sum * 2^k, k a whole number: z log2(e) - k is then one multiply-add with one
+// rounding, and the sums of different columns are scaled by powers of two only.  k is the greatest of the first 16 logits in
+// base 2: any k near the greatest one does, and one that is known early lets the maxima be found beside the exponentials.
+// Where the exponential of a logit is above 2^(k + 64) after all, or all 16 are -inf, the sum is made again with the greatest of
+// all.  NaN and +inf logits make the sum NaN.
 __device__ __forceinline__ float exponent_of(float top) { return fmaxf(-INFINITY, rintf(top * kLog2e)); }      // (NaN: -inf)
-template <int FROM, int TO>
-__device__ __forceinline__ void add_exponentials(const float* z, float shift, float* s) {
+__device__ __forceinline__ void sum_exponentials(const float* z, float shift, float* s) {
+  s[0] = s[1] = s[2] = s[3] = 0.f;
 #pragma unroll
-  for (int e = FROM; e < TO; e += 2) {
+  for (int e = 0; e < 128; e += 2) {
     float p0, p1;
     fma2(p0, p1, z[e], z[e + 1], kLog2e, -shift);
     add2(s[e & 2], s[(e & 2) + 1], ex2(p0), ex2(p1));
@@ -418,104 +418,104 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
   HeadItem t;
 
   if (warp < 4) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
-  if (skip) {
-    // nothing
-  } else if (warp == 0 || warp == 2) {
-    // ------------------------------------------------------------------ producers (all lanes run, one issues)
-    const bool leader = elect_one(), is_a = warp == 0;
-    const uint32_t pair_full = uniform(shared_of(sh.full, 0));
-    int stage = 0;
-    uint32_t phase = 0, issued = 0;
-    bool ok = true;
-    for (int seq = 0; ok && walk.item_uniform<BACKWARD>(pair, seq, t); ++seq) {
-      const CUtensorMap* map;
-      int x, y, n_box = 1;                 // K-major: one box of 128 rows, x runs; MN-major: boxes of 64 columns, y runs
-      const int half = t.bn / 2, o_row = a.o_buf * a.planes * a.t_pad;
-      if (is_a) {
-        if (t.cls == CLS_DW) { map = &a.gn; x = t.m0 + (int)rank * 128; y = o_row; n_box = 2; }
-        else if (t.cls == CLS_DH) { map = &a.gk; x = 0; y = o_row + t.m0 + (int)rank * 128; }
-        else { map = compacted ? &a.ck : &a.hk; x = 0; y = t.m0 + (int)rank * 128; }
-      } else {
-        if (t.cls == CLS_LOGITS) { map = &a.wk; x = 0; y = (BACKWARD ? a.g_begin : 0) + t.n0 + (int)rank * 128; }
-        else {
-          map = t.cls == CLS_DH ? &a.wn : (compacted ? &a.cn : &a.hn);
-          x = t.n0 + (int)rank * half; y = t.cls == CLS_DH ? a.o_begin : 0; n_box = half > 64 ? 2 : 1;
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
+    if (skip) {
+      // nothing
+    } else if (warp == 0 || warp == 2) {
+      // ------------------------------------------------------------------ producers (all lanes run, one issues)
+      const bool leader = elect_one(), is_a = warp == 0;
+      const uint32_t pair_full = uniform(shared_of(sh.full, 0));
+      int stage = 0;
+      uint32_t phase = 0, issued = 0;
+      bool ok = true;
+      for (int seq = 0; ok && walk.item_uniform<BACKWARD>(pair, seq, t); ++seq) {
+        const CUtensorMap* map;
+        int x, y, n_box = 1;                 // K-major: one box of 128 rows, x runs; MN-major: boxes of 64 columns, y runs
+        const int half = t.bn / 2, o_row = a.o_buf * a.planes * a.t_pad;
+        if (is_a) {
+          if (t.cls == CLS_DW) { map = &a.gn; x = t.m0 + (int)rank * 128; y = o_row; n_box = 2; }
+          else if (t.cls == CLS_DH) { map = &a.gk; x = 0; y = o_row + t.m0 + (int)rank * 128; }
+          else { map = compacted ? &a.ck : &a.hk; x = 0; y = t.m0 + (int)rank * 128; }
+        } else {
+          if (t.cls == CLS_LOGITS) { map = &a.wk; x = 0; y = (BACKWARD ? a.g_begin : 0) + t.n0 + (int)rank * 128; }
+          else {
+            map = t.cls == CLS_DH ? &a.wn : (compacted ? &a.cn : &a.hn);
+            x = t.n0 + (int)rank * half; y = t.cls == CLS_DH ? a.o_begin : 0; n_box = half > 64 ? 2 : 1;
+          }
         }
-      }
-      const bool along_y = is_a ? t.cls == CLS_DW : t.cls != CLS_LOGITS;
-      const uint32_t bytes = along_y ? (uint32_t)n_box * (kOperandBytes / 2) : kOperandBytes;
-      const int plane_step = is_a && t.cls != CLS_LOGITS ? a.t_pad : 0;
-      const int plane0 = t.k0 / t.per_plane, kx = along_y ? 0 : kStageK, ky = along_y ? kStageK : 0;
-      int k = t.k0 - plane0 * t.per_plane;
-      y += plane0 * plane_step + k * ky;
-      x += k * kx;
-      for (int left = t.count; left > 0; --left) {
-        if (!mbar_wait_warp<WAIT_PAIR>(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
-        uint8_t* const dst = stages + stage * (2 * kOperandBytes) + (is_a ? 0 : kOperandBytes);
-        if (leader) {
-          if (rank == 0) mbar_arrive_expect_tx(&sh.full[stage], 2 * bytes);
-          const uint32_t bar = pair_full + 8u * (uint32_t)stage;
-          tma_load_box_pair(dst, map, x, y, bar);
-          if (n_box == 2) tma_load_box_pair(dst + kOperandBytes / 2, map, x + 64, y, bar);
-        }
-        __syncwarp();
-        x += kx;
-        y += ky;
-        if (++k == t.per_plane) {                 // the next plane of A, the same B again
-          k = 0;
-          x -= kx * t.per_plane;
-          y += plane_step - ky * t.per_plane;
-        }
-        ++issued;
-        if (++stage == kHeadStages) { stage = 0; phase ^= 1u; }
-      }
-    }
-    if (!ok) drain_ring<true>(sh.full, stage, phase, issued, kHeadStages, rank);
-  } else if (warp == 1 && rank == 0) {
-    // ------------------------------------------------------------------ MMA issuer (all lanes run, one issues)
-    const bool leader = elect_one();
-    int stage = 0;
-    uint32_t phase = 0;
-    bool ok = true;
-    const uint32_t ring = uniform(smem_u32(stages)), d0 = uniform(tmem_base), dhi = desc_hi();
-    uint32_t run = 0;                     // segments so far
-    for (int seq = 0; ok && walk.item_uniform<BACKWARD>(pair, seq, t); ++seq) {
-      const bool a_mn = t.cls == CLS_DW, b_mn = t.cls != CLS_LOGITS;
-      const uint32_t idesc = uniform(make_idesc(t.bn, a_mn, b_mn, false, 256));
-      // per K step of 16: 32 bytes inside a K-major row, 16 rows of 128 bytes of an MN-major box (in 16-byte units)
-      const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
-      int left = t.count, n_seg, each;
-      segments(left, t.cls == CLS_LOGITS ? a.seg_logits : t.cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
-      for (; left > 0 && ok; left -= each, ++run) {
-        const int acc = (int)(run & 1);
-        if (!mbar_wait_warp<WAIT_PAIR_TC>(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t d = d0 + (uint32_t)(acc * kTile);
-        uint32_t accumulate = 0;
-        for (int i = min(each, left); i > 0; --i) {
-          if (!mbar_wait_warp<WAIT_PAIR>(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t slot = ring + (uint32_t)(stage * 2 * kOperandBytes);
-          const uint32_t alo = desc_lo(slot, a_mn ? kOperandBytes / 2 : 16u);
-          const uint32_t blo = desc_lo(slot + kOperandBytes, b_mn ? kOperandBytes / 2 : 16u);
+        const bool along_y = is_a ? t.cls == CLS_DW : t.cls != CLS_LOGITS;
+        const uint32_t bytes = along_y ? (uint32_t)n_box * (kOperandBytes / 2) : kOperandBytes;
+        const int plane_step = is_a && t.cls != CLS_LOGITS ? a.t_pad : 0;
+        const int plane0 = t.k0 / t.per_plane, kx = along_y ? 0 : kStageK, ky = along_y ? kStageK : 0;
+        int k = t.k0 - plane0 * t.per_plane;
+        y += plane0 * plane_step + k * ky;
+        x += k * kx;
+        for (int left = t.count; left > 0; --left) {
+          if (!mbar_wait_warp<WAIT_PAIR>(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+          uint8_t* const dst = stages + stage * (2 * kOperandBytes) + (is_a ? 0 : kOperandBytes);
           if (leader) {
-#pragma unroll
-            for (int q = 0; q < kStageK / 16; ++q)
-              mma_bf16<true>(d, desc_join(alo + q * a_step, dhi), desc_join(blo + q * b_step, dhi), idesc, q ? 1u : accumulate);
-            mma_commit<true>(&sh.empty[stage]);
+            if (rank == 0) mbar_arrive_expect_tx(&sh.full[stage], 2 * bytes);
+            const uint32_t bar = pair_full + 8u * (uint32_t)stage;
+            tma_load_box_pair(dst, map, x, y, bar);
+            if (n_box == 2) tma_load_box_pair(dst + kOperandBytes / 2, map, x + 64, y, bar);
           }
           __syncwarp();
-          accumulate = 1;
+          x += kx;
+          y += ky;
+          if (++k == t.per_plane) {                 // the next plane of A, the same B again
+            k = 0;
+            x -= kx * t.per_plane;
+            y += plane_step - ky * t.per_plane;
+          }
+          ++issued;
           if (++stage == kHeadStages) { stage = 0; phase ^= 1u; }
         }
-        if (ok && leader) mma_commit<true>(&sh.tfull[acc]);
-        __syncwarp();
+      }
+      if (!ok) drain_ring<true>(sh.full, stage, phase, issued, kHeadStages, rank);
+    } else if (warp == 1 && rank == 0) {
+      // ------------------------------------------------------------------ MMA issuer (all lanes run, one issues)
+      const bool leader = elect_one();
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      const uint32_t ring = uniform(smem_u32(stages)), d0 = uniform(tmem_base), dhi = desc_hi();
+      uint32_t run = 0;                     // segments so far
+      for (int seq = 0; ok && walk.item_uniform<BACKWARD>(pair, seq, t); ++seq) {
+        const bool a_mn = t.cls == CLS_DW, b_mn = t.cls != CLS_LOGITS;
+        const uint32_t idesc = uniform(make_idesc(t.bn, a_mn, b_mn, false, 256));
+        // per K step of 16: 32 bytes inside a K-major row, 16 rows of 128 bytes of an MN-major box (in 16-byte units)
+        const uint32_t a_step = a_mn ? 128u : 2u, b_step = b_mn ? 128u : 2u;
+        int left = t.count, n_seg, each;
+        segments(left, t.cls == CLS_LOGITS ? a.seg_logits : t.cls == CLS_DH ? a.seg_dh : a.seg_dw, n_seg, each);
+        for (; left > 0 && ok; left -= each, ++run) {
+          const int acc = (int)(run & 1);
+          if (!mbar_wait_warp<WAIT_PAIR_TC>(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t d = d0 + (uint32_t)(acc * kTile);
+          uint32_t accumulate = 0;
+          for (int i = min(each, left); i > 0; --i) {
+            if (!mbar_wait_warp<WAIT_PAIR>(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t slot = ring + (uint32_t)(stage * 2 * kOperandBytes);
+            const uint32_t alo = desc_lo(slot, a_mn ? kOperandBytes / 2 : 16u);
+            const uint32_t blo = desc_lo(slot + kOperandBytes, b_mn ? kOperandBytes / 2 : 16u);
+            if (leader) {
+#pragma unroll
+              for (int q = 0; q < kStageK / 16; ++q)
+                mma_bf16<true>(d, desc_join(alo + q * a_step, dhi), desc_join(blo + q * b_step, dhi), idesc, q ? 1u : accumulate);
+              mma_commit<true>(&sh.empty[stage]);
+            }
+            __syncwarp();
+            accumulate = 1;
+            if (++stage == kHeadStages) { stage = 0; phase ^= 1u; }
+          }
+          if (ok && leader) mma_commit<true>(&sh.tfull[acc]);
+          __syncwarp();
+        }
       }
     }
-  }
   } else {
-  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kDrainRegs));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kDrainRegs));
     // ------------------------------------------------------------------ epilogue: a thread has one row of the tile and, by its
     // group of four warps, the lower or upper half of the columns, all of them in registers
     const int q = 32 * (warp & 3) + lane, grp = (warp - 4) >> 2;
@@ -566,12 +566,8 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         if (!ok) break;
         tc_fence_after();
         const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * half);
-        if (i > 0) {
-          take_add<0, 128>(at, half, v);
-        } else {
-          take<0, 128>(at, half, v);
-          tmem_ld_wait();
-        }
+        if (i > 0) take_add(at, half, v);
+        else take(at, half, v);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_relaxed_at(shared_of(&sh.tempty[acc], 0));
@@ -580,7 +576,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
       if (!BACKWARD) {
         const int n = min(128, a.vocab - n0 - 128 * grp);
         if ((unsigned)y < 128u && y < n) a.z_target[row] = pick(v, y);
-        float total = 0.f, s[4] = {0.f, 0.f, 0.f, 0.f};
+        float total = 0.f, s[4];
         if (n < 128) {
           total = cut_row(v, n);
         } else if (a.smooth != 0.f) {
@@ -590,12 +586,11 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
           total = (t[0] + t[1]) + (t[2] + t[3]);
         }
         float k = exponent_of(greatest<0, 16>(v));
-        add_exponentials<0, 128>(v, k == -INFINITY ? 0.f : k, s);
+        sum_exponentials(v, k == -INFINITY ? 0.f : k, s);
         const float all = exponent_of(greatest<16, 128>(v));
         if (all > k && (all > k + 64.f || k == -INFINITY)) {
           k = all;
-          s[0] = s[1] = s[2] = s[3] = 0.f;
-          add_exponentials<0, 128>(v, k, s);
+          sum_exponentials(v, k, s);
         }
         const float sum = (s[0] + s[1]) + (s[2] + s[3]);
         if (row < tv) {
