@@ -398,8 +398,8 @@ struct NormGradArgs {
 // A CTA takes row after row; a thread has the same columns in each, whose share of dw it keeps.  The next row's elements are
 // on their way while a row is worked on.  16384 x 1600 in bf16 with dropout 62.5 us (4.2 TB/s), of which the sum of the CTAs'
 // shares takes 6; 79 us without the look-ahead.  Not kept: rows copied ahead into shared memory (cp.async, three rows deep: 70),
-// three CTAs of 256 threads per SM with the registers of two (86, spills).  NC = 4 (rows above 8192 columns): dw alone fills the registers, so a row is read a
-// second time, out of L2.
+// three CTAs of 256 threads per SM with the registers of two (86, spills), five of 128 with 96 registers (75).  NC = 4 (rows above
+// 8192 columns): dw alone fills the registers, so a row is read a second time, out of L2.
 template <typename T, int NC, int FORM, bool DROP>
 __global__ void __launch_bounds__(NC == 1 ? 256 : NC == 2 ? 512 : 1024) rmsnorm_backward_kernel(const NormGradArgs a) {
   using E = Elem<T>;
