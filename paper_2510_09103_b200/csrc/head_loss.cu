@@ -720,13 +720,14 @@ __global__ void __launch_bounds__(256) head_final_kernel(const FinalArgs a) {
 
 struct SumArgs {
   const int32_t* head;
+  const Walk* walk;              // of the launch that made the gradients of the first piece
   const int32_t* token;
   struct Job {
     const float* acc;            // [parts][pitch of a part in rows][hidden]
     void* out;
     int64_t ld, part_rows;
-    int32_t rows;                // < 0: the tokens with a target, whose places in `out` are `token`
-    int32_t most, stages, planes_of_tokens;      // K in stages, or (planes > 0) as many planes of the tokens with a target
+    int32_t rows;                // of dw; < 0: dh, of the tokens with a target, whose places in `out` are `token`
+    int32_t most;                // parts, at most
     int32_t f32, accumulate;
   } job[2];
   int32_t hidden, ctas[2];       // ... of each job
@@ -740,8 +741,7 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
   const int job = (int)blockIdx.x < a.ctas[0] ? 0 : 1, cta = (int)blockIdx.x - (job ? a.ctas[0] : 0);
   const SumArgs::Job& j = a.job[job];
   const int tv = a.head[HD_COUNT], rows = j.rows < 0 ? tv : j.rows, vec = a.hidden / 4;
-  int n, each;
-  parts_of(j.planes_of_tokens ? max(1, (tv + kStageK - 1) / kStageK) * j.planes_of_tokens : j.stages, j.most, n, each);
+  const int n = j.rows < 0 ? a.walk->parts_dh : a.walk->parts_dw;
   const int64_t part = j.part_rows * a.hidden, total = (int64_t)rows * vec;
   // many parts: the eight warps of a CTA share those of 32 places; few: a thread has a place to itself
   const bool shared = n >= 8;
@@ -997,12 +997,10 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   if (!sum_dh && !sum_dw) return ADAPM_OK;
   SumArgs u;
   std::memset(&u, 0, sizeof(u));
-  u.head = a.head; u.token = a.token; u.hidden = a.hidden; u.scale = scale;
+  u.head = a.head; u.walk = (const Walk*)(base + l.walks) + 1; u.token = a.token; u.hidden = a.hidden; u.scale = scale;
   int jobs = 0;
-  if (sum_dh)
-    u.job[jobs++] = {a.dh_acc, dhidden, d->hidden_ld, l.t_pad, -1, a.split_dh,
-                     (int32_t)((std::min(l.piece, d->vocab) + kStageK - 1) / kStageK) * plan.planes_dh, 0, a.dh_f32, 0};
-  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, 0, plan.planes_dw, a.dw_f32, a.accumulate};
+  if (sum_dh) u.job[jobs++] = {a.dh_acc, dhidden, d->hidden_ld, l.t_pad, -1, a.split_dh, a.dh_f32, 0};
+  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, a.dw_f32, a.accumulate};
   for (int i = 0; i < jobs; ++i) {
     const int64_t places = (u.job[i].rows < 0 ? d->tokens : d->vocab) * (d->hidden / 4), each = u.job[i].most >= 8 ? 32 : 256;
     u.ctas[i] = (int32_t)std::min<int64_t>((places + each - 1) / each, 4096);

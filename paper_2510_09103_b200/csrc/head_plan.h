@@ -73,6 +73,7 @@ struct Plan {
 struct Walk {
   int tv, pairs, n_dh, n_long, n_short, extra, skip, rounds;
   int m_tiles, tiles_dw, base_d, more_d, k_logits, k_dh, k_dw, each_dh, each_dw, all_dh, all_dw, last_group;
+  int parts_dh, parts_dw;        // of a gradient, as its sum takes them: those of the call's longest piece
   Divisor by_group, by_last, by_d, by_m, by_dw;
 
   __host__ __device__ void make(const Plan& p, int i, int tv_) {
@@ -86,20 +87,22 @@ struct Walk {
     by_d.set(nt_d); by_m.set(m_tiles ? m_tiles : 1);
     k_logits = (p.hidden + kStageK - 1) / kStageK;
     n_short = m_tiles * nt_v;
-    n_dh = n_long = extra = skip = rounds = k_dh = k_dw = each_dh = each_dw = all_dh = all_dw = tiles_dw = 0;
+    n_dh = n_long = extra = skip = rounds = k_dh = k_dw = each_dh = each_dw = all_dh = all_dw = tiles_dw = parts_dh = parts_dw = 0;
     const int o_cols = p.backward ? p.cols(i - 1) : 0;
     by_dw.set(1);
     if (o_cols == 0) return;
     k_dh = (o_cols + kStageK - 1) / kStageK;
     k_dw = tv > 0 ? (tv + kStageK - 1) / kStageK : 1;
-    int split_dh, split_dw;
     all_dh = k_dh * p.planes_dh; all_dw = k_dw * p.planes_dw;
-    parts_of(all_dh, p.split_dh, split_dh, each_dh);
-    parts_of(all_dw, p.split_dw, split_dw, each_dw);
+    // The first piece is as long as any, and the length of its parts is that of every piece's: a shorter piece has as many parts
+    // or fewer.  (Cut by itself it can have more, 50 parts of 2045 stages beside 49 of 2052, and nothing would sum the last.)
+    parts_of((p.cols(0) + kStageK - 1) / kStageK * p.planes_dh, p.split_dh, parts_dh, each_dh);
+    parts_of(all_dw, p.split_dw, parts_dw, each_dw);
+    const int split_dh = (all_dh + each_dh - 1) / each_dh;
     tiles_dw = (o_cols + kTile - 1) / kTile;
     by_dw.set(tiles_dw);
     n_dh = p.dh ? m_tiles * nt_d * split_dh : 0;
-    n_long = n_dh + (p.dw ? tiles_dw * nt_d * split_dw : 0);
+    n_long = n_dh + (p.dw ? tiles_dw * nt_d * parts_dw : 0);
     rounds = n_long / pairs;
     extra = n_long % pairs;
     const int surplus = load(0) - load(pairs - 1);
