@@ -387,8 +387,8 @@ typedef struct {
   float   label_smoothing;         /* 0 .. 1                                                                           */
   float   z_loss;                  /* >= 0                                                                             */
   int32_t dhidden_dtype, dweight_dtype;   /* ADAPM_TYPE_* of the gradients.  F32: the logits' gradient is carried as
-                                      three bf16 numbers (24 bits) into that product, at three times its cost; BF16: it is
-                                      rounded to bf16 once                                                             */
+                                      three bf16 numbers (24 bits) into that product, at three times its cost; BF16: as one
+                                      (8 bits), or with at most 64 tokens that have a valid target as two (16 bits)      */
   int32_t accumulate;              /* 1: dweight is added to what is there (a tied embedding, micro-batches)           */
 } adapm_head_loss;
 

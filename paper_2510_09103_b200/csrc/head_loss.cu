@@ -56,13 +56,13 @@ struct HeadArgs {
   float2* part;                  // forward: (exponent, sum) [2 n_tiles][t_pad]
   float* part_sum;               // forward with smoothing: sum of the logits, same layout
   float* z_target;               // forward: logit of the target of a compacted row
-  uint16_t* g;                   // [2 buffers][planes][t_pad][piece]
+  uint16_t* g;                   // [2 buffers][g_rows][piece]: the planes of the walk one behind the other
   float* dh_acc;                 // [split_dh][t_pad][hidden], between two pieces and before the splits are added up
   float* dw_acc;                 // [split_dw][vocab][hidden], before the splits are added up
   void* dh;
   void* dw;
   int64_t hidden_ld, weight_ld;
-  int32_t tokens, vocab, hidden, t_pad, piece, planes;
+  int32_t tokens, vocab, hidden, t_pad, piece, g_rows;
   int32_t g_begin, g_cols, g_buf;          // piece whose g this launch makes (g_cols = 0: none)
   int32_t o_begin, o_cols, o_buf;          // piece whose gradients it makes (o_cols = 0: none)
   int32_t first, last;                     // of the pieces, for dh
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
       for (int seq = 0; ok && walk.item_uniform<BACKWARD>(pair, seq, t); ++seq) {
         const CUtensorMap* map;
         int x, y, n_box = 1;                 // K-major: one box of 128 rows, x runs; MN-major: boxes of 64 columns, y runs
-        const int half = t.bn / 2, o_row = a.o_buf * a.planes * a.t_pad;
+        const int half = t.bn / 2, o_row = a.o_buf * a.g_rows;
         if (is_a) {
           if (t.cls == CLS_DW) { map = &a.gn; x = t.m0 + (int)rank * 128; y = o_row; n_box = 2; }
           else if (t.cls == CLS_DH) { map = &a.gk; x = 0; y = o_row + t.m0 + (int)rank * 128; }
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         }
         const bool along_y = is_a ? t.cls == CLS_DW : t.cls != CLS_LOGITS;
         const uint32_t bytes = along_y ? (uint32_t)n_box * (kOperandBytes / 2) : kOperandBytes;
-        const int plane_step = is_a && t.cls != CLS_LOGITS ? a.t_pad : 0;
+        const int plane_step = is_a && t.cls != CLS_LOGITS ? uniform(walk.plane_rows) : 0;
         const int plane0 = t.k0 / t.per_plane, kx = along_y ? 0 : kStageK, ky = along_y ? kStageK : 0;
         int k = t.k0 - plane0 * t.per_plane;
         y += plane0 * plane_step + k * ky;
@@ -468,8 +468,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         const float up = dl * ex2(-rest) * fmaf(2.f * a.z_loss, lse, 1.f);
         const float down = dl * (a.smooth / (float)a.vocab), at_y = dl * (1.f - a.smooth);
         const int n = row < tv ? a.vocab - a.g_begin - n0 - 128 * grp : 0;            // columns that exist
-        uint16_t* const dst = a.g + ((int64_t)(a.g_buf * a.planes) * a.t_pad + row) * a.piece + n0 + 128 * grp;
-        const int64_t plane = (int64_t)a.t_pad * a.piece;
+        uint16_t* const dst = a.g + ((int64_t)a.g_buf * a.g_rows + row) * a.piece + n0 + 128 * grp;
+        const int planes = walk.planes;
+        const int64_t plane = (int64_t)walk.plane_rows * a.piece;
 #pragma unroll
         for (int c = 0; c < 128; c += 16) {
           float* const z = v + c;
@@ -489,14 +490,14 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
             for (int e = 0; e < 16; ++e)
               if (c + e >= n) z[e] = 0.f;
           }
-          // g in bf16 (off by 2^-8 of itself at most, like the gradients it makes), or, where a gradient is wanted in fp32, as
-          // the sum of three bf16 numbers, which have its 24 bits
+          // g in bf16 (off by 2^-8 of itself at most, like the gradients it makes), or as the sum of two bf16 numbers (2^-16), or,
+          // where a gradient is wanted in fp32, of three, which have its 24 bits
           for (int p = 0;;) {
             uint32_t w[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2_rn(z[2 * e], z[2 * e + 1]);
             st_b32x8(dst + p * plane + c, w);
-            if (++p == a.planes) break;
+            if (++p == planes) break;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               z[2 * e] -= __uint_as_float(w[e] << 16);
@@ -887,7 +888,7 @@ extern "C" int adapm_head_loss_forward(const adapm_head_loss* d, const void* hid
   a.targets = l.direct ? targets : nullptr;
   a.part = (float2*)(base + l.part); a.part_sum = (float*)(base + l.part_sum); a.z_target = (float*)(base + l.z_target);
   a.tokens = (int32_t)d->tokens; a.vocab = (int32_t)d->vocab; a.hidden = (int32_t)d->hidden; a.t_pad = (int32_t)l.t_pad;
-  a.planes = a.split_dh = a.split_dw = 1;
+  a.split_dh = a.split_dw = 1;
   a.seg_logits = kSegForward;
   a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
 
@@ -953,7 +954,7 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   HeadArgs a;
   std::memset(&a, 0, sizeof(a));
   uint16_t* const g = (uint16_t*)(base + l.g);
-  const int64_t g_rows = l.n_buf * l.planes * l.t_pad;
+  const int64_t g_rows = l.n_buf * l.g_rows;
   if (!maps_of_operands(a, *d, hidden, weight, base + l.compact, l.t_pad, false, true) || !encode_bf16_matrix(&a.gk, g, g_rows, l.piece, l.piece, 128) ||
       !encode_bf16_matrix(&a.gn, g, g_rows, l.piece, l.piece, 64)) {
     set_error_text("cuTensorMapEncodeTiled failed for the head");
@@ -965,13 +966,13 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   a.g = g; a.dh_acc = (float*)(base + l.dh_acc); a.dw_acc = (float*)(base + l.dw_acc); a.dh = dhidden; a.dw = dweight;
   a.hidden_ld = d->hidden_ld; a.weight_ld = d->weight_ld;
   a.tokens = (int32_t)d->tokens; a.vocab = (int32_t)d->vocab; a.hidden = (int32_t)d->hidden; a.t_pad = (int32_t)l.t_pad; a.piece = (int32_t)l.piece;
-  a.planes = (int32_t)l.planes;
+  a.g_rows = (int32_t)l.g_rows;
   a.split_dh = (int32_t)l.split_dh; a.split_dw = (int32_t)l.split_dw;
   a.dh_f32 = d->dhidden_dtype == ADAPM_TYPE_F32; a.dw_f32 = d->dweight_dtype == ADAPM_TYPE_F32;
   a.dh_wide = (uintptr_t)dhidden % 32 == 0 && (a.dh_f32 || d->hidden_ld % 16 == 0);
   a.dw_wide = (uintptr_t)dweight % 32 == 0 && (a.dw_f32 || d->weight_ld % 16 == 0);
   a.accumulate = d->accumulate != 0;
-  a.seg_logits = l.planes > 2 ? kSegF32 : kSegBf16;
+  a.seg_logits = a.dh_f32 || a.dw_f32 ? kSegF32 : kSegBf16;
   a.seg_dh = a.dh_f32 ? kSegF32 : kSegBf16; a.seg_dw = a.dw_f32 ? kSegF32 : kSegBf16;
   a.scale = scale; a.smooth = d->label_smoothing; a.z_loss = d->z_loss;
 

@@ -51,9 +51,16 @@ struct Divisor {
 // `planes` planes of per_plane stages laid end to end.
 struct HeadItem { int cls, m0, n0, bn, k0, count, per_plane, split; };
 
+// bf16 numbers that g is carried as into the product of a gradient, by the gradient's type and the tokens with a target.  Three for
+// fp32.  One for bf16, but two where there are few tokens: a token's gradient is mostly its target's element of g, whose rounding
+// is averaged out over the tokens only (a norm's error of one token's gradients was up to 2.4 times that of their own rounding, of 64
+// tokens 1.4 times), and with so few of them the weight's way through memory takes the time.
+constexpr int kFewTokens = 64;
+__host__ __device__ __forceinline__ int planes_of(bool f32, int with_target) { return f32 ? 3 : with_target <= kFewTokens ? 2 : 1; }
+
 // What the items of a call follow from, beside the number of tokens with a target.
 struct Plan {
-  int32_t tokens, vocab, hidden, piece, n_pieces, planes_dh, planes_dw, split_dh, split_dw, dh, dw, backward, pairs;
+  int32_t tokens, vocab, hidden, piece, n_pieces, f32_dh, f32_dw, split_dh, split_dw, dh, dw, backward, pairs;
   __host__ __device__ int cols(int i) const {               // of piece i of the vocabulary
     const int left = vocab - i * piece;
     return i < 0 || i >= n_pieces ? 0 : left < piece ? left : piece;
@@ -74,6 +81,7 @@ struct Walk {
   int tv, pairs, n_dh, n_long, n_short, extra, skip, rounds;
   int m_tiles, tiles_dw, base_d, more_d, k_logits, k_dh, k_dw, each_dh, each_dw, all_dh, all_dw, last_group;
   int parts_dh, parts_dw;        // of a gradient, as its sum takes them: those of the call's longest piece
+  int planes, planes_dh, planes_dw, plane_rows;      // of g as it is made, of those that a gradient takes; rows from one to the next
   Divisor by_group, by_last, by_d, by_m, by_dw;
 
   __host__ __device__ void make(const Plan& p, int i, int tv_) {
@@ -88,15 +96,19 @@ struct Walk {
     k_logits = (p.hidden + kStageK - 1) / kStageK;
     n_short = m_tiles * nt_v;
     n_dh = n_long = extra = skip = rounds = k_dh = k_dw = each_dh = each_dw = all_dh = all_dw = tiles_dw = parts_dh = parts_dw = 0;
+    planes_dh = planes_of(p.f32_dh, tv);
+    planes_dw = planes_of(p.f32_dw, tv);
+    planes = planes_dh > planes_dw ? planes_dh : planes_dw;
+    plane_rows = m_tiles * kTile;
     const int o_cols = p.backward ? p.cols(i - 1) : 0;
     by_dw.set(1);
     if (o_cols == 0) return;
     k_dh = (o_cols + kStageK - 1) / kStageK;
     k_dw = tv > 0 ? (tv + kStageK - 1) / kStageK : 1;
-    all_dh = k_dh * p.planes_dh; all_dw = k_dw * p.planes_dw;
+    all_dh = k_dh * planes_dh; all_dw = k_dw * planes_dw;
     // The first piece is as long as any, and the length of its parts is that of every piece's: a shorter piece has as many parts
     // or fewer.  (Cut by itself it can have more, 50 parts of 2045 stages beside 49 of 2052, and nothing would sum the last.)
-    parts_of((p.cols(0) + kStageK - 1) / kStageK * p.planes_dh, p.split_dh, parts_dh, each_dh);
+    parts_of((p.cols(0) + kStageK - 1) / kStageK * planes_dh, p.split_dh, parts_dh, each_dh);
     parts_of(all_dw, p.split_dw, parts_dw, each_dw);
     const int split_dh = (all_dh + each_dh - 1) / each_dh;
     tiles_dw = (o_cols + kTile - 1) / kTile;
@@ -165,7 +177,7 @@ struct Walk {
 };
 
 struct Layout {
-  int64_t t_pad, n_tiles, piece, n_pieces, n_buf, planes, planes_dh, planes_dw, split_dh, split_dw;
+  int64_t t_pad, n_tiles, piece, n_pieces, n_buf, g_rows, split_dh, split_dw;      // g_rows: of one buffer of g
   bool direct;                   // forward over at most a tile of tokens: they are not compacted
   int64_t token, target, compact, lse, dloss, part, part_sum, z_target, g, dh_acc, dw_acc, walks, bytes;      // byte offsets
 };
@@ -175,13 +187,6 @@ struct Layout {
 // memory once per piece).
 constexpr int64_t kPlanPairs = 74;       // what the scratch is planned for (148 SMs)
 constexpr int64_t kPieceElems = (int64_t)64 << 20, kPieceMin = 2048;
-
-// bf16 numbers that g is carried as into the product of a gradient of type `t`.  One for bf16, but two where there are few tokens:
-// a token's gradient is mostly its target's element of g, whose rounding is averaged out over the tokens only (a norm's error of
-// one token's gradients was up to 2.4 times that of their own rounding, of 64 tokens 1.4 times), and with so few of them the
-// weight's way through memory takes the time.
-constexpr int64_t kFewTokens = 64;
-inline int64_t planes_of(const adapm_head_loss& d, int32_t t) { return t == ADAPM_TYPE_F32 ? 3 : d.tokens <= kFewTokens ? 2 : 1; }
 
 inline int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   if (d.tokens < 0 || d.vocab <= 0 || d.hidden <= 0) return ADAPM_EINVAL;
@@ -194,15 +199,15 @@ inline int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   if (backward && (!known_type(d.dhidden_dtype) || !known_type(d.dweight_dtype))) return ADAPM_EINVAL;
   l.t_pad = round_up(d.tokens < 1 ? 1 : d.tokens, kTile);
   l.n_tiles = (d.vocab + kTile - 1) / kTile;
-  l.planes_dh = backward ? planes_of(d, d.dhidden_dtype) : 1;
-  l.planes_dw = backward ? planes_of(d, d.dweight_dtype) : 1;
-  l.planes = std::max(l.planes_dh, l.planes_dw);
+  // The tokens with a target are counted on the device: with few of them there are two planes of a tile's rows, with more one.
+  const bool f32_dh = d.dhidden_dtype == ADAPM_TYPE_F32, f32_dw = d.dweight_dtype == ADAPM_TYPE_F32;
+  l.g_rows = f32_dh || f32_dw ? 3 * l.t_pad : std::max<int64_t>(l.t_pad, 2 * kTile);
   const int64_t most = std::max(kPieceMin, kPieceElems / l.t_pad / kTile * kTile);
   l.n_pieces = (d.vocab + most - 1) / most;
   l.piece = round_up((d.vocab + l.n_pieces - 1) / l.n_pieces, kTile);
   l.n_pieces = (d.vocab + l.piece - 1) / l.piece;
   l.n_buf = l.n_pieces > 1 ? 2 : 1;
-  if (l.t_pad / kTile * l.n_tiles > (1 << 30) || l.n_buf * l.planes * l.t_pad >= ((int64_t)1 << 31)) return ADAPM_ERANGE;
+  if (l.t_pad / kTile * l.n_tiles > (1 << 30) || l.n_buf * l.g_rows >= ((int64_t)1 << 31)) return ADAPM_ERANGE;
   // A gradient's K is cut into parts where an item of it would take more than half of what all items take divided over the
   // pairs: few tokens leave dh a handful of tiles with the whole vocabulary as their K, a small vocabulary does the same to dw.
   // A part is at least 16 stages (5 us), because the parts cost a launch and their way through memory.  512 tokens of 4096 x 256
@@ -210,8 +215,8 @@ inline int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   l.split_dh = l.split_dw = 1;
   if (backward) {
     const int64_t mt = l.t_pad / kTile, nt_d = (d.hidden + kTile - 1) / kTile, tiles = l.piece / kTile;
-    const int64_t k_dh = (std::min(l.piece, d.vocab) + kStageK - 1) / kStageK * l.planes_dh;
-    const int64_t k_dw = l.t_pad / kStageK * l.planes_dw;
+    const int64_t k_dh = (std::min(l.piece, d.vocab) + kStageK - 1) / kStageK * planes_of(f32_dh, (int)d.tokens);
+    const int64_t k_dw = l.t_pad / kStageK * planes_of(f32_dw, (int)d.tokens);
     const int64_t logits = l.n_pieces > 1 ? mt * tiles * ((d.hidden + kStageK - 1) / kStageK) : 0;
     const int64_t share = std::max<int64_t>(1, (nt_d * (mt * k_dh + tiles * k_dw) + logits) / kPlanPairs);
     auto parts = [&](int64_t k) { return std::max<int64_t>(1, std::min({(2 * k + share - 1) / share, k / 16, (int64_t)256})); };
@@ -229,7 +234,7 @@ inline int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   if (backward) {
     l.lse = take(l.t_pad * 4);
     l.dloss = take(l.t_pad * 4);
-    l.g = take(l.n_buf * l.planes * l.t_pad * l.piece * 2);
+    l.g = take(l.n_buf * l.g_rows * l.piece * 2);
     if (l.n_pieces > 1 || l.split_dh > 1) l.dh_acc = take(l.split_dh * l.t_pad * d.hidden * 4);
     if (l.split_dw > 1) l.dw_acc = take(l.split_dw * d.vocab * d.hidden * 4);
   } else {
@@ -245,7 +250,7 @@ inline Plan plan_of(const adapm_head_loss& d, const Layout& l, bool backward, bo
   Plan p;
   p.tokens = (int32_t)d.tokens; p.vocab = (int32_t)d.vocab; p.hidden = (int32_t)d.hidden;
   p.piece = (int32_t)(backward ? l.piece : d.vocab); p.n_pieces = (int32_t)(backward ? l.n_pieces : 1);
-  p.planes_dh = (int32_t)l.planes_dh; p.planes_dw = (int32_t)l.planes_dw;
+  p.f32_dh = d.dhidden_dtype == ADAPM_TYPE_F32; p.f32_dw = d.dweight_dtype == ADAPM_TYPE_F32;
   p.split_dh = (int32_t)l.split_dh; p.split_dw = (int32_t)l.split_dw;
   p.dh = dh; p.dw = dw; p.backward = backward; p.pairs = pairs;
   return p;

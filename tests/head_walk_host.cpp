@@ -23,6 +23,7 @@ static std::string wrong(const adapm_head_loss& d, bool backward, bool dh, bool 
   Walk first;
   if (backward) first.make(p, 1, tv);
   if (backward && (first.parts_dh < 1 || first.parts_dh > l.split_dh || first.parts_dw < 1 || first.parts_dw > l.split_dw)) return "more parts than the scratch holds";
+  if (backward && (first.plane_rows < tv || (int64_t)first.planes * first.plane_rows > l.g_rows)) return "planes of g that the scratch does not hold";
   for (int i = 0; i < launches; ++i) {
     Walk w;
     w.make(p, i, tv);
@@ -57,7 +58,9 @@ static std::string wrong(const adapm_head_loss& d, bool backward, bool dh, bool 
         if (part.first != at || part.second.second != split++) return "parts of K that do not follow one another";
         at += part.second.first;
       }
-      const int planes = is_dh ? p.planes_dh : p.planes_dw;
+      const bool f32 = (is_dh ? d.dhidden_dtype : d.dweight_dtype) == ADAPM_TYPE_F32;
+      const int planes = f32 ? 3 : tv <= 64 ? 2 : 1;
+      if (planes > w.planes) return "more planes of g than are made";
       if (at != planes * (((is_dh ? before : tv > 0 ? tv : 1) + kStageK - 1) / kStageK)) return "K of a gradient";
       if (is_dh && i == 1 && split != first.parts_dh) return "parts of dhidden that the first piece does not write";
       if (!is_dh && split != first.parts_dw) return "parts of dweight";
