@@ -303,7 +303,8 @@ int adapm_group_meansq_static(const void* g, int32_t grad_dtype, int64_t n_group
  * may be captured into a graph.  `stream` must belong to the current device, and every buffer must be memory
  * of that device: a host pointer or another device's memory is refused with ADAPM_EINVAL.  A `_ld` is the
  * pitch of a matrix: elements from one row to the next, at least the row's length; what lies between two rows
- * is neither read nor written.  A scratch buffer is 256-byte aligned, its contents need not be kept or
+ * is neither read nor written, and a matrix of the same pitch in bytes may lie there (x and y as columns of one
+ * buffer); matrices of different pitches must not reach into one another.  A scratch buffer is 256-byte aligned, its contents need not be kept or
  * cleared, and calls that may overlap on the GPU (captured graphs included) need one each.  Unless said
  * otherwise an output must not overlap an input.  Results do not depend on the run: no sum is made by atomics.
  */

@@ -866,7 +866,8 @@ extern "C" int adapm_head_loss_forward(const adapm_head_loss* d, const void* hid
   if (!hidden || !weight || !targets || !loss || !lse || !scratch) return ADAPM_EINVAL;
   if ((uintptr_t)hidden % 16 || (uintptr_t)weight % 16 || (uintptr_t)targets % 8 || (uintptr_t)loss % 4 || (uintptr_t)lse % 4 || (uintptr_t)scratch % 256) return ADAPM_EALIGN;
   if (scratch_bytes < (size_t)l.bytes) return ADAPM_ENOWORKSPACE;
-  if (overlap(loss, d->tokens * 4, lse, d->tokens * 4) || overlap(loss, d->tokens * 4, targets, d->tokens * 8) || overlap(lse, d->tokens * 4, targets, d->tokens * 8)) {
+  const Place ploss = vector_at(loss, d->tokens, 4), plse = vector_at(lse, d->tokens, 4), pt = vector_at(targets, d->tokens, 8);
+  if (share(ploss, plse) || share(ploss, pt) || share(plse, pt)) {
     set_error_text("adapm_head_loss_forward: the losses, their lse and the targets overlap");
     return ADAPM_EINVAL;
   }
@@ -937,12 +938,13 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
   }
   if (!hidden || !weight || !targets || !lse || !scratch) return ADAPM_EINVAL;
   if (scratch_bytes < (size_t)l.bytes) return ADAPM_ENOWORKSPACE;
-  const int64_t h_bytes = d->tokens * d->hidden_ld * 2, w_bytes = d->vocab * d->weight_ld * 2;
-  const int64_t dh_bytes = d->tokens * d->hidden_ld * type_bytes(d->dhidden_dtype), dw_bytes = d->vocab * dw_row;
-  if (overlap(hidden, h_bytes, dhidden, dh_bytes) || overlap(hidden, h_bytes, dweight, dw_bytes) || overlap(weight, w_bytes, dhidden, dh_bytes) ||
-      overlap(weight, w_bytes, dweight, dw_bytes) || overlap(dhidden, dh_bytes, dweight, dw_bytes) || overlap(lse, d->tokens * 4, dhidden, dh_bytes) ||
-      overlap(lse, d->tokens * 4, dweight, dw_bytes) || overlap(targets, d->tokens * 8, dhidden, dh_bytes) || overlap(targets, d->tokens * 8, dweight, dw_bytes) ||
-      overlap(dloss, d->tokens * 4, dhidden, dh_bytes) || overlap(dloss, d->tokens * 4, dweight, dw_bytes)) {
+  const Place ph = matrix_at(hidden, d->tokens, d->hidden_ld, d->hidden, 2), pw = matrix_at(weight, d->vocab, d->weight_ld, d->hidden, 2),
+              pt = vector_at(targets, d->tokens, 8), plse = vector_at(lse, d->tokens, 4), pdl = vector_at(dloss, d->tokens, 4),
+              pdh = matrix_at(dhidden, d->tokens, d->hidden_ld, d->hidden, type_bytes(d->dhidden_dtype)),
+              pdw = matrix_at(dweight, d->vocab, d->weight_ld, d->hidden, type_bytes(d->dweight_dtype));
+  bool apart = !share(pdh, pdw);
+  for (const Place& in : {ph, pw, pt, plse, pdl}) apart = apart && !share(pdh, in) && !share(pdw, in);
+  if (!apart) {
     set_error_text("adapm_head_loss_backward: a gradient overlaps an input or the other gradient");
     return ADAPM_EINVAL;
   }

@@ -650,7 +650,8 @@ extern "C" int adapm_dropout(const void* x, const void* residual, void* y, int32
   rc = check_rows({{x, x_ld, eb}, {residual, residual_ld, eb}, {y, y_ld, eb}}, rows, cols, form);
   if (rc != ADAPM_OK) return rc;
   if ((uintptr_t)step % 8) return ADAPM_EALIGN;
-  if (!apart_or_same(y, y_ld, x, x_ld, rows, cols, eb) || !apart_or_same(y, y_ld, residual, residual_ld, rows, cols, eb)) {
+  const Place out = matrix_at(y, rows, y_ld, cols, eb);
+  if (!apart_or_same(out, matrix_at(x, rows, x_ld, cols, eb)) || !apart_or_same(out, matrix_at(residual, rows, residual_ld, cols, eb))) {
     set_error_text("adapm_dropout: the output lies over an input, but not element on element");
     return ADAPM_EINVAL;
   }
@@ -688,14 +689,12 @@ extern "C" int adapm_rmsnorm_forward(const adapm_rmsnorm* d, const void* x, cons
   if (rc != ADAPM_OK) return rc;
   if ((uintptr_t)weight % 16 || slots_of(d->cols, form) > kMaxCols / 8 || (form == SHIFTED && y8 && d->q8_group)) form = SCALAR;
   if ((uintptr_t)weight % (uintptr_t)type_bytes(d->weight_dtype) || (uintptr_t)y8_scales % 4 || (uintptr_t)rstd % 4 || (uintptr_t)d->step % 8) return ADAPM_EALIGN;
-  auto extent = [&](int64_t ld, int64_t bytes) { return ((d->rows - 1) * ld + d->cols) * bytes; };
-  const int64_t wb = d->cols * type_bytes(d->weight_dtype);
-  bool apart = !overlap(sum, extent(d->sum_ld, eb), y, extent(d->y_ld, eb)) && !overlap(y8, extent(d->y8_ld, 1), x, extent(d->x_ld, eb)) &&
-               !overlap(y8, extent(d->y8_ld, 1), residual, extent(d->residual_ld, eb)) && !overlap(y8, extent(d->y8_ld, 1), sum, extent(d->sum_ld, eb)) &&
-               !overlap(y8, extent(d->y8_ld, 1), y, extent(d->y_ld, eb)) && !overlap(sum, extent(d->sum_ld, eb), weight, wb) &&
-               !overlap(y, extent(d->y_ld, eb), weight, wb) && !overlap(y8, extent(d->y8_ld, 1), weight, wb);
-  apart = apart && apart_or_same(sum, d->sum_ld, x, d->x_ld, d->rows, d->cols, eb) && apart_or_same(sum, d->sum_ld, residual, d->residual_ld, d->rows, d->cols, eb) &&
-          apart_or_same(y, d->y_ld, x, d->x_ld, d->rows, d->cols, eb) && apart_or_same(y, d->y_ld, residual, d->residual_ld, d->rows, d->cols, eb);
+  const Place px = matrix_at(x, d->rows, d->x_ld, d->cols, eb), pr = matrix_at(residual, d->rows, d->residual_ld, d->cols, eb),
+              ps = matrix_at(sum, d->rows, d->sum_ld, d->cols, eb), py = matrix_at(y, d->rows, d->y_ld, d->cols, eb),
+              pq = matrix_at(y8, d->rows, d->y8_ld, d->cols, 1), pw = vector_at(weight, d->cols, type_bytes(d->weight_dtype));
+  bool apart = !share(ps, py);
+  for (const Place& out : {ps, py}) apart = apart && apart_or_same(out, px) && apart_or_same(out, pr) && !share(out, pw);
+  for (const Place& t : {px, pr, ps, py, pw}) apart = apart && !share(pq, t);
   if (!apart) {
     set_error_text("adapm_rmsnorm_forward: an output lies over an input, but not element on element, or over another output");
     return ADAPM_EINVAL;
@@ -763,14 +762,14 @@ extern "C" int adapm_rmsnorm_backward(const adapm_rmsnorm* d, const void* dy, co
   // elements, 227 by windows (in fp32 108 and 90)
   if (form == SHIFTED && d->dtype == ADAPM_TYPE_BF16 && d->cols < 768) form = SCALAR;
   if ((uintptr_t)weight % (uintptr_t)type_bytes(d->weight_dtype) || (uintptr_t)rstd % 4 || (uintptr_t)d->step % 8) return ADAPM_EALIGN;
-  auto extent = [&](int64_t ld) { return ((d->rows - 1) * ld + d->cols) * eb; };
-  bool apart = !overlap(dresidual, extent(d->residual_ld), dx, extent(d->x_ld));
-  for (int o = 0; o < 2; ++o) {
-    const void* const out = o ? dx : dresidual;
-    const int64_t ld = o ? d->x_ld : d->residual_ld;
-    apart = apart && apart_or_same(out, ld, dy, d->y_ld, d->rows, d->cols, eb) && apart_or_same(out, ld, dsum, d->sum_ld, d->rows, d->cols, eb) &&
-            apart_or_same(out, ld, sum, d->sum_ld, d->rows, d->cols, eb) && !overlap(out, extent(ld), weight, d->cols * type_bytes(d->weight_dtype)) &&
-            !overlap(out, extent(ld), dweight, d->cols * gb) && !overlap(out, extent(ld), rstd, d->rows * 4);
+  const Place pdy = matrix_at(dy, d->rows, d->y_ld, d->cols, eb), pds = matrix_at(dsum, d->rows, d->sum_ld, d->cols, eb),
+              ps = matrix_at(sum, d->rows, d->sum_ld, d->cols, eb), pdr = matrix_at(dresidual, d->rows, d->residual_ld, d->cols, eb),
+              pdx = matrix_at(dx, d->rows, d->x_ld, d->cols, eb), pw = vector_at(weight, d->cols, type_bytes(d->weight_dtype)),
+              pdw = vector_at(dweight, d->cols, gb), prstd = vector_at(rstd, d->rows, 4);
+  bool apart = !share(pdr, pdx);
+  for (const Place& out : {pdr, pdx}) {
+    for (const Place& in : {pdy, pds, ps}) apart = apart && apart_or_same(out, in);
+    for (const Place& t : {pw, pdw, prstd}) apart = apart && !share(out, t);
   }
   if (!apart) {
     set_error_text("adapm_rmsnorm_backward: an output lies over an input, but not element on element, or over another output");

@@ -32,17 +32,39 @@ inline int check_on_this_device(std::initializer_list<const void*> ptrs, int* de
   return ADAPM_OK;
 }
 
-// Whether [a, a + an) and [b, b + bn) share a byte (null ranges do not).
-inline bool overlap(const void* a, int64_t an, const void* b, int64_t bn) {
-  if (!a || !b) return false;
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + (uintptr_t)bn && y < x + (uintptr_t)an;
+// Where a matrix lies: `rows` rows of `bytes` bytes, `pitch` bytes apart.  A vector is one row.  (Null: nowhere.)
+struct Place {
+  const void* p;
+  int64_t rows, pitch, bytes;
+  uint64_t begin() const { return (uint64_t)(uintptr_t)p; }
+  uint64_t end() const { return begin() + (uint64_t)((rows - 1) * pitch + bytes); }
+};
+inline Place matrix_at(const void* p, int64_t rows, int64_t ld, int64_t cols, int64_t bytes) {
+  return Place{p, rows, (rows > 1 ? ld : cols) * bytes, cols * bytes};
+}
+inline Place vector_at(const void* p, int64_t n, int64_t bytes) { return Place{p, 1, n * bytes, n * bytes}; }
+
+// Whether two matrices share a byte.  What lies between the rows of one belongs to neither, so that another one of the same pitch may
+// lie there; two matrices of different pitches count as sharing where one begins before the other ends.
+inline bool share(const Place& a, const Place& b) {
+  if (!a.p || !b.p || a.rows <= 0 || b.rows <= 0 || a.bytes <= 0 || b.bytes <= 0) return false;
+  if (a.begin() >= b.end() || b.begin() >= a.end()) return false;
+  if (a.rows == 1 || b.rows == 1) {
+    const Place &one = a.rows == 1 ? a : b, &m = a.rows == 1 ? b : a;
+    if (m.rows == 1) return true;
+    // the first row of m that ends behind the beginning of the other
+    const uint64_t pitch = (uint64_t)m.pitch, first_end = m.begin() + (uint64_t)m.bytes;
+    const uint64_t k = one.begin() < first_end ? 0 : (one.begin() - first_end) / pitch + 1;
+    return k < (uint64_t)m.rows && m.begin() + k * pitch < one.end();
+  }
+  if (a.pitch != b.pitch) return true;
+  const uint64_t pitch = (uint64_t)a.pitch, ahead = a.begin() <= b.begin() ? (b.begin() - a.begin()) % pitch : (pitch - (a.begin() - b.begin()) % pitch) % pitch;
+  return ahead < (uint64_t)a.bytes || ahead + (uint64_t)b.bytes > pitch;
 }
 
-// Whether an output [rows, cols] may lie where an input does: apart, or element on element.
-inline bool apart_or_same(const void* out, int64_t out_ld, const void* in, int64_t in_ld, int64_t rows, int64_t cols, int64_t bytes) {
-  if (out == in && (out_ld == in_ld || rows <= 1)) return true;
-  return !overlap(out, ((rows - 1) * out_ld + cols) * bytes, in, ((rows - 1) * in_ld + cols) * bytes);
+// Whether an output may lie where an input does: apart, or element on element.
+inline bool apart_or_same(const Place& out, const Place& in) {
+  return (out.p == in.p && out.bytes == in.bytes && out.pitch == in.pitch) || !share(out, in);
 }
 
 }  // namespace adapm

@@ -2,9 +2,10 @@
 test_gpu_operators.py, whose helpers and derivations these use."""
 import pytest
 
+import paper_2510_09103_b200 as A
 import test_gpu_operators as T
 from oracle import operators_oracle as R
-from test_gpu_operators import BF16, F32, HALF, _backward, _check_backward, _close, _gen, _head_case
+from test_gpu_operators import BF16, F32, GUARD, HALF, TYPE, _backward, _check_backward, _close, _gen, _head_case
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -56,3 +57,61 @@ def test_head_loss_gradient_of_few_tokens_with_a_target(tokens, valid, dht, dwt)
         got = dh[at] if out is dh else dw
         _close(got, want, bound + want.abs() * HALF[out.dtype] * 1.01 + 1e-30, "dhidden" if out is dh else "dweight")
     assert (dh[ignored] == 0).all()
+
+
+# ---- matrices side by side in one buffer ------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols,ld", [(7, 64, 128), (5, 33, 66), (300, 1601, 3202), (9, 40, 96), (4, 9000, 18000)])
+def test_operators_on_columns_of_one_buffer(dtype, rows, cols, ld):
+    """x and y as neighbouring columns of one matrix: they share no element."""
+    g = _gen(rows)
+    buf = torch.randn(rows, ld, generator=g, device="cuda").to(dtype)
+    x, y = buf[:, :cols], buf[:, cols:2 * cols]
+    behind = buf[:, 2 * cols:].clone()
+    xs, r = x.contiguous(), torch.randn(rows, cols, generator=g, device="cuda").to(dtype)
+    want = torch.empty_like(xs)
+    A.adapm_dropout(xs, r, want, TYPE[dtype], rows, cols, 0.3, 1, 2)
+    A.adapm_dropout(x, r, y, TYPE[dtype], rows, cols, 0.3, 1, 2, x_ld=ld, y_ld=ld)
+    assert torch.equal(y, want) and torch.equal(x, xs) and torch.equal(buf[:, 2 * cols:], behind)
+    w = torch.randn(cols, generator=g, device="cuda").to(dtype)
+    rstd, again = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    A.adapm_rmsnorm_forward(A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[dtype]), xs, None, w, None, want, None, None, rstd)
+    A.adapm_rmsnorm_forward(A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[dtype], x_ld=ld, y_ld=ld), x, None, w, None, y, None, None, again)
+    _close(y, want.double(), want.double().abs() * (2 * HALF[dtype] + 2.0**-16), "y")          # (another layout may take another order of the sum)
+    _close(again, rstd.double(), rstd.double() * 2.0**-16, "rstd")
+    assert torch.equal(x, xs) and torch.equal(buf[:, 2 * cols:], behind)
+    dy = torch.randn(rows, cols, generator=g, device="cuda").to(dtype)
+    A.adapm_rmsnorm_backward(A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[dtype]), dy, None, xs, rstd, w, want, None, None, A.TYPE_F32, False, None)
+    A.adapm_rmsnorm_backward(A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[dtype], sum_ld=ld, residual_ld=ld), dy, None, x, rstd, w, y, None, None, A.TYPE_F32, False, None)
+    size = (rstd[:, None] * (dy.float() * w.float()).abs()).double()
+    _close(y, want.double(), want.double().abs() * 2 * HALF[dtype] + (size + size.amax(1, keepdim=True)) * 2.0**-16 * (1 + x.double().abs()), "dresidual")
+    assert torch.equal(x, xs) and torch.equal(buf[:, 2 * cols:], behind)
+
+
+def test_head_gradients_beside_their_operands():
+    """dhidden in the columns beside hidden's, dweight in those beside the weight's."""
+    hidden, _, weight, _, targets = _head_case(300, 1000, 64, ignored=0.2)
+    lse = R.head_loss(hidden, weight, targets)[1].float()
+    dh, dw = _backward(hidden, weight, targets, lse)
+    hb, wb = torch.full((300, 136), GUARD, dtype=BF16, device="cuda"), torch.full((1000, 128), GUARD, dtype=BF16, device="cuda")
+    hb[:, :64], wb[:, 64:] = hidden, weight
+    d = A.head_loss_desc(300, 1000, 64, 136, 128)
+    scratch = torch.empty(A.adapm_head_loss_scratch_bytes(d, True), dtype=torch.uint8, device="cuda")
+    A.adapm_head_loss_backward(d, hb, wb[:, 64:], targets, lse, None, 1.0, hb[:, 64:], wb, scratch)
+    assert torch.equal(hb[:, 64:128], dh) and torch.equal(wb[:, :64], dw)
+    assert torch.equal(hb[:, :64].nan_to_num(3), hidden.nan_to_num(3)) and torch.equal(wb[:, 64:], weight) and (hb[:, 128:] == GUARD).all()
+
+
+def test_head_gradients_directly_behind_a_view_of_their_operands():
+    """hidden as columns of a wider matrix whose last row ends before its pitch does: what follows may be an output."""
+    hidden, _, weight, _, targets = _head_case(40, 300, 64)
+    lse = R.head_loss(hidden, weight, targets)[1].float()
+    dh, _ = _backward(hidden, weight, targets, lse)
+    arena = torch.full((39 * 128 + 64 + 39 * 128 + 64,), GUARD, dtype=BF16, device="cuda")
+    h, out = arena[:39 * 128 + 64].as_strided((40, 64), (128, 1)), arena.as_strided((40, 64), (128, 1), 39 * 128 + 64)
+    h.copy_(hidden)
+    d = A.head_loss_desc(40, 300, 64, 128)
+    scratch = torch.empty(A.adapm_head_loss_scratch_bytes(d, True), dtype=torch.uint8, device="cuda")
+    A.adapm_head_loss_backward(d, h, weight, targets, lse, None, 1.0, out, None, scratch)
+    assert torch.equal(out, dh) and torch.equal(h, hidden)
