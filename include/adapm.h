@@ -306,7 +306,7 @@ int adapm_group_meansq_static(const void* g, int32_t grad_dtype, int64_t n_group
  * is neither read nor written, and a matrix of the same pitch in bytes may lie there (x and y as columns of one
  * buffer); matrices of different pitches must not reach into one another.  A scratch buffer is 256-byte aligned, its contents need not be kept or
  * cleared, and calls that may overlap on the GPU (captured graphs included) need one each.  Unless said
- * otherwise an output must not overlap an input.  Results do not depend on the run: no sum is made by atomics.
+ * otherwise an output and the scratch overlap no other buffer of the call: ADAPM_EINVAL.  Results do not depend on the run: no sum is made by atomics.
  */
 enum { ADAPM_TYPE_F32 = 0, ADAPM_TYPE_BF16 = 1 };    /* element types; the numbers of ADAPM_GRAD_*    */
 

@@ -866,9 +866,13 @@ extern "C" int adapm_head_loss_forward(const adapm_head_loss* d, const void* hid
   if (!hidden || !weight || !targets || !loss || !lse || !scratch) return ADAPM_EINVAL;
   if ((uintptr_t)hidden % 16 || (uintptr_t)weight % 16 || (uintptr_t)targets % 8 || (uintptr_t)loss % 4 || (uintptr_t)lse % 4 || (uintptr_t)scratch % 256) return ADAPM_EALIGN;
   if (scratch_bytes < (size_t)l.bytes) return ADAPM_ENOWORKSPACE;
-  const Place ploss = vector_at(loss, d->tokens, 4), plse = vector_at(lse, d->tokens, 4), pt = vector_at(targets, d->tokens, 8);
-  if (share(ploss, plse) || share(ploss, pt) || share(plse, pt)) {
-    set_error_text("adapm_head_loss_forward: the losses, their lse and the targets overlap");
+  const Place ph = matrix_at(hidden, d->tokens, d->hidden_ld, d->hidden, 2), pw = matrix_at(weight, d->vocab, d->weight_ld, d->hidden, 2),
+              pt = vector_at(targets, d->tokens, 8), ploss = vector_at(loss, d->tokens, 4), plse = vector_at(lse, d->tokens, 4),
+              own = vector_at(scratch, l.bytes, 1);
+  bool apart = !share(ploss, plse) && !share(own, ploss) && !share(own, plse);
+  for (const Place& in : {ph, pw, pt}) apart = apart && !share(ploss, in) && !share(plse, in) && !share(own, in);
+  if (!apart) {
+    set_error_text("adapm_head_loss_forward: the losses, their lse or the scratch overlap another buffer");
     return ADAPM_EINVAL;
   }
   int device, pairs;
@@ -942,10 +946,11 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
               pt = vector_at(targets, d->tokens, 8), plse = vector_at(lse, d->tokens, 4), pdl = vector_at(dloss, d->tokens, 4),
               pdh = matrix_at(dhidden, d->tokens, d->hidden_ld, d->hidden, type_bytes(d->dhidden_dtype)),
               pdw = matrix_at(dweight, d->vocab, d->weight_ld, d->hidden, type_bytes(d->dweight_dtype));
-  bool apart = !share(pdh, pdw);
-  for (const Place& in : {ph, pw, pt, plse, pdl}) apart = apart && !share(pdh, in) && !share(pdw, in);
+  const Place own = vector_at(scratch, l.bytes, 1);
+  bool apart = !share(pdh, pdw) && !share(own, pdh) && !share(own, pdw);
+  for (const Place& in : {ph, pw, pt, plse, pdl}) apart = apart && !share(pdh, in) && !share(pdw, in) && !share(own, in);
   if (!apart) {
-    set_error_text("adapm_head_loss_backward: a gradient overlaps an input or the other gradient");
+    set_error_text("adapm_head_loss_backward: a gradient or the scratch overlaps another buffer");
     return ADAPM_EINVAL;
   }
   rc = check_on_this_device({hidden, weight, targets, lse, dloss, dhidden, dweight, scratch}, &device);

@@ -651,7 +651,8 @@ extern "C" int adapm_dropout(const void* x, const void* residual, void* y, int32
   if (rc != ADAPM_OK) return rc;
   if ((uintptr_t)step % 8) return ADAPM_EALIGN;
   const Place out = matrix_at(y, rows, y_ld, cols, eb);
-  if (!apart_or_same(out, matrix_at(x, rows, x_ld, cols, eb)) || !apart_or_same(out, matrix_at(residual, rows, residual_ld, cols, eb))) {
+  if (!apart_or_same(out, matrix_at(x, rows, x_ld, cols, eb)) || !apart_or_same(out, matrix_at(residual, rows, residual_ld, cols, eb)) ||
+      share(out, vector_at(step, 1, 8))) {
     set_error_text("adapm_dropout: the output lies over an input, but not element on element");
     return ADAPM_EINVAL;
   }
@@ -691,10 +692,13 @@ extern "C" int adapm_rmsnorm_forward(const adapm_rmsnorm* d, const void* x, cons
   if ((uintptr_t)weight % (uintptr_t)type_bytes(d->weight_dtype) || (uintptr_t)y8_scales % 4 || (uintptr_t)rstd % 4 || (uintptr_t)d->step % 8) return ADAPM_EALIGN;
   const Place px = matrix_at(x, d->rows, d->x_ld, d->cols, eb), pr = matrix_at(residual, d->rows, d->residual_ld, d->cols, eb),
               ps = matrix_at(sum, d->rows, d->sum_ld, d->cols, eb), py = matrix_at(y, d->rows, d->y_ld, d->cols, eb),
-              pq = matrix_at(y8, d->rows, d->y8_ld, d->cols, 1), pw = vector_at(weight, d->cols, type_bytes(d->weight_dtype));
-  bool apart = !share(ps, py);
-  for (const Place& out : {ps, py}) apart = apart && apart_or_same(out, px) && apart_or_same(out, pr) && !share(out, pw);
-  for (const Place& t : {px, pr, ps, py, pw}) apart = apart && !share(pq, t);
+              pq = matrix_at(y8, d->rows, d->y8_ld, d->cols, 1), pw = vector_at(weight, d->cols, type_bytes(d->weight_dtype)),
+              pscales = vector_at(y8 ? y8_scales : nullptr, d->rows * (d->q8_group ? (d->cols + 127) / 128 : 1), 4), prstd = vector_at(rstd, d->rows, 4),
+              pstep = vector_at(d->step, 1, 8);
+  bool apart = !share(ps, py) && !share(pscales, prstd);
+  for (const Place& out : {ps, py}) apart = apart && apart_or_same(out, px) && apart_or_same(out, pr) && !share(out, pw) && !share(out, pstep);
+  for (const Place& t : {px, pr, ps, py, pw, pstep}) apart = apart && !share(pq, t) && !share(pscales, t) && !share(prstd, t);
+  apart = apart && !share(pq, pscales) && !share(pq, prstd);
   if (!apart) {
     set_error_text("adapm_rmsnorm_forward: an output lies over an input, but not element on element, or over another output");
     return ADAPM_EINVAL;
@@ -765,12 +769,13 @@ extern "C" int adapm_rmsnorm_backward(const adapm_rmsnorm* d, const void* dy, co
   const Place pdy = matrix_at(dy, d->rows, d->y_ld, d->cols, eb), pds = matrix_at(dsum, d->rows, d->sum_ld, d->cols, eb),
               ps = matrix_at(sum, d->rows, d->sum_ld, d->cols, eb), pdr = matrix_at(dresidual, d->rows, d->residual_ld, d->cols, eb),
               pdx = matrix_at(dx, d->rows, d->x_ld, d->cols, eb), pw = vector_at(weight, d->cols, type_bytes(d->weight_dtype)),
-              pdw = vector_at(dweight, d->cols, gb), prstd = vector_at(rstd, d->rows, 4);
+              pdw = vector_at(dweight, d->cols, gb), prstd = vector_at(rstd, d->rows, 4), pstep = vector_at(d->step, 1, 8);
   bool apart = !share(pdr, pdx);
   for (const Place& out : {pdr, pdx}) {
     for (const Place& in : {pdy, pds, ps}) apart = apart && apart_or_same(out, in);
-    for (const Place& t : {pw, pdw, prstd}) apart = apart && !share(out, t);
+    for (const Place& t : {pw, pdw, prstd, pstep}) apart = apart && !share(out, t);
   }
+  for (const Place& in : {pdy, pds, ps, pw, prstd, pstep}) apart = apart && !share(pdw, in);
   if (!apart) {
     set_error_text("adapm_rmsnorm_backward: an output lies over an input, but not element on element, or over another output");
     return ADAPM_EINVAL;
@@ -778,7 +783,13 @@ extern "C" int adapm_rmsnorm_backward(const adapm_rmsnorm* d, const void* dy, co
   if (dweight) {
     if (!scratch) return ADAPM_EINVAL;
     if ((uintptr_t)scratch % 256) return ADAPM_EALIGN;
-    if (scratch_bytes < adapm_rmsnorm_backward_scratch_bytes(d)) return ADAPM_ENOWORKSPACE;
+    const size_t needed = adapm_rmsnorm_backward_scratch_bytes(d);
+    if (scratch_bytes < needed) return ADAPM_ENOWORKSPACE;
+    for (const Place& t : {pdy, pds, ps, pdr, pdx, pw, pdw, prstd, pstep}) apart = apart && !share(vector_at(scratch, (int64_t)needed, 1), t);
+    if (!apart) {
+      set_error_text("adapm_rmsnorm_backward: the scratch overlaps another buffer");
+      return ADAPM_EINVAL;
+    }
   }
   rc = check_on_this_device({dy, dsum, sum, rstd, weight, dresidual, dx, dweight, dweight ? scratch : nullptr, d->step}, &device);
   if (rc == ADAPM_OK) rc = sm_count(device, &sms);

@@ -4,7 +4,7 @@ import pytest
 
 import paper_2510_09103_b200 as A
 import test_operators_host as H
-from test_operators_host import ECUDA, EINVAL, P, _dropout, _head_grad, _norm, _norm_grad
+from test_operators_host import ECUDA, EINVAL, P, _Scratch, _dropout, _head, _head_grad, _norm, _norm_grad
 
 pytestmark = pytest.mark.skipif(not H._no_device(), reason="addresses that stand for buffers are for a machine without a device")
 
@@ -44,3 +44,60 @@ def test_head_gradients_between_rows(at, ok):
     assert _head_grad(desc, dhidden=None, dweight=2 * P + at) == want
     assert _head_grad(desc, hidden=20 * P, dhidden=2 * P + at) == want
     assert _head_grad(desc, hidden=20 * P, weight=21 * P, dhidden=6 * P, dweight=6 * P + at) == want
+
+
+# ---- vectors and scratch ----------------------------------------------------------------------------------
+
+def test_dropout_over_its_step_word():
+    assert _dropout(y=2 * P, step=2 * P + 8) == EINVAL and _dropout(y=2 * P, step=2 * P + 128) == ECUDA
+
+
+def test_norm_vectors_over_matrices():
+    desc = A.rmsnorm_desc(4, 64)
+    for name in ("x", "residual", "sum", "y", "weight"):
+        at = dict(x=10 * P, residual=11 * P, sum=12 * P, y=13 * P, weight=14 * P)
+        end = at[name] + (4 if name != "weight" else 1) * 128
+        assert _norm(desc, rstd=at[name] + 4, **at) == EINVAL, name
+        assert _norm(desc, rstd=end, **at) == ECUDA, name
+        assert _norm(desc, y8=20 * P, y8_scales=at[name] + 4, **at) == EINVAL, name
+        assert _norm(desc, y8=20 * P, y8_scales=end, **at) == ECUDA, name
+    assert _norm(desc, y8=20 * P, y8_scales=20 * P + 8) == EINVAL and _norm(desc, y8=20 * P, y8_scales=21 * P, rstd=21 * P + 12) == EINVAL
+    assert _norm(desc, y8=20 * P, y8_scales=21 * P, rstd=21 * P + 16) == ECUDA and _norm(desc, y8=20 * P, y8_scales=21 * P, rstd=20 * P) == EINVAL
+    for out in ("sum", "y"):
+        assert _norm(A.rmsnorm_desc(4, 64, drop_p=0.1, step=30 * P), **{"y": None, out: 30 * P - 64}) == EINVAL
+    # a vector between the rows of a matrix
+    wide = A.rmsnorm_desc(4, 64, x_ld=128)
+    assert _norm(wide, rstd=P + 128) == ECUDA and _norm(wide, rstd=P + 124) == EINVAL and _norm(wide, rstd=P + 244) == EINVAL
+    assert _norm(wide, rstd=P + 3 * 256 + 128) == ECUDA and _norm(wide, rstd=P - 16) == ECUDA and _norm(wide, rstd=P - 12) == EINVAL
+
+
+def test_norm_gradient_vectors_and_scratch_over_matrices():
+    desc = A.rmsnorm_desc(4, 64, drop_p=0.1, step=30 * P)
+    at = dict(dy=10 * P, dsum=11 * P, sum=12 * P, rstd=13 * P, weight=14 * P, dresidual=15 * P, dx=16 * P, dweight=17 * P)
+    n = A.adapm_rmsnorm_backward_scratch_bytes(desc)
+    assert _norm_grad(desc, scratch=_Scratch(n, 20 * P), **at) == ECUDA
+    for name, where in at.items():
+        assert _norm_grad(desc, scratch=_Scratch(n, where), **at) == EINVAL, name
+        if name not in ("dresidual", "dx", "dweight"):
+            assert _norm_grad(desc, scratch=_Scratch(n, 20 * P), **dict(at, dweight=where + 4)) == EINVAL, name
+    assert _norm_grad(desc, scratch=_Scratch(n, 30 * P), **at) == EINVAL
+    assert _norm_grad(desc, scratch=_Scratch(n, 20 * P), **dict(at, dweight=30 * P - 8)) == EINVAL
+    assert _norm_grad(desc, scratch=_Scratch(n, 20 * P), **dict(at, dx=30 * P)) == EINVAL
+
+
+def test_head_vectors_and_scratch_over_matrices():
+    desc = A.head_loss_desc(4, 100, 64)
+    n, m = A.adapm_head_loss_scratch_bytes(desc, False), A.adapm_head_loss_scratch_bytes(desc, True)
+    at = dict(hidden=10 * P, weight=11 * P, targets=12 * P, loss=13 * P, lse=14 * P)
+    assert _head(desc, scratch=_Scratch(n, 30 * P), **at) == ECUDA
+    for name, where in at.items():
+        assert _head(desc, scratch=_Scratch(n, where), **at) == EINVAL, name
+        for vector in ("loss", "lse"):
+            if name != vector:
+                assert _head(desc, scratch=_Scratch(n, 30 * P), **dict(at, **{vector: where + 8})) == EINVAL, (name, vector)
+    at = dict(hidden=10 * P, weight=11 * P, targets=12 * P, lse=14 * P, dloss=15 * P, dhidden=16 * P, dweight=17 * P)
+    assert _head_grad(desc, scratch=_Scratch(m, 30 * P), **at) == ECUDA
+    for name, where in at.items():
+        assert _head_grad(desc, scratch=_Scratch(m, where), **at) == EINVAL, name
+    # a larger buffer than the call needs may hold something else behind what it needs
+    assert _head_grad(desc, scratch=_Scratch(1 << 40, 10 * P - m), **dict(at, hidden=10 * P)) == ECUDA
