@@ -5,7 +5,7 @@ import pytest
 import paper_2510_09103_b200 as A
 import test_gpu_operators as T
 from oracle import operators_oracle as R
-from test_gpu_operators import BF16, F32, GUARD, HALF, TYPE, _backward, _check_backward, _close, _gen, _head_case
+from test_gpu_operators import BF16, F32, GUARD, HALF, TYPE, _backward, _check_backward, _check_forward, _close, _forward, _gen, _head_case
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -57,6 +57,48 @@ def test_head_loss_gradient_of_few_tokens_with_a_target(tokens, valid, dht, dwt)
         got = dh[at] if out is dh else dw
         _close(got, want, bound + want.abs() * HALF[out.dtype] * 1.01 + 1e-30, "dhidden" if out is dh else "dweight")
     assert (dh[ignored] == 0).all()
+
+
+# ---- head loss: logits that overflow, and parts of the vocabulary that are far below the rest --------------
+
+@pytest.mark.parametrize("dht", [BF16, F32])
+@pytest.mark.parametrize("below", [[(0, 16)], [(128, 144)], [(0, 128)], [(256, 512)], [(0, 16), (128, 256), (384, 500)], [(16, 500)], [(1, 500)]])
+def test_head_loss_where_logits_are_minus_infinity(below, dht):
+    """Products of -1e20 and 1e20 overflow: those logits are -inf, their tokens' losses are those of the rest of the vocabulary,
+    and their weight's rows get no gradient."""
+    tokens, vocab, width = 70, 500, 64
+    hidden, _, weight, _, targets = _head_case(tokens, vocab, width)
+    hidden[:, 0], weight[:, 0] = 1e20, 0
+    rest = torch.ones(vocab, dtype=torch.bool, device="cuda")
+    for a, b in below:
+        weight[a:b] = 0
+        weight[a:b, 0] = -1e20
+        rest[a:b] = False
+    left = rest.nonzero()[:, 0]
+    targets = left[torch.randint(0, len(left), (tokens,), generator=_gen(3), device="cuda")]
+    loss, lse = _forward(hidden, weight, targets)
+    h, w = hidden.clone(), weight[left]
+    h[:, 0] = 0                                          # (times a column of zeros)
+    place = torch.searchsorted(left, targets)
+    _check_forward(h, w, place, loss, lse)
+    lse = R.head_loss(h, w, place)[1].float()
+    dh, dw = _backward(hidden, weight, targets, lse, None, 1.0, dht, BF16)
+    assert (dw[~rest] == 0).all()
+    # column 0 apart: there a gradient of (about) nothing meets 1e20
+    _check_backward(h[:, 1:].contiguous(), w[:, 1:].contiguous(), place, lse, dh[:, 1:], dw[left][:, 1:])
+
+
+@pytest.mark.parametrize("low", [(0, 16), (128, 144), (256, 300), (384, 500), (0, 128)])
+def test_head_loss_where_the_first_logits_of_a_part_are_far_below_the_rest(low):
+    """The sum of exponentials starts from the greatest of 16 logits; here the others are up to 2^184 times larger."""
+    tokens, vocab, width = 70, 500, 64
+    hidden, _, weight, _, targets = _head_case(tokens, vocab, width)
+    hidden[:, 0], weight[:, 0] = 8, 0
+    weight[low[0]:low[1], 0] = -16
+    loss, lse = _forward(hidden, weight, targets, label_smoothing=0.1)
+    _check_forward(hidden, weight, targets, loss, lse, smooth=0.1)
+    dh, dw = _backward(hidden, weight, targets, lse, None, 1.0, F32, F32, label_smoothing=0.1)
+    _check_backward(hidden, weight, targets, lse, dh, dw, smooth=0.1)
 
 
 # ---- matrices side by side in one buffer ------------------------------------------------------------------
