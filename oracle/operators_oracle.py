@@ -38,6 +38,20 @@ def keep_mask(rows: int, cols: int, p: float, seed: int, offset: int) -> torch.T
     return mask
 
 
+def keep_mask_wide(rows: int, cols: int, p: float, seed: int, offset: int, device="cpu") -> torch.Tensor:
+    """The same for large sizes: all counters at once in 64-bit tensors, whose products keep the lower 64 bits."""
+    low, groups = 0xFFFFFFFF, (cols + 7) // 8
+    q = torch.arange(rows * groups, device=device)
+    c = [q & low, q >> 32, torch.full_like(q, offset & low), torch.full_like(q, offset >> 32)]
+    k = [seed & low, seed >> 32]
+    for _ in range(10):
+        a, b = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
+        c = [(b >> 32) & low ^ c[1] ^ k[0], b & low, (a >> 32) & low ^ c[3] ^ k[1], a & low]
+        k = [(k[0] + 0x9E3779B9) & low, (k[1] + 0xBB67AE85) & low]
+    halves = torch.stack([c[j // 2] >> (16 * (j % 2)) & 0xFFFF for j in range(8)], 1)
+    return halves.view(rows, 8 * groups)[:, :cols] >= least_kept(p)
+
+
 def drop(x: torch.Tensor, keep, p: float) -> torch.Tensor:
     least = least_kept(p)
     if least == 0:

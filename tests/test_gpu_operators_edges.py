@@ -5,7 +5,7 @@ import pytest
 import paper_2510_09103_b200 as A
 import test_gpu_operators as T
 from oracle import operators_oracle as R
-from test_gpu_operators import BF16, F32, GUARD, HALF, TYPE, _backward, _check_backward, _check_forward, _close, _forward, _gen, _head_case
+from test_gpu_operators import BF16, F32, GUARD, HALF, TYPE, _backward, _check_backward, _check_forward, _close, _forward, _gen, _head_case, _rows
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -157,3 +157,80 @@ def test_head_gradients_directly_behind_a_view_of_their_operands():
     scratch = torch.empty(A.adapm_head_loss_scratch_bytes(d, True), dtype=torch.uint8, device="cuda")
     A.adapm_head_loss_backward(d, h, weight, targets, lse, None, 1.0, out, None, scratch)
     assert torch.equal(out, dh) and torch.equal(h, hidden)
+
+
+# ---- RMS norm: every form of its kernels with the branch's dropout ----------------------------------------
+
+DROP_SIZES = [  # rows, cols, pitch added, shift of the buffers in elements
+    (2400, 64, 0, 0), (2400, 248, 8, 0), (2400, 512, 0, 0), (2371, 1024, 0, 0), (2369, 1600, 0, 0), (9, 1600, 0, 0), (9, 9000, 0, 0), (5, 20000, 8, 0),
+    (2400, 333, 0, 1), (7, 9000, 0, 1), (2400, 1001, 0, 0), (2400, 255, 0, 8), (20, 1001, 0, 0), (9, 9001, 0, 0), (2400, 769, 0, 0),
+    (1200, 8195, 0, 0), (1300, 2056, 3, 0), (5000, 41, 0, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols,pad,shift", DROP_SIZES)
+def test_rmsnorm_with_dropout_in_every_form(dtype, rows, cols, pad, shift):
+    g = _gen(rows + 5 * cols)
+    ld = cols + pad
+    x, xb = _rows(g, rows, cols, dtype, ld, shift)
+    r, _ = _rows(g, rows, cols, dtype, ld + 8, shift, std=3.0)
+    w = (1 + 0.2 * torch.randn(cols, generator=g, device="cuda")).to(dtype)
+    p, seed, offset = 0.25, 0x77_12345678, (1 << 33) + 6
+    keep = R.keep_mask_wide(rows, cols, p, seed, offset, "cuda")
+    x[~keep] = float("nan")                            # what is dropped reaches nothing
+    (s, sb), (y, yb) = (_rows(g, rows, cols, dtype, ld, shift, 0.0) for _ in range(2))
+    rstd = torch.empty(rows, device="cuda")
+    d = A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[dtype], 1e-5, drop_p=p, seed=seed, offset=offset, x_ld=ld, residual_ld=ld + 8, sum_ld=ld, y_ld=ld)
+    A.adapm_rmsnorm_forward(d, x, r, w, s, y, None, None, rstd)
+    ws, wr, wy = R.rmsnorm(x, r, w, 1e-5, keep, p)
+    fp = (64 + 15 + 8) * 2.0**-24
+    most = R.drop(x.double(), keep, p).abs() + r.double().abs()          # the product and the sum are rounded to fp32 before the last rounding
+    sums = (most.square().sum(1) / ws.square().sum(1)).sqrt()
+    _close(s, ws, ws.abs() * HALF[dtype] * 1.01 + most * 2.0**-23, "sum")
+    _close(rstd, wr, wr * (fp + sums * 2.0**-22), "rstd")
+    _close(y, wy, wy.abs() * (HALF[dtype] * 1.01 + fp + sums[:, None] * 2.0**-22 + 2.0**-22) + most * 2.0**-22 * wr[:, None] * w.double().abs(), "y")
+    for m, b in ((s, sb), (y, yb)):
+        T._guards_stand(m, b)
+    # its gradient: the same mask
+    dy, _ = _rows(g, rows, cols, dtype, ld, shift)
+    dsum, _ = _rows(g, rows, cols, dtype, ld, shift)
+    (dres, db), (dx, dxb) = _rows(g, rows, cols, dtype, ld + 8, shift, 0.0), _rows(g, rows, cols, dtype, ld, shift, 0.0)
+    dw = torch.empty(cols, device="cuda")
+    scratch = torch.empty(A.adapm_rmsnorm_backward_scratch_bytes(d), dtype=torch.uint8, device="cuda")
+    A.adapm_rmsnorm_backward(d, dy, dsum, s, rstd, w, dres, dx, dw, A.TYPE_F32, False, scratch)
+    want, wdx, wdw = R.rmsnorm_grad(dy, dsum, s, rstd, w, keep, p)
+    xh, dyw = s.double() * rstd.double()[:, None], dy.double() * w.double()
+    inner = (dyw * xh).abs().mean(1, keepdim=True)
+    bound = rstd.double()[:, None] * (dyw.abs() * 2.0**-21 + xh.abs() * inner * (fp + 2.0**-21)) + dsum.double().abs() * 2.0**-23
+    _close(dres, want, bound + want.abs() * HALF[dtype] * 1.01, "dresidual")
+    _close(dx, wdx, 4 / 3 * bound * 1.01 + wdx.abs() * (HALF[dtype] * 1.01 + 2.0**-22), "dx")
+    assert (dx[~keep] == 0).all()
+    _close(dw, wdw, (dy.double() * xh).abs().sum(0) * ((rows / 100 + 64 + 8) * 2.0**-24), "dweight")
+    for m, b in ((dres, db), (dx, dxb)):
+        T._guards_stand(m, b)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols,shift", [(2400, 512, 0), (2369, 1600, 0), (9, 9000, 0), (5, 1000, 1), (2400, 1001, 0)])
+@pytest.mark.parametrize("group", [0, 128])
+def test_rmsnorm_with_dropout_in_8_bits(dtype, rows, cols, shift, group):
+    """The scales and values are those of y as the plain form has it."""
+    g = _gen(rows * 3 + cols)
+    x, _ = _rows(g, rows, cols, dtype, cols, shift)
+    r, _ = _rows(g, rows, cols, dtype, cols, shift)
+    w = torch.ones(cols, dtype=dtype, device="cuda")
+    keep = R.keep_mask_wide(rows, cols, 0.1, 3, 4, "cuda")
+    q, scales = torch.empty(rows, cols, dtype=torch.uint8, device="cuda"), torch.empty(rows, -(-cols // group) if group else 1, device="cuda")
+    A.adapm_rmsnorm_forward(A.rmsnorm_desc(rows, cols, TYPE[dtype], TYPE[dtype], 1e-5, drop_p=0.1, seed=3, offset=4, q8_group=group),
+                            x, r, w, None, None, q, scales, None)
+    ws, wr, wy = R.rmsnorm(x, r, w, 1e-5, keep, 0.1)
+    most = R.drop(x.double(), keep, 0.1).abs() + r.double().abs()
+    sums = (most.square().sum(1) / ws.square().sum(1)).sqrt()[:, None]
+    fp = (64 + 15 + 8) * 2.0**-24 + 2.0**-21 + sums * 2.0**-22
+    want = R.quantize_scales(wy, group)
+    absolute = most * 2.0**-22 * wr[:, None]
+    per = scales.double().repeat_interleave(group or cols, 1)[:, :cols]
+    _close(scales, want, want * fp + absolute.amax(1, keepdim=True) / 448, "scales")
+    # e4m3: half a step is 2^-4 of the value, and 2^-10 below the smallest normal number
+    _close(q.view(torch.float8_e4m3fn).double() * per, wy, wy.abs() * (2.0**-4 + 2 * fp) + per * 2.0**-10 + 2 * absolute.amax(1, keepdim=True), "y8")

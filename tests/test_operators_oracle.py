@@ -35,6 +35,12 @@ def test_dropout_keeps_the_share_it_says():
     assert not torch.equal(R.keep_mask(8, 64, 0.5, 7, 1), R.keep_mask(8, 64, 0.5, 7, 2))
 
 
+def test_the_mask_made_at_once_is_the_mask_made_element_by_element():
+    for rows, cols, p, seed, offset in ((1, 1, 0.5, 0, 0), (7, 33, 0.3, 0x1234567_89ABCDEF, (1 << 40) + 3), (64, 64, 0.1, 2**64 - 1, 2**63 - 1)):
+        assert torch.equal(R.keep_mask_wide(rows, cols, p, seed, offset), R.keep_mask(rows, cols, p, seed, offset))
+    assert R.keep_mask_wide(4, 20, 0.0, 7, 1).all() and not R.keep_mask_wide(4, 20, 1.0, 7, 1).any()
+
+
 def test_rmsnorm_is_torchs_and_its_gradient_autograds():
     g = _gen(1)
     x, res, w = torch.randn(5, 37, generator=g, dtype=D), torch.randn(5, 37, generator=g, dtype=D), torch.randn(37, generator=g, dtype=D)
