@@ -295,9 +295,9 @@ int adapm_group_meansq_static(const void* g, int32_t grad_dtype, int64_t n_group
  *
  * What stands between a decoder's last layers and the gradients that adapm_step reads: the dropout of a
  * branch, the RMS norm with the residual's addition, and the output head's loss over the vocabulary, each
- * with its gradient.  Their weights are read where the step keeps them (the bf16 copy set by
- * adapm_set_shadow_params, or params, at the block's offset), and the gradients of those weights are
- * written, or added, where adapm_step reads them (grads, at the block's offset).
+ * with its gradient.  Their weights are read where the step keeps them (the head's in bf16 alone: the copy set by
+ * adapm_set_shadow_params, at the block's offset; the norm's there or, as fp32, in params), and the gradients of
+ * those weights are written, or added, where adapm_step reads them (grads, at the block's offset).
  *
  * They need no context.  Every call is asynchronous on `stream`, allocates nothing, never synchronises and
  * may be captured into a graph.  `stream` must belong to the current device, and every buffer must be memory
@@ -329,10 +329,11 @@ int adapm_dropout(const void* x, const void* residual, void* y, int32_t dtype, i
 /*
  * RMS norm of a residual stream:
  *   s = residual + drop(x)    rstd = 1 / sqrt(mean(s^2) + eps)    y = s rstd w
- * Arithmetic in fp32; s enters the statistic and the output unrounded and is rounded where `sum` is stored.
+ * Arithmetic in fp32; s enters the statistic and the output unrounded and is rounded where `sum` is stored.  mean(s^2) + eps
+ * has to be a normal fp32 number (a row of zeros wants an eps); a row whose sum of s^2 overflows has rstd = 0, y = 0.
  */
 typedef struct {
-  int64_t rows, cols;      /* cols: 1 .. 32768                                                       */
+  int64_t rows, cols;      /* cols: 1 .. 32768; rows below 2^31                                      */
   int64_t x_ld;            /* pitch of x and of its gradient dx                                      */
   int64_t residual_ld;     /* of residual and dresidual                                              */
   int64_t sum_ld;          /* of sum and dsum                                                        */
@@ -398,7 +399,7 @@ size_t adapm_head_loss_scratch_bytes(const adapm_head_loss* d, int32_t backward)
 /*
  * targets [tokens]: int64 on the device.  loss, lse [tokens] fp32 outputs.  A token whose target is ignore_index has
  * loss = lse = 0; one whose target is otherwise outside [0, vocab) has loss = lse = NaN.  The hidden states of both kinds
- * are not read into any product.  tokens = 0 does nothing.
+ * reach no output, whatever they hold.  tokens = 0 does nothing.
  * Errors: ADAPM_EINVAL, ADAPM_EALIGN (16 bytes for matrices, pitches), ADAPM_ERANGE (tokens or vocab above 2^24, hidden above 2^16), ADAPM_EUNSUPPORTED
  * (hidden % 8), ADAPM_ENOWORKSPACE, ADAPM_ECUDA.
  */

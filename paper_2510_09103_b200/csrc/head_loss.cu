@@ -11,8 +11,9 @@
 //   logits -> g, rounded, into one of two buffers of a piece       backward, piece i + 1
 //   g W and g^T h -> dh (summed over the pieces in fp32) and dW    backward, piece i, in the same launch
 // The three kinds of items of a launch do not depend on one another, so that the many short logits items fill what the long
-// ones of the two gradients leave at the end.  Tokens without a target are taken out first (head_prepare_kernel): they cost
-// nothing, and whatever their hidden states hold (a padded batch's may be NaN) reaches neither gradient.
+// ones of the two gradients leave at the end.  Tokens without a target are taken out first (head_prepare_kernel): no product is made
+// for them, and whatever their hidden states hold (a padded batch's may be NaN) reaches neither gradient.  A forward call of at most
+// a tile of tokens leaves them in: no row's loss depends on another row, and theirs are replaced at the end.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -230,8 +231,8 @@ __device__ __forceinline__ float cut_row(float* z, int n) {
 
 // What bounds it: the tensor cores, and with them the power cap, where there are a few hundred tokens or more.  8192 x 50257 x 1600
 // forward 0.95 ms = 1.38 PFLOP/s (cuBLAS sustains 1.38 on this card, 1.62 in a burst), both gradients 3.25 to 3.4 ms = 1.16 to
-// 1.22, with half the tokens of 8192 x 128256 x 4096 10.0 to 10.3 ms = 1.25 to 1.29; tensor pipe 83 % active in the forward
-// launch, 76 to 80 % in those of the gradients, DRAM 10 and 30 %.  With few tokens the weight's way from memory and back (100 tokens of
+// 1.22, with half the tokens of 8192 x 128256 x 4096 10.0 to 10.3 ms = 1.25 to 1.29; tensor pipe 82 % active in the forward
+// launch, 76 to 78 % in those of the gradients, DRAM 10 and 30 %.  With few tokens the weight's way from memory and back (100 tokens of
 // 128256 x 4096: both gradients 0.98 ms for 3.2 GB), and below a few ten microseconds the launches themselves.  With D = 256 the
 // exponentials: a tile of 256 x 256 is multiplied in 2 thousand cycles, and its epilogue takes 4 (2 of them the pipe that
 // makes 16 exponentials a cycle).
@@ -464,7 +465,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         // p = exp(z - lse) = 2^(z log2(e) - k) 2^(k - lse log2(e)) with k whole: the first exponent is one multiply-add
         // with one rounding, the second factor belongs to the row
         const float k = rintf(lse * kLog2e);
-        const float rest = fmaf(lse, kLog2e, -k) + lse * 1.925963033500e-8f;       // log2(e) - fp32(log2(e))
+        const float rest = fmaf(lse, kLog2e, -k) + lse * (float)(1.44269504088896340736 - (double)kLog2e);
         const float up = dl * ex2(-rest) * fmaf(2.f * a.z_loss, lse, 1.f);
         const float down = dl * (a.smooth / (float)a.vocab), at_y = dl * (1.f - a.smooth);
         const int n = row < tv ? a.vocab - a.g_begin - n0 - 128 * grp : 0;            // columns that exist

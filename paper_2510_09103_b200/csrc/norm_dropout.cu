@@ -3,8 +3,10 @@
 //   s = residual + drop(x)      rstd = 1 / sqrt(mean(s^2) + eps)      y = s rstd w      q = e4m3(y 448 / amax|y|)
 //   xh = s rstd    ds = rstd (dy w - xh mean(dy w xh)) + dsum    dx = drop(ds)    dw = sum over rows of dy xh
 //
-// All three read and write every element once and are bound by HBM; a row is held in registers between its reduction and its
-// output (up to 32768 columns), in chunks of eight elements: one 16-byte access in bf16, one counter of the generator.
+// Every element is read and written once (the norm's gradient reads rows above 8192 columns twice); a row is held in registers
+// between its reduction and its output (up to 32768 columns), in chunks of eight elements: one 16-byte access in bf16, one
+// counter of the generator.  Dropout is bound by HBM, the norm and its gradient by issue slots and by the reduction between a
+// row's loads and its stores; odd widths by the two blocks of the generator that a chunk takes.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -85,7 +87,6 @@ __device__ __forceinline__ typename Elem<T>::raw8 fetch8(const T* row, const Spa
 }
 template <int FORM>
 __device__ __forceinline__ void load_weight8(const void* w, int f32, const Span& s, float* x) {      // (w is aligned, the windows of a row are not)
-  constexpr int kForm = FORM == VEC ? VEC : FORM;
   if (FORM == SHIFTED) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -94,8 +95,8 @@ __device__ __forceinline__ void load_weight8(const void* w, int f32, const Span&
     }
     return;
   }
-  if (f32) Elem<float>::unpack(fetch8<kForm>(static_cast<const float*>(w), s), x);
-  else Elem<uint16_t>::unpack(fetch8<kForm>(static_cast<const uint16_t*>(w), s), x);
+  if (f32) Elem<float>::unpack(fetch8<FORM>(static_cast<const float*>(w), s), x);
+  else Elem<uint16_t>::unpack(fetch8<FORM>(static_cast<const uint16_t*>(w), s), x);
 }
 template <int FORM, typename T>
 __device__ __forceinline__ void store8(T* row, const Span& s, const float* x) {
@@ -762,8 +763,10 @@ extern "C" int adapm_rmsnorm_backward(const adapm_rmsnorm* d, const void* dy, co
                   d->rows, d->cols, form);
   if (rc != ADAPM_OK) return rc;
   if ((uintptr_t)weight % 16 || slots_of(d->cols, form) > kMaxCols / 8) form = SCALAR;
-  // in short rows the two cut chunks, which go element by element, are most of a warp's work: 49554 x 529 in bf16 167 us by
-  // elements, 227 by windows (in fp32 108 and 90)
+  // In short rows the two cut chunks, which go element by element, fall to one warp and are most of its work; above 96 chunks they
+  // fall to two.  bf16 with dropout, by elements and by windows, us: 49554 x 529 174 and 227, 39420 x 665 157 and 194, 34447 x 761
+  // 143 and 172, 33825 x 775 143 and 128, 29224 x 897 137 and 114, 25575 x 1025 163 and 146 (without dropout 761 columns 114 and
+  // 141, 775 114 and 98).  In fp32 windows are faster there too: 24777 x 529 108 and 90.
   if (form == SHIFTED && d->dtype == ADAPM_TYPE_BF16 && d->cols < 768) form = SCALAR;
   if ((uintptr_t)weight % (uintptr_t)type_bytes(d->weight_dtype) || (uintptr_t)rstd % 4 || (uintptr_t)d->step % 8) return ADAPM_EALIGN;
   const Place pdy = matrix_at(dy, d->rows, d->y_ld, d->cols, eb), pds = matrix_at(dsum, d->rows, d->sum_ld, d->cols, eb),
