@@ -58,7 +58,7 @@ struct HeadArgs {
   float* part_sum;               // forward with smoothing: sum of the logits, same layout
   float* z_target;               // forward: logit of the target of a compacted row
   uint16_t* g;                   // [2 buffers][g_rows][piece]: the planes of the walk one behind the other
-  float* dh_acc;                 // [split_dh][t_pad][hidden], between two pieces and before the splits are added up
+  float* dh_acc;                 // [split_dh][t_pad][hidden], between two pieces and before the splits (and planes) are added up
   float* dw_acc;                 // [split_dw][vocab][hidden], before the splits are added up
   void* dh;
   void* dw;
@@ -290,6 +290,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
       int stage = 0;
       uint32_t phase = 0, issued = 0;
       bool ok = true;
+      const int plane_rows = uniform(walk.plane_rows);          // (read anew for every item: 100 x 128256 x 4096 988 us for 971)
       for (int seq = 0; ok && walk.item_uniform<BACKWARD>(pair, seq, t); ++seq) {
         const CUtensorMap* map;
         int x, y, n_box = 1;                 // K-major: one box of 128 rows, x runs; MN-major: boxes of 64 columns, y runs
@@ -307,7 +308,7 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
         }
         const bool along_y = is_a ? t.cls == CLS_DW : t.cls != CLS_LOGITS;
         const uint32_t bytes = along_y ? (uint32_t)n_box * (kOperandBytes / 2) : kOperandBytes;
-        const int plane_step = is_a && t.cls != CLS_LOGITS ? uniform(walk.plane_rows) : 0;
+        const int plane_step = is_a && t.cls != CLS_LOGITS ? plane_rows : 0;
         const int plane0 = t.k0 / t.per_plane, kx = along_y ? 0 : kStageK, ky = along_y ? kStageK : 0;
         int k = t.k0 - plane0 * t.per_plane;
         y += plane0 * plane_step + k * ky;
@@ -509,8 +510,9 @@ __global__ void __launch_bounds__(kHeadThreads, 1) head_items_kernel(const __gri
       } else {
         const int col0 = n0 + grp * half;
         const bool is_dh = cls == CLS_DH;
-        const bool row_ok = row < (is_dh ? tv : a.o_cols), none = tv == 0;
-        const bool cut = is_dh ? a.split_dh > 1 : a.split_dw > 1;
+        const bool stacked = is_dh && walk.stacked;
+        const bool row_ok = row < (stacked ? 2 * kFewTokens : is_dh ? tv : a.o_cols), none = tv == 0;
+        const bool cut = is_dh ? stacked || a.split_dh > 1 : a.split_dw > 1;
         const bool to_acc = cut || (is_dh && !a.last), from_acc = is_dh && !a.first, from_out = !to_acc && !is_dh && a.accumulate;
         const int64_t out_row = is_dh ? (int64_t)token * a.hidden_ld : (int64_t)(a.o_begin + row) * a.weight_ld;
         float* const acc_row = is_dh ? a.dh_acc + ((int64_t)split * a.t_pad + row) * a.hidden : a.dw_acc + ((int64_t)split * a.vocab + row) * a.hidden;
@@ -730,6 +732,7 @@ struct SumArgs {
     int64_t ld, part_rows;
     int32_t rows;                // of dw; < 0: dh, of the tokens with a target, whose places in `out` are `token`
     int32_t most;                // parts, at most
+    int32_t may_stack;           // dh in bf16
     int32_t f32, accumulate;
   } job[2];
   int32_t hidden, ctas[2];       // ... of each job
@@ -743,7 +746,9 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
   const int job = (int)blockIdx.x < a.ctas[0] ? 0 : 1, cta = (int)blockIdx.x - (job ? a.ctas[0] : 0);
   const SumArgs::Job& j = a.job[job];
   const int tv = a.head[HD_COUNT], rows = j.rows < 0 ? tv : j.rows, vec = a.hidden / 4;
-  const int n = j.rows < 0 ? a.walk->parts_dh : a.walk->parts_dw;
+  // two planes of dh as rows of one tile are summed like parts: the second is kFewTokens rows behind the first
+  const int n = j.rows < 0 ? a.walk->parts_dh : a.walk->parts_dw, planes = j.may_stack && a.walk->stacked ? 2 : 1;
+  if (j.most * planes == 1) return;
   const int64_t part = j.part_rows * a.hidden, total = (int64_t)rows * vec;
   // many parts: the eight warps of a CTA share those of 32 places; few: a thread has a place to itself
   const bool shared = n >= 8;
@@ -756,16 +761,20 @@ __global__ void __launch_bounds__(256) head_sum_kernel(const SumArgs a) {
     const int c = live ? (int)(i - row * vec) * 4 : 0, step = shared ? 8 : 1;
     float x[4] = {0.f, 0.f, 0.f, 0.f};
     const float* p = j.acc + row * a.hidden + c;
-    for (int u = shared ? warp : 0; u < n; u += 4 * step) {
-      float4 v[4];
+    auto add_parts = [&](const float* p) {
+      for (int u = shared ? warp : 0; u < n; u += 4 * step) {
+        float4 v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = __ldcg(reinterpret_cast<const float4*>(p + min(u + k * step, n - 1) * part));      // (the last one again past the end)
+        for (int k = 0; k < 4; ++k) v[k] = __ldcg(reinterpret_cast<const float4*>(p + min(u + k * step, n - 1) * part));      // (the last one again past the end)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const bool counts = u + k * step < n;
-        x[0] += counts ? v[k].x : 0.f; x[1] += counts ? v[k].y : 0.f; x[2] += counts ? v[k].z : 0.f; x[3] += counts ? v[k].w : 0.f;
+        for (int k = 0; k < 4; ++k) {
+          const bool counts = u + k * step < n;
+          x[0] += counts ? v[k].x : 0.f; x[1] += counts ? v[k].y : 0.f; x[2] += counts ? v[k].z : 0.f; x[3] += counts ? v[k].w : 0.f;
+        }
       }
-    }
+    };
+    add_parts(p);
+    if (planes == 2) add_parts(p + (int64_t)kFewTokens * a.hidden);
     if (shared) {
       __syncthreads();
       sums[warp][lane] = make_float4(x[0], x[1], x[2], x[3]);
@@ -1002,16 +1011,18 @@ extern "C" int adapm_head_loss_backward(const adapm_head_loss* d, const void* hi
     a.first = i == 1; a.last = i == plan.n_pieces;
     ADAPM_CUDA(launch_clusters(true, 2, head_items_kernel<true>, 2 * (unsigned)plan.used(i), kHeadThreads, kHeadSmem, s, a));
   }
-  const bool sum_dh = dhidden && l.split_dh > 1, sum_dw = dweight && l.split_dw > 1;
+  // (whether two planes of dh are to be summed is known on the device alone)
+  const bool sum_dh = dhidden && (l.split_dh > 1 || !a.dh_f32), sum_dw = dweight && l.split_dw > 1;
   if (!sum_dh && !sum_dw) return ADAPM_OK;
   SumArgs u;
   std::memset(&u, 0, sizeof(u));
   u.head = a.head; u.walk = (const Walk*)(base + l.walks) + 1; u.token = a.token; u.hidden = a.hidden; u.scale = scale;
   int jobs = 0;
-  if (sum_dh) u.job[jobs++] = {a.dh_acc, dhidden, d->hidden_ld, l.t_pad, -1, a.split_dh, a.dh_f32, 0};
-  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, a.dw_f32, a.accumulate};
+  if (sum_dh) u.job[jobs++] = {a.dh_acc, dhidden, d->hidden_ld, l.t_pad, -1, a.split_dh, !a.dh_f32, a.dh_f32, 0};
+  if (sum_dw) u.job[jobs++] = {a.dw_acc, dweight, d->weight_ld, d->vocab, a.vocab, a.split_dw, 0, a.dw_f32, a.accumulate};
   for (int i = 0; i < jobs; ++i) {
-    const int64_t places = (u.job[i].rows < 0 ? d->tokens : d->vocab) * (d->hidden / 4), each = u.job[i].most >= 8 ? 32 : 256;
+    const int64_t rows = u.job[i].rows >= 0 ? d->vocab : l.split_dh > 1 ? d->tokens : std::min<int64_t>(d->tokens, kFewTokens);
+    const int64_t places = rows * (d->hidden / 4), each = u.job[i].most >= 8 ? 32 : 256;
     u.ctas[i] = (int32_t)std::min<int64_t>((places + each - 1) / each, 4096);
   }
   ADAPM_CUDA(launch_chained(true, head_sum_kernel, (unsigned)(u.ctas[0] + u.ctas[1]), 256, 0, s, u));

@@ -54,8 +54,11 @@ struct HeadItem { int cls, m0, n0, bn, k0, count, per_plane, split; };
 // bf16 numbers that g is carried as into the product of a gradient, by the gradient's type and the tokens with a target.  Three for
 // fp32.  One for bf16, but two where there are few tokens: a token's gradient is mostly its target's element of g, whose rounding
 // is averaged out over the tokens only (a norm's error of one token's gradients was up to 2.4 times that of their own rounding, of 64
-// tokens 1.4 times), and with so few of them the weight's way through memory takes the time.
+// tokens 1.4 times).  With so few of them the planes lie 64 rows apart: dw takes them one stage of K after the other, and dh, in
+// bf16, as the upper and lower half of one CTA's rows, which are summed like parts of K, so that the weight is multiplied once and not
+// twice (100 x 128256 x 4096 with 10 targets: 970 us for 1290; with one plane 940).
 constexpr int kFewTokens = 64;
+static_assert(kFewTokens == kStageK && 2 * kFewTokens == kTile / 2, "a plane of few tokens is a stage of K of dw and half of a CTA's rows of dh");
 __host__ __device__ __forceinline__ int planes_of(bool f32, int with_target) { return f32 ? 3 : with_target <= kFewTokens ? 2 : 1; }
 
 // What the items of a call follow from, beside the number of tokens with a target.
@@ -81,7 +84,8 @@ struct Walk {
   int tv, pairs, n_dh, n_long, n_short, extra, skip, rounds;
   int m_tiles, tiles_dw, base_d, more_d, k_logits, k_dh, k_dw, each_dh, each_dw, all_dh, all_dw, last_group;
   int parts_dh, parts_dw;        // of a gradient, as its sum takes them: those of the call's longest piece
-  int planes, planes_dh, planes_dw, plane_rows;      // of g as it is made, of those that a gradient takes; rows from one to the next
+  int planes, planes_dw, plane_rows;      // of g as it is made, of those that dw takes along K; rows from one to the next
+  int planes_dh, stacked;                 // of those that dh takes along K; 1: it takes two as rows of one tile
   Divisor by_group, by_last, by_d, by_m, by_dw;
 
   __host__ __device__ void make(const Plan& p, int i, int tv_) {
@@ -96,10 +100,11 @@ struct Walk {
     k_logits = (p.hidden + kStageK - 1) / kStageK;
     n_short = m_tiles * nt_v;
     n_dh = n_long = extra = skip = rounds = k_dh = k_dw = each_dh = each_dw = all_dh = all_dw = tiles_dw = parts_dh = parts_dw = 0;
-    planes_dh = planes_of(p.f32_dh, tv);
+    planes_dh = p.f32_dh ? 3 : 1;
     planes_dw = planes_of(p.f32_dw, tv);
-    planes = planes_dh > planes_dw ? planes_dh : planes_dw;
-    plane_rows = m_tiles * kTile;
+    planes = planes_of(p.f32_dh || p.f32_dw, tv);
+    plane_rows = tv <= kFewTokens ? kFewTokens : m_tiles * kTile;
+    stacked = !p.f32_dh && tv <= kFewTokens;
     const int o_cols = p.backward ? p.cols(i - 1) : 0;
     by_dw.set(1);
     if (o_cols == 0) return;
@@ -199,9 +204,8 @@ inline int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   if (backward && (!known_type(d.dhidden_dtype) || !known_type(d.dweight_dtype))) return ADAPM_EINVAL;
   l.t_pad = round_up(d.tokens < 1 ? 1 : d.tokens, kTile);
   l.n_tiles = (d.vocab + kTile - 1) / kTile;
-  // The tokens with a target are counted on the device: with few of them there are two planes of a tile's rows, with more one.
   const bool f32_dh = d.dhidden_dtype == ADAPM_TYPE_F32, f32_dw = d.dweight_dtype == ADAPM_TYPE_F32;
-  l.g_rows = f32_dh || f32_dw ? 3 * l.t_pad : std::max<int64_t>(l.t_pad, 2 * kTile);
+  l.g_rows = f32_dh || f32_dw ? 3 * l.t_pad : l.t_pad;      // (two planes of few tokens lie in the rows of one tile)
   const int64_t most = std::max(kPieceMin, kPieceElems / l.t_pad / kTile * kTile);
   l.n_pieces = (d.vocab + most - 1) / most;
   l.piece = round_up((d.vocab + l.n_pieces - 1) / l.n_pieces, kTile);
@@ -215,7 +219,7 @@ inline int plan(const adapm_head_loss& d, bool backward, Layout& l) {
   l.split_dh = l.split_dw = 1;
   if (backward) {
     const int64_t mt = l.t_pad / kTile, nt_d = (d.hidden + kTile - 1) / kTile, tiles = l.piece / kTile;
-    const int64_t k_dh = (std::min(l.piece, d.vocab) + kStageK - 1) / kStageK * planes_of(f32_dh, (int)d.tokens);
+    const int64_t k_dh = (std::min(l.piece, d.vocab) + kStageK - 1) / kStageK * (f32_dh ? 3 : 1);
     const int64_t k_dw = l.t_pad / kStageK * planes_of(f32_dw, (int)d.tokens);
     const int64_t logits = l.n_pieces > 1 ? mt * tiles * ((d.hidden + kStageK - 1) / kStageK) : 0;
     const int64_t share = std::max<int64_t>(1, (nt_d * (mt * k_dh + tiles * k_dw) + logits) / kPlanPairs);
@@ -236,6 +240,7 @@ inline int plan(const adapm_head_loss& d, bool backward, Layout& l) {
     l.dloss = take(l.t_pad * 4);
     l.g = take(l.n_buf * l.g_rows * l.piece * 2);
     if (l.n_pieces > 1 || l.split_dh > 1) l.dh_acc = take(l.split_dh * l.t_pad * d.hidden * 4);
+    else if (!f32_dh) l.dh_acc = take(2 * kFewTokens * d.hidden * 4);
     if (l.split_dw > 1) l.dw_acc = take(l.split_dw * d.vocab * d.hidden * 4);
   } else {
     l.part = take(2 * l.n_tiles * l.t_pad * 8);

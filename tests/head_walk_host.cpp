@@ -23,7 +23,9 @@ static std::string wrong(const adapm_head_loss& d, bool backward, bool dh, bool 
   Walk first;
   if (backward) first.make(p, 1, tv);
   if (backward && (first.parts_dh < 1 || first.parts_dh > l.split_dh || first.parts_dw < 1 || first.parts_dw > l.split_dw)) return "more parts than the scratch holds";
-  if (backward && (first.plane_rows < tv || (int64_t)first.planes * first.plane_rows > l.g_rows)) return "planes of g that the scratch does not hold";
+  // what is written, and what the boxes of a tile's 256 rows reach
+  if (backward && (first.plane_rows < tv || first.plane_rows % kStageK || (int64_t)first.planes * first.plane_rows > l.g_rows ||
+                   (int64_t)(first.planes_dh - 1) * first.plane_rows + (m > 1 ? m : 1) * kTile > l.g_rows)) return "planes of g that the scratch does not hold";
   for (int i = 0; i < launches; ++i) {
     Walk w;
     w.make(p, i, tv);
@@ -59,8 +61,9 @@ static std::string wrong(const adapm_head_loss& d, bool backward, bool dh, bool 
         at += part.second.first;
       }
       const bool f32 = (is_dh ? d.dhidden_dtype : d.dweight_dtype) == ADAPM_TYPE_F32;
-      const int planes = f32 ? 3 : tv <= 64 ? 2 : 1;
-      if (planes > w.planes) return "more planes of g than are made";
+      // up to 64 tokens dhidden in bf16 takes two planes as rows of one tile, dweight along K
+      const int planes = f32 ? 3 : !is_dh && tv <= 64 ? 2 : 1;
+      if (planes > w.planes || (is_dh && w.stacked != (!f32 && tv <= 64)) || (w.stacked && (w.planes < 2 || m > 1))) return "planes of g";
       if (at != planes * (((is_dh ? before : tv > 0 ? tv : 1) + kStageK - 1) / kStageK)) return "K of a gradient";
       if (is_dh && i == 1 && split != first.parts_dh) return "parts of dhidden that the first piece does not write";
       if (!is_dh && split != first.parts_dw) return "parts of dweight";

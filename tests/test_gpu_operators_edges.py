@@ -59,6 +59,23 @@ def test_head_loss_gradient_of_few_tokens_with_a_target(tokens, valid, dht, dwt)
     assert (dh[ignored] == 0).all()
 
 
+@pytest.mark.parametrize("dht,dwt", [(BF16, BF16), (F32, BF16), (BF16, F32)])
+@pytest.mark.parametrize("tokens,vocab,width,ignored", [(32768, 4400, 72, 0.999), (2000, 40000, 72, 0.98), (100, 262208, 256, 0.5), (130, 262208, 64, 0.6), (8192, 20000, 520, 0.995)])
+def test_head_loss_gradient_of_few_targets_over_pieces_and_parts(tokens, vocab, width, ignored, dht, dwt):
+    """Two planes of few tokens as rows of one tile, summed over several pieces of the vocabulary, cut or not."""
+    hidden, _, weight, _, targets = _head_case(tokens, vocab, width, ignored=ignored, std=0.3)
+    valid = int((targets != -100).sum())
+    assert valid <= 64
+    lse = R.head_loss(hidden, weight, targets)[1].float()
+    into = torch.randn(vocab, width, device="cuda").to(dwt)
+    dh, dw = _backward(hidden, weight, targets, lse, None, 0.25, dht, dwt, into=into)
+    _check_backward(hidden, weight, targets, lse, dh, dw, None, 0.25, into=into)
+    # the tokens by themselves: the same sums, in another order at most
+    at = (targets != -100).nonzero()[:, 0]
+    alone, _ = _backward(hidden[at].contiguous(), weight, targets[at].contiguous(), lse[at].contiguous(), None, 0.25, dht, dwt, want_dw=False)
+    _close(dh[at], alone.double(), alone.double().abs() * 2 * HALF[dht] + alone.double().abs().amax(1, keepdim=True) * 2.0**-12, "alone")
+
+
 # ---- head loss: logits that overflow, and parts of the vocabulary that are far below the rest --------------
 
 @pytest.mark.parametrize("dht", [BF16, F32])
