@@ -76,6 +76,31 @@ def test_head_loss_gradient_of_few_targets_over_pieces_and_parts(tokens, vocab, 
     _close(dh[at], alone.double(), alone.double().abs() * 2 * HALF[dht] + alone.double().abs().amax(1, keepdim=True) * 2.0**-12, "alone")
 
 
+@pytest.mark.parametrize("dht", [BF16, F32])
+def test_head_loss_gradient_captured_with_many_targets_and_replayed_with_few(dht):
+    """How the planes lie and what is summed follows from the targets of the replay, not from those of the capture."""
+    tokens, vocab, width = 700, 5003, 520
+    hidden, _, weight, _, targets = _head_case(tokens, vocab, width)
+    hidden, weight = hidden.contiguous(), weight.contiguous()
+    lse = R.head_loss(hidden, weight, targets)[1].float()
+    d = A.head_loss_desc(tokens, vocab, width, dhidden_dtype=TYPE[dht])
+    scratch = torch.empty(A.adapm_head_loss_scratch_bytes(d, True), dtype=torch.uint8, device="cuda")
+    dh, dw = torch.empty(tokens, width, dtype=dht, device="cuda"), torch.empty_like(weight)
+    A.adapm_head_loss_backward(d, hidden, weight, targets, lse, None, 0.5, dh, dw, scratch)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.adapm_head_loss_backward(d, hidden, weight, targets, lse, None, 0.5, dh, dw, scratch)
+    whole = targets.clone()
+    for n in (700, 1, 64, 65, 0, 256, 257, 33):
+        kept = torch.randperm(tokens, generator=_gen(n), device="cuda")[:n]
+        targets.fill_(-100)
+        targets[kept] = whole[kept]
+        graph.replay()
+        want = _backward(hidden, weight, targets, lse, None, 0.5, dht, BF16)
+        assert torch.equal(dh, want[0]) and torch.equal(dw, want[1]), n
+        _check_backward(hidden, weight, targets, lse, dh, dw, None, 0.5)
+
+
 # ---- head loss: logits that overflow, and parts of the vocabulary that are far below the rest --------------
 
 @pytest.mark.parametrize("dht", [BF16, F32])
