@@ -423,6 +423,90 @@ int adapm_head_loss_backward(const adapm_head_loss* d, const void* hidden, const
  */
 int adapm_head_loss_status(const void* scratch, adapm_stream stream, int32_t* status);
 
+/* ---- Linear layers in 8 bits ----------------------------------------------------------------------------
+ *
+ * A linear layer whose operands are 8-bit codes: the activations are taken to 8 bits once, multiplied in that
+ * form, and kept in it for the backward pass; the weight's codes are made from the bf16 copy that the step
+ * writes (adapm_set_shadow_params, at the block's offset), once per step, and its gradient is written, or added,
+ * where the step reads it.  The conventions are those of the operators around the step.
+ *
+ *   y = (xs x8) (ws w8)^T       dx = dy (ws w8)       dweight = dy^T (xs x8)
+ *
+ * Codes and scales of a matrix x [rows, cols]; a scale stands for a row, or for 128 columns of it (the last
+ * group may be shorter):
+ *   m = max |x| of the group;  top = 127 (int8) or 448 (e4m3)
+ *   scale = max(fl(m / top), 2^-126), fl: to the nearest fp32 number; with `pow2` the least power of two, 2^-126
+ *     or above, that is m / top or more; 1 where m = 0
+ *   code  = x / scale to the nearest code, ties to the even one (the quotient itself is not rounded before)
+ * A group with an infinity or a NaN has scale NaN and codes 0: all of it comes back as NaN.  What a code stands
+ * for is code * scale; where the scale is a power of two that is a bf16 number (above 2^-133).
+ */
+enum { ADAPM_CODE_INT8 = 0, ADAPM_CODE_E4M3 = 1 };
+
+typedef struct {
+  int64_t rows, cols;      /* rows below 2^31, cols 1 .. 2^24                                        */
+  int64_t x_ld, codes_ld;  /* pitches                                                                */
+  int32_t dtype;           /* ADAPM_TYPE_* of x                                                      */
+  int32_t code;            /* ADAPM_CODE_*                                                           */
+  int32_t group;           /* columns per scale: 0 = one scale per row, or 128                       */
+  int32_t pow2;            /* scales are powers of two.  E4M3 has no other form to quant8            */
+} adapm_codes8;
+
+/*
+ * codes [rows, cols] bytes, scales [rows, ceil(cols / group) or 1] fp32.  quant8 makes them from x; dequant8 writes
+ * x = code * scale, computed in fp32 and rounded to x's type, from codes and scales of any origin (the e4m3 output of adapm_rmsnorm_forward
+ * too).  rows = 0 does nothing.
+ * Errors: ADAPM_EINVAL (overlapping buffers among them), ADAPM_ERANGE, ADAPM_EALIGN (a pointer that is no multiple of its
+ * element), ADAPM_EUNSUPPORTED (quant8 to e4m3 without pow2), ADAPM_ECUDA.
+ */
+int adapm_quant8(const adapm_codes8* d, const void* x, void* codes, float* scales, adapm_stream stream);
+int adapm_dequant8(const adapm_codes8* d, const void* codes, const float* scales, void* x, adapm_stream stream);
+
+/*
+ * The products.  x8 [tokens, in_features] and w8 [out_features, in_features] are codes, xs and ws their scales: ws
+ * [out_features] one per row of int8 codes, xs [tokens] or, for the gradient of the weight, also [tokens,
+ * ceil(in_features / 128)], of either kind of codes.  y, dy [tokens, out_features]; dx [tokens, in_features]; dweight
+ * [out_features, in_features].
+ */
+typedef struct {
+  int64_t tokens, out_features, in_features;   /* features: multiples of 8, up to 2^16; tokens up to 2^24    */
+  int64_t x8_ld, w8_ld;    /* pitches of the codes: multiples of 16                                  */
+  int64_t y_ld;            /* of y and dy; this and the next two: multiples of 8                     */
+  int64_t dx_ld;
+  int64_t dweight_ld;
+  int32_t x_code;          /* ADAPM_CODE_* of x8; the forward product takes INT8                     */
+  int32_t x_group;         /* columns per scale of x8: 0 = one scale per token, or 128; the forward product takes 0 */
+  int32_t y_dtype, dx_dtype, dweight_dtype;    /* ADAPM_TYPE_* of the outputs; dy is bf16           */
+  int32_t accumulate;      /* 1: dweight is added to what is there (micro-batches)                   */
+} adapm_linear8;
+
+enum { ADAPM_LINEAR8_FORWARD = 0, ADAPM_LINEAR8_INPUT_GRAD = 1, ADAPM_LINEAR8_WEIGHT_GRAD = 2 };
+size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which);
+
+/*
+ *   forward: y[t, n] = fl(xs[t] ws[n] sum_k x8[t, k] w8[n, k]); the sum is of whole numbers, without rounding.
+ *   input_grad: dx[t, k] = sum_n dy[t, n] ws[n] w8[n, k];  weight_grad: dweight[n, k] = sum_t dy[t, n] xs[t, group of k] x8[t, k].
+ *     code * scale is rounded to bf16 on its way into the product, which changes nothing where the scale is a power of two
+ *     and is off by 2^-8 of it at most where not; sums in fp32.
+ * A scale that is NaN makes its row or column (of dweight: its 128 columns, of dx: all of it) NaN.  tokens = 0: nothing, or
+ * dweight = 0 (unless accumulate).
+ * Errors: ADAPM_EINVAL, ADAPM_EALIGN (16 bytes for matrices, pitches), ADAPM_ERANGE, ADAPM_EUNSUPPORTED (features % 8;
+ * forward with x_code or x_group other than above), ADAPM_ENOWORKSPACE, ADAPM_ECUDA.
+ */
+int adapm_linear8_forward(const adapm_linear8* d, const void* x8, const float* xs, const void* w8, const float* ws, void* y,
+                          void* scratch, size_t scratch_bytes, adapm_stream stream);
+int adapm_linear8_input_grad(const adapm_linear8* d, const void* dy, const void* w8, const float* ws, void* dx,
+                             void* scratch, size_t scratch_bytes, adapm_stream stream);
+int adapm_linear8_weight_grad(const adapm_linear8* d, const void* dy, const void* x8, const float* xs, void* dweight,
+                              void* scratch, size_t scratch_bytes, adapm_stream stream);
+
+/*
+ * Every wait inside the three calls above is bounded.  This call synchronises `stream` and returns ADAPM_EDEVICE and the
+ * status word of the last call that used `scratch` if one of its waits ran out (the output is then not to be used);
+ * 0: fine.
+ */
+int adapm_linear8_status(const void* scratch, adapm_stream stream, int32_t* status);
+
 #ifdef __cplusplus
 }
 #endif

@@ -7,4 +7,7 @@ from .binding import (  # noqa: F401
     TYPE_F32, TYPE_BF16, adapm_rmsnorm, adapm_head_loss, rmsnorm_desc, head_loss_desc, adapm_dropout, adapm_rmsnorm_forward,
     adapm_rmsnorm_backward_scratch_bytes, adapm_rmsnorm_backward, adapm_head_loss_scratch_bytes, adapm_head_loss_forward,
     adapm_head_loss_backward, adapm_head_loss_status,
+    CODE_INT8, CODE_E4M3, LINEAR8_FORWARD, LINEAR8_INPUT_GRAD, LINEAR8_WEIGHT_GRAD, adapm_codes8, adapm_linear8, quant8_desc, linear8_desc,
+    adapm_quant8, adapm_dequant8, adapm_linear8_scratch_bytes, adapm_linear8_forward, adapm_linear8_input_grad,
+    adapm_linear8_weight_grad, adapm_linear8_status,
 )

@@ -16,6 +16,8 @@ MOM_NONE, MOM_FULL, MOM_LOWRANK = 0, 1, 2
 V_ELEMENT, V_BLOCKMEAN = 0, 1
 GRAD_F32, GRAD_BF16 = 0, 1
 TYPE_F32, TYPE_BF16 = 0, 1
+CODE_INT8, CODE_E4M3 = 0, 1
+LINEAR8_FORWARD, LINEAR8_INPUT_GRAD, LINEAR8_WEIGHT_GRAD = 0, 1, 2
 PATH_AUTO, PATH_SIMT, PATH_TENSOR = 0, 1, 2
 STATE_M, STATE_L, STATE_R, STATE_V = 0, 1, 2, 3
 FLAG_NO_PANEL_TEAMS, FLAG_FORCE_PANEL_TEAMS, FLAG_NO_SUMSQ_FOLD, FLAG_CHECK_FINITE = 1, 2, 4, 8
@@ -31,6 +33,8 @@ EXPORTS = (
     "adapm_init_omega_floats", "adapm_init_omega_layout", "adapm_state_init_from_grads",
     "adapm_dropout", "adapm_rmsnorm_forward", "adapm_rmsnorm_backward_scratch_bytes", "adapm_rmsnorm_backward",
     "adapm_head_loss_scratch_bytes", "adapm_head_loss_forward", "adapm_head_loss_backward", "adapm_head_loss_status",
+    "adapm_quant8", "adapm_dequant8", "adapm_linear8_scratch_bytes", "adapm_linear8_forward", "adapm_linear8_input_grad",
+    "adapm_linear8_weight_grad", "adapm_linear8_status",
 )
 
 
@@ -97,6 +101,33 @@ def head_loss_desc(tokens, vocab, hidden, hidden_ld=None, weight_ld=None, ignore
                            ignore_index, label_smoothing, z_loss, dhidden_dtype, dweight_dtype, accumulate)
 
 
+class adapm_codes8(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("x_ld", C.c_int64), ("codes_ld", C.c_int64), ("dtype", C.c_int32),
+                ("code", C.c_int32), ("group", C.c_int32), ("pow2", C.c_int32)]
+
+
+def quant8_desc(rows, cols, dtype=TYPE_BF16, code=CODE_INT8, group=0, pow2=False, x_ld=None, codes_ld=None) -> adapm_codes8:
+    """Pitches that are not given are `cols`."""
+    return adapm_codes8(rows, cols, cols if x_ld is None else x_ld, cols if codes_ld is None else codes_ld, dtype, code, group,
+                        1 if pow2 else 0)
+
+
+class adapm_linear8(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("out_features", C.c_int64), ("in_features", C.c_int64), ("x8_ld", C.c_int64),
+                ("w8_ld", C.c_int64), ("y_ld", C.c_int64), ("dx_ld", C.c_int64), ("dweight_ld", C.c_int64), ("x_code", C.c_int32),
+                ("x_group", C.c_int32), ("y_dtype", C.c_int32), ("dx_dtype", C.c_int32), ("dweight_dtype", C.c_int32),
+                ("accumulate", C.c_int32)]
+
+
+def linear8_desc(tokens, out_features, in_features, x_code=CODE_INT8, x_group=0, y_dtype=TYPE_BF16, dx_dtype=TYPE_BF16,
+                 dweight_dtype=TYPE_BF16, accumulate=False, x8_ld=None, w8_ld=None, y_ld=None, dx_ld=None, dweight_ld=None) -> adapm_linear8:
+    """Pitches that are not given are the matrix's own number of columns."""
+    ld = lambda v, cols: cols if v is None else v  # noqa: E731
+    return adapm_linear8(tokens, out_features, in_features, ld(x8_ld, in_features), ld(w8_ld, in_features), ld(y_ld, out_features),
+                         ld(dx_ld, in_features), ld(dweight_ld, in_features), x_code, x_group, y_dtype, dx_dtype, dweight_dtype,
+                         1 if accumulate else 0)
+
+
 class AdapmError(RuntimeError):
     def __init__(self, code: int, what: str):
         self.code = code
@@ -161,6 +192,13 @@ def load(build_if_missing: bool = True) -> C.CDLL:
         "adapm_head_loss_forward": (C.c_int, [C.POINTER(adapm_head_loss)] + [vp] * 6 + [sz, vp]),
         "adapm_head_loss_backward": (C.c_int, [C.POINTER(adapm_head_loss)] + [vp] * 5 + [C.c_float, vp, vp, vp, sz, vp]),
         "adapm_head_loss_status": (C.c_int, [vp, vp, C.POINTER(i32)]),
+        "adapm_quant8": (C.c_int, [C.POINTER(adapm_codes8)] + [vp] * 4),
+        "adapm_dequant8": (C.c_int, [C.POINTER(adapm_codes8)] + [vp] * 4),
+        "adapm_linear8_scratch_bytes": (sz, [C.POINTER(adapm_linear8), i32]),
+        "adapm_linear8_forward": (C.c_int, [C.POINTER(adapm_linear8)] + [vp] * 6 + [sz, vp]),
+        "adapm_linear8_input_grad": (C.c_int, [C.POINTER(adapm_linear8)] + [vp] * 5 + [sz, vp]),
+        "adapm_linear8_weight_grad": (C.c_int, [C.POINTER(adapm_linear8)] + [vp] * 5 + [sz, vp]),
+        "adapm_linear8_status": (C.c_int, [vp, vp, C.POINTER(i32)]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -405,4 +443,39 @@ def adapm_head_loss_status(scratch, stream=None) -> int:
     rc = load().adapm_head_loss_status(_ptr(scratch), _stream(stream), C.byref(st))
     if rc not in (0, -7):
         _check(rc, "adapm_head_loss_status")
+    return st.value
+
+
+def adapm_quant8(desc: adapm_codes8, x, codes, scales, stream=None) -> None:
+    _check(load().adapm_quant8(C.byref(desc), _ptr(x), _ptr(codes), _ptr(scales), _stream(stream)), "adapm_quant8")
+
+
+def adapm_dequant8(desc: adapm_codes8, codes, scales, x, stream=None) -> None:
+    _check(load().adapm_dequant8(C.byref(desc), _ptr(codes), _ptr(scales), _ptr(x), _stream(stream)), "adapm_dequant8")
+
+
+def adapm_linear8_scratch_bytes(desc: adapm_linear8, which: int) -> int:
+    return load().adapm_linear8_scratch_bytes(C.byref(desc), which)
+
+
+def adapm_linear8_forward(desc: adapm_linear8, x8, xs, w8, ws, y, scratch, stream=None) -> None:
+    _check(load().adapm_linear8_forward(C.byref(desc), _ptr(x8), _ptr(xs), _ptr(w8), _ptr(ws), _ptr(y), _ptr(scratch), _bytes(scratch),
+                                        _stream(stream)), "adapm_linear8_forward")
+
+
+def adapm_linear8_input_grad(desc: adapm_linear8, dy, w8, ws, dx, scratch, stream=None) -> None:
+    _check(load().adapm_linear8_input_grad(C.byref(desc), _ptr(dy), _ptr(w8), _ptr(ws), _ptr(dx), _ptr(scratch), _bytes(scratch),
+                                           _stream(stream)), "adapm_linear8_input_grad")
+
+
+def adapm_linear8_weight_grad(desc: adapm_linear8, dy, x8, xs, dweight, scratch, stream=None) -> None:
+    _check(load().adapm_linear8_weight_grad(C.byref(desc), _ptr(dy), _ptr(x8), _ptr(xs), _ptr(dweight), _ptr(scratch), _bytes(scratch),
+                                            _stream(stream)), "adapm_linear8_weight_grad")
+
+
+def adapm_linear8_status(scratch, stream=None) -> int:
+    st = C.c_int32(0)
+    rc = load().adapm_linear8_status(_ptr(scratch), _stream(stream), C.byref(st))
+    if rc not in (0, -7):
+        _check(rc, "adapm_linear8_status")
     return st.value

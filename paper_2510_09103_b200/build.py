@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libadapm.so")
 SOURCES = ["planner.cpp", "ctx.cu", "stream_kernels.cu", "lowrank_simt.cu", "lowrank_fp32.cu", "lowrank_tc.cu", "static_scratch.cu",
-           "norm_dropout.cu", "head_loss.cu"]
+           "norm_dropout.cu", "head_loss.cu", "quant8.cu", "linear8.cu"]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,50 @@
+// Walks through the items of a product of a linear layer in 8 bits on the host (linear8_plan.h) and says what is wrong with them: null,
+// or a text.
+#include <map>
+#include <string>
+#include <vector>
+
+#include "linear8_plan.h"
+
+namespace adapm {
+void set_error_text(const char*) {}
+}  // namespace adapm
+
+using namespace adapm;
+using namespace adapm::linear8;
+
+static std::string wrong(const adapm_linear8& d, int which) {
+  if (check_desc(d, which) != ADAPM_OK) return "refused";
+  const Plan p = plan_of(d, which);
+  const int64_t k = which == FORWARD ? d.in_features : which == INPUT_GRAD ? d.out_features : d.tokens;
+  const int step = which == FORWARD ? 128 : 64;
+  if ((int64_t)p.stages * step < k || (int64_t)(p.stages - 1) * step >= k) return "stages";
+  if (p.parts > 1 && which == FORWARD) return "a forward product that is cut";
+  if (scratch_bytes(p) < kHeadBytes + (p.parts > 1 ? 4ll * p.parts * p.rows * p.cols : 0)) return "scratch";
+  std::map<std::pair<int, int>, std::vector<Cut>> tiles;
+  Cut t;
+  int n = 0;
+  for (; p.item(n, t); ++n) {
+    if (t.m0 < 0 || t.m0 >= p.rows || t.m0 % kTile || t.n0 < 0 || t.n0 >= p.cols || t.n0 % kTile) return "an item's tile";
+    if (t.bn != kTile && t.bn != kTile / 2) return "an item's columns";
+    if (t.n0 + t.bn < p.cols && t.bn != kTile) return "columns left out";
+    if (t.count < 1 || t.part < 0 || t.part >= p.parts) return "an item's part";
+    auto& of = tiles[{t.m0, t.n0}];
+    const int at = of.empty() ? 0 : of.back().k0 + of.back().count;
+    if (t.k0 != at || t.part != (int)of.size()) return "parts of K that do not follow one another";
+    of.push_back(t);
+  }
+  if (n != p.items || p.item(n, t)) return "the number of items";
+  if ((int64_t)tiles.size() != (int64_t)p.m_tiles * p.n_tiles || (int64_t)p.m_tiles * kTile < p.rows || (int64_t)p.n_tiles * kTile < p.cols) return "tiles left out";
+  for (const auto& of : tiles)
+    if (of.second.back().k0 + of.second.back().count != p.stages || (int)of.second.size() != p.parts) return "K";
+  return "";
+}
+
+extern "C" const char* linear8_plan_wrong(const adapm_linear8* d, int which) {
+  static std::string what;
+  what = wrong(*d, which);
+  return what.empty() ? nullptr : what.c_str();
+}
+
+extern "C" int linear8_parts(const adapm_linear8* d, int which) { return plan_of(*d, which).parts; }
