@@ -4,15 +4,14 @@
 //   input grad   dx[t, k] = sum_n dy[t, n] (ws[n] w8[n, k])           bf16 x codes
 //   weight grad  dw[n, k] = sum_t dy[t, n] (xs[t] x8[t, k])           bf16 x codes
 //
-// The gradients' codes travel as bytes as far as shared memory; there eight warps turn them into bf16 numbers, times their scales,
-// in the order that the tensor cores read (kind::f16, sums in fp32).  The scale stands beside an index of K, so it cannot wait for
-// the end as in the forward product; where it is a power of two, code x scale is a bf16 number and nothing is rounded.
+// The scale of a gradient's codes stands beside an index of K, so it cannot wait for the end as in the forward product: code x scale is
+// made a bf16 number first (which rounds nothing where the scale is a power of two), by a launch of its own, and then multiplied
+// (kind::f16, sums in fp32).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <mutex>
 
-#include "codes.cuh"
 #include "linear8_plan.h"
 #include "tc_engine.cuh"
 #include "tc_host.h"
@@ -25,39 +24,34 @@ using namespace tc;
 
 constexpr int kOperandBytes = 16384;             // of one CTA and stage: 128 rows or columns of an operand, 128 bytes of K (or the reverse)
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kRawBytes = 64 * 128;              // codes of a CTA's half of a stage
 constexpr int kSegLong = 4, kSegShort = 64;      // stages of 64 K between two sums in registers: gradients in fp32, long ones in bf16
 
 template <int OP, bool LONG>
 struct Shape {
   static constexpr bool kGrad = OP != FORWARD;
-  static constexpr int kConvert = !kGrad ? 0 : LONG ? 4 : 8;         // warps that make bf16 numbers of codes
-  static constexpr int kWarps = 12 + kConvert;                      // after four that issue and eight that drain
-  static constexpr int kThreads = 32 * kWarps;
-  static constexpr int kStages = kGrad ? 5 : 6;
-  static constexpr int kRawStages = kGrad ? 6 : 0;
-  static constexpr int kSmem = kStages * kStageBytes + kRawStages * kRawBytes + 1024;
+  static constexpr int kThreads = 384;           // four warps that issue, eight that drain
+  static constexpr int kStages = 6;
+  static constexpr int kSmem = kStages * kStageBytes + 1024;
 };
-// LONG: registers as the four groups of four warps divide those of the launch (the eight that drain keep 128 sums each).
-constexpr int kLongRegs = 128, kLongIssue = 48, kLongConvert = 48, kLongDrain = 208;
-static_assert(kLongIssue + kLongConvert + 2 * kLongDrain <= 4 * kLongRegs, "a block has the registers that it was launched with");
+// LONG: registers of the launch, and as the first four and the other eight warps divide them (the eight keep 128 sums each).
+constexpr int kLongRegs = 168, kLongIssue = 88, kLongDrain = 208;
+static_assert(4 * kLongIssue + 8 * kLongDrain <= 12 * kLongRegs, "a block has the registers that it was launched with");
 
 struct Args {
-  CUtensorMap a, b;              // b: K-major (forward) or the codes as they lie (gradients)
+  CUtensorMap a, b;
   Plan plan;
-  const float* a_scale;          // forward: xs
-  const float* b_scale;          // ws, or xs of the weight's gradient [K][b_groups]
+  const float *a_scale, *b_scale;      // forward: xs, ws
   void* out;
   float* part;                   // [parts][rows][cols], where K is cut
   int32_t* status;
   int64_t out_ld;
-  int32_t k, b_groups, pairs, out_f32, wide, accumulate, seg, e4m3;
+  int32_t pairs, out_f32, wide, accumulate, seg;
 };
 
 template <int OP, bool LONG>
 struct __align__(8) Shared {
   using S = Shape<OP, LONG>;
-  uint64_t full[S::kStages], empty[S::kStages], raw_full[S::kRawStages + 1], raw_empty[S::kRawStages + 1], tfull[2], tempty[2];
+  uint64_t full[S::kStages], empty[S::kStages], tfull[2], tempty[2];
   uint32_t tmem_base;
   int abort;
 };
@@ -76,12 +70,6 @@ __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}" ::"r"(d_tmem), "l"(a_desc),
                  "l"(b_desc), "r"(idesc), "r"(accumulate)
                  : "memory");
-}
-
-// Arrives at the barrier of another CTA of the cluster (address from shared_of) and makes what this thread wrote, or saw written,
-// visible to who waits there.
-__device__ __forceinline__ void mbar_arrive_release_at(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void put4(void* p, const uint32_t* v) { *reinterpret_cast<uint4*>(p) = make_uint4(v[0], v[1], v[2], v[3]); }
@@ -147,19 +135,6 @@ __device__ __forceinline__ void finish16(const Args& a, const Cut& t, int row, i
   store_row16(a.out, at, x, n, a.out_f32, a.wide);
 }
 
-// 16 codes of one row, times its scale, as bf16 numbers: two chunks of 16 bytes.
-template <bool E4M3>
-__device__ __forceinline__ void decode16(const uint4& q, float s, uint32_t* w) {
-  const uint32_t c[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float x[4];
-    unpack4<E4M3>(c[i], x);
-    w[2 * i] = pack_bf16x2_rn(x[0] * s, x[1] * s);
-    w[2 * i + 1] = pack_bf16x2_rn(x[2] * s, x[3] * s);
-  }
-}
-
 // An item's K in segments of even length: how many, and the stages of each but the last.
 __device__ __forceinline__ void segments(int stages, int most, int& n, int& each) {
   n = (stages + most - 1) / most;
@@ -167,8 +142,7 @@ __device__ __forceinline__ void segments(int stages, int most, int& n, int& each
   n = (stages + each - 1) / each;
 }
 
-// Pairs of CTAs (cta_group::2), 256 x 256 tiles.  Warp 0 loads A, warp 2 loads B or the codes, warp 1 issues the MMAs, warps 4 to 11
-// drain the accumulators; gradients have 8 more (LONG: 4) that turn codes into bf16 numbers.
+// Pairs of CTAs (cta_group::2), 256 x 256 tiles.  Warp 0 loads A, warp 2 B, warp 1 issues the MMAs, warps 4 to 11 drain the accumulators.
 // LONG: K in segments that the epilogue adds up in registers, because the tensor cores cut every partial sum off toward zero (a K step of 16 leaves
 // an accumulator up to 2^-23 of itself too small).  For gradients in fp32, and for sums above 16384 terms.
 template <int OP, bool LONG>
@@ -179,17 +153,15 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
   wait_for_previous_kernel();
   const uint32_t rank = cluster_rank();
   uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~(uintptr_t)1023);
-  uint8_t* const raw = ring + S::kStages * kStageBytes;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = (int)(blockIdx.x >> 1);
   volatile int* const abort = &sh.abort;
   int32_t* const status = a.status + pair;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
-      mbar_init(&sh.full[i], S::kGrad ? 1 + 2 * S::kConvert : 2);
+      mbar_init(&sh.full[i], 2);                    // A and B, those of rank 0 for both CTAs
       mbar_init(&sh.empty[i], 1);
     }
-    for (int i = 0; i < S::kRawStages; ++i) { mbar_init(&sh.raw_full[i], 1); mbar_init(&sh.raw_empty[i], S::kConvert); }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 16); }
     sh.abort = 0;
     if (rank == 0) *status = 0;                        // (the cluster barrier below orders it before what either CTA adds)
@@ -210,11 +182,11 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
 
   if (warp < 4) {
     if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLongIssue));
-    if (warp == 0 || (warp == 2 && !S::kGrad)) {
-      // ------------------------------------------------------------------ operands that are multiplied as they lie
+    if (warp == 0 || warp == 2) {
+      // ------------------------------------------------------------------ producers (all lanes run, one issues)
       const bool leader = elect_one(), is_a = warp == 0;
       const uint32_t pair_full = uniform(shared_of(sh.full, 0));
-      constexpr bool kAlongY = OP == WEIGHT_GRAD;      // rows are K: two boxes of 64 columns
+      const bool along_y = is_a ? OP == WEIGHT_GRAD : S::kGrad;      // rows are K: boxes of 64 columns
       constexpr int kStep = OP == FORWARD ? 128 : 64;
       int stage = 0;
       uint32_t phase = 0, issued = 0;
@@ -223,16 +195,18 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         const CUtensorMap* const map = is_a ? &a.a : &a.b;
         const int mine = uniform(is_a ? t.m0 + (int)rank * 128 : t.n0 + (int)rank * (t.bn / 2));
         const int count = uniform(t.count);
+        const bool two = is_a || t.bn > 128;
+        const uint32_t bytes = along_y && !two ? kOperandBytes : 2 * kOperandBytes;
         int k = uniform(t.k0) * kStep;
         for (int left = count; left > 0; --left, k += kStep) {
           if (!mbar_wait_warp<WAIT_PAIR>(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
           uint8_t* const dst = ring + stage * kStageBytes + (is_a ? 0 : kOperandBytes);
           if (leader) {
-            if (rank == 0) mbar_arrive_expect_tx(&sh.full[stage], 2 * kOperandBytes);
+            if (rank == 0) mbar_arrive_expect_tx(&sh.full[stage], bytes);
             const uint32_t bar = pair_full + 8u * (uint32_t)stage;
-            if (kAlongY) {
+            if (along_y) {
               tma_load_box_pair(dst, map, mine, k, bar);
-              tma_load_box_pair(dst + kOperandBytes / 2, map, mine + 64, k, bar);
+              if (two) tma_load_box_pair(dst + kOperandBytes / 2, map, mine + 64, k, bar);
             } else {
               tma_load_box_pair(dst, map, k, mine, bar);
             }
@@ -243,27 +217,6 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         }
       }
       if (!ok) drain_ring<true>(sh.full, stage, phase, issued, S::kStages, rank);
-    } else if (warp == 2) {
-      // ------------------------------------------------------------------ codes, into a ring of their own
-      const bool leader = elect_one();
-      int stage = 0;
-      uint32_t phase = 0, issued = 0;
-      bool ok = true;
-      for (int i = pair; ok && a.plan.item(i, t); i += a.pairs) {
-        const int x = uniform(t.n0 + (int)rank * (t.bn / 2)), count = uniform(t.count);
-        int y = uniform(t.k0) * 64;
-        for (int left = count; left > 0; --left, y += 64) {
-          if (!mbar_wait_warp(&sh.raw_empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
-          if (leader) {
-            mbar_arrive_expect_tx(&sh.raw_full[stage], kRawBytes);
-            tma_load_box(raw + stage * kRawBytes, &a.b, x, y, &sh.raw_full[stage]);
-          }
-          __syncwarp();
-          ++issued;
-          if (++stage == S::kRawStages) { stage = 0; phase ^= 1u; }
-        }
-      }
-      if (!ok) drain_ring<false>(sh.raw_full, stage, phase, issued, S::kRawStages, rank);
     } else if (warp == 1 && rank == 0) {
       // ------------------------------------------------------------------ MMA issuer (all lanes run, one issues)
       const bool leader = elect_one();
@@ -306,66 +259,6 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
           if (ok && leader) mma_commit<true>(&sh.tfull[acc]);
           __syncwarp();
         }
-      }
-    }
-  } else if (S::kGrad && warp >= 12) {
-    if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kLongConvert));
-    // ------------------------------------------------------------------ codes to bf16 numbers: a warp has four rows of K at a time,
-    // eight lanes to a row, 16 codes to a lane
-    constexpr int kPasses = S::kGrad ? 64 / (4 * (S::kConvert ? S::kConvert : 1)) : 1;
-    const int row0 = 4 * (warp - 12) + (lane >> 3), j = lane & 7;
-    const uint32_t pair_full = shared_of(sh.full, 0);
-    int stage = 0, rs = 0;
-    uint32_t phase = 0, raw_phase = 0;
-    bool ok = true;
-    for (int i = pair; ok && a.plan.item(i, t); i += a.pairs) {
-      const int half = t.bn / 2, group = a.b_groups > 1 ? (t.n0 + (int)rank * half) / 128 : 0;
-      const bool live = 16 * j < half && group < a.b_groups;
-      const float* const scale = a.b_scale + group;
-      int k = t.k0 * 64 + row0;
-      float s[kPasses];
-      auto scales = [&]() {
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) {
-          const int at = k + p * 4 * S::kConvert;
-          s[p] = live && at < a.k ? __ldg(scale + (int64_t)at * a.b_groups) : 0.f;
-        }
-      };
-      scales();
-      for (int left = t.count; left > 0; --left) {
-        float now[kPasses];
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) now[p] = s[p];
-        k += 64;
-        if (left > 1) scales();                        // of the next stage
-        if (!mbar_wait_warp(&sh.raw_full[rs], raw_phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
-        uint4 q[kPasses];
-#pragma unroll
-        for (int p = 0; p < kPasses; ++p) q[p] = *reinterpret_cast<const uint4*>(raw + rs * kRawBytes + (row0 + p * 4 * S::kConvert) * 128 + 16 * j);
-        if (!mbar_wait_warp<WAIT_PAIR>(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
-        uint8_t* const dst = ring + stage * kStageBytes + kOperandBytes + (j >> 2) * (kOperandBytes / 2);
-        if (16 * j < half) {
-#pragma unroll
-          for (int p = 0; p < kPasses; ++p) {
-            const int row = row0 + p * 4 * S::kConvert;
-            uint32_t w[8];
-            if (a.e4m3) decode16<true>(q[p], now[p], w);
-            else decode16<false>(q[p], now[p], w);
-            // the 128-byte swizzle; lanes 4 to 7 write their second chunk first, so that eight lanes meet no bank twice
-            const int c = 2 * (j & 3), odd = j >> 2;
-            uint8_t* const line = dst + row * 128;
-            put4(line + ((c + odd) ^ (row & 7)) * 16, odd ? w + 4 : w);
-            put4(line + ((c + 1 - odd) ^ (row & 7)) * 16, odd ? w : w + 4);
-          }
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&sh.raw_empty[rs]);
-          mbar_arrive_release_at(pair_full + 8u * (uint32_t)stage);
-        }
-        if (++rs == S::kRawStages) { rs = 0; raw_phase ^= 1u; }
-        if (++stage == S::kStages) { stage = 0; phase ^= 1u; }
       }
     }
   } else {
@@ -510,10 +403,179 @@ __global__ void __launch_bounds__(256) linear8_sum_kernel(const SumArgs a) {
   }
 }
 
+// ---- few tokens ------------------------------------------------------------------------------------------------------
+// The weight is the operand with 128 rows, the tokens are the columns (up to 256), so that few tokens cost few products, and the
+// CTAs of a cluster take parts of K, whose sums they add up through each other's shared memory: whole numbers, in any order.
+
+struct FewArgs {
+  CUtensorMap w, x;
+  FewPlan plan;
+  const float *xs, *ws;
+  void* y;
+  int32_t* status;
+  int64_t y_ld;
+  int32_t tokens, out, f32;
+};
+
+struct __align__(8) FewShared {
+  uint64_t full[8], empty[8], tfull;
+  uint32_t tmem_base;
+  int abort;
+};
+
+__device__ __forceinline__ int4 load_shared4_at(uint32_t at) {
+  int4 v;
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+
+constexpr int kFewThreads = 256;       // warp 0 loads, warp 1 issues the MMAs, warps 4 to 7 drain the accumulator, all put the parts together
+
+// A CTA puts its share of the features together, a thread four of them, for every few tokens: eight loads of four sums on their way
+// at a time.
+template <int SPLIT>
+__device__ __forceinline__ void few_together(const FewArgs& a, const uint8_t* sums, int rank, int n0, int t0) {
+  constexpr int kShare = 128 / SPLIT, kFours = kShare / 4, kStep = kFewThreads / kFours, kAtOnce = 8 / SPLIT;
+  const int f = rank * kShare + 4 * ((int)threadIdx.x % kFours), n = n0 + f, tokens = min(a.plan.tn, a.tokens - t0);
+  if (n >= a.out) return;
+  const float4 ws = *reinterpret_cast<const float4*>(a.ws + n);
+  uint32_t from[SPLIT];
+#pragma unroll
+  for (int r = 0; r < SPLIT; ++r) {
+    from[r] = smem_u32(sums) + 4u * (uint32_t)f;
+    if (SPLIT > 1) from[r] = shared_of(sums + 4 * f, (uint32_t)r);
+  }
+  for (int t = (int)threadIdx.x / kFours; t < tokens; t += kAtOnce * kStep) {
+    int4 v[kAtOnce][SPLIT];
+    float xs[kAtOnce];
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int at = min(t + u * kStep, tokens - 1);
+      xs[u] = a.xs[t0 + at];
+#pragma unroll
+      for (int r = 0; r < SPLIT; ++r) v[u][r] = load_shared4_at(from[r] + 512u * (uint32_t)at);
+    }
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      if (t + u * kStep >= tokens) continue;
+      int4 sum = v[u][0];
+#pragma unroll
+      for (int r = 1; r < SPLIT; ++r) { sum.x += v[u][r].x; sum.y += v[u][r].y; sum.z += v[u][r].z; sum.w += v[u][r].w; }
+      const float y[4] = {(float)sum.x * xs[u] * ws.x, (float)sum.y * xs[u] * ws.y, (float)sum.z * xs[u] * ws.z, (float)sum.w * xs[u] * ws.w};
+      const int64_t to = (int64_t)(t0 + t + u * kStep) * a.y_ld + n;
+      if (a.f32) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + to) = make_float4(y[0], y[1], y[2], y[3]);
+      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + to) = make_uint2(pack_bf16x2_rn(y[0], y[1]), pack_bf16x2_rn(y[2], y[3]));
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kFewThreads) linear8_few_kernel(const __grid_constant__ FewArgs a) {
+  extern __shared__ uint8_t dyn_smem[];
+  __shared__ FewShared sh;
+  wait_for_previous_kernel();
+  const FewPlan& p = a.plan;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, split = p.split, rank = split > 1 ? (int)cluster_rank() : 0;
+  const int tile = (int)blockIdx.x / split, t_tile = tile / p.n_tiles, n0 = (tile - t_tile * p.n_tiles) * 128, t0 = t_tile * p.tn;
+  const int k0 = p.first(rank), count = p.first(rank + 1) - k0, bytes = 16384 + 128 * p.tn;
+  uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~(uintptr_t)1023);
+  volatile int* const abort = &sh.abort;
+  int32_t* const status = a.status + blockIdx.x;
+  const uint32_t tmem_cols = p.tn <= 32 ? 32 : p.tn <= 64 ? 64 : p.tn <= 128 ? 128 : 256;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < p.ring; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+    mbar_init(&sh.tfull, 1);
+    sh.abort = 0;
+    *status = 0;
+    mbar_fence_init();
+  }
+  if (blockIdx.x == 0)
+    for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += kFewThreads) a.status[i] = 0;      // words of no CTA
+  if (warp == 1) {
+    tmem_alloc(&sh.tmem_base, tmem_cols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = sh.tmem_base;
+
+  if (warp == 0) {
+    const bool leader = elect_one();
+    int stage = 0;
+    uint32_t phase = 0, issued = 0;
+    bool ok = true;
+    for (int i = 0; i < count; ++i) {
+      if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+      if (leader) {
+        uint8_t* const dst = ring + stage * bytes;
+        mbar_arrive_expect_tx(&sh.full[stage], (uint32_t)bytes);
+        tma_load_box(dst, &a.w, (k0 + i) * 128, n0, &sh.full[stage]);
+        tma_load_box(dst + 16384, &a.x, (k0 + i) * 128, t0, &sh.full[stage]);
+      }
+      __syncwarp();
+      ++issued;
+      if (++stage == p.ring) { stage = 0; phase ^= 1u; }
+    }
+    if (!ok) drain_ring<false>(sh.full, stage, phase, issued, p.ring, 0);
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    int stage = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    const uint32_t ring0 = uniform(smem_u32(ring)), d = uniform(tmem_base), dhi = desc_hi(), idesc = uniform(i8_idesc(p.tn, 128));
+    for (int i = 0; i < count; ++i) {
+      if (!mbar_wait_warp(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t slot = ring0 + (uint32_t)(stage * bytes), alo = desc_lo(slot, 16u), blo = desc_lo(slot + 16384, 16u);
+      if (leader) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mma_i8<false>(d, desc_join(alo + q * 2u, dhi), desc_join(blo + q * 2u, dhi), idesc, i || q ? 1u : 0u);
+        mma_commit(&sh.empty[stage]);
+      }
+      __syncwarp();
+      if (++stage == p.ring) { stage = 0; phase ^= 1u; }
+    }
+    if (ok && leader) mma_commit(&sh.tfull);
+    __syncwarp();
+  } else if (warp >= 4) {
+    // this CTA's sums [tokens][128], over the ring: all that was in it has been multiplied
+    bool ok = true;
+    if (lane == 0) ok = mbar_wait(&sh.tfull, 0, abort, status, ST_WAIT_TMEM_FULL, kWaitSpinDefault);
+    ok = __shfl_sync(0xffffffffu, ok, 0);
+    tc_fence_after();
+    if (ok) {
+      int* const sums = reinterpret_cast<int*>(ring) + 32 * (warp & 3) + lane;
+      for (int c = 0; c < p.tn; c += 16) {
+        float v[16];
+        tmem_ld16(tmem_base + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)c, v);
+        tmem_ld_wait();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sums[(c + e) * 128] = __float_as_int(v[e]);
+      }
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (split > 1) cluster_sync();
+
+  if (split == 1) few_together<1>(a, ring, rank, n0, t0);
+  else if (split == 2) few_together<2>(a, ring, rank, n0, t0);
+  else if (split == 4) few_together<4>(a, ring, rank, n0, t0);
+  else few_together<8>(a, ring, rank, n0, t0);
+
+  __syncwarp();
+  if (split > 1) cluster_sync();      // no CTA leaves while another may still read its sums
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, tmem_cols);
+  }
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------
 
-// A row-major matrix of bytes in boxes of 128 columns x box_rows rows, with the 128-byte swizzle or as it lies.
-bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, bool swizzle) {
+// A row-major matrix of bytes in boxes of 128 columns x box_rows rows, with the 128-byte swizzle.
+bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {cols, rows};
@@ -521,8 +583,7 @@ bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t co
   const cuuint32_t box[2] = {128, box_rows};
   const cuuint32_t estr[2] = {1, 1};
   return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int OP, bool LONG>
@@ -558,6 +619,7 @@ int pairs_of(int device, int* pairs) {
   if (!known[device]) {
     int sms = 0;
     ADAPM_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
+    ADAPM_CUDA(cudaFuncSetAttribute(linear8_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem + 1024));
     int n = std::min(sms / 2, (int)kMostWords);
     int rc = allow<FORWARD, false>(&n, sms);
     if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, false>(&n, sms);
@@ -612,25 +674,25 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
   Args a;
   std::memset(&a, 0, sizeof(a));
   a.plan = plan;
-  a.k = (int32_t)(weight ? d.tokens : d.out_features);
-  const int64_t codes_ld = weight ? d.x8_ld : d.w8_ld;
-  if (!encode_bf16_matrix(&a.a, dy, d.tokens, d.out_features, d.y_ld, weight ? 64 : 128) ||
-      !encode_bytes(&a.b, codes, a.k, d.in_features, codes_ld, 64, false)) {
+  void* const decoded = (char*)scratch + kHeadBytes;
+  adapm_codes8 q;
+  q.rows = weight ? d.tokens : d.out_features; q.cols = d.in_features; q.x_ld = d.in_features; q.codes_ld = weight ? d.x8_ld : d.w8_ld;
+  q.dtype = ADAPM_TYPE_BF16; q.code = weight ? d.x_code : ADAPM_CODE_INT8; q.group = weight ? d.x_group : 0; q.pow2 = 0;
+  if (!encode_bf16_matrix(&a.a, dy, d.tokens, d.out_features, d.y_ld, weight ? 64 : 128) || !encode_bf16_matrix(&a.b, decoded, q.rows, q.cols, q.cols, 64)) {
     set_error_text("cuTensorMapEncodeTiled failed for a gradient of linear8");
     return ADAPM_ECUDA;
   }
-  a.b_scale = scales;
-  a.b_groups = weight && d.x_group ? (int32_t)((d.in_features + 127) / 128) : 1;
   a.out = out; a.out_ld = out_ld;
   a.status = (int32_t*)scratch;
-  a.part = (float*)((char*)scratch + kHeadBytes);
+  a.part = (float*)((char*)scratch + plan.part_at);
   a.out_f32 = out_dtype == ADAPM_TYPE_F32;
   a.wide = (uintptr_t)out % 32 == 0 && (a.out_f32 || out_ld % 16 == 0);
   a.accumulate = weight && d.accumulate != 0;
-  a.e4m3 = weight && d.x_code == ADAPM_CODE_E4M3;
   a.pairs = std::min(pairs, plan.items);
   a.seg = a.out_f32 ? kSegLong : kSegShort;
   const bool is_long = a.out_f32 || plan.each > kShortStages;
+  const int rc = launch_dequant8(q, codes, scales, decoded, s);
+  if (rc != ADAPM_OK) return rc;
   ADAPM_CUDA(weight ? (is_long ? launch<WEIGHT_GRAD, true>(a, s) : launch<WEIGHT_GRAD, false>(a, s))
                     : (is_long ? launch<INPUT_GRAD, true>(a, s) : launch<INPUT_GRAD, false>(a, s)));
   if (plan.parts == 1) return ADAPM_OK;
@@ -648,7 +710,7 @@ using namespace adapm;
 
 extern "C" size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which) {
   if (!d || check_desc(*d, which) != ADAPM_OK) return 0;
-  return (size_t)scratch_bytes(plan_of(*d, which));
+  return (size_t)plan_of(*d, which).bytes;
 }
 
 extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, const float* xs, const void* w8, const float* ws, void* y,
@@ -660,18 +722,33 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
   int device, pairs;
   rc = check_buffers({codes_at(x8, d->tokens, d->x8_ld, d->in_features), floats_at(xs, d->tokens, 4), codes_at(w8, d->out_features, d->w8_ld, d->in_features),
                       floats_at(ws, d->out_features, 16)},
-                     bf16_or_f32(y, d->tokens, d->y_ld, d->out_features, d->y_dtype), scratch, scratch_size, scratch_bytes(plan),
+                     bf16_or_f32(y, d->tokens, d->y_ld, d->out_features, d->y_dtype), scratch, scratch_size, plan.bytes,
                      "adapm_linear8_forward: the output or the scratch overlaps another buffer", &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
   if (rc != ADAPM_OK) return rc;
+  const FewPlan few = few_plan_of(d->tokens, d->out_features, d->in_features, 128);
+  if (few_is_faster(few, plan)) {
+    FewArgs f;
+    std::memset(&f, 0, sizeof(f));
+    f.plan = few;
+    if (!encode_bytes(&f.w, w8, d->out_features, d->in_features, d->w8_ld, 128) || !encode_bytes(&f.x, x8, d->tokens, d->in_features, d->x8_ld, (uint32_t)few.tn)) {
+      set_error_text("cuTensorMapEncodeTiled failed for linear8");
+      return ADAPM_ECUDA;
+    }
+    f.xs = xs; f.ws = ws; f.y = y; f.y_ld = d->y_ld; f.status = (int32_t*)scratch;
+    f.tokens = (int32_t)d->tokens; f.out = (int32_t)d->out_features; f.f32 = d->y_dtype == ADAPM_TYPE_F32;
+    ADAPM_CUDA(launch_clusters(true, (unsigned)few.split, linear8_few_kernel, (unsigned)few.ctas, kFewThreads, (size_t)few.ring * few_stage_bytes(few.tn) + 1024,
+                               (cudaStream_t)stream, f));
+    return ADAPM_OK;
+  }
   Args a;
   std::memset(&a, 0, sizeof(a));
   a.plan = plan;
-  if (!encode_bytes(&a.a, x8, d->tokens, d->in_features, d->x8_ld, 128, true) || !encode_bytes(&a.b, w8, d->out_features, d->in_features, d->w8_ld, 128, true)) {
+  if (!encode_bytes(&a.a, x8, d->tokens, d->in_features, d->x8_ld, 128) || !encode_bytes(&a.b, w8, d->out_features, d->in_features, d->w8_ld, 128)) {
     set_error_text("cuTensorMapEncodeTiled failed for linear8");
     return ADAPM_ECUDA;
   }
-  a.a_scale = xs; a.b_scale = ws; a.b_groups = 1; a.k = (int32_t)d->in_features;
+  a.a_scale = xs; a.b_scale = ws;
   a.out = y; a.out_ld = d->y_ld; a.out_f32 = d->y_dtype == ADAPM_TYPE_F32;
   a.wide = (uintptr_t)y % 32 == 0 && (a.out_f32 || d->y_ld % 16 == 0);
   a.status = (int32_t*)scratch;
@@ -689,7 +766,7 @@ extern "C" int adapm_linear8_input_grad(const adapm_linear8* d, const void* dy, 
   int device, pairs;
   rc = check_buffers({bf16_or_f32(dy, d->tokens, d->y_ld, d->out_features, ADAPM_TYPE_BF16), codes_at(w8, d->out_features, d->w8_ld, d->in_features),
                       floats_at(ws, d->out_features, 4)},
-                     bf16_or_f32(dx, d->tokens, d->dx_ld, d->in_features, d->dx_dtype), scratch, scratch_size, scratch_bytes(plan),
+                     bf16_or_f32(dx, d->tokens, d->dx_ld, d->in_features, d->dx_dtype), scratch, scratch_size, plan.bytes,
                      "adapm_linear8_input_grad: the output or the scratch overlaps another buffer", &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
   if (rc != ADAPM_OK) return rc;
@@ -717,7 +794,7 @@ extern "C" int adapm_linear8_weight_grad(const adapm_linear8* d, const void* dy,
   const int64_t groups = d->x_group ? (d->in_features + 127) / 128 : 1;
   rc = check_buffers({bf16_or_f32(dy, d->tokens, d->y_ld, d->out_features, ADAPM_TYPE_BF16), codes_at(x8, d->tokens, d->x8_ld, d->in_features),
                       floats_at(xs, d->tokens * groups, 4)},
-                     bf16_or_f32(dweight, d->out_features, d->dweight_ld, d->in_features, d->dweight_dtype), scratch, scratch_size, scratch_bytes(plan),
+                     bf16_or_f32(dweight, d->out_features, d->dweight_ld, d->in_features, d->dweight_dtype), scratch, scratch_size, plan.bytes,
                      "adapm_linear8_weight_grad: the output or the scratch overlaps another buffer", &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
   if (rc != ADAPM_OK) return rc;

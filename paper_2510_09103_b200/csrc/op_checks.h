@@ -11,6 +11,8 @@
 namespace adapm {
 
 void set_error_text(const char* text);   // ctx.cu
+// quant8.cu: codes to numbers, its arguments checked before
+int launch_dequant8(const adapm_codes8& d, const void* codes, const float* scales, void* x, cudaStream_t s);
 
 inline bool known_type(int32_t t) { return t == ADAPM_TYPE_F32 || t == ADAPM_TYPE_BF16; }
 inline int64_t type_bytes(int32_t t) { return t == ADAPM_TYPE_F32 ? 4 : 2; }

@@ -336,8 +336,8 @@ int check_desc(const adapm_codes8& d) {
   return ADAPM_OK;
 }
 
-// What both directions check of their buffers; `vec`: whether the rows lie so that eight elements are one access.
-int check_buffers(const adapm_codes8& d, const void* x, const void* codes, const void* scales, bool to_codes, const char* overlap, bool* vec) {
+// What both directions check of their buffers.
+int check_buffers(const adapm_codes8& d, const void* x, const void* codes, const void* scales, bool to_codes, const char* overlap) {
   const int64_t eb = type_bytes(d.dtype), groups = d.group ? (d.cols + 127) / 128 : 1;
   if (!x || !codes || !scales || d.x_ld < d.cols || d.codes_ld < d.cols) return ADAPM_EINVAL;
   if (d.rows > 1 && std::max(d.x_ld, d.codes_ld) > INT64_MAX / 8 / d.rows) return ADAPM_ERANGE;
@@ -347,7 +347,6 @@ int check_buffers(const adapm_codes8& d, const void* x, const void* codes, const
     set_error_text(overlap);
     return ADAPM_EINVAL;
   }
-  *vec = (uintptr_t)x % 16 == 0 && (uintptr_t)codes % 8 == 0 && (d.rows <= 1 || (d.x_ld * eb % 16 == 0 && d.codes_ld % 8 == 0));
   int device;
   return check_on_this_device({x, codes, scales}, &device);
 }
@@ -371,7 +370,30 @@ cudaError_t rows_form(const QuantArgs& a, int sms, cudaStream_t s) {
   return launch_rows<T, 0, false, VEC>(a, s);
 }
 
+// Whether eight elements of a row are one access.
+bool rows_of_eights(const adapm_codes8& d, const void* x, const void* codes) {
+  const int64_t eb = type_bytes(d.dtype);
+  return (uintptr_t)x % 16 == 0 && (uintptr_t)codes % 8 == 0 && (d.rows <= 1 || (d.x_ld * eb % 16 == 0 && d.codes_ld % 8 == 0));
+}
+
 }  // namespace
+
+int launch_dequant8(const adapm_codes8& d, const void* codes, const float* scales, void* x, cudaStream_t s) {
+  DequantArgs a;
+  a.codes = static_cast<const uint8_t*>(codes); a.scales = scales; a.x = x;
+  a.x_ld = d.x_ld; a.codes_ld = d.codes_ld; a.cols = d.cols; a.groups = (d.cols + 127) / 128; a.total = d.rows * a.groups;
+  a.per_row = d.group == 0;
+  const int64_t grid = (a.total + 16 * kUnits - 1) / (16 * kUnits);
+  if (grid > INT32_MAX) return ADAPM_ERANGE;
+  const bool f32 = d.dtype == ADAPM_TYPE_F32, e4m3 = d.code == ADAPM_CODE_E4M3, vec = rows_of_eights(d, x, codes);
+#define ADAPM_DEQUANT(T, E, VEC) launch_chained(true, dequant8_kernel<T, E, VEC>, (unsigned)grid, 256, 0, s, a)
+#define ADAPM_DEQUANT_OF(T) (e4m3 ? (vec ? ADAPM_DEQUANT(T, true, true) : ADAPM_DEQUANT(T, true, false)) : (vec ? ADAPM_DEQUANT(T, false, true) : ADAPM_DEQUANT(T, false, false)))
+  ADAPM_CUDA(f32 ? ADAPM_DEQUANT_OF(float) : ADAPM_DEQUANT_OF(uint16_t));
+#undef ADAPM_DEQUANT_OF
+#undef ADAPM_DEQUANT
+  return ADAPM_OK;
+}
+
 }  // namespace adapm
 
 using namespace adapm;
@@ -382,8 +404,7 @@ extern "C" int adapm_quant8(const adapm_codes8* d, const void* x, void* codes, f
   if (rc != ADAPM_OK) return rc;
   if (d->code == ADAPM_CODE_E4M3 && !d->pow2) return ADAPM_EUNSUPPORTED;
   if (d->rows == 0) return ADAPM_OK;
-  bool vec;
-  rc = check_buffers(*d, x, codes, scales, true, "adapm_quant8: the codes or the scales overlap another buffer", &vec);
+  rc = check_buffers(*d, x, codes, scales, true, "adapm_quant8: the codes or the scales overlap another buffer");
   if (rc != ADAPM_OK) return rc;
   QuantArgs a;
   a.x = x; a.codes = static_cast<uint8_t*>(codes); a.scales = scales;
@@ -391,7 +412,7 @@ extern "C" int adapm_quant8(const adapm_codes8* d, const void* x, void* codes, f
   a.groups = (d->cols + 127) / 128; a.total = d->rows * a.groups;
   a.mode = d->code == ADAPM_CODE_E4M3 ? E4M3_POW2 : d->pow2 ? INT8_POW2 : INT8_MAX_SCALE;
   cudaStream_t s = (cudaStream_t)stream;
-  const bool f32 = d->dtype == ADAPM_TYPE_F32;
+  const bool f32 = d->dtype == ADAPM_TYPE_F32, vec = rows_of_eights(*d, x, codes);
   if (d->group) {
     const int64_t grid = (a.total + 16 * kUnits - 1) / (16 * kUnits);
     if (grid > INT32_MAX) return ADAPM_ERANGE;
@@ -412,21 +433,7 @@ extern "C" int adapm_dequant8(const adapm_codes8* d, const void* codes, const fl
   if (!d) return ADAPM_EINVAL;
   int rc = check_desc(*d);
   if (rc != ADAPM_OK || d->rows == 0) return rc;
-  bool vec;
-  rc = check_buffers(*d, x, codes, scales, false, "adapm_dequant8: the output overlaps another buffer", &vec);
+  rc = check_buffers(*d, x, codes, scales, false, "adapm_dequant8: the output overlaps another buffer");
   if (rc != ADAPM_OK) return rc;
-  DequantArgs a;
-  a.codes = static_cast<const uint8_t*>(codes); a.scales = scales; a.x = x;
-  a.x_ld = d->x_ld; a.codes_ld = d->codes_ld; a.cols = d->cols; a.groups = (d->cols + 127) / 128; a.total = d->rows * a.groups;
-  a.per_row = d->group == 0;
-  const int64_t grid = (a.total + 16 * kUnits - 1) / (16 * kUnits);
-  if (grid > INT32_MAX) return ADAPM_ERANGE;
-  cudaStream_t s = (cudaStream_t)stream;
-  const bool f32 = d->dtype == ADAPM_TYPE_F32, e4m3 = d->code == ADAPM_CODE_E4M3;
-#define ADAPM_DEQUANT(T, E, VEC) launch_chained(true, dequant8_kernel<T, E, VEC>, (unsigned)grid, 256, 0, s, a)
-#define ADAPM_DEQUANT_OF(T) (e4m3 ? (vec ? ADAPM_DEQUANT(T, true, true) : ADAPM_DEQUANT(T, true, false)) : (vec ? ADAPM_DEQUANT(T, false, true) : ADAPM_DEQUANT(T, false, false)))
-  ADAPM_CUDA(f32 ? ADAPM_DEQUANT_OF(float) : ADAPM_DEQUANT_OF(uint16_t));
-#undef ADAPM_DEQUANT_OF
-#undef ADAPM_DEQUANT
-  return ADAPM_OK;
+  return launch_dequant8(*d, codes, scales, x, (cudaStream_t)stream);
 }
