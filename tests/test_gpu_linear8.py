@@ -90,6 +90,27 @@ def test_codes_next_to_half_a_step(dtype):
         _check_quant(x, code, group, pow2)
 
 
+def test_codes_of_every_bf16_number_below_every_maximum():
+    """All mantissas of the maximum, and all numbers of its eight binades below it, of both signs."""
+    m = torch.arange(128, 256, device="cuda")
+    x = (m[None, None, :] / 2.0 ** torch.arange(9, device="cuda")[:, None, None]).expand(9, 128, 128).permute(1, 0, 2).reshape(128, -1).double()
+    x = torch.minimum(torch.cat([m[:, None].double(), x, -x], 1), m[:, None].double()).maximum(-m[:, None].double())
+    for power in (0, -7, 40, -120):
+        y = (x * 2.0**power).to(BF16)
+        assert torch.equal(y.double(), x * 2.0**power)
+        _check_quant(y, "int8", 0, False)
+        _check_quant(y.T.contiguous().T.reshape(-1, 1 + 2 * 9 * 128)[:, :129].contiguous(), "int8", 0, False)
+
+
+def test_codes_on_half_a_step_of_scales_that_are_whole_numbers():
+    """fp32 numbers whose quotient is half a step exactly, for scales that are no powers of two: ties go to the even code."""
+    s = torch.tensor([3.0, 5.0, 7.0, 6.0, 97.0, 12345.0, 1.5, 0.375 * 2.0**-90, 3 * 2.0**60], device="cuda", dtype=torch.float64)
+    x = torch.cat([127 * s[:, None], (torch.arange(-127, 127, device="cuda").double() + 0.5)[None, :] * s[:, None]], 1).float()
+    assert torch.equal(x.double()[:, 5], -122.5 * s)
+    codes, scales = _check_quant(x, "int8", 0, False)
+    assert torch.equal(scales[:, 0].double(), s)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_scales_at_the_ends_of_the_range(dtype):
     tiny = torch.finfo(dtype).smallest_normal
