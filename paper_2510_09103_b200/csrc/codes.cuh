@@ -4,6 +4,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include "philox.cuh"
+
 namespace adapm {
 
 // The four codes of a word as numbers.  int8: the byte, shifted to 0 .. 255, becomes the low bits of a number from 2^23 on, whose
@@ -18,7 +20,11 @@ __device__ __forceinline__ void unpack4(uint32_t w, float* x) {
   } else {
     const uint32_t u = w ^ 0x80808080u;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440u + (uint32_t)i)) - 8388736.f;
+    for (int i = 0; i < 4; i += 2) {
+      const float2 t = add2(make_float2(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440u + (uint32_t)i)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7441u + (uint32_t)i))),
+                            make_float2(-8388736.f, -8388736.f));
+      x[i] = t.x; x[i + 1] = t.y;
+    }
   }
 }
 

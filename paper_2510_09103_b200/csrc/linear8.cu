@@ -12,6 +12,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "codes.cuh"
 #include "linear8_plan.h"
 #include "tc_engine.cuh"
 #include "tc_host.h"
@@ -403,22 +404,33 @@ __global__ void __launch_bounds__(256) linear8_sum_kernel(const SumArgs a) {
   }
 }
 
-// ---- few tokens ------------------------------------------------------------------------------------------------------
-// The weight is the operand with 128 rows, the tokens are the columns (up to 256), so that few tokens cost few products, and the
-// CTAs of a cluster take parts of K, whose sums they add up through each other's shared memory: whole numbers, in any order.
+// ---- strips: few columns, or few tiles -----------------------------------------------------------------------------------
+// A CTA has 128 features of the 8-bit operand (the rows of an MMA, so that few tokens cost few products) and up to 256 columns of the
+// other one; the CTAs of a cluster take parts of K, whose sums they add up through each other's shared memory, in a fixed order.
+//   forward       output features of w8 x tokens of x8         both read as they lie (kind::i8)
+//   input grad    input features of w8 x tokens of dy          codes made bf16 numbers on their way: sixteen warps, four to a stage,
+//   weight grad   input features of x8 x output features of dy     write them into shared memory, times their scales
+// The result lies across: out[column][feature].
 
-struct FewArgs {
-  CUtensorMap w, x;
-  FewPlan plan;
-  const float *xs, *ws;
-  void* y;
+struct StripArgs {
+  CUtensorMap codes, other;
+  StripPlan plan;
+  const float *xs, *ws;          // forward: of a column, of a feature
+  const float* scale;            // gradients: of a row of K [K][scale_groups]
+  void* out;
   int32_t* status;
-  int64_t y_ld;
-  int32_t tokens, out, f32;
+  int64_t out_ld;
+  int32_t columns, features, k, scale_groups, f32, accumulate, e4m3;
 };
 
-struct __align__(8) FewShared {
-  uint64_t full[8], empty[8], tfull;
+template <int OP>
+struct StripShape {
+  static constexpr bool kGrad = OP != FORWARD;
+  static constexpr int kThreads = kGrad ? 768 : 256;       // warp 0 loads, 1 issues the MMAs, 4 to 7 drain, 8 to 23 make numbers of codes
+};
+
+struct __align__(8) StripShared {
+  uint64_t full[kStripRing], empty[kStripRing], raw_full[kStripRing], raw_empty[kStripRing], tfull;
   uint32_t tmem_base;
   int abort;
 };
@@ -429,68 +441,97 @@ __device__ __forceinline__ int4 load_shared4_at(uint32_t at) {
   return v;
 }
 
-constexpr int kFewThreads = 256;       // warp 0 loads, warp 1 issues the MMAs, warps 4 to 7 drain the accumulator, all put the parts together
+// Eight codes of one row, times its scale, as bf16 numbers: 16 bytes.
+template <bool E4M3>
+__device__ __forceinline__ void decode8(uint32_t c0, uint32_t c1, float s, uint32_t* w) {
+  float x[8];
+  unpack4<E4M3>(c0, x);
+  unpack4<E4M3>(c1, x + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 t = mul2(make_float2(x[2 * i], x[2 * i + 1]), make_float2(s, s));
+    w[i] = pack_bf16x2_rn(t.x, t.y);
+  }
+}
 
-// A CTA puts its share of the features together, a thread four of them, for every few tokens: eight loads of four sums on their way
+// A CTA puts its share of the features together, a thread four of them, for every few columns: eight loads of four sums on their way
 // at a time.
-template <int SPLIT>
-__device__ __forceinline__ void few_together(const FewArgs& a, const uint8_t* sums, int rank, int n0, int t0) {
-  constexpr int kShare = 128 / SPLIT, kFours = kShare / 4, kStep = kFewThreads / kFours, kAtOnce = 8 / SPLIT;
-  const int f = rank * kShare + 4 * ((int)threadIdx.x % kFours), n = n0 + f, tokens = min(a.plan.tn, a.tokens - t0);
-  if (n >= a.out) return;
-  const float4 ws = *reinterpret_cast<const float4*>(a.ws + n);
+template <int OP, int SPLIT>
+__device__ __forceinline__ void put_together(const StripArgs& a, const uint8_t* sums, int rank, int f0, int c0) {
+  constexpr int kShare = 128 / SPLIT, kFours = kShare / 4, kStep = StripShape<OP>::kThreads / kFours, kAtOnce = 8 / SPLIT;
+  const int mine = rank * kShare + 4 * ((int)threadIdx.x % kFours), f = f0 + mine, columns = min(a.plan.width, a.columns - c0);
+  if (f >= a.features) return;
+  float4 ws = make_float4(1.f, 1.f, 1.f, 1.f);
+  if (OP == FORWARD) ws = *reinterpret_cast<const float4*>(a.ws + f);
   uint32_t from[SPLIT];
 #pragma unroll
-  for (int r = 0; r < SPLIT; ++r) {
-    from[r] = smem_u32(sums) + 4u * (uint32_t)f;
-    if (SPLIT > 1) from[r] = shared_of(sums + 4 * f, (uint32_t)r);
-  }
-  for (int t = (int)threadIdx.x / kFours; t < tokens; t += kAtOnce * kStep) {
+  for (int r = 0; r < SPLIT; ++r) from[r] = SPLIT > 1 ? shared_of(sums + 4 * mine, (uint32_t)r) : smem_u32(sums + 4 * mine);
+  for (int c = (int)threadIdx.x / kFours; c < columns; c += kAtOnce * kStep) {
     int4 v[kAtOnce][SPLIT];
     float xs[kAtOnce];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      const int at = min(t + u * kStep, tokens - 1);
-      xs[u] = a.xs[t0 + at];
+      const int at = min(c + u * kStep, columns - 1);
+      xs[u] = OP == FORWARD ? a.xs[c0 + at] : 1.f;
 #pragma unroll
       for (int r = 0; r < SPLIT; ++r) v[u][r] = load_shared4_at(from[r] + 512u * (uint32_t)at);
     }
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
-      if (t + u * kStep >= tokens) continue;
-      int4 sum = v[u][0];
+      if (c + u * kStep >= columns) continue;
+      const int64_t to = (int64_t)(c0 + c + u * kStep) * a.out_ld + f;
+      float y[4];
+      if (OP == FORWARD) {
+        int4 sum = v[u][0];
 #pragma unroll
-      for (int r = 1; r < SPLIT; ++r) { sum.x += v[u][r].x; sum.y += v[u][r].y; sum.z += v[u][r].z; sum.w += v[u][r].w; }
-      const float y[4] = {(float)sum.x * xs[u] * ws.x, (float)sum.y * xs[u] * ws.y, (float)sum.z * xs[u] * ws.z, (float)sum.w * xs[u] * ws.w};
-      const int64_t to = (int64_t)(t0 + t + u * kStep) * a.y_ld + n;
-      if (a.f32) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + to) = make_float4(y[0], y[1], y[2], y[3]);
-      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + to) = make_uint2(pack_bf16x2_rn(y[0], y[1]), pack_bf16x2_rn(y[2], y[3]));
+        for (int r = 1; r < SPLIT; ++r) { sum.x += v[u][r].x; sum.y += v[u][r].y; sum.z += v[u][r].z; sum.w += v[u][r].w; }
+        y[0] = (float)sum.x * xs[u] * ws.x; y[1] = (float)sum.y * xs[u] * ws.y; y[2] = (float)sum.z * xs[u] * ws.z; y[3] = (float)sum.w * xs[u] * ws.w;
+      } else {
+        y[0] = __int_as_float(v[u][0].x); y[1] = __int_as_float(v[u][0].y); y[2] = __int_as_float(v[u][0].z); y[3] = __int_as_float(v[u][0].w);
+#pragma unroll
+        for (int r = 1; r < SPLIT; ++r) {
+          y[0] += __int_as_float(v[u][r].x); y[1] += __int_as_float(v[u][r].y); y[2] += __int_as_float(v[u][r].z); y[3] += __int_as_float(v[u][r].w);
+        }
+        if (a.accumulate) {
+          const uint2 o = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.out) + to);
+          y[0] += __uint_as_float(o.x << 16); y[1] += __uint_as_float(o.x & 0xffff0000u);
+          y[2] += __uint_as_float(o.y << 16); y[3] += __uint_as_float(o.y & 0xffff0000u);
+        }
+      }
+      if (OP == FORWARD && a.f32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y[0], y[1], y[2], y[3]);
+      else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to) = make_uint2(pack_bf16x2_rn(y[0], y[1]), pack_bf16x2_rn(y[2], y[3]));
     }
   }
 }
 
-__global__ void __launch_bounds__(kFewThreads) linear8_few_kernel(const __grid_constant__ FewArgs a) {
+template <int OP>
+__global__ void __launch_bounds__(StripShape<OP>::kThreads) linear8_strip_kernel(const __grid_constant__ StripArgs a) {
+  using S = StripShape<OP>;
+  constexpr int kStep = S::kGrad ? 64 : 128;                       // K of a stage
   extern __shared__ uint8_t dyn_smem[];
-  __shared__ FewShared sh;
+  __shared__ StripShared sh;
   wait_for_previous_kernel();
-  const FewPlan& p = a.plan;
+  const StripPlan& p = a.plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, split = p.split, rank = split > 1 ? (int)cluster_rank() : 0;
-  const int tile = (int)blockIdx.x / split, t_tile = tile / p.n_tiles, n0 = (tile - t_tile * p.n_tiles) * 128, t0 = t_tile * p.tn;
-  const int k0 = p.first(rank), count = p.first(rank + 1) - k0, bytes = 16384 + 128 * p.tn;
+  const int tile = (int)blockIdx.x / split, c_tile = tile / p.f_tiles, f0 = (tile - c_tile * p.f_tiles) * 128, c0 = c_tile * p.width;
+  const int k0 = p.first(rank), count = p.first(rank + 1) - k0, bytes = strip_stage_bytes(p.width);
   uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~(uintptr_t)1023);
+  uint8_t* const raw = ring + p.ring * bytes;
   volatile int* const abort = &sh.abort;
   int32_t* const status = a.status + blockIdx.x;
-  const uint32_t tmem_cols = p.tn <= 32 ? 32 : p.tn <= 64 ? 64 : p.tn <= 128 ? 128 : 256;
+  const uint32_t tmem_cols = p.width <= 32 ? 32 : p.width <= 64 ? 64 : p.width <= 128 ? 128 : 256;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.ring; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], 1); }
+    for (int i = 0; i < p.ring; ++i) { mbar_init(&sh.full[i], S::kGrad ? 1 + 4 : 1); mbar_init(&sh.empty[i], 1); }
+    if (S::kGrad)
+      for (int i = 0; i < p.raw; ++i) { mbar_init(&sh.raw_full[i], 1); mbar_init(&sh.raw_empty[i], 4); }
     mbar_init(&sh.tfull, 1);
     sh.abort = 0;
     *status = 0;
     mbar_fence_init();
   }
   if (blockIdx.x == 0)
-    for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += kFewThreads) a.status[i] = 0;      // words of no CTA
+    for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no CTA
   if (warp == 1) {
     tmem_alloc(&sh.tmem_base, tmem_cols);
     tmem_relinquish();
@@ -501,6 +542,7 @@ __global__ void __launch_bounds__(kFewThreads) linear8_few_kernel(const __grid_c
   const uint32_t tmem_base = sh.tmem_base;
 
   if (warp == 0) {
+    // ------------------------------------------------------------------ the operands (forward), the other operand (gradients)
     const bool leader = elect_one();
     int stage = 0;
     uint32_t phase = 0, issued = 0;
@@ -509,28 +551,59 @@ __global__ void __launch_bounds__(kFewThreads) linear8_few_kernel(const __grid_c
       if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
       if (leader) {
         uint8_t* const dst = ring + stage * bytes;
-        mbar_arrive_expect_tx(&sh.full[stage], (uint32_t)bytes);
-        tma_load_box(dst, &a.w, (k0 + i) * 128, n0, &sh.full[stage]);
-        tma_load_box(dst + 16384, &a.x, (k0 + i) * 128, t0, &sh.full[stage]);
+        uint64_t* const bar = &sh.full[stage];
+        const int k = (k0 + i) * kStep;
+        mbar_arrive_expect_tx(bar, (uint32_t)(S::kGrad ? bytes - 16384 : bytes));
+        if (OP == FORWARD) tma_load_box(dst, &a.codes, k, f0, bar);
+        if (OP == WEIGHT_GRAD) {
+          for (int c = 0; c < p.width; c += 64) tma_load_box(dst + 16384 + c * 128, &a.other, c0 + c, k, bar);
+        } else {
+          tma_load_box(dst + 16384, &a.other, k, c0, bar);
+        }
       }
       __syncwarp();
       ++issued;
       if (++stage == p.ring) { stage = 0; phase ^= 1u; }
     }
     if (!ok) drain_ring<false>(sh.full, stage, phase, issued, p.ring, 0);
+  } else if (S::kGrad && warp == 2) {
+    // ------------------------------------------------------------------ codes, as they lie
+    const bool leader = elect_one();
+    int stage = 0;
+    uint32_t phase = 0, issued = 0;
+    bool ok = true;
+    for (int i = 0; i < count; ++i) {
+      if (!mbar_wait_warp(&sh.raw_empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+      if (leader) {
+        mbar_arrive_expect_tx(&sh.raw_full[stage], kStripRawBytes);
+        tma_load_box(raw + stage * kStripRawBytes, &a.codes, f0, (k0 + i) * kStep, &sh.raw_full[stage]);
+      }
+      __syncwarp();
+      ++issued;
+      if (++stage == p.raw) { stage = 0; phase ^= 1u; }
+    }
+    if (!ok) drain_ring<false>(sh.raw_full, stage, phase, issued, p.raw, 0);
   } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer (all lanes run, one issues)
     const bool leader = elect_one();
     int stage = 0;
     uint32_t phase = 0;
     bool ok = true;
-    const uint32_t ring0 = uniform(smem_u32(ring)), d = uniform(tmem_base), dhi = desc_hi(), idesc = uniform(i8_idesc(p.tn, 128));
+    constexpr bool kAmn = S::kGrad, kBmn = OP == WEIGHT_GRAD;
+    constexpr uint32_t kAstep = kAmn ? 128u : 2u, kBstep = kBmn ? 128u : 2u;
+    const uint32_t ring0 = uniform(smem_u32(ring)), d = uniform(tmem_base), dhi = desc_hi();
+    const uint32_t idesc = uniform(S::kGrad ? make_idesc(p.width, kAmn, kBmn, false, 128) : i8_idesc(p.width, 128));
     for (int i = 0; i < count; ++i) {
       if (!mbar_wait_warp(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
       tc_fence_after();
-      const uint32_t slot = ring0 + (uint32_t)(stage * bytes), alo = desc_lo(slot, 16u), blo = desc_lo(slot + 16384, 16u);
+      const uint32_t slot = ring0 + (uint32_t)(stage * bytes), alo = desc_lo(slot, kAmn ? 8192u : 16u), blo = desc_lo(slot + 16384, kBmn ? 8192u : 16u);
       if (leader) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) mma_i8<false>(d, desc_join(alo + q * 2u, dhi), desc_join(blo + q * 2u, dhi), idesc, i || q ? 1u : 0u);
+        for (int q = 0; q < 4; ++q) {
+          const uint64_t da = desc_join(alo + q * kAstep, dhi), db = desc_join(blo + q * kBstep, dhi);
+          if (S::kGrad) mma_bf16<false>(d, da, db, idesc, i || q ? 1u : 0u);
+          else mma_i8<false>(d, da, db, idesc, i || q ? 1u : 0u);
+        }
         mma_commit(&sh.empty[stage]);
       }
       __syncwarp();
@@ -538,15 +611,67 @@ __global__ void __launch_bounds__(kFewThreads) linear8_few_kernel(const __grid_c
     }
     if (ok && leader) mma_commit(&sh.tfull);
     __syncwarp();
+  } else if (S::kGrad && warp >= 8) {
+    // ------------------------------------------------------------------ codes to bf16 numbers: the teams take turns; a warp has
+    // four of every sixteen rows of K, eight lanes to a row, 16 codes to a lane
+    const int team = (warp - 8) >> 2, row0 = 4 * (warp & 3) + (lane >> 3), j = lane & 7, sub = row0 & 7;
+    // the 128-byte swizzle; lanes 4 to 7 write their second chunk first, so that eight lanes meet no bank twice
+    const int odd = j >> 2, from = row0 * 128 + 16 * j, to = odd * 8192 + row0 * 128;
+    const int at0 = to + ((2 * (j & 3) + odd) ^ sub) * 16, at1 = to + ((2 * (j & 3) + 1 - odd) ^ sub) * 16;
+    // a lane asks for the scale of one of its row's four, a turn ahead
+    const float* const scale = a.scale + (a.scale_groups > 1 ? f0 / 128 : 0);
+    auto scale_at = [&](int i) {
+      const int k = (k0 + i) * 64 + 16 * j + row0;
+      return j < 4 && i < count && k < a.k ? __ldg(scale + (int64_t)k * a.scale_groups) : 0.f;
+    };
+    int stage = team, rs = team;           // (either ring has at least as many stages as there are teams)
+    uint32_t phase = 0, raw_phase = 0;
+    float next = scale_at(team);
+    for (int i = team; i < count; i += kStripTeams) {
+      const float mine = next;
+      next = scale_at(i + kStripTeams);
+      if (!mbar_wait_warp(&sh.raw_full[rs], raw_phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) break;
+      uint4 q[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const uint4*>(raw + rs * kStripRawBytes + from + r * 2048);
+      if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) break;
+      uint8_t* const dst = ring + stage * bytes;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float s = __shfl_sync(0xffffffffu, mine, (lane & 24) | r);
+        const uint32_t c0 = odd ? q[r].z : q[r].x, c1 = odd ? q[r].w : q[r].y, c2 = odd ? q[r].x : q[r].z, c3 = odd ? q[r].y : q[r].w;
+        uint32_t u[4], v[4];
+        if (a.e4m3) {
+          decode8<true>(c0, c1, s, u);
+          decode8<true>(c2, c3, s, v);
+        } else {
+          decode8<false>(c0, c1, s, u);
+          decode8<false>(c2, c3, s, v);
+        }
+        put4(dst + at0 + r * 2048, u);
+        put4(dst + at1 + r * 2048, v);
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&sh.raw_empty[rs]);
+        mbar_arrive(&sh.full[stage]);
+      }
+      stage += kStripTeams;
+      if (stage >= p.ring) { stage -= p.ring; phase ^= 1u; }
+      rs += kStripTeams;
+      if (rs >= p.raw) { rs -= p.raw; raw_phase ^= 1u; }
+    }
   } else if (warp >= 4) {
-    // this CTA's sums [tokens][128], over the ring: all that was in it has been multiplied
+    // ------------------------------------------------------------------ this CTA's sums [columns][128], over the ring: all that was
+    // in it has been multiplied
     bool ok = true;
     if (lane == 0) ok = mbar_wait(&sh.tfull, 0, abort, status, ST_WAIT_TMEM_FULL, kWaitSpinDefault);
     ok = __shfl_sync(0xffffffffu, ok, 0);
     tc_fence_after();
     if (ok) {
       int* const sums = reinterpret_cast<int*>(ring) + 32 * (warp & 3) + lane;
-      for (int c = 0; c < p.tn; c += 16) {
+      for (int c = 0; c < p.width; c += 16) {
         float v[16];
         tmem_ld16(tmem_base + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)c, v);
         tmem_ld_wait();
@@ -558,12 +683,10 @@ __global__ void __launch_bounds__(kFewThreads) linear8_few_kernel(const __grid_c
   }
   __syncthreads();
   if (split > 1) cluster_sync();
-
-  if (split == 1) few_together<1>(a, ring, rank, n0, t0);
-  else if (split == 2) few_together<2>(a, ring, rank, n0, t0);
-  else if (split == 4) few_together<4>(a, ring, rank, n0, t0);
-  else few_together<8>(a, ring, rank, n0, t0);
-
+  if (split == 1) put_together<OP, 1>(a, ring, rank, f0, c0);
+  else if (split == 2) put_together<OP, 2>(a, ring, rank, f0, c0);
+  else if (split == 4) put_together<OP, 4>(a, ring, rank, f0, c0);
+  else put_together<OP, 8>(a, ring, rank, f0, c0);
   __syncwarp();
   if (split > 1) cluster_sync();      // no CTA leaves while another may still read its sums
   if (warp == 1) {
@@ -574,8 +697,8 @@ __global__ void __launch_bounds__(kFewThreads) linear8_few_kernel(const __grid_c
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 
-// A row-major matrix of bytes in boxes of 128 columns x box_rows rows, with the 128-byte swizzle.
-bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows) {
+// A row-major matrix of bytes in boxes of 128 columns x box_rows rows, with the 128-byte swizzle or as they lie.
+bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, bool swizzle = true) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t dims[2] = {cols, rows};
@@ -583,7 +706,8 @@ bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t co
   const cuuint32_t box[2] = {128, box_rows};
   const cuuint32_t estr[2] = {1, 1};
   return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <int OP, bool LONG>
@@ -619,7 +743,9 @@ int pairs_of(int device, int* pairs) {
   if (!known[device]) {
     int sms = 0;
     ADAPM_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-    ADAPM_CUDA(cudaFuncSetAttribute(linear8_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem + 1024));
+    ADAPM_CUDA(cudaFuncSetAttribute(linear8_strip_kernel<FORWARD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem + 1024));
+    ADAPM_CUDA(cudaFuncSetAttribute(linear8_strip_kernel<INPUT_GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem + 1024));
+    ADAPM_CUDA(cudaFuncSetAttribute(linear8_strip_kernel<WEIGHT_GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem + 1024));
     int n = std::min(sms / 2, (int)kMostWords);
     int rc = allow<FORWARD, false>(&n, sms);
     if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, false>(&n, sms);
@@ -667,10 +793,34 @@ Buffer bf16_or_f32(const void* p, int64_t rows, int64_t ld, int64_t cols, int32_
 Buffer codes_at(const void* p, int64_t rows, int64_t ld, int64_t cols) { return Buffer{p, 16, matrix_at(p, rows, ld, cols, 1)}; }
 Buffer floats_at(const float* p, int64_t n, int64_t align) { return Buffer{p, align, vector_at(p, n, 4)}; }
 
+template <int OP>
+cudaError_t launch_strips(const StripArgs& a, cudaStream_t s) {
+  const size_t smem = (size_t)a.plan.ring * strip_stage_bytes(a.plan.width) + (size_t)a.plan.raw * kStripRawBytes + 1024;
+  return launch_clusters(true, (unsigned)a.plan.split, linear8_strip_kernel<OP>, (unsigned)a.plan.ctas, (unsigned)StripShape<OP>::kThreads, smem, s, a);
+}
+
 // A gradient: [rows, cols] = A [rows, K] (or its transpose) times codes [K, cols].
 int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* codes, const float* scales, void* out, int32_t out_dtype, int64_t out_ld,
              void* scratch, const Plan& plan, int pairs, cudaStream_t s) {
   const bool weight = which == WEIGHT_GRAD;
+  const StripPlan strip = strip_plan_of(d, which);
+  if (strips_are_faster(d, which, strip, plan)) {
+    StripArgs t;
+    std::memset(&t, 0, sizeof(t));
+    t.plan = strip;
+    t.k = (int32_t)(weight ? d.tokens : d.out_features);
+    if (!encode_bytes(&t.codes, codes, t.k, d.in_features, weight ? d.x8_ld : d.w8_ld, 64, false) ||
+        !encode_bf16_matrix(&t.other, dy, d.tokens, d.out_features, d.y_ld, weight ? 64 : (uint32_t)strip.width)) {
+      set_error_text("cuTensorMapEncodeTiled failed for a gradient of linear8");
+      return ADAPM_ECUDA;
+    }
+    t.scale = scales; t.scale_groups = weight && d.x_group ? (int32_t)((d.in_features + 127) / 128) : 1;
+    t.out = out; t.out_ld = out_ld; t.status = (int32_t*)scratch;
+    t.columns = (int32_t)(weight ? d.out_features : d.tokens); t.features = (int32_t)d.in_features;
+    t.accumulate = weight && d.accumulate != 0; t.e4m3 = weight && d.x_code == ADAPM_CODE_E4M3;
+    ADAPM_CUDA(weight ? launch_strips<WEIGHT_GRAD>(t, s) : launch_strips<INPUT_GRAD>(t, s));
+    return ADAPM_OK;
+  }
   Args a;
   std::memset(&a, 0, sizeof(a));
   a.plan = plan;
@@ -726,19 +876,19 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
                      "adapm_linear8_forward: the output or the scratch overlaps another buffer", &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
   if (rc != ADAPM_OK) return rc;
-  const FewPlan few = few_plan_of(d->tokens, d->out_features, d->in_features, 128);
-  if (few_is_faster(few, plan)) {
-    FewArgs f;
-    std::memset(&f, 0, sizeof(f));
-    f.plan = few;
-    if (!encode_bytes(&f.w, w8, d->out_features, d->in_features, d->w8_ld, 128) || !encode_bytes(&f.x, x8, d->tokens, d->in_features, d->x8_ld, (uint32_t)few.tn)) {
+  const StripPlan strip = strip_plan_of(*d, FORWARD);
+  if (strips_are_faster(*d, FORWARD, strip, plan)) {
+    StripArgs t;
+    std::memset(&t, 0, sizeof(t));
+    t.plan = strip;
+    if (!encode_bytes(&t.codes, w8, d->out_features, d->in_features, d->w8_ld, 128) ||
+        !encode_bytes(&t.other, x8, d->tokens, d->in_features, d->x8_ld, (uint32_t)strip.width)) {
       set_error_text("cuTensorMapEncodeTiled failed for linear8");
       return ADAPM_ECUDA;
     }
-    f.xs = xs; f.ws = ws; f.y = y; f.y_ld = d->y_ld; f.status = (int32_t*)scratch;
-    f.tokens = (int32_t)d->tokens; f.out = (int32_t)d->out_features; f.f32 = d->y_dtype == ADAPM_TYPE_F32;
-    ADAPM_CUDA(launch_clusters(true, (unsigned)few.split, linear8_few_kernel, (unsigned)few.ctas, kFewThreads, (size_t)few.ring * few_stage_bytes(few.tn) + 1024,
-                               (cudaStream_t)stream, f));
+    t.xs = xs; t.ws = ws; t.out = y; t.out_ld = d->y_ld; t.status = (int32_t*)scratch;
+    t.columns = (int32_t)d->tokens; t.features = (int32_t)d->out_features; t.f32 = d->y_dtype == ADAPM_TYPE_F32;
+    ADAPM_CUDA(launch_strips<FORWARD>(t, (cudaStream_t)stream));
     return ADAPM_OK;
   }
   Args a;

@@ -44,7 +44,7 @@ struct Plan {
 };
 
 // K is cut where there are fewer tiles than pairs of CTAs, so that its parts, summed by one more launch, take less time.  In units of a stage (512
-// cycles): an item takes its stages and four more, the sums a launch of about ten and the parts' way to memory and back.
+// cycles): an item takes its stages and four more, the sums a launch of about eight and the parts' way to memory and back.
 inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool grad) {
   Plan p;
   const bool may_cut = grad;
@@ -58,7 +58,7 @@ inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool gra
     const int each = (p.stages + n - 1) / n, parts = (p.stages + each - 1) / each;
     if (parts != n) continue;
     const double rounds = (double)((tiles * parts + kPlannedPairs - 1) / kPlannedPairs);
-    const double t = rounds * (each + 4) + (parts > 1 ? 10 + 8.0 * (double)(rows * cols) * parts / 1e6 : 0);
+    const double t = rounds * (each + 4) + (parts > 1 ? 8 + 2.5 * (double)(rows * cols) * parts / 1e6 : 0);
     if (n == 1 || t < best) { best = t; p.parts = parts; p.each = each; }
   }
   p.items = (int32_t)(tiles * p.parts);
@@ -91,35 +91,56 @@ inline Plan plan_of(const adapm_linear8& d, int32_t which) {
   return plan_of(d.out_features, d.in_features, d.tokens, 64, true);
 }
 
-// ---- few tokens ----------------------------------------------------------------------------------------------------
-// A tile is 128 features x `tn` tokens; the `split` CTAs of a cluster share its K.  The ring has `ring` stages.
-struct FewPlan {
-  int32_t tn, t_tiles, n_tiles, stages, split, ring, ctas;
+// ---- strips -----------------------------------------------------------------------------------------------------------
+// A tile is 128 features of the 8-bit operand x `width` columns of the other; the `split` CTAs of a cluster share its K.  The ring has `ring`
+// stages, that of a gradient's codes as they lie `raw`.
+struct StripPlan {
+  int32_t width, c_tiles, f_tiles, stages, split, ring, raw, ctas;
   __host__ __device__ int first(int part) const { return (int)((int64_t)stages * part / split); }      // stage of a part of K
 };
 
-constexpr int kFewTokens = 256, kFewSmem = 220 * 1024;
+constexpr int kStripWidth = 256, kStripSmem = 224 * 1024, kStripRing = 8;
+constexpr int kStripTeams = 4, kStripRawBytes = 64 * 128;        // gradients: stages that are decoded at the same time; bytes of a stage's codes
 
-inline int few_stage_bytes(int tn) { return 16384 + 128 * tn; }
+__host__ __device__ __forceinline__ int strip_stage_bytes(int width) { return 16384 + 128 * width; }
 
-inline FewPlan few_plan_of(int64_t tokens, int64_t features, int64_t k, int stage_k) {
-  FewPlan p;
-  p.t_tiles = (int32_t)((tokens + kFewTokens - 1) / kFewTokens);
-  p.tn = (int32_t)round_up((tokens + p.t_tiles - 1) / std::max(1, p.t_tiles), 16);
-  p.n_tiles = (int32_t)((features + 127) / 128);
-  p.stages = (int32_t)((k + stage_k - 1) / stage_k);
-  const int64_t tiles = (int64_t)p.t_tiles * p.n_tiles;
-  const int bytes = few_stage_bytes(p.tn);
-  p.ring = std::min(8, kFewSmem / bytes);
+inline StripPlan strip_plan_of(const adapm_linear8& d, int32_t which) {
+  const int64_t features = which == FORWARD ? d.out_features : d.in_features, columns = which == WEIGHT_GRAD ? d.out_features : d.tokens;
+  const int64_t k = which == FORWARD ? d.in_features : which == INPUT_GRAD ? d.out_features : d.tokens;
+  StripPlan p;
+  p.c_tiles = (int32_t)((columns + kStripWidth - 1) / kStripWidth);
+  p.width = (int32_t)round_up((columns + p.c_tiles - 1) / std::max(1, p.c_tiles), which == WEIGHT_GRAD ? 64 : 16);
+  p.f_tiles = (int32_t)((features + 127) / 128);
+  const int step = which == FORWARD ? 128 : 64;
+  p.stages = (int32_t)((k + step - 1) / step);
+  const int64_t tiles = (int64_t)p.c_tiles * p.f_tiles;
+  const int bytes = strip_stage_bytes(p.width), kept = which == FORWARD ? 0 : kStripRing * kStripRawBytes;
+  p.ring = std::max(kStripTeams, std::min(kStripRing, (kStripSmem - kept) / bytes));
+  p.raw = which == FORWARD ? 0 : std::min(kStripRing, (kStripSmem - p.ring * bytes) / kStripRawBytes);
   p.split = 1;
-  while (p.split < 8 && 2 * tiles * p.split <= 2 * kPlannedPairs && 4 * p.split <= p.stages) p.split *= 2;
+  // (sixteen clusters of eight do not fit the device's groups of SMs at the same time: 1024 x 512 x 14336 in eighths 29 us, in quarters 20)
+  while (p.split < (tiles <= 8 ? 8 : 4) && tiles * p.split <= kPlannedPairs && 4 * p.split <= p.stages) p.split *= 2;
   p.ctas = (int32_t)std::min<int64_t>(tiles * p.split, INT32_MAX);
   return p;
 }
 
-// Whether the forward product goes by tiles of few tokens.
-inline bool few_is_faster(const FewPlan& few, const Plan& plan) {
-  return few.ctas <= kMostWords && plan.m_tiles * plan.n_tiles < kPlannedPairs;
+// Whether a call goes by strips, by what both forms were measured to take (us): a strip's start and end, longer with its width, and its stages;
+// a pair's 256 x 256 tiles, for a gradient with the launch that decodes its codes and the one that sums the parts of K.
+inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const StripPlan& s, const Plan& p) {
+  if (s.ctas > kMostWords) return false;
+  const bool f32 = which == INPUT_GRAD ? d.dx_dtype == ADAPM_TYPE_F32 : which == WEIGHT_GRAD && d.dweight_dtype == ADAPM_TYPE_F32;
+  const int each = (s.stages + s.split - 1) / s.split;
+  if (f32 || (which != FORWARD && each > kShortStages)) return false;
+  const bool grad = which != FORWARD;
+  int levels = 0;                                     // of the cluster
+  while ((1 << levels) < s.split) ++levels;
+  const double rounds = (double)((s.ctas + 2 * kPlannedPairs - 1) / (2 * kPlannedPairs));
+  const double stage = grad ? 0.36 + 0.0005 * s.width : 0.16 + 0.0006 * s.width, level = grad ? 0.4 + 0.006 * s.width : 0.3 + 0.0025 * s.width;
+  const double strips = 2.0 + rounds * ((grad ? 2.3 : 3.2) + 0.012 * s.width + each * stage + levels * level);
+  const double pair_rounds = (double)((p.items + kPlannedPairs - 1) / kPlannedPairs);
+  double pairs = 6.0 + pair_rounds * (1.0 + 0.31 * p.each);
+  if (grad) pairs += 2.0 + 5e-7 * p.stages * 64.0 * p.cols + (p.parts > 1 ? 2.5 + 5e-7 * p.rows * (double)p.cols * p.parts : 0);
+  return strips < pairs;
 }
 
 }  // namespace linear8
