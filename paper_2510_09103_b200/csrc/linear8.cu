@@ -25,6 +25,7 @@ using namespace tc;
 
 constexpr int kOperandBytes = 16384;             // of one CTA and stage: 128 rows or columns of an operand, 128 bytes of K (or the reverse)
 constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kBoxBytesOut = 4096;                // of a warp's box of results
 constexpr int kSegLong = 4, kSegShort = 64;      // stages of 64 K between two sums in registers: gradients in fp32, long ones in bf16
 
 template <int OP, bool LONG>
@@ -32,21 +33,20 @@ struct Shape {
   static constexpr bool kGrad = OP != FORWARD;
   static constexpr int kThreads = 384;           // four warps that issue, eight that drain
   static constexpr int kStages = 6;
-  static constexpr int kSmem = kStages * kStageBytes + 1024;
+  static constexpr int kSmem = kStages * kStageBytes + 8 * kBoxBytesOut + 1024;
 };
 // LONG: registers of the launch, and as the first four and the other eight warps divide them (the eight keep 128 sums each).
 constexpr int kLongRegs = 168, kLongIssue = 88, kLongDrain = 208;
 static_assert(4 * kLongIssue + 8 * kLongDrain <= 12 * kLongRegs, "a block has the registers that it was launched with");
 
 struct Args {
-  CUtensorMap a, b;
+  CUtensorMap a, b, o;           // o: the result, or the parts of K [parts][rows][cols]
   Plan plan;
   const float *a_scale, *b_scale;      // forward: xs, ws
   void* out;
-  float* part;                   // [parts][rows][cols], where K is cut
   int32_t* status;
   int64_t out_ld;
-  int32_t pairs, out_f32, wide, accumulate, seg;
+  int32_t pairs, out_f32, accumulate, seg;
 };
 
 template <int OP, bool LONG>
@@ -75,36 +75,10 @@ __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_
 
 __device__ __forceinline__ void put4(void* p, const uint32_t* v) { *reinterpret_cast<uint4*>(p) = make_uint4(v[0], v[1], v[2], v[3]); }
 
-// 16 values of a row of which those below n (a multiple of 8) exist, to addresses that are multiples of 32 (wide) or 16 bytes.
-__device__ __forceinline__ void store_row16(void* base, int64_t at, const float* x, int n, bool f32, bool wide) {
-  if (f32) {
-    float* p = static_cast<float*>(base) + at;
+// x += 32 values of a row of which those below n (a multiple of 8) exist.
+__device__ __forceinline__ void add_row32(const void* base, int64_t at, float* x, int n, bool f32) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if (8 * h < n) {
-        if (wide) st_f32x8(p + 8 * h, x + 8 * h);
-        else {
-          *reinterpret_cast<float4*>(p + 8 * h) = make_float4(x[8 * h], x[8 * h + 1], x[8 * h + 2], x[8 * h + 3]);
-          *reinterpret_cast<float4*>(p + 8 * h + 4) = make_float4(x[8 * h + 4], x[8 * h + 5], x[8 * h + 6], x[8 * h + 7]);
-        }
-      }
-    }
-    return;
-  }
-  uint16_t* p = static_cast<uint16_t*>(base) + at;
-  uint32_t w[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2_rn(x[2 * e], x[2 * e + 1]);
-  if (wide && n >= 16) st_b32x8(p, w);
-  else {
-    if (n > 0) put4(p, w);
-    if (n > 8) put4(p + 8, w + 4);
-  }
-}
-// x += 16 values of a row of which those below n exist.
-__device__ __forceinline__ void add_row16(const void* base, int64_t at, float* x, int n, bool f32) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < 4; ++h) {
     if (8 * h >= n) continue;
     if (f32) {
       const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at + 8 * h);
@@ -123,17 +97,52 @@ __device__ __forceinline__ void add_row16(const void* base, int64_t at, float* x
   }
 }
 
-// What a gradient's item does with 16 columns of its sums.
-__device__ __forceinline__ void finish16(const Args& a, const Cut& t, int row, int col, float* x) {
-  if (row >= a.plan.rows) return;
-  const int n = a.plan.cols - col;
-  if (a.plan.parts > 1) {
-    store_row16(a.part, ((int64_t)t.part * a.plan.rows + row) * a.plan.cols + col, x, n, true, true);
-    return;
+// A warp's way out: 32 rows of 128 bytes (32 columns in fp32, 64 in bf16) are put into its box in shared memory, with the 128-byte
+// swizzle, and stored as a whole by TMA, which leaves out what the result does not have.  (Every thread storing 32 bytes of a row of its
+// own: weight gradient of 1 x 14336 x 4096 36 to 42 us, with a box 27 to 30; two boxes per warp and five stages of operands instead of six: 2048 x
+// 4096 x 4096 53 -> 56.)
+struct Outlet {
+  const CUtensorMap* map;
+  uint8_t* box;
+  int lane;
+  // 32 columns from column `col` on of the rows from `row0` on, the lane's own in x; `part`: of K.
+  __device__ __forceinline__ void put32(const float* x, int col, int row0, int part, bool f32, int rows, int cols) {
+    const bool first = f32 || (col & 32) == 0, last = f32 || (col & 32) != 0;
+    if (first) {
+      if (lane == 0) bulk_wait_group_read<0>();
+      __syncwarp();
+    }
+    uint8_t* const line = box + lane * 128;
+    if (f32) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        *reinterpret_cast<float4*>(line + ((c ^ (lane & 7)) * 16)) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+    } else {
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2_rn(x[8 * c + 2 * e], x[8 * c + 2 * e + 1]);
+        put4(line + (((c + (first ? 0 : 4)) ^ (lane & 7)) * 16), w);
+      }
+    }
+    if (!last) return;
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      const int x0 = f32 ? col : col - 32;
+      if (row0 < rows && x0 < cols) tma_store_box3(map, x0, row0, part, box);
+      bulk_commit_group();
+    }
   }
-  const int64_t at = (int64_t)row * a.out_ld + col;
-  if (a.accumulate) add_row16(a.out, at, x, n, a.out_f32);
-  store_row16(a.out, at, x, n, a.out_f32, a.wide);
+};
+
+// What a gradient's item does with 32 columns of its sums.
+__device__ __forceinline__ void finish32(const Args& a, const Cut& t, Outlet& out, int row0, int col, float* x) {
+  const int row = row0 + out.lane;
+  if (a.accumulate && a.plan.parts == 1 && row < a.plan.rows) add_row32(a.out, (int64_t)row * a.out_ld + col, x, a.plan.cols - col, a.out_f32);
+  __syncwarp();
+  out.put32(x, col, row0, t.part, a.plan.parts > 1 || a.out_f32, a.plan.rows, a.plan.cols);
 }
 
 // An item's K in segments of even length: how many, and the stages of each but the last.
@@ -268,6 +277,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
     // group of four warps, the lower or upper half of the columns
     const int q = 32 * (warp & 3) + lane, grp = (warp - 4) >> 2;
     const uint32_t lane_addr = (uint32_t)(32 * (warp & 3)) << 16;
+    Outlet out = {&a.o, ring + S::kStages * kStageBytes + (warp - 4) * kBoxBytesOut, lane};
     uint32_t run = 0;
     bool ok = true;
     auto wait_full = [&](int acc) {
@@ -314,8 +324,8 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         }
         if (!ok) break;
 #pragma unroll
-        for (int c = 0; c < 128; c += 16)
-          if (c < half) finish16(a, t, row, col0 + c, v + c);
+        for (int c = 0; c < 128; c += 32)
+          if (c < half) finish32(a, t, out, row - lane, col0 + c, v + c);
       } else {
         const int acc = (int)(run & 1);
         const float xs = OP == FORWARD && row < a.plan.rows ? a.a_scale[row] : 0.f;
@@ -331,31 +341,26 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
           tmem_ld16(at + c + 16, v + 16);
           tmem_ld_wait();
           if (c + 32 >= half) release(acc);
+          const int col = col0 + c;
+          if (OP == FORWARD) {
 #pragma unroll
-          for (int h = 0; h < 32; h += 16) {
-            float* const x = v + h;
-            const int col = col0 + c + h;
-            if (OP == FORWARD) {
-              const int n = a.plan.cols - col;
-              if (row >= a.plan.rows || n <= 0) continue;
-#pragma unroll
-              for (int e = 0; e < 16; e += 4) {
-                if (e >= n) continue;
-                const float4 ws = __ldg(reinterpret_cast<const float4*>(a.b_scale + col + e));
-                x[e] = (float)__float_as_int(x[e]) * xs * ws.x;
-                x[e + 1] = (float)__float_as_int(x[e + 1]) * xs * ws.y;
-                x[e + 2] = (float)__float_as_int(x[e + 2]) * xs * ws.z;
-                x[e + 3] = (float)__float_as_int(x[e + 3]) * xs * ws.w;
-              }
-              store_row16(a.out, (int64_t)row * a.out_ld + col, x, n, a.out_f32, a.wide);
-            } else {
-              finish16(a, t, row, col, x);
+            for (int e = 0; e < 32; e += 4) {
+              const float4 ws = col + e < a.plan.cols ? __ldg(reinterpret_cast<const float4*>(a.b_scale + col + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+              v[e] = (float)__float_as_int(v[e]) * xs * ws.x;
+              v[e + 1] = (float)__float_as_int(v[e + 1]) * xs * ws.y;
+              v[e + 2] = (float)__float_as_int(v[e + 2]) * xs * ws.z;
+              v[e + 3] = (float)__float_as_int(v[e + 3]) * xs * ws.w;
             }
+            out.put32(v, col, row - lane, 0, a.out_f32, a.plan.rows, a.plan.cols);
+          } else {
+            finish32(a, t, out, row - lane, col, v);
           }
         }
         ++run;
       }
     }
+    if (lane == 0) bulk_wait_group<0>();
+    __syncwarp();
   }
 
   tc_fence_before();
@@ -697,6 +702,19 @@ __global__ void __launch_bounds__(StripShape<OP>::kThreads) linear8_strip_kernel
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 
+// `parts` results [rows, cols], one behind the other, in boxes of 32 rows of 128 bytes with the 128-byte swizzle.
+bool encode_result(CUtensorMap* out, void* base, int64_t parts, int64_t rows, int64_t cols, int64_t pitch, bool f32) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint64_t bytes = f32 ? 4 : 2, line = (cuuint64_t)pitch * bytes;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
+  const cuuint64_t strides[2] = {line, parts > 1 ? (cuuint64_t)rows * line : line};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / bytes), 32, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // A row-major matrix of bytes in boxes of 128 columns x box_rows rows, with the 128-byte swizzle or as they lie.
 bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, bool swizzle = true) {
   EncodeTiledFn fn = encode_tiled_fn();
@@ -834,20 +852,23 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
   }
   a.out = out; a.out_ld = out_ld;
   a.status = (int32_t*)scratch;
-  a.part = (float*)((char*)scratch + plan.part_at);
+  float* const parts = (float*)((char*)scratch + plan.part_at);
   a.out_f32 = out_dtype == ADAPM_TYPE_F32;
-  a.wide = (uintptr_t)out % 32 == 0 && (a.out_f32 || out_ld % 16 == 0);
   a.accumulate = weight && d.accumulate != 0;
   a.pairs = std::min(pairs, plan.items);
   a.seg = a.out_f32 ? kSegLong : kSegShort;
   const bool is_long = a.out_f32 || plan.each > kShortStages;
+  if (!(plan.parts > 1 ? encode_result(&a.o, parts, plan.parts, plan.rows, plan.cols, plan.cols, true) : encode_result(&a.o, out, 1, plan.rows, plan.cols, out_ld, a.out_f32))) {
+    set_error_text("cuTensorMapEncodeTiled failed for a gradient of linear8");
+    return ADAPM_ECUDA;
+  }
   const int rc = launch_dequant8(q, codes, scales, decoded, s);
   if (rc != ADAPM_OK) return rc;
   ADAPM_CUDA(weight ? (is_long ? launch<WEIGHT_GRAD, true>(a, s) : launch<WEIGHT_GRAD, false>(a, s))
                     : (is_long ? launch<INPUT_GRAD, true>(a, s) : launch<INPUT_GRAD, false>(a, s)));
   if (plan.parts == 1) return ADAPM_OK;
   SumArgs u;
-  u.part = a.part; u.out = out; u.out_ld = out_ld; u.fours = plan.cols / 4; u.places = (int64_t)plan.rows * u.fours;
+  u.part = parts; u.out = out; u.out_ld = out_ld; u.fours = plan.cols / 4; u.places = (int64_t)plan.rows * u.fours;
   u.part_elems = (int64_t)plan.rows * plan.cols; u.parts = plan.parts; u.f32 = a.out_f32; u.accumulate = a.accumulate;
   ADAPM_CUDA(launch_chained(true, linear8_sum_kernel, (unsigned)std::min<int64_t>((u.places + 255) / 256, 148 * 8), 256, 0, s, u));
   return ADAPM_OK;
@@ -894,13 +915,13 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
   Args a;
   std::memset(&a, 0, sizeof(a));
   a.plan = plan;
-  if (!encode_bytes(&a.a, x8, d->tokens, d->in_features, d->x8_ld, 128) || !encode_bytes(&a.b, w8, d->out_features, d->in_features, d->w8_ld, 128)) {
+  if (!encode_bytes(&a.a, x8, d->tokens, d->in_features, d->x8_ld, 128) || !encode_bytes(&a.b, w8, d->out_features, d->in_features, d->w8_ld, 128) ||
+      !encode_result(&a.o, y, 1, d->tokens, d->out_features, d->y_ld, d->y_dtype == ADAPM_TYPE_F32)) {
     set_error_text("cuTensorMapEncodeTiled failed for linear8");
     return ADAPM_ECUDA;
   }
   a.a_scale = xs; a.b_scale = ws;
   a.out = y; a.out_ld = d->y_ld; a.out_f32 = d->y_dtype == ADAPM_TYPE_F32;
-  a.wide = (uintptr_t)y % 32 == 0 && (a.out_f32 || d->y_ld % 16 == 0);
   a.status = (int32_t*)scratch;
   a.pairs = std::min(pairs, plan.items);
   ADAPM_CUDA((launch<FORWARD, false>(a, (cudaStream_t)stream)));
