@@ -60,6 +60,10 @@ __device__ __forceinline__ void wait_for_previous_kernel() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
+// The same in two steps, for a kernel that sets up its shared and tensor memory in between: nothing in global memory, read or written, comes
+// before the second.
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_what_is_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif
 
 constexpr int64_t kAlignElems = 8;      // block offsets: multiples of 8 elements

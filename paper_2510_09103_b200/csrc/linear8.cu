@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
   using S = Shape<OP, LONG>;
   extern __shared__ uint8_t dyn_smem[];
   __shared__ Shared<OP, LONG> sh;
-  wait_for_previous_kernel();
+  let_next_kernel_start();
   const uint32_t rank = cluster_rank();
   uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~(uintptr_t)1023);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = (int)(blockIdx.x >> 1);
@@ -174,16 +174,17 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
     }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 16); }
     sh.abort = 0;
-    if (rank == 0) *status = 0;                        // (the cluster barrier below orders it before what either CTA adds)
     mbar_fence_init();
   }
-  if (blockIdx.x == 0)
-    for (int i = a.pairs + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no pair
   if (warp == 1) {
     tmem_alloc<true>(&sh.tmem_base, 512);
     tmem_relinquish<true>();
   }
   tc_fence_before();
+  wait_for_what_is_before();
+  if (rank == 0 && threadIdx.x == 0) *status = 0;      // (the cluster barrier orders it before what either CTA adds)
+  if (blockIdx.x == 0)
+    for (int i = a.pairs + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no pair
   __syncthreads();
   cluster_sync();
   tc_fence_after();
@@ -428,14 +429,19 @@ struct StripArgs {
   int32_t columns, features, k, scale_groups, f32, accumulate, e4m3;
 };
 
-template <int OP>
+// LONG: K in segments that the epilogue adds up in registers, as above: for gradients in fp32, at most 128 columns wide.
+template <int OP, bool LONG>
 struct StripShape {
   static constexpr bool kGrad = OP != FORWARD;
   static constexpr int kThreads = kGrad ? 768 : 256;       // warp 0 loads, 1 issues the MMAs, 4 to 7 drain, 8 to 23 make numbers of codes
+  static constexpr int kAccs = LONG ? 2 : 1;
 };
+// LONG: registers of the launch, and as the four warps that issue, the four that drain and the sixteen that decode divide them.
+constexpr int kStripRegs = 80, kStripIssue = 56, kStripDrain = 200, kStripDecode = 56;
+static_assert(4 * kStripIssue + 4 * kStripDrain + 16 * kStripDecode <= 24 * kStripRegs, "a block has the registers that it was launched with");
 
 struct __align__(8) StripShared {
-  uint64_t full[kStripRing], empty[kStripRing], raw_full[kStripRing], raw_empty[kStripRing], tfull;
+  uint64_t full[kStripRing], empty[kStripRing], raw_full[kStripRing], raw_empty[kStripRing], tfull[2], tempty[2];
   uint32_t tmem_base;
   int abort;
 };
@@ -461,9 +467,9 @@ __device__ __forceinline__ void decode8(uint32_t c0, uint32_t c1, float s, uint3
 
 // A CTA puts its share of the features together, a thread four of them, for every few columns: eight loads of four sums on their way
 // at a time.
-template <int OP, int SPLIT>
+template <int OP, bool LONG, int SPLIT>
 __device__ __forceinline__ void put_together(const StripArgs& a, const uint8_t* sums, int rank, int f0, int c0) {
-  constexpr int kShare = 128 / SPLIT, kFours = kShare / 4, kStep = StripShape<OP>::kThreads / kFours, kAtOnce = 8 / SPLIT;
+  constexpr int kShare = 128 / SPLIT, kFours = kShare / 4, kStep = StripShape<OP, LONG>::kThreads / kFours, kAtOnce = 8 / SPLIT;
   const int mine = rank * kShare + 4 * ((int)threadIdx.x % kFours), f = f0 + mine, columns = min(a.plan.width, a.columns - c0);
   if (f >= a.features) return;
   float4 ws = make_float4(1.f, 1.f, 1.f, 1.f);
@@ -497,25 +503,28 @@ __device__ __forceinline__ void put_together(const StripArgs& a, const uint8_t* 
         for (int r = 1; r < SPLIT; ++r) {
           y[0] += __int_as_float(v[u][r].x); y[1] += __int_as_float(v[u][r].y); y[2] += __int_as_float(v[u][r].z); y[3] += __int_as_float(v[u][r].w);
         }
-        if (a.accumulate) {
+        if (LONG && a.accumulate) {
+          const float4 o = *reinterpret_cast<const float4*>(static_cast<const float*>(a.out) + to);
+          y[0] += o.x; y[1] += o.y; y[2] += o.z; y[3] += o.w;
+        } else if (a.accumulate) {
           const uint2 o = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.out) + to);
           y[0] += __uint_as_float(o.x << 16); y[1] += __uint_as_float(o.x & 0xffff0000u);
           y[2] += __uint_as_float(o.y << 16); y[3] += __uint_as_float(o.y & 0xffff0000u);
         }
       }
-      if (OP == FORWARD && a.f32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y[0], y[1], y[2], y[3]);
+      if (LONG || (OP == FORWARD && a.f32)) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y[0], y[1], y[2], y[3]);
       else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to) = make_uint2(pack_bf16x2_rn(y[0], y[1]), pack_bf16x2_rn(y[2], y[3]));
     }
   }
 }
 
-template <int OP>
-__global__ void __launch_bounds__(StripShape<OP>::kThreads) linear8_strip_kernel(const __grid_constant__ StripArgs a) {
-  using S = StripShape<OP>;
+template <int OP, bool LONG>
+__global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_strip_kernel(const __grid_constant__ StripArgs a) {
+  using S = StripShape<OP, LONG>;
   constexpr int kStep = S::kGrad ? 64 : 128;                       // K of a stage
   extern __shared__ uint8_t dyn_smem[];
   __shared__ StripShared sh;
-  wait_for_previous_kernel();
+  let_next_kernel_start();
   const StripPlan& p = a.plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, split = p.split, rank = split > 1 ? (int)cluster_rank() : 0;
   const int tile = (int)blockIdx.x / split, c_tile = tile / p.f_tiles, f0 = (tile - c_tile * p.f_tiles) * 128, c0 = c_tile * p.width;
@@ -524,99 +533,111 @@ __global__ void __launch_bounds__(StripShape<OP>::kThreads) linear8_strip_kernel
   uint8_t* const raw = ring + p.ring * bytes;
   volatile int* const abort = &sh.abort;
   int32_t* const status = a.status + blockIdx.x;
-  const uint32_t tmem_cols = p.width <= 32 ? 32 : p.width <= 64 ? 64 : p.width <= 128 ? 128 : 256;
+  const uint32_t acc_cols = p.width <= 32 ? 32 : p.width <= 64 ? 64 : p.width <= 128 ? 128 : 256, tmem_cols = S::kAccs * acc_cols;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < p.ring; ++i) { mbar_init(&sh.full[i], S::kGrad ? 1 + 4 : 1); mbar_init(&sh.empty[i], 1); }
     if (S::kGrad)
       for (int i = 0; i < p.raw; ++i) { mbar_init(&sh.raw_full[i], 1); mbar_init(&sh.raw_empty[i], 4); }
-    mbar_init(&sh.tfull, 1);
+    for (int i = 0; i < S::kAccs; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 4); }
     sh.abort = 0;
-    *status = 0;
     mbar_fence_init();
   }
-  if (blockIdx.x == 0)
-    for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no CTA
   if (warp == 1) {
     tmem_alloc(&sh.tmem_base, tmem_cols);
     tmem_relinquish();
   }
   tc_fence_before();
+  wait_for_what_is_before();
+  if (threadIdx.x == 0) *status = 0;
+  if (blockIdx.x == 0)
+    for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no CTA
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = sh.tmem_base;
-
-  if (warp == 0) {
-    // ------------------------------------------------------------------ the operands (forward), the other operand (gradients)
-    const bool leader = elect_one();
-    int stage = 0;
-    uint32_t phase = 0, issued = 0;
-    bool ok = true;
-    for (int i = 0; i < count; ++i) {
-      if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
-      if (leader) {
-        uint8_t* const dst = ring + stage * bytes;
-        uint64_t* const bar = &sh.full[stage];
-        const int k = (k0 + i) * kStep;
-        mbar_arrive_expect_tx(bar, (uint32_t)(S::kGrad ? bytes - 16384 : bytes));
-        if (OP == FORWARD) tma_load_box(dst, &a.codes, k, f0, bar);
-        if (OP == WEIGHT_GRAD) {
-          for (int c = 0; c < p.width; c += 64) tma_load_box(dst + 16384 + c * 128, &a.other, c0 + c, k, bar);
-        } else {
-          tma_load_box(dst + 16384, &a.other, k, c0, bar);
+  if (warp < 4) {
+    if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripIssue));
+    if (warp == 0) {
+      // ------------------------------------------------------------------ the operands (forward), the other operand (gradients)
+      const bool leader = elect_one();
+      int stage = 0;
+      uint32_t phase = 0, issued = 0;
+      bool ok = true;
+      for (int i = 0; i < count; ++i) {
+        if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+        if (leader) {
+          uint8_t* const dst = ring + stage * bytes;
+          uint64_t* const bar = &sh.full[stage];
+          const int k = (k0 + i) * kStep;
+          mbar_arrive_expect_tx(bar, (uint32_t)(S::kGrad ? bytes - 16384 : bytes));
+          if (OP == FORWARD) tma_load_box(dst, &a.codes, k, f0, bar);
+          if (OP == WEIGHT_GRAD) {
+            for (int c = 0; c < p.width; c += 64) tma_load_box(dst + 16384 + c * 128, &a.other, c0 + c, k, bar);
+          } else {
+            tma_load_box(dst + 16384, &a.other, k, c0, bar);
+          }
         }
+        __syncwarp();
+        ++issued;
+        if (++stage == p.ring) { stage = 0; phase ^= 1u; }
       }
-      __syncwarp();
-      ++issued;
-      if (++stage == p.ring) { stage = 0; phase ^= 1u; }
-    }
-    if (!ok) drain_ring<false>(sh.full, stage, phase, issued, p.ring, 0);
-  } else if (S::kGrad && warp == 2) {
-    // ------------------------------------------------------------------ codes, as they lie
-    const bool leader = elect_one();
-    int stage = 0;
-    uint32_t phase = 0, issued = 0;
-    bool ok = true;
-    for (int i = 0; i < count; ++i) {
-      if (!mbar_wait_warp(&sh.raw_empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
-      if (leader) {
-        mbar_arrive_expect_tx(&sh.raw_full[stage], kStripRawBytes);
-        tma_load_box(raw + stage * kStripRawBytes, &a.codes, f0, (k0 + i) * kStep, &sh.raw_full[stage]);
+      if (!ok) drain_ring<false>(sh.full, stage, phase, issued, p.ring, 0);
+    } else if (S::kGrad && warp == 2) {
+      // ------------------------------------------------------------------ codes, as they lie
+      const bool leader = elect_one();
+      int stage = 0;
+      uint32_t phase = 0, issued = 0;
+      bool ok = true;
+      for (int i = 0; i < count; ++i) {
+        if (!mbar_wait_warp(&sh.raw_empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+        if (leader) {
+          mbar_arrive_expect_tx(&sh.raw_full[stage], kStripRawBytes);
+          tma_load_box(raw + stage * kStripRawBytes, &a.codes, f0, (k0 + i) * kStep, &sh.raw_full[stage]);
+        }
+        __syncwarp();
+        ++issued;
+        if (++stage == p.raw) { stage = 0; phase ^= 1u; }
       }
-      __syncwarp();
-      ++issued;
-      if (++stage == p.raw) { stage = 0; phase ^= 1u; }
-    }
-    if (!ok) drain_ring<false>(sh.raw_full, stage, phase, issued, p.raw, 0);
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer (all lanes run, one issues)
-    const bool leader = elect_one();
-    int stage = 0;
-    uint32_t phase = 0;
-    bool ok = true;
-    constexpr bool kAmn = S::kGrad, kBmn = OP == WEIGHT_GRAD;
-    constexpr uint32_t kAstep = kAmn ? 128u : 2u, kBstep = kBmn ? 128u : 2u;
-    const uint32_t ring0 = uniform(smem_u32(ring)), d = uniform(tmem_base), dhi = desc_hi();
-    const uint32_t idesc = uniform(S::kGrad ? make_idesc(p.width, kAmn, kBmn, false, 128) : i8_idesc(p.width, 128));
-    for (int i = 0; i < count; ++i) {
-      if (!mbar_wait_warp(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
-      tc_fence_after();
-      const uint32_t slot = ring0 + (uint32_t)(stage * bytes), alo = desc_lo(slot, kAmn ? 8192u : 16u), blo = desc_lo(slot + 16384, kBmn ? 8192u : 16u);
-      if (leader) {
+      if (!ok) drain_ring<false>(sh.raw_full, stage, phase, issued, p.raw, 0);
+    } else if (warp == 1) {
+      // ------------------------------------------------------------------ MMA issuer (all lanes run, one issues)
+      const bool leader = elect_one();
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      constexpr bool kAmn = S::kGrad, kBmn = OP == WEIGHT_GRAD;
+      constexpr uint32_t kAstep = kAmn ? 128u : 2u, kBstep = kBmn ? 128u : 2u;
+      const uint32_t ring0 = uniform(smem_u32(ring)), d0 = uniform(tmem_base), dhi = desc_hi();
+      const uint32_t idesc = uniform(S::kGrad ? make_idesc(p.width, kAmn, kBmn, false, 128) : i8_idesc(p.width, 128));
+      const int each = LONG ? kSegLong : count;
+      uint32_t run = 0;
+      for (int at = 0; at < count && ok; at += each, ++run) {
+        const int acc = LONG ? (int)(run & 1) : 0;
+        if (LONG && !mbar_wait_warp(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+        if (LONG) tc_fence_after();
+        const uint32_t d = d0 + (uint32_t)acc * acc_cols;
+        for (int i = 0; i < min(each, count - at); ++i) {
+          if (!mbar_wait_warp(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t slot = ring0 + (uint32_t)(stage * bytes), alo = desc_lo(slot, kAmn ? 8192u : 16u), blo = desc_lo(slot + 16384, kBmn ? 8192u : 16u);
+          if (leader) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint64_t da = desc_join(alo + q * kAstep, dhi), db = desc_join(blo + q * kBstep, dhi);
-          if (S::kGrad) mma_bf16<false>(d, da, db, idesc, i || q ? 1u : 0u);
-          else mma_i8<false>(d, da, db, idesc, i || q ? 1u : 0u);
+            for (int q = 0; q < 4; ++q) {
+              const uint64_t da = desc_join(alo + q * kAstep, dhi), db = desc_join(blo + q * kBstep, dhi);
+              if (S::kGrad) mma_bf16<false>(d, da, db, idesc, i || q ? 1u : 0u);
+              else mma_i8<false>(d, da, db, idesc, i || q ? 1u : 0u);
+            }
+            mma_commit(&sh.empty[stage]);
+          }
+          __syncwarp();
+          if (++stage == p.ring) { stage = 0; phase ^= 1u; }
         }
-        mma_commit(&sh.empty[stage]);
+        if (ok && leader) mma_commit(&sh.tfull[acc]);
+        __syncwarp();
       }
-      __syncwarp();
-      if (++stage == p.ring) { stage = 0; phase ^= 1u; }
     }
-    if (ok && leader) mma_commit(&sh.tfull);
-    __syncwarp();
   } else if (S::kGrad && warp >= 8) {
+    if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripDecode));
     // ------------------------------------------------------------------ codes to bf16 numbers: the teams take turns; a warp has
     // four of every sixteen rows of K, eight lanes to a row, 16 codes to a lane
     const int team = (warp - 8) >> 2, row0 = 4 * (warp & 3) + (lane >> 3), j = lane & 7, sub = row0 & 7;
@@ -667,31 +688,69 @@ __global__ void __launch_bounds__(StripShape<OP>::kThreads) linear8_strip_kernel
       rs += kStripTeams;
       if (rs >= p.raw) { rs -= p.raw; raw_phase ^= 1u; }
     }
-  } else if (warp >= 4) {
-    // ------------------------------------------------------------------ this CTA's sums [columns][128], over the ring: all that was
+  } else {
+    if (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStripDrain));
+    // ------------------------------------------------------------------ this CTA's sums [columns][128], over the ring once all that was
     // in it has been multiplied
     bool ok = true;
-    if (lane == 0) ok = mbar_wait(&sh.tfull, 0, abort, status, ST_WAIT_TMEM_FULL, kWaitSpinDefault);
-    ok = __shfl_sync(0xffffffffu, ok, 0);
-    tc_fence_after();
-    if (ok) {
-      int* const sums = reinterpret_cast<int*>(ring) + 32 * (warp & 3) + lane;
-      for (int c = 0; c < p.width; c += 16) {
-        float v[16];
-        tmem_ld16(tmem_base + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)c, v);
-        tmem_ld_wait();
+    const uint32_t lane_addr = tmem_base + ((uint32_t)(32 * (warp & 3)) << 16);
+    int* const sums = reinterpret_cast<int*>(ring) + 32 * (warp & 3) + lane;
+    auto wait_full = [&](int acc, uint32_t parity) {
+      if (lane == 0) ok = mbar_wait(&sh.tfull[acc], parity, abort, status, ST_WAIT_TMEM_FULL, kWaitSpinDefault);
+      ok = __shfl_sync(0xffffffffu, ok, 0);
+      tc_fence_after();
+    };
+    if (LONG) {
+      float v[128];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sums[(c + e) * 128] = __float_as_int(v[e]);
+      for (int e = 0; e < 128; ++e) v[e] = 0.f;
+      const int n_seg = (count + kSegLong - 1) / kSegLong;
+#pragma unroll 1
+      for (int s = 0; s < n_seg && ok; ++s) {
+        const int acc = s & 1;
+        wait_full(acc, (uint32_t)(s >> 1) & 1u);
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < 128; c += 16) {
+          if (c < p.width) {
+            float x[16];
+            tmem_ld16(lane_addr + (uint32_t)acc * acc_cols + (uint32_t)c, x);
+            tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[c + e] += x[e];
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh.tempty[acc]);
+      }
+#pragma unroll
+      for (int c = 0; c < 128; ++c)
+        if (ok && c < p.width) sums[c * 128] = __float_as_int(v[c]);
+    } else {
+      wait_full(0, 0);
+      if (ok) {
+        for (int c = 0; c < p.width; c += 16) {
+          float v[16];
+          tmem_ld16(lane_addr + (uint32_t)c, v);
+          tmem_ld_wait();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sums[(c + e) * 128] = __float_as_int(v[e]);
+        }
       }
     }
     tc_fence_before();
+    __syncwarp();
+    if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripRegs));
   }
   __syncthreads();
+  // (not before: the warps that drain have taken theirs and given them back by now, so that nobody waits for registers of a warp that waits here)
+  if (LONG && (warp < 4 || warp >= 8)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStripRegs));
   if (split > 1) cluster_sync();
-  if (split == 1) put_together<OP, 1>(a, ring, rank, f0, c0);
-  else if (split == 2) put_together<OP, 2>(a, ring, rank, f0, c0);
-  else if (split == 4) put_together<OP, 4>(a, ring, rank, f0, c0);
-  else put_together<OP, 8>(a, ring, rank, f0, c0);
+  if (split == 1) put_together<OP, LONG, 1>(a, ring, rank, f0, c0);
+  else if (split == 2) put_together<OP, LONG, 2>(a, ring, rank, f0, c0);
+  else if (split == 4) put_together<OP, LONG, 4>(a, ring, rank, f0, c0);
+  else put_together<OP, LONG, 8>(a, ring, rank, f0, c0);
   __syncwarp();
   if (split > 1) cluster_sync();      // no CTA leaves while another may still read its sums
   if (warp == 1) {
@@ -752,6 +811,20 @@ int allow(int* resident, int sms) {
   return ADAPM_OK;
 }
 
+template <int OP, bool LONG>
+int allow_strips() {
+  ADAPM_CUDA(cudaFuncSetAttribute(linear8_strip_kernel<OP, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem + 1024));
+  if (LONG) {
+    cudaFuncAttributes fa;                  // (as above)
+    ADAPM_CUDA(cudaFuncGetAttributes(&fa, linear8_strip_kernel<OP, LONG>));
+    if (fa.numRegs < kStripRegs) {
+      set_error_text("linear8_strip_kernel was built with fewer registers than it divides among its warps");
+      return ADAPM_EUNSUPPORTED;
+    }
+  }
+  return ADAPM_OK;
+}
+
 // Pairs of CTAs that run at the same time on this device; the kernels' shared memory is allowed on the way.  (Once per device.)
 int pairs_of(int device, int* pairs) {
   static std::mutex mu;
@@ -761,15 +834,17 @@ int pairs_of(int device, int* pairs) {
   if (!known[device]) {
     int sms = 0;
     ADAPM_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
-    ADAPM_CUDA(cudaFuncSetAttribute(linear8_strip_kernel<FORWARD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem + 1024));
-    ADAPM_CUDA(cudaFuncSetAttribute(linear8_strip_kernel<INPUT_GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem + 1024));
-    ADAPM_CUDA(cudaFuncSetAttribute(linear8_strip_kernel<WEIGHT_GRAD>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStripSmem + 1024));
     int n = std::min(sms / 2, (int)kMostWords);
     int rc = allow<FORWARD, false>(&n, sms);
     if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, false>(&n, sms);
     if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, true>(&n, sms);
     if (rc == ADAPM_OK) rc = allow<WEIGHT_GRAD, false>(&n, sms);
     if (rc == ADAPM_OK) rc = allow<WEIGHT_GRAD, true>(&n, sms);
+    if (rc == ADAPM_OK) rc = allow_strips<FORWARD, false>();
+    if (rc == ADAPM_OK) rc = allow_strips<INPUT_GRAD, false>();
+    if (rc == ADAPM_OK) rc = allow_strips<INPUT_GRAD, true>();
+    if (rc == ADAPM_OK) rc = allow_strips<WEIGHT_GRAD, false>();
+    if (rc == ADAPM_OK) rc = allow_strips<WEIGHT_GRAD, true>();
     if (rc != ADAPM_OK) return rc;
     known[device] = std::max(1, n);
   }
@@ -811,10 +886,10 @@ Buffer bf16_or_f32(const void* p, int64_t rows, int64_t ld, int64_t cols, int32_
 Buffer codes_at(const void* p, int64_t rows, int64_t ld, int64_t cols) { return Buffer{p, 16, matrix_at(p, rows, ld, cols, 1)}; }
 Buffer floats_at(const float* p, int64_t n, int64_t align) { return Buffer{p, align, vector_at(p, n, 4)}; }
 
-template <int OP>
+template <int OP, bool LONG>
 cudaError_t launch_strips(const StripArgs& a, cudaStream_t s) {
   const size_t smem = (size_t)a.plan.ring * strip_stage_bytes(a.plan.width) + (size_t)a.plan.raw * kStripRawBytes + 1024;
-  return launch_clusters(true, (unsigned)a.plan.split, linear8_strip_kernel<OP>, (unsigned)a.plan.ctas, (unsigned)StripShape<OP>::kThreads, smem, s, a);
+  return launch_clusters(true, (unsigned)a.plan.split, linear8_strip_kernel<OP, LONG>, (unsigned)a.plan.ctas, (unsigned)StripShape<OP, LONG>::kThreads, smem, s, a);
 }
 
 // A gradient: [rows, cols] = A [rows, K] (or its transpose) times codes [K, cols].
@@ -836,7 +911,8 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
     t.out = out; t.out_ld = out_ld; t.status = (int32_t*)scratch;
     t.columns = (int32_t)(weight ? d.out_features : d.tokens); t.features = (int32_t)d.in_features;
     t.accumulate = weight && d.accumulate != 0; t.e4m3 = weight && d.x_code == ADAPM_CODE_E4M3;
-    ADAPM_CUDA(weight ? launch_strips<WEIGHT_GRAD>(t, s) : launch_strips<INPUT_GRAD>(t, s));
+    ADAPM_CUDA(out_dtype == ADAPM_TYPE_F32 ? (weight ? launch_strips<WEIGHT_GRAD, true>(t, s) : launch_strips<INPUT_GRAD, true>(t, s))
+                                           : (weight ? launch_strips<WEIGHT_GRAD, false>(t, s) : launch_strips<INPUT_GRAD, false>(t, s)));
     return ADAPM_OK;
   }
   Args a;
@@ -909,7 +985,7 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
     }
     t.xs = xs; t.ws = ws; t.out = y; t.out_ld = d->y_ld; t.status = (int32_t*)scratch;
     t.columns = (int32_t)d->tokens; t.features = (int32_t)d->out_features; t.f32 = d->y_dtype == ADAPM_TYPE_F32;
-    ADAPM_CUDA(launch_strips<FORWARD>(t, (cudaStream_t)stream));
+    ADAPM_CUDA((launch_strips<FORWARD, false>(t, (cudaStream_t)stream)));
     return ADAPM_OK;
   }
   Args a;

@@ -107,8 +107,10 @@ __host__ __device__ __forceinline__ int strip_stage_bytes(int width) { return 16
 inline StripPlan strip_plan_of(const adapm_linear8& d, int32_t which) {
   const int64_t features = which == FORWARD ? d.out_features : d.in_features, columns = which == WEIGHT_GRAD ? d.out_features : d.tokens;
   const int64_t k = which == FORWARD ? d.in_features : which == INPUT_GRAD ? d.out_features : d.tokens;
+  const bool f32_grad = which == INPUT_GRAD ? d.dx_dtype == ADAPM_TYPE_F32 : which == WEIGHT_GRAD && d.dweight_dtype == ADAPM_TYPE_F32;
+  const int widest = f32_grad ? kStripWidth / 2 : kStripWidth;          // (a thread keeps its row's sums)
   StripPlan p;
-  p.c_tiles = (int32_t)((columns + kStripWidth - 1) / kStripWidth);
+  p.c_tiles = (int32_t)((columns + widest - 1) / widest);
   p.width = (int32_t)round_up((columns + p.c_tiles - 1) / std::max(1, p.c_tiles), which == WEIGHT_GRAD ? 64 : 16);
   p.f_tiles = (int32_t)((features + 127) / 128);
   const int step = which == FORWARD ? 128 : 64;
@@ -130,13 +132,13 @@ inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const Strip
   if (s.ctas > kMostWords) return false;
   const bool f32 = which == INPUT_GRAD ? d.dx_dtype == ADAPM_TYPE_F32 : which == WEIGHT_GRAD && d.dweight_dtype == ADAPM_TYPE_F32;
   const int each = (s.stages + s.split - 1) / s.split;
-  if (f32 || (which != FORWARD && each > kShortStages)) return false;
+  if (which != FORWARD && !f32 && each > kShortStages) return false;
   const bool grad = which != FORWARD;
   int levels = 0;                                     // of the cluster
   while ((1 << levels) < s.split) ++levels;
   const double rounds = (double)((s.ctas + 2 * kPlannedPairs - 1) / (2 * kPlannedPairs));
   const double stage = grad ? 0.36 + 0.0005 * s.width : 0.16 + 0.0006 * s.width, level = grad ? 0.4 + 0.006 * s.width : 0.3 + 0.0025 * s.width;
-  const double strips = 2.0 + rounds * ((grad ? 2.3 : 3.2) + 0.012 * s.width + each * stage + levels * level);
+  const double strips = 2.0 + rounds * ((f32 ? 4.3 : grad ? 2.3 : 3.2) + 0.012 * s.width + each * stage + levels * level);
   const double pair_rounds = (double)((p.items + kPlannedPairs - 1) / kPlannedPairs);
   double pairs = 6.0 + pair_rounds * (1.0 + 0.31 * p.each);
   if (grad) pairs += 2.0 + 5e-7 * p.stages * 64.0 * p.cols + (p.parts > 1 ? 2.5 + 5e-7 * p.rows * (double)p.cols * p.parts : 0);
