@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
   } else {
     if (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kLongDrain));
     // ------------------------------------------------------------------ epilogue: a thread has one row of the tile and, by its
-    // group of four warps, the lower or upper half of the columns
+    // group of four warps, the first 128 columns or the others
     const int q = 32 * (warp & 3) + lane, grp = (warp - 4) >> 2;
     const uint32_t lane_addr = (uint32_t)(32 * (warp & 3)) << 16;
     Outlet out = {&a.o, ring + S::kStages * kStageBytes + (warp - 4) * kBoxBytesOut, lane};
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
       if (lane == 0) mbar_arrive_relaxed_at(shared_of(&sh.tempty[acc], 0));
     };
     for (int i = pair; ok && a.plan.item(i, t); i += a.pairs) {
-      const int row = t.m0 + (int)rank * 128 + q, half = t.bn / 2, col0 = t.n0 + grp * half;
+      const int row = t.m0 + (int)rank * 128 + q, mine = grp ? t.bn - 128 : min(t.bn, 128), col0 = t.n0 + grp * 128;
       if (LONG) {
         float v[128];
         int n_seg, each;
@@ -302,16 +302,16 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
           const int acc = (int)(run & 1);
           wait_full(acc);
           if (!ok) break;
-          const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * half);
+          const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * 128);
           if (s == 0) {
 #pragma unroll
             for (int c = 0; c < 128; c += 16)
-              if (c < half) tmem_ld16(at + c, v + c);
+              if (c < mine) tmem_ld16(at + c, v + c);
             tmem_ld_wait();
           } else {
 #pragma unroll
             for (int c = 0; c < 128; c += 32) {
-              if (c < half) {
+              if (c < mine) {
                 float x[32];
                 tmem_ld16(at + c, x);
                 tmem_ld16(at + c + 16, x + 16);
@@ -326,37 +326,45 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         if (!ok) break;
 #pragma unroll
         for (int c = 0; c < 128; c += 32)
-          if (c < half) finish32(a, t, out, row - lane, col0 + c, v + c);
+          if (c < mine) finish32(a, t, out, row - lane, col0 + c, v + c);
       } else {
         const int acc = (int)(run & 1);
         const float xs = OP == FORWARD && row < a.plan.rows ? a.a_scale[row] : 0.f;
+        // (the columns' scales are asked for a chunk of columns ahead: 2048 x 2736 x 1024 forward 13.3 -> 11.4 us)
+        float4 ws[8];
+        auto scales_of = [&](int col) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) ws[e] = col + 4 * e < a.plan.cols ? __ldg(reinterpret_cast<const float4*>(a.b_scale + col + 4 * e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        };
+        if (OP == FORWARD) scales_of(col0);
         wait_full(acc);
         if (!ok) break;
-        const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * half);
+        const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * 128);
 #pragma unroll
         for (int c = 0; c < 128; c += 32) {
-          if (c >= half) continue;
+          if (c >= mine) continue;
           __syncwarp();
           float v[32];
           tmem_ld16(at + c, v);
           tmem_ld16(at + c + 16, v + 16);
           tmem_ld_wait();
-          if (c + 32 >= half) release(acc);
+          if (c + 32 >= mine) release(acc);
           const int col = col0 + c;
           if (OP == FORWARD) {
 #pragma unroll
-            for (int e = 0; e < 32; e += 4) {
-              const float4 ws = col + e < a.plan.cols ? __ldg(reinterpret_cast<const float4*>(a.b_scale + col + e)) : make_float4(0.f, 0.f, 0.f, 0.f);
-              v[e] = (float)__float_as_int(v[e]) * xs * ws.x;
-              v[e + 1] = (float)__float_as_int(v[e + 1]) * xs * ws.y;
-              v[e + 2] = (float)__float_as_int(v[e + 2]) * xs * ws.z;
-              v[e + 3] = (float)__float_as_int(v[e + 3]) * xs * ws.w;
+            for (int e = 0; e < 8; ++e) {
+              v[4 * e] = (float)__float_as_int(v[4 * e]) * xs * ws[e].x;
+              v[4 * e + 1] = (float)__float_as_int(v[4 * e + 1]) * xs * ws[e].y;
+              v[4 * e + 2] = (float)__float_as_int(v[4 * e + 2]) * xs * ws[e].z;
+              v[4 * e + 3] = (float)__float_as_int(v[4 * e + 3]) * xs * ws[e].w;
             }
+            if (c + 32 < mine) scales_of(col + 32);
             out.put32(v, col, row - lane, 0, a.out_f32, a.plan.rows, a.plan.cols);
           } else {
             finish32(a, t, out, row - lane, col, v);
           }
         }
+        if (mine <= 0) release(acc);
         ++run;
       }
     }

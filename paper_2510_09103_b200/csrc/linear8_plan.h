@@ -14,7 +14,7 @@ namespace linear8 {
 
 enum : int32_t { FORWARD = ADAPM_LINEAR8_FORWARD, INPUT_GRAD = ADAPM_LINEAR8_INPUT_GRAD, WEIGHT_GRAD = ADAPM_LINEAR8_WEIGHT_GRAD };
 
-constexpr int kTile = 256;                       // rows and columns of a pair's tile of the result
+constexpr int kTile = 256;                       // rows of a pair's tile of the result, and its columns at most
 constexpr int kBand = 16;                        // row tiles that share the columns' operand at a time
 constexpr int kMostWords = 2048;                 // status words, one per pair of CTAs or per CTA, at the head of the scratch
 constexpr int kHeadBytes = 4 * kMostWords;
@@ -25,7 +25,7 @@ struct Cut { int m0, n0, bn, k0, count, part; };
 
 // A result of `rows` x `cols`, K of `stages` stages, cut into `parts` parts of `each` stages (the last may be shorter).
 struct Plan {
-  int32_t rows, cols, m_tiles, n_tiles, stages, parts, each, items;
+  int32_t rows, cols, m_tiles, n_tiles, width, stages, parts, each, items;
   int64_t part_at, bytes;        // of the scratch: the parts of K (before them: bf16 numbers of a gradient's codes), and all of it
 
   // Item i; false past the last.  Tiles go down a band of kBand row tiles, column after column.
@@ -35,36 +35,41 @@ struct Plan {
     const int left = m_tiles - band * kBand, high = left < kBand ? left : kBand, n = in / high;
     t.part = i - tile * parts;
     t.m0 = (band * kBand + in - n * high) * kTile;
-    t.n0 = n * kTile;
-    t.bn = cols - t.n0 <= kTile / 2 ? kTile / 2 : kTile;
+    t.n0 = n * width;
+    const int there = (cols - t.n0 + 63) / 64 * 64;
+    t.bn = there < width ? there : width;
     t.k0 = t.part * each;
     t.count = stages - t.k0 < each ? stages - t.k0 : each;
     return true;
   }
 };
 
-// K is cut where there are fewer tiles than pairs of CTAs, so that its parts, summed by one more launch, take less time.  In units of a stage (512
-// cycles): an item takes its stages and four more, the sums a launch of about eight and the parts' way to memory and back.
+// How wide the tiles are, and into how many parts K is cut (summed by one more launch, where there are fewer tiles than pairs of CTAs): what takes
+// least.  In units of a stage of 256 columns (512 cycles): an item takes its stages, narrower ones not quite in
+// proportion, and four more, the sums a launch of about eight and the
+// parts' way to memory and back.  (2048 x 6400 x 1600: 56 tiles of 256 columns for 74 pairs, or 72 of 192.)
 inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool grad) {
   Plan p;
-  const bool may_cut = grad;
   p.rows = (int32_t)rows; p.cols = (int32_t)cols;
-  p.m_tiles = (int32_t)((rows + kTile - 1) / kTile); p.n_tiles = (int32_t)((cols + kTile - 1) / kTile);
+  p.m_tiles = (int32_t)((rows + kTile - 1) / kTile);
   p.stages = (int32_t)((k + stage_k - 1) / stage_k);
-  const int64_t tiles = (int64_t)p.m_tiles * p.n_tiles;
-  p.parts = 1; p.each = p.stages;
-  double best = 0;
-  for (int n = 1; n <= (may_cut && tiles > 0 && tiles < kPlannedPairs ? std::min(64, p.stages / 4) : 0); ++n) {
-    const int each = (p.stages + n - 1) / n, parts = (p.stages + each - 1) / each;
-    if (parts != n) continue;
-    const double rounds = (double)((tiles * parts + kPlannedPairs - 1) / kPlannedPairs);
-    const double t = rounds * (each + 4) + (parts > 1 ? 8 + 2.5 * (double)(rows * cols) * parts / 1e6 : 0);
-    if (n == 1 || t < best) { best = t; p.parts = parts; p.each = each; }
+  double best = -1;
+  for (int width = kTile; width >= 128; width -= 64) {
+    const int64_t n_tiles = (cols + width - 1) / width, tiles = p.m_tiles * n_tiles;
+    const int most = grad && tiles < kPlannedPairs ? std::max(1, std::min(64, p.stages / 4)) : 1;
+    for (int n = 1; n <= most; ++n) {
+      const int each = (p.stages + n - 1) / n, parts = each ? (p.stages + each - 1) / each : 1;
+      if (parts != n) continue;
+      const double rounds = (double)((tiles * parts + kPlannedPairs - 1) / kPlannedPairs);
+      const double t = rounds * (each * (0.2 + 0.8 / 256 * width) + 4) + (parts > 1 ? 8 + 2.5 * (double)(rows * cols) * parts / 1e6 : 0);
+      if (best >= 0 && t >= best) continue;
+      best = t;
+      p.width = width; p.n_tiles = (int32_t)n_tiles; p.parts = parts; p.each = each;
+      p.items = (int32_t)(tiles * parts);
+    }
   }
-  p.items = (int32_t)(tiles * p.parts);
   p.part_at = kHeadBytes + (grad ? round_up(k * cols * 2, 256) : 0);
-  p.bytes = p.part_at;
-  if (p.parts > 1) p.bytes += round_up((int64_t)p.parts * rows * cols * 4, 256);
+  p.bytes = p.part_at + (p.parts > 1 ? round_up((int64_t)p.parts * rows * cols * 4, 256) : 0);
   return p;
 }
 
@@ -140,7 +145,7 @@ inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const Strip
   const double stage = grad ? 0.36 + 0.0005 * s.width : 0.16 + 0.0006 * s.width, level = grad ? 0.4 + 0.006 * s.width : 0.3 + 0.0025 * s.width;
   const double strips = 2.0 + rounds * ((f32 ? 4.3 : grad ? 2.3 : 3.2) + 0.012 * s.width + each * stage + levels * level);
   const double pair_rounds = (double)((p.items + kPlannedPairs - 1) / kPlannedPairs);
-  double pairs = 6.0 + pair_rounds * (1.0 + 0.31 * p.each);
+  double pairs = 6.0 + pair_rounds * (1.0 + 0.31 * p.each * (0.2 + 0.8 / 256 * p.width));
   if (grad) pairs += 2.0 + 5e-7 * p.stages * 64.0 * p.cols + (p.parts > 1 ? 2.5 + 5e-7 * p.rows * (double)p.cols * p.parts : 0);
   return strips < pairs;
 }

@@ -26,9 +26,9 @@ static std::string wrong(const adapm_linear8& d, int which) {
   Cut t;
   int n = 0;
   for (; p.item(n, t); ++n) {
-    if (t.m0 < 0 || t.m0 >= p.rows || t.m0 % kTile || t.n0 < 0 || t.n0 >= p.cols || t.n0 % kTile) return "an item's tile";
-    if (t.bn != kTile && t.bn != kTile / 2) return "an item's columns";
-    if (t.n0 + t.bn < p.cols && t.bn != kTile) return "columns left out";
+    if (t.m0 < 0 || t.m0 >= p.rows || t.m0 % kTile || t.n0 < 0 || t.n0 >= p.cols || t.n0 % p.width) return "an item's tile";
+    if (t.bn % 64 || t.bn < 64 || t.bn > p.width || p.width > kTile) return "an item's columns";
+    if (t.n0 + t.bn < p.cols && t.bn != p.width) return "columns left out";
     if (t.count < 1 || t.part < 0 || t.part >= p.parts) return "an item's part";
     auto& of = tiles[{t.m0, t.n0}];
     const int at = of.empty() ? 0 : of.back().k0 + of.back().count;
@@ -36,7 +36,7 @@ static std::string wrong(const adapm_linear8& d, int which) {
     of.push_back(t);
   }
   if (n != p.items || p.item(n, t)) return "the number of items";
-  if ((int64_t)tiles.size() != (int64_t)p.m_tiles * p.n_tiles || (int64_t)p.m_tiles * kTile < p.rows || (int64_t)p.n_tiles * kTile < p.cols) return "tiles left out";
+  if ((int64_t)tiles.size() != (int64_t)p.m_tiles * p.n_tiles || (int64_t)p.m_tiles * kTile < p.rows || (int64_t)p.n_tiles * p.width < p.cols) return "tiles left out";
   const StripPlan q = strip_plan_of(d, which);
   const int64_t features = which == FORWARD ? d.out_features : d.in_features, columns = which == WEIGHT_GRAD ? d.out_features : d.tokens;
   if (q.width < 1 || q.width > 256 || q.width % (which == WEIGHT_GRAD ? 64 : 16)) return "a strip's width";
