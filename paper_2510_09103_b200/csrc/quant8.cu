@@ -142,10 +142,9 @@ __device__ __forceinline__ Scale scale_of(uint32_t m, int mode) {
 }
 
 // The codes of four elements.  F32: they may have more than the 8 bits of bf16.
-template <bool F32>
-__device__ __forceinline__ uint32_t encode4(const float* x, const Scale& k, int mode) {
-  if (!(k.s <= 3.402823466e38f)) return 0;
-  if (mode == E4M3_POW2) {
+template <bool F32, int MODE>
+__device__ __forceinline__ uint32_t encode4(const float* x, const Scale& k) {
+  if (MODE == E4M3_POW2) {
     uint16_t lo, hi;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[1] * k.inv), "f"(x[0] * k.inv));
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[3] * k.inv), "f"(x[2] * k.inv));
@@ -159,7 +158,7 @@ __device__ __forceinline__ uint32_t encode4(const float* x, const Scale& k, int 
     const float2 q = fma2(make_float2(x[e], x[e + 1]), make_float2(k.inv, k.inv), make_float2(kMagic, kMagic));
     t[e] = q.x; t[e + 1] = q.y;
   }
-  if (mode == INT8_MAX_SCALE) {
+  if (MODE == INT8_MAX_SCALE) {
     // 1 / s is rounded, so that a quotient next to half a step may have gone the wrong way.  What is left, d = x - code s, has no
     // rounding (it is a multiple of half the last place of s, and below s), and code + d / s is rounded once more.  With s = f 2^e, 1 <= f < 2, a quotient
     // that is not half a step is at least 2^-24 / f away from it, and d (1 / s) is off by f 2^-26 at most, which is less.  A quotient
@@ -190,15 +189,22 @@ __device__ __forceinline__ uint32_t encode4(const float* x, const Scale& k, int 
   return __byte_perm(__byte_perm(__float_as_uint(t[0]), __float_as_uint(t[1]), 0x0040), __byte_perm(__float_as_uint(t[2]), __float_as_uint(t[3]), 0x0040), 0x5410);
 }
 
+template <bool F32, int MODE>
+__device__ __forceinline__ void encode16(const float* x, const Scale& k, uint32_t* q) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) q[i] = encode4<F32, MODE>(x + 4 * i, k);
+}
+// (the form is chosen once for sixteen elements; once for four: 8192 x 14336 in groups 62 us, 57 now)
 template <typename T>
 __device__ __forceinline__ void encode16(const Eight<T>* x, const Scale& k, int mode, uint32_t* q) {
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float v[8];
-    x[h].unpack(v);
-    q[2 * h] = encode4<sizeof(T) == 4>(v, k, mode);
-    q[2 * h + 1] = encode4<sizeof(T) == 4>(v + 4, k, mode);
-  }
+  constexpr bool kF32 = sizeof(T) == 4;
+  float v[16];
+  x[0].unpack(v);
+  x[1].unpack(v + 8);
+  if (mode == INT8_POW2) encode16<kF32, INT8_POW2>(v, k, q);
+  else if (mode == INT8_MAX_SCALE) encode16<kF32, INT8_MAX_SCALE>(v, k, q);
+  else encode16<kF32, E4M3_POW2>(v, k, q);
+  if (!(k.s <= 3.402823466e38f)) q[0] = q[1] = q[2] = q[3] = 0;
 }
 
 struct QuantArgs {
@@ -284,7 +290,9 @@ __global__ void __launch_bounds__(256) quant8_odd_groups_kernel(const QuantArgs 
     const Scale k = scale_of(__reduce_max_sync(0xffffffffu, __float_as_uint(m)), a.mode);
     const int64_t group = base / 128 + g;
     if (lane == 0 && group < a.groups) a.scales[row * a.groups + group] = k.s;
-    q[g] = encode4<sizeof(T) == 4>(v + 4 * g, k, a.mode);
+    constexpr bool kF32 = sizeof(T) == 4;
+    q[g] = a.mode == INT8_POW2 ? encode4<kF32, INT8_POW2>(v + 4 * g, k) : a.mode == INT8_MAX_SCALE ? encode4<kF32, INT8_MAX_SCALE>(v + 4 * g, k) : encode4<kF32, E4M3_POW2>(v + 4 * g, k);
+    if (!(k.s <= 3.402823466e38f)) q[g] = 0;
   }
   put_codes<false>(codes, base, lane, 32, a.cols, false, q);
 }
