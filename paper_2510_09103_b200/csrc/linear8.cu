@@ -767,6 +767,95 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
   }
 }
 
+// ---- forward, one or two tokens --------------------------------------------------------------------------------------
+// The weight once past the tokens: a warp has kRowsOfWarp rows of the weight, 512 bytes of each at a time, which a lane multiplies four codes at a
+// time (dp4a) with those of every token; `split` warps of a CTA share a row's K.  Bound by HBM: the rows are read end to end, which
+// the strips' boxes of 128 x 128 bytes do not do (1 x 14336 x 4096, codes from HBM: 13.2 -> 11.5 us = 5.1 TB/s).  With more tokens the
+// products take longer than the rows' way (4 tokens 15.5 us from L2, strips 10.5).
+constexpr int kRowsOfWarp = 4, kLineThreads = 256;
+
+struct LineArgs {
+  const uint8_t *x, *w;
+  const float *xs, *ws;
+  void* y;
+  int32_t* status;
+  int64_t y_ld;
+  int32_t x_ld, w_ld, out, in, split, f32;
+};
+
+// The 16 codes of a row from byte k on, as far as the row goes (rows are multiples of eight long).
+__device__ __forceinline__ uint4 codes16(const uint8_t* row, int k, int n) {
+  if (k + 16 <= n) return __ldg(reinterpret_cast<const uint4*>(row + k));
+  uint4 q = make_uint4(0, 0, 0, 0);
+  if (k + 8 <= n) { const uint2 h = __ldg(reinterpret_cast<const uint2*>(row + k)); q.x = h.x; q.y = h.y; }
+  return q;
+}
+__device__ __forceinline__ int dot16(const uint4& a, const uint4& b, int sum) {
+  sum = __dp4a((int)a.x, (int)b.x, sum);
+  sum = __dp4a((int)a.y, (int)b.y, sum);
+  sum = __dp4a((int)a.z, (int)b.z, sum);
+  return __dp4a((int)a.w, (int)b.w, sum);
+}
+
+template <int TOKENS>
+__global__ void __launch_bounds__(kLineThreads) linear8_line_kernel(const LineArgs a) {
+  __shared__ int part[8][kRowsOfWarp][TOKENS];
+  wait_for_previous_kernel();
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < kMostWords; i += kLineThreads) a.status[i] = 0;      // (nothing here waits)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, groups = 8 / a.split, group = warp / a.split, share = warp - group * a.split;
+  const int n0 = ((int)blockIdx.x * groups + group) * kRowsOfWarp;
+  const uint8_t* rows[kRowsOfWarp];
+#pragma unroll
+  for (int r = 0; r < kRowsOfWarp; ++r) rows[r] = a.w + (int64_t)min(n0 + r, a.out - 1) * a.w_ld;
+  int sum[kRowsOfWarp][TOKENS] = {};
+  const int step = 512 * a.split;
+  auto add = [&](const uint4* w, int k) {
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+      const uint4 x = codes16(a.x + (int64_t)t * a.x_ld, k, a.in);
+#pragma unroll
+      for (int r = 0; r < kRowsOfWarp; ++r) sum[r][t] = dot16(w[r], x, sum[r][t]);
+    }
+  };
+  if (n0 < a.out) {
+    int k = 512 * share + 16 * lane;
+    for (; k + step < a.in; k += 2 * step) {            // two pieces of every row on their way
+      uint4 w[2][kRowsOfWarp];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int r = 0; r < kRowsOfWarp; ++r) w[u][r] = codes16(rows[r], k + u * step, a.in);
+      add(w[0], k);
+      add(w[1], k + step);
+    }
+    if (k < a.in) {
+      uint4 w[kRowsOfWarp];
+#pragma unroll
+      for (int r = 0; r < kRowsOfWarp; ++r) w[r] = codes16(rows[r], k, a.in);
+      add(w, k);
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < kRowsOfWarp; ++r)
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+      const int all = __reduce_add_sync(0xffffffffu, sum[r][t]);
+      if (lane == 0) part[warp][r][t] = all;
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < groups * kRowsOfWarp * TOKENS; i += kLineThreads) {
+    const int r = i % kRowsOfWarp, t = i / kRowsOfWarp % TOKENS, g = i / (kRowsOfWarp * TOKENS);
+    const int n = ((int)blockIdx.x * groups + g) * kRowsOfWarp + r;
+    if (n >= a.out) continue;
+    int all = 0;
+    for (int s = 0; s < a.split; ++s) all += part[g * a.split + s][r][t];
+    const float y = (float)all * a.xs[t] * a.ws[n];
+    if (a.f32) static_cast<float*>(a.y)[(int64_t)t * a.y_ld + n] = y;
+    else static_cast<uint16_t*>(a.y)[(int64_t)t * a.y_ld + n] = (uint16_t)pack_bf16x2_rn(y, 0.f);
+  }
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------
 
 // `parts` results [rows, cols], one behind the other, in boxes of 32 rows of 128 bytes with the 128-byte swizzle.
@@ -884,10 +973,8 @@ int check_buffers(std::initializer_list<Buffer> in, const Buffer& out, void* scr
     set_error_text(overlap);
     return ADAPM_EINVAL;
   }
-  int rc = check_on_this_device({out.p, scratch}, device);
-  for (const Buffer& b : in)
-    if (rc == ADAPM_OK) rc = check_on_this_device({b.p}, device);
-  return rc;
+  const Buffer* const at = in.begin();
+  return check_on_this_device({out.p, scratch, at[0].p, at[1].p, at[2].p, in.size() > 3 ? at[3].p : nullptr}, device);
 }
 
 Buffer bf16_or_f32(const void* p, int64_t rows, int64_t ld, int64_t cols, int32_t dtype) { return Buffer{p, 16, matrix_at(p, rows, ld, cols, type_bytes(dtype))}; }
@@ -981,6 +1068,21 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
                      "adapm_linear8_forward: the output or the scratch overlaps another buffer", &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
   if (rc != ADAPM_OK) return rc;
+  if (d->tokens <= kLineTokens) {
+    LineArgs l;
+    l.x = static_cast<const uint8_t*>(x8); l.w = static_cast<const uint8_t*>(w8); l.xs = xs; l.ws = ws; l.y = y;
+    l.status = (int32_t*)scratch; l.y_ld = d->y_ld; l.x_ld = (int32_t)d->x8_ld; l.w_ld = (int32_t)d->w8_ld;
+    l.out = (int32_t)d->out_features; l.in = (int32_t)d->in_features; l.f32 = d->y_dtype == ADAPM_TYPE_F32;
+    // as many warps as give every SM sixteen, a piece of K for each
+    const int64_t row_groups = (d->out_features + kRowsOfWarp - 1) / kRowsOfWarp;
+    l.split = 1;
+    while (l.split < 8 && row_groups * l.split < 2 * kPlannedPairs * 16 && 512 * l.split < d->in_features) l.split *= 2;
+    const unsigned grid = (unsigned)((row_groups * l.split + 7) / 8);
+    cudaStream_t s = (cudaStream_t)stream;
+    ADAPM_CUDA(d->tokens == 1 ? launch_chained(true, linear8_line_kernel<1>, grid, kLineThreads, 0, s, l)
+                             : launch_chained(true, linear8_line_kernel<2>, grid, kLineThreads, 0, s, l));
+    return ADAPM_OK;
+  }
   const StripPlan strip = strip_plan_of(*d, FORWARD);
   if (strips_are_faster(*d, FORWARD, strip, plan)) {
     StripArgs t;

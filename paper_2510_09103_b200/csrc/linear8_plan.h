@@ -104,6 +104,7 @@ struct StripPlan {
   __host__ __device__ int first(int part) const { return (int)((int64_t)stages * part / split); }      // stage of a part of K
 };
 
+constexpr int kLineTokens = 2;                   // up to so many a forward product goes by rows of the weight, end to end
 constexpr int kStripWidth = 256, kStripSmem = 224 * 1024, kStripRing = 8;
 constexpr int kStripTeams = 4, kStripRawBytes = 64 * 128;        // gradients: stages that are decoded at the same time; bytes of a stage's codes
 
