@@ -25,15 +25,16 @@ using namespace tc;
 
 constexpr int kOperandBytes = 16384;             // of one CTA and stage: 128 rows or columns of an operand, 128 bytes of K (or the reverse)
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kBoxBytesOut = 4096;                // of a warp's box of results
+constexpr int kBoxBytesOut = 2048;                // of a warp's box of results
 constexpr int kSegLong = 4, kSegShort = 64;      // stages of 64 K between two sums in registers: gradients in fp32, long ones in bf16
 
 template <int OP, bool LONG>
 struct Shape {
   static constexpr bool kGrad = OP != FORWARD;
-  static constexpr int kThreads = 384;           // four warps that issue, eight that drain
+  static constexpr int kDrain = LONG ? 8 : 16;   // warps that drain, after four that issue
+  static constexpr int kThreads = 32 * (4 + kDrain);
   static constexpr int kStages = 6;
-  static constexpr int kSmem = kStages * kStageBytes + 8 * kBoxBytesOut + 1024;
+  static constexpr int kSmem = kStages * kStageBytes + kDrain * kBoxBytesOut + 1024;
 };
 // LONG: registers of the launch, and as the first four and the other eight warps divide them (the eight keep 128 sums each).
 constexpr int kLongRegs = 168, kLongIssue = 88, kLongDrain = 208;
@@ -97,54 +98,52 @@ __device__ __forceinline__ void add_row32(const void* base, int64_t at, float* x
   }
 }
 
-// A warp's way out: 32 rows of 128 bytes (32 columns in fp32, 64 in bf16) are put into its box in shared memory, with the 128-byte
+// A warp's way out: 32 rows of 64 bytes (16 columns in fp32, 32 in bf16) are put into its box in shared memory, with the 64-byte
 // swizzle, and stored as a whole by TMA, which leaves out what the result does not have.  (Every thread storing 32 bytes of a row of its
-// own: weight gradient of 1 x 14336 x 4096 36 to 42 us, with a box 27 to 30; two boxes per warp and five stages of operands instead of six: 2048 x
-// 4096 x 4096 53 -> 56.)
+// own: weight gradient of 1 x 14336 x 4096 36 to 42 us, with a box 27.  Eight warps with boxes of 128 bytes for 128 columns each instead of
+// sixteen for 64: forward 8192 x 14336 x 512 92 us for 76.)
 struct Outlet {
   const CUtensorMap* map;
   uint8_t* box;
   int lane;
-  // 32 columns, the c-th on from column col0, which is a multiple of 64, of the rows from `row0` on, the lane's own in x; `part`: of K.  (Which half of
-  // a box they are goes by c, which the compiler knows: by the column, weight gradient of 1 x 14336 x 4096 27 -> 32 us.)
-  __device__ __forceinline__ void put32(const float* x, int col0, int c, int row0, int part, bool f32, int rows, int cols) {
-    const bool first = f32 || (c & 32) == 0, last = f32 || (c & 32) != 0;
-    const int col = col0 + c;
-    if (first) {
+  // 32 columns from column `col` on of the rows from `row0` on, the lane's own in x; `part`: of K.
+  __device__ __forceinline__ void put32(const float* x, int col, int row0, int part, bool f32, int rows, int cols) {
+    uint8_t* const line = box + lane * 64;
+    const int swap = (lane >> 1) & 3;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (!f32 && h == 1) break;
       if (lane == 0) bulk_wait_group_read<0>();
       __syncwarp();
-    }
-    uint8_t* const line = box + lane * 128;
-    if (f32) {
+      if (f32) {
 #pragma unroll
-      for (int c = 0; c < 8; ++c)
-        *reinterpret_cast<float4*>(line + ((c ^ (lane & 7)) * 16)) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
-    } else {
+        for (int c = 0; c < 4; ++c)
+          *reinterpret_cast<float4*>(line + ((c ^ swap) * 16)) = make_float4(x[16 * h + 4 * c], x[16 * h + 4 * c + 1], x[16 * h + 4 * c + 2], x[16 * h + 4 * c + 3]);
+      } else {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t w[4];
+        for (int c = 0; c < 4; ++c) {
+          uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2_rn(x[8 * c + 2 * e], x[8 * c + 2 * e + 1]);
-        put4(line + (((c + (first ? 0 : 4)) ^ (lane & 7)) * 16), w);
+          for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2_rn(x[8 * c + 2 * e], x[8 * c + 2 * e + 1]);
+          put4(line + ((c ^ swap) * 16), w);
+        }
       }
-    }
-    if (!last) return;
-    fence_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      const int x0 = f32 ? col : col - 32;
-      if (row0 < rows && x0 < cols) tma_store_box3(map, x0, row0, part, box);
-      bulk_commit_group();
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        if (row0 < rows && col + 16 * h < cols) tma_store_box3(map, col + 16 * h, row0, part, box);
+        bulk_commit_group();
+      }
     }
   }
 };
 
 // What a gradient's item does with 32 columns of its sums.
-__device__ __forceinline__ void finish32(const Args& a, const Cut& t, Outlet& out, int row0, int col0, int c, float* x) {
-  const int row = row0 + out.lane, col = col0 + c;
+__device__ __forceinline__ void finish32(const Args& a, const Cut& t, Outlet& out, int row0, int col, float* x) {
+  const int row = row0 + out.lane;
   if (a.accumulate && a.plan.parts == 1 && row < a.plan.rows) add_row32(a.out, (int64_t)row * a.out_ld + col, x, a.plan.cols - col, a.out_f32);
   __syncwarp();
-  out.put32(x, col0, c, row0, t.part, a.plan.parts > 1 || a.out_f32, a.plan.rows, a.plan.cols);
+  out.put32(x, col, row0, t.part, a.plan.parts > 1 || a.out_f32, a.plan.rows, a.plan.cols);
 }
 
 // An item's K in segments of even length: how many, and the stages of each but the last.
@@ -154,7 +153,7 @@ __device__ __forceinline__ void segments(int stages, int most, int& n, int& each
   n = (stages + each - 1) / each;
 }
 
-// Pairs of CTAs (cta_group::2), 256 x 256 tiles.  Warp 0 loads A, warp 2 B, warp 1 issues the MMAs, warps 4 to 11 drain the accumulators.
+// Pairs of CTAs (cta_group::2), 256 x 256 tiles.  Warp 0 loads A, warp 2 B, warp 1 issues the MMAs, the others drain the accumulators.
 // LONG: K in segments that the epilogue adds up in registers, because the tensor cores cut every partial sum off toward zero (a K step of 16 leaves
 // an accumulator up to 2^-23 of itself too small).  For gradients in fp32, and for sums above 16384 terms.
 template <int OP, bool LONG>
@@ -174,7 +173,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
       mbar_init(&sh.full[i], 2);                    // A and B, those of rank 0 for both CTAs
       mbar_init(&sh.empty[i], 1);
     }
-    for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 16); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 2 * S::kDrain); }
     sh.abort = 0;
     mbar_fence_init();
   }
@@ -277,7 +276,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
   } else {
     if (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kLongDrain));
     // ------------------------------------------------------------------ epilogue: a thread has one row of the tile and, by its
-    // group of four warps, the first 128 columns or the others
+    // group of four warps, 64 (LONG: 128) of the columns
     const int q = 32 * (warp & 3) + lane, grp = (warp - 4) >> 2;
     const uint32_t lane_addr = (uint32_t)(32 * (warp & 3)) << 16;
     Outlet out = {&a.o, ring + S::kStages * kStageBytes + (warp - 4) * kBoxBytesOut, lane};
@@ -294,8 +293,9 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
       if (lane == 0) mbar_arrive_relaxed_at(shared_of(&sh.tempty[acc], 0));
     };
     for (int i = pair; ok && a.plan.item(i, t); i += a.pairs) {
-      const int row = t.m0 + (int)rank * 128 + q, mine = grp ? t.bn - 128 : min(t.bn, 128), col0 = t.n0 + grp * 128;
+      const int row = t.m0 + (int)rank * 128 + q, col0 = t.n0 + grp * (LONG ? 128 : 64);
       if (LONG) {
+        const int mine = grp ? t.bn - 128 : min(t.bn, 128);
         float v[128];
         int n_seg, each;
         segments(t.count, a.seg, n_seg, each);
@@ -328,11 +328,11 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         if (!ok) break;
 #pragma unroll
         for (int c = 0; c < 128; c += 32)
-          if (c < mine) finish32(a, t, out, row - lane, col0, c, v + c);
+          if (c < mine) finish32(a, t, out, row - lane, col0 + c, v + c);
       } else {
         const int acc = (int)(run & 1);
         const float xs = OP == FORWARD && row < a.plan.rows ? a.a_scale[row] : 0.f;
-        // (the columns' scales are asked for a chunk of columns ahead: 2048 x 2736 x 1024 forward 13.3 -> 11.4 us)
+        // (the columns' scales are asked for 32 columns ahead: 2048 x 2736 x 1024 forward 13.3 -> 11.4 us)
         float4 ws[8];
         auto scales_of = [&](int col) {
 #pragma unroll
@@ -341,34 +341,30 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         if (OP == FORWARD) scales_of(col0);
         wait_full(acc);
         if (!ok) break;
-        const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * 128);
-        auto chunk = [&](int c, bool last) {           // 32 columns
-          __syncwarp();
-          float v[32];
-          tmem_ld16(at + c, v);
-          tmem_ld16(at + c + 16, v + 16);
-          tmem_ld_wait();
-          if (last) release(acc);
-          if (OP == FORWARD) {
+        const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * 64);
+        if (64 * grp < t.bn) {                         // (tiles are multiples of 64 wide)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              v[4 * e] = (float)__float_as_int(v[4 * e]) * xs * ws[e].x;
-              v[4 * e + 1] = (float)__float_as_int(v[4 * e + 1]) * xs * ws[e].y;
-              v[4 * e + 2] = (float)__float_as_int(v[4 * e + 2]) * xs * ws[e].z;
-              v[4 * e + 3] = (float)__float_as_int(v[4 * e + 3]) * xs * ws[e].w;
+          for (int c = 0; c < 64; c += 32) {
+            __syncwarp();
+            float v[32];
+            tmem_ld16(at + c, v);
+            tmem_ld16(at + c + 16, v + 16);
+            tmem_ld_wait();
+            if (c == 32) release(acc);
+            if (OP == FORWARD) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                v[4 * e] = (float)__float_as_int(v[4 * e]) * xs * ws[e].x;
+                v[4 * e + 1] = (float)__float_as_int(v[4 * e + 1]) * xs * ws[e].y;
+                v[4 * e + 2] = (float)__float_as_int(v[4 * e + 2]) * xs * ws[e].z;
+                v[4 * e + 3] = (float)__float_as_int(v[4 * e + 3]) * xs * ws[e].w;
+              }
+              if (c == 0) scales_of(col0 + 32);
+              out.put32(v, col0 + c, row - lane, 0, a.out_f32, a.plan.rows, a.plan.cols);
+            } else {
+              finish32(a, t, out, row - lane, col0 + c, v);
             }
-            if (!last) scales_of(col0 + c + 32);
-            out.put32(v, col0, c, row - lane, 0, a.out_f32, a.plan.rows, a.plan.cols);
-          } else {
-            finish32(a, t, out, row - lane, col0, c, v);
           }
-        };
-        if (mine == 128) {
-#pragma unroll
-          for (int c = 0; c < 128; c += 32) chunk(c, c == 96);
-        } else if (mine == 64) {
-          chunk(0, false);
-          chunk(32, true);
         } else {
           release(acc);
         }
@@ -865,17 +861,17 @@ __global__ void __launch_bounds__(kLineThreads) linear8_line_kernel(const LineAr
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 
-// `parts` results [rows, cols], one behind the other, in boxes of 32 rows of 128 bytes with the 128-byte swizzle.
+// `parts` results [rows, cols], one behind the other, in boxes of 32 rows of 64 bytes with the 64-byte swizzle.
 bool encode_result(CUtensorMap* out, void* base, int64_t parts, int64_t rows, int64_t cols, int64_t pitch, bool f32) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t bytes = f32 ? 4 : 2, line = (cuuint64_t)pitch * bytes;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
   const cuuint64_t strides[2] = {line, parts > 1 ? (cuuint64_t)rows * line : line};
-  const cuuint32_t box[3] = {(cuuint32_t)(128 / bytes), 32, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)(64 / bytes), 32, 1};
   const cuuint32_t estr[3] = {1, 1, 1};
   return fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 // A row-major matrix of bytes in boxes of 128 columns x box_rows rows, with the 128-byte swizzle or as they lie.
