@@ -486,12 +486,15 @@ size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which);
 /*
  *   forward: y[t, n] = fl(xs[t] ws[n] sum_k x8[t, k] w8[n, k]); the sum is of whole numbers, without rounding.
  *   input_grad: dx[t, k] = sum_n dy[t, n] ws[n] w8[n, k];  weight_grad: dweight[n, k] = sum_t dy[t, n] xs[t, group of k] x8[t, k].
- *     code * scale is rounded to bf16 on its way into the product, which changes nothing where the scale is a power of two
- *     and is off by 2^-8 of it at most where not; sums in fp32.
+ *     Sums in fp32.  code * scale enters the product of a gradient in bf16 rounded to bf16, which changes nothing where the scale is a
+ *     power of two and is off by 2^-8 of it at most where not; that of a gradient in fp32 with the 24 bits of an fp32 product (as
+ *     three bf16 numbers, at three times the product's cost, where some scale is no power of two).
  * A scale that is NaN makes its row or column (of dweight: its 128 columns, of dx: all of it) NaN.  tokens = 0: nothing, or
  * dweight = 0 (unless accumulate).
- * Errors: ADAPM_EINVAL, ADAPM_EALIGN (16 bytes for matrices, pitches), ADAPM_ERANGE, ADAPM_EUNSUPPORTED (features % 8;
- * forward with x_code or x_group other than above), ADAPM_ENOWORKSPACE, ADAPM_ECUDA.
+ * The scratch of a gradient holds what the codes of its 8-bit operand stand for in bf16 (three times that for a gradient in fp32), and
+ * parts of its sums: one buffer, the largest that any layer asks for, does for all layers of a program that runs on one stream.
+ * Errors: ADAPM_EINVAL, ADAPM_EALIGN (16 bytes for matrices and for the ws of the forward product, pitches), ADAPM_ERANGE (pitches from 2^31 on
+ * among them), ADAPM_EUNSUPPORTED (features % 8; forward with x_code or x_group other than above), ADAPM_ENOWORKSPACE, ADAPM_ECUDA.
  */
 int adapm_linear8_forward(const adapm_linear8* d, const void* x8, const float* xs, const void* w8, const float* ws, void* y,
                           void* scratch, size_t scratch_bytes, adapm_stream stream);

@@ -41,11 +41,12 @@ constexpr int kLongRegs = 168, kLongIssue = 88, kLongDrain = 208;
 static_assert(4 * kLongIssue + 8 * kLongDrain <= 12 * kLongRegs, "a block has the registers that it was launched with");
 
 struct Args {
-  CUtensorMap a, b, o;           // o: the result, or the parts of K [parts][rows][cols]
+  CUtensorMap a, b, o;           // b of a gradient: [planes][K][cols]; o: the result, or the parts of K [parts][rows][cols]
   Plan plan;
   const float *a_scale, *b_scale;      // forward: xs, ws
   void* out;
   int32_t* status;
+  const int32_t* scale_words;    // a gradient in fp32: not all zero where B has three planes
   int64_t out_ld;
   int32_t pairs, out_f32, accumulate, seg;
 };
@@ -186,7 +187,9 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
   if (rank == 0 && threadIdx.x == 0) *status = 0;      // (the cluster barrier orders it before what either CTA adds)
   if (blockIdx.x == 0)
     for (int i = a.pairs + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no pair
-  __syncthreads();
+  int planes = 1;
+  if (LONG) planes = __syncthreads_or(a.scale_words && threadIdx.x < kScaleWords ? a.scale_words[threadIdx.x] : 0) ? kPlanesF32 : 1;
+  else __syncthreads();
   cluster_sync();
   tc_fence_after();
   const uint32_t tmem_base = sh.tmem_base;
@@ -209,16 +212,20 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         const int count = uniform(t.count);
         const bool two = is_a || t.bn > 128;
         const uint32_t bytes = along_y && !two ? kOperandBytes : 2 * kOperandBytes;
-        int k = uniform(t.k0) * kStep;
-        for (int left = count; left > 0; --left, k += kStep) {
+        const int first = uniform(t.k0) * kStep;
+        int k = first, plane = 0;
+        for (int left = count * planes; left > 0; --left) {
           if (!mbar_wait_warp<WAIT_PAIR>(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
           uint8_t* const dst = ring + stage * kStageBytes + (is_a ? 0 : kOperandBytes);
           if (leader) {
             if (rank == 0) mbar_arrive_expect_tx(&sh.full[stage], bytes);
             const uint32_t bar = pair_full + 8u * (uint32_t)stage;
-            if (along_y) {
+            if (S::kGrad && !is_a) {
+              tma_load_box3_pair(dst, map, mine, k, plane, bar);
+              if (two) tma_load_box3_pair(dst + kOperandBytes / 2, map, mine + 64, k, plane, bar);
+            } else if (along_y) {
               tma_load_box_pair(dst, map, mine, k, bar);
-              if (two) tma_load_box_pair(dst + kOperandBytes / 2, map, mine + 64, k, bar);
+              tma_load_box_pair(dst + kOperandBytes / 2, map, mine + 64, k, bar);
             } else {
               tma_load_box_pair(dst, map, k, mine, bar);
             }
@@ -226,6 +233,8 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
           __syncwarp();
           ++issued;
           if (++stage == S::kStages) { stage = 0; phase ^= 1u; }
+          k += kStep;
+          if (LONG && k == first + count * kStep) { k = first; ++plane; }          // the next plane of B, the same A again
         }
       }
       if (!ok) drain_ring<true>(sh.full, stage, phase, issued, S::kStages, rank);
@@ -242,7 +251,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
       uint32_t run = 0;
       for (int i = pair; ok && a.plan.item(i, t); i += a.pairs) {
         const uint32_t idesc = uniform(S::kGrad ? make_idesc(t.bn, kAmn, kBmn, false, 256) : i8_idesc(t.bn, 256));
-        int left = uniform(t.count), n_seg = 1, each = left;
+        int left = uniform(t.count) * planes, n_seg = 1, each = left;
         if (LONG) segments(left, a.seg, n_seg, each);
         for (; left > 0 && ok; left -= each, ++run) {
           const int acc = (int)(run & 1);
@@ -298,7 +307,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         const int mine = grp ? t.bn - 128 : min(t.bn, 128);
         float v[128];
         int n_seg, each;
-        segments(t.count, a.seg, n_seg, each);
+        segments(t.count * planes, a.seg, n_seg, each);
 #pragma unroll 1
         for (int s = 0; s < n_seg; ++s, ++run) {
           const int acc = (int)(run & 1);
@@ -384,6 +393,75 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
   }
 }
 
+// ---- codes to bf16 numbers for a gradient in fp32 -------------------------------------------------------------------
+// One bf16 number has 8 of the up to 32 bits of code x scale: enough where the scale is a power of two, and about as good as a bf16
+// gradient's own rounding where not; an fp32 gradient then takes three, which have the 24 bits of the product in fp32.
+
+// Up to so many scales every CTA of linear8_planes_kernel looks through by itself, which takes less time than a launch.
+constexpr int64_t kFewScales = 4096;
+
+// words[i] != 0: some scale that CTA i has seen is no power of two.
+__global__ void __launch_bounds__(256) linear8_scales_kernel(const float* scales, int64_t n, int32_t* words) {
+  wait_for_previous_kernel();
+  int others = 0;
+#pragma unroll 8
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) others |= __float_as_int(scales[i]) & 0x7fffff;
+  others = __syncthreads_or(others);
+  if (threadIdx.x == 0) words[blockIdx.x] = others;
+  if (blockIdx.x == 0)
+    for (int i = (int)(gridDim.x + threadIdx.x); i < kScaleWords; i += 256) words[i] = 0;      // of no CTA
+}
+
+// What a bf16 number leaves of x (nothing where it is not finite).
+__device__ __forceinline__ float2 left_of_bf16(float2 x) {
+  const uint32_t w = pack_bf16x2_rn(x.x, x.y);
+  const float hi[2] = {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
+  return make_float2(fabsf(hi[0]) <= 3.402823466e38f ? x.x - hi[0] : 0.f, fabsf(hi[1]) <= 3.402823466e38f ? x.y - hi[1] : 0.f);
+}
+
+struct PlanesArgs {
+  const uint8_t* codes;
+  const float* scales;
+  int32_t* words;
+  uint16_t* out;                 // [planes][rows][cols]
+  int64_t codes_ld, rows, scan;  // scan: scales to look through, 0: the words say it
+  int32_t cols, groups;          // cols: a multiple of eight; scales per row
+};
+
+template <bool E4M3>
+__global__ void __launch_bounds__(256) linear8_planes_kernel(const PlanesArgs a) {
+  wait_for_previous_kernel();
+  static_assert(kScaleWords == 256, "a thread has a word");
+  int others = a.scan ? 0 : a.words[threadIdx.x];
+#pragma unroll 16
+  for (int64_t i = threadIdx.x; i < a.scan; i += 256) others |= __float_as_int(a.scales[i]) & 0x7fffff;
+  others = __syncthreads_or(others);
+  if (a.scan && blockIdx.x == 0) a.words[threadIdx.x] = others;
+  const int planes = others ? kPlanesF32 : 1, eights = a.cols / 8;
+  const int64_t chunks = a.rows * eights, plane = a.rows * a.cols;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = chunks <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)eights) : i / eights;
+    const int c = 8 * (int)(i - row * eights);
+    const uint2 q = *reinterpret_cast<const uint2*>(a.codes + row * a.codes_ld + c);
+    const float s = a.scales[a.groups > 1 ? row * a.groups + c / 128 : row];
+    float x[8];
+    unpack4<E4M3>(q.x, x);
+    unpack4<E4M3>(q.y, x + 4);
+    float2 v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = make_float2(x[2 * e] * s, x[2 * e + 1] * s);
+    for (int p = 0; p < planes; ++p) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        w[e] = pack_bf16x2_rn(v[e].x, v[e].y);
+        v[e] = left_of_bf16(v[e]);
+      }
+      put4(a.out + p * plane + i * 8, w);
+    }
+  }
+}
+
 // ---- a gradient whose K was cut: its parts, put together ------------------------------------------------------------
 
 struct SumArgs {
@@ -463,15 +541,17 @@ __device__ __forceinline__ int4 load_shared4_at(uint32_t at) {
   return v;
 }
 
-// Eight codes of one row, times its scale, as bf16 numbers: 16 bytes.
-template <bool E4M3>
-__device__ __forceinline__ void decode8(uint32_t c0, uint32_t c1, float s, uint32_t* w) {
+// Eight codes of one row, times its scale, as bf16 numbers: 16 bytes; plane 1, 2: what the planes before it leave.
+template <bool E4M3, bool LONG>
+__device__ __forceinline__ void decode8(uint32_t c0, uint32_t c1, float s, int plane, uint32_t* w) {
   float x[8];
   unpack4<E4M3>(c0, x);
   unpack4<E4M3>(c1, x + 4);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 t = mul2(make_float2(x[2 * i], x[2 * i + 1]), make_float2(s, s));
+    float2 t = mul2(make_float2(x[2 * i], x[2 * i + 1]), make_float2(s, s));
+    if (LONG)
+      for (int p = 0; p < plane; ++p) t = left_of_bf16(t);
     w[i] = pack_bf16x2_rn(t.x, t.y);
   }
 }
@@ -563,8 +643,17 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
   if (threadIdx.x == 0) *status = 0;
   if (blockIdx.x == 0)
     for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no CTA
-  __syncthreads();
+  int planes = 1;
+  if (LONG) {                          // whether all scales of this CTA's part of K are powers of two
+    int others = 0;
+    const float* const scale = a.scale + (a.scale_groups > 1 ? f0 / 128 : 0);
+    for (int k = 64 * k0 + (int)threadIdx.x; k < min(a.k, 64 * (k0 + count)); k += S::kThreads) others |= __float_as_int(scale[(int64_t)k * a.scale_groups]) & 0x7fffff;
+    planes = __syncthreads_or(others) ? kPlanesF32 : 1;
+  } else {
+    __syncthreads();
+  }
   tc_fence_after();
+  const int total = count * planes;
   const uint32_t tmem_base = sh.tmem_base;
   if (warp < 4) {
     if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripIssue));
@@ -574,12 +663,12 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       int stage = 0;
       uint32_t phase = 0, issued = 0;
       bool ok = true;
-      for (int i = 0; i < count; ++i) {
+      for (int i = 0, at = 0; i < total; ++i, at = at + 1 == count ? 0 : at + 1) {
         if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
         if (leader) {
           uint8_t* const dst = ring + stage * bytes;
           uint64_t* const bar = &sh.full[stage];
-          const int k = (k0 + i) * kStep;
+          const int k = (k0 + at) * kStep;
           mbar_arrive_expect_tx(bar, (uint32_t)(S::kGrad ? bytes - 16384 : bytes));
           if (OP == FORWARD) tma_load_box(dst, &a.codes, k, f0, bar);
           if (OP == WEIGHT_GRAD) {
@@ -599,11 +688,11 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       int stage = 0;
       uint32_t phase = 0, issued = 0;
       bool ok = true;
-      for (int i = 0; i < count; ++i) {
+      for (int i = 0, at = 0; i < total; ++i, at = at + 1 == count ? 0 : at + 1) {
         if (!mbar_wait_warp(&sh.raw_empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
         if (leader) {
           mbar_arrive_expect_tx(&sh.raw_full[stage], kStripRawBytes);
-          tma_load_box(raw + stage * kStripRawBytes, &a.codes, f0, (k0 + i) * kStep, &sh.raw_full[stage]);
+          tma_load_box(raw + stage * kStripRawBytes, &a.codes, f0, (k0 + at) * kStep, &sh.raw_full[stage]);
         }
         __syncwarp();
         ++issued;
@@ -620,14 +709,14 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       constexpr uint32_t kAstep = kAmn ? 128u : 2u, kBstep = kBmn ? 128u : 2u;
       const uint32_t ring0 = uniform(smem_u32(ring)), d0 = uniform(tmem_base), dhi = desc_hi();
       const uint32_t idesc = uniform(S::kGrad ? make_idesc(p.width, kAmn, kBmn, false, 128) : i8_idesc(p.width, 128));
-      const int each = LONG ? kSegLong : count;
+      const int each = LONG ? kSegLong : total;
       uint32_t run = 0;
-      for (int at = 0; at < count && ok; at += each, ++run) {
+      for (int at = 0; at < total && ok; at += each, ++run) {
         const int acc = LONG ? (int)(run & 1) : 0;
         if (LONG && !mbar_wait_warp(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
         if (LONG) tc_fence_after();
         const uint32_t d = d0 + (uint32_t)acc * acc_cols;
-        for (int i = 0; i < min(each, count - at); ++i) {
+        for (int i = 0; i < min(each, total - at); ++i) {
           if (!mbar_wait_warp(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
           tc_fence_after();
           const uint32_t slot = ring0 + (uint32_t)(stage * bytes), alo = desc_lo(slot, kAmn ? 8192u : 16u), blo = desc_lo(slot + 16384, kBmn ? 8192u : 16u);
@@ -658,13 +747,14 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
     // a lane asks for the scale of one of its row's four, a turn ahead
     const float* const scale = a.scale + (a.scale_groups > 1 ? f0 / 128 : 0);
     auto scale_at = [&](int i) {
-      const int k = (k0 + i) * 64 + 16 * j + row0;
-      return j < 4 && i < count && k < a.k ? __ldg(scale + (int64_t)k * a.scale_groups) : 0.f;
+      const int k = (k0 + (LONG ? i % count : i)) * 64 + 16 * j + row0;
+      return j < 4 && i < total && k < a.k ? __ldg(scale + (int64_t)k * a.scale_groups) : 0.f;
     };
     int stage = team, rs = team;           // (either ring has at least as many stages as there are teams)
     uint32_t phase = 0, raw_phase = 0;
     float next = scale_at(team);
-    for (int i = team; i < count; i += kStripTeams) {
+    for (int i = team; i < total; i += kStripTeams) {
+      const int plane = LONG ? i / count : 0;
       const float mine = next;
       next = scale_at(i + kStripTeams);
       if (!mbar_wait_warp(&sh.raw_full[rs], raw_phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) break;
@@ -679,11 +769,11 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
         const uint32_t c0 = odd ? q[r].z : q[r].x, c1 = odd ? q[r].w : q[r].y, c2 = odd ? q[r].x : q[r].z, c3 = odd ? q[r].y : q[r].w;
         uint32_t u[4], v[4];
         if (a.e4m3) {
-          decode8<true>(c0, c1, s, u);
-          decode8<true>(c2, c3, s, v);
+          decode8<true, LONG>(c0, c1, s, plane, u);
+          decode8<true, LONG>(c2, c3, s, plane, v);
         } else {
-          decode8<false>(c0, c1, s, u);
-          decode8<false>(c2, c3, s, v);
+          decode8<false, LONG>(c0, c1, s, plane, u);
+          decode8<false, LONG>(c2, c3, s, plane, v);
         }
         put4(dst + at0 + r * 2048, u);
         put4(dst + at1 + r * 2048, v);
@@ -715,7 +805,7 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       float v[128];
 #pragma unroll
       for (int e = 0; e < 128; ++e) v[e] = 0.f;
-      const int n_seg = (count + kSegLong - 1) / kSegLong;
+      const int n_seg = (total + kSegLong - 1) / kSegLong;
 #pragma unroll 1
       for (int s = 0; s < n_seg && ok; ++s) {
         const int acc = s & 1;
@@ -860,6 +950,18 @@ __global__ void __launch_bounds__(kLineThreads) linear8_line_kernel(const LineAr
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
+
+// `planes` matrices of bf16 numbers [rows, cols], one behind the other, in boxes of 64 columns x 64 rows.
+bool encode_planes(CUtensorMap* out, const void* base, int64_t planes, int64_t rows, int64_t cols) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
+  const cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)(rows * cols) * 2};
+  const cuuint32_t box[3] = {64, 64, 1};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 // `parts` results [rows, cols], one behind the other, in boxes of 32 rows of 64 bytes with the 64-byte swizzle.
 bool encode_result(CUtensorMap* out, void* base, int64_t parts, int64_t rows, int64_t cols, int64_t pitch, bool f32) {
@@ -1020,7 +1122,8 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
   adapm_codes8 q;
   q.rows = weight ? d.tokens : d.out_features; q.cols = d.in_features; q.x_ld = d.in_features; q.codes_ld = weight ? d.x8_ld : d.w8_ld;
   q.dtype = ADAPM_TYPE_BF16; q.code = weight ? d.x_code : ADAPM_CODE_INT8; q.group = weight ? d.x_group : 0; q.pow2 = 0;
-  if (!encode_bf16_matrix(&a.a, dy, d.tokens, d.out_features, d.y_ld, weight ? 64 : 128) || !encode_bf16_matrix(&a.b, decoded, q.rows, q.cols, q.cols, 64)) {
+  const int planes = out_dtype == ADAPM_TYPE_F32 ? kPlanesF32 : 1;
+  if (!encode_bf16_matrix(&a.a, dy, d.tokens, d.out_features, d.y_ld, weight ? 64 : 128) || !encode_planes(&a.b, decoded, planes, q.rows, q.cols)) {
     set_error_text("cuTensorMapEncodeTiled failed for a gradient of linear8");
     return ADAPM_ECUDA;
   }
@@ -1036,8 +1139,22 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
     set_error_text("cuTensorMapEncodeTiled failed for a gradient of linear8");
     return ADAPM_ECUDA;
   }
-  const int rc = launch_dequant8(q, codes, scales, decoded, s);
-  if (rc != ADAPM_OK) return rc;
+  if (a.out_f32) {
+    int32_t* const words = (int32_t*)scratch + kMostWords;
+    a.scale_words = words;
+    const int64_t n = q.rows * (q.group ? (q.cols + 127) / 128 : 1);
+    if (n > kFewScales) ADAPM_CUDA(launch_chained(true, linear8_scales_kernel, (unsigned)std::min<int64_t>(kScaleWords, (n + 2047) / 2048), 256, 0, s, scales, n, words));
+    PlanesArgs p;
+    p.codes = static_cast<const uint8_t*>(codes); p.scales = scales; p.words = words; p.out = (uint16_t*)decoded;
+    p.scan = n > kFewScales ? 0 : n;
+    p.codes_ld = q.codes_ld; p.rows = q.rows; p.cols = (int32_t)q.cols; p.groups = q.group ? (int32_t)((q.cols + 127) / 128) : 1;
+    const int64_t chunks = q.rows * (q.cols / 8);
+    const unsigned grid = (unsigned)std::min<int64_t>((chunks + 255) / 256, 148 * 16);
+    ADAPM_CUDA(q.code == ADAPM_CODE_E4M3 ? launch_chained(true, linear8_planes_kernel<true>, grid, 256, 0, s, p) : launch_chained(true, linear8_planes_kernel<false>, grid, 256, 0, s, p));
+  } else {
+    const int rc = launch_dequant8(q, codes, scales, decoded, s);
+    if (rc != ADAPM_OK) return rc;
+  }
   ADAPM_CUDA(weight ? (is_long ? launch<WEIGHT_GRAD, true>(a, s) : launch<WEIGHT_GRAD, false>(a, s))
                     : (is_long ? launch<INPUT_GRAD, true>(a, s) : launch<INPUT_GRAD, false>(a, s)));
   if (plan.parts == 1) return ADAPM_OK;

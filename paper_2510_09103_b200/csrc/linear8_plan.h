@@ -17,7 +17,9 @@ enum : int32_t { FORWARD = ADAPM_LINEAR8_FORWARD, INPUT_GRAD = ADAPM_LINEAR8_INP
 constexpr int kTile = 256;                       // rows of a pair's tile of the result, and its columns at most
 constexpr int kBand = 16;                        // row tiles that share the columns' operand at a time
 constexpr int kMostWords = 2048;                 // status words, one per pair of CTAs or per CTA, at the head of the scratch
-constexpr int kHeadBytes = 4 * kMostWords;
+constexpr int kScaleWords = 256;                 // behind them, of a gradient in fp32: whether the scales that a CTA saw are powers of two
+constexpr int kHeadBytes = 4 * (kMostWords + kScaleWords);
+constexpr int kPlanesF32 = 3;                    // bf16 numbers that code x scale is carried as into a gradient in fp32, where some scale is no power of two
 constexpr int kPlannedPairs = 74;                // what the number of parts goes by: results do not depend on the device's own number
 constexpr int kShortStages = 256;                // longest K, in stages of 64, that one accumulator takes for a gradient in bf16
 
@@ -48,7 +50,7 @@ struct Plan {
 // least.  In units of a stage of 256 columns (512 cycles): an item takes its stages, narrower ones not quite in
 // proportion, and four more, the sums a launch of about eight and the
 // parts' way to memory and back.  (2048 x 6400 x 1600: 56 tiles of 256 columns for 74 pairs, or 72 of 192.)
-inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool grad) {
+inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool grad, bool f32) {
   Plan p;
   p.rows = (int32_t)rows; p.cols = (int32_t)cols;
   p.m_tiles = (int32_t)((rows + kTile - 1) / kTile);
@@ -68,7 +70,7 @@ inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool gra
       p.items = (int32_t)(tiles * parts);
     }
   }
-  p.part_at = kHeadBytes + (grad ? round_up(k * cols * 2, 256) : 0);
+  p.part_at = kHeadBytes + (grad ? round_up(k * cols * 2 * (f32 ? kPlanesF32 : 1), 256) : 0);
   p.bytes = p.part_at + (p.parts > 1 ? round_up((int64_t)p.parts * rows * cols * 4, 256) : 0);
   return p;
 }
@@ -91,9 +93,9 @@ inline int check_desc(const adapm_linear8& d, int32_t which) {
 }
 
 inline Plan plan_of(const adapm_linear8& d, int32_t which) {
-  if (which == FORWARD) return plan_of(d.tokens, d.out_features, d.in_features, 128, false);
-  if (which == INPUT_GRAD) return plan_of(d.tokens, d.in_features, d.out_features, 64, true);
-  return plan_of(d.out_features, d.in_features, d.tokens, 64, true);
+  if (which == FORWARD) return plan_of(d.tokens, d.out_features, d.in_features, 128, false, false);
+  if (which == INPUT_GRAD) return plan_of(d.tokens, d.in_features, d.out_features, 64, true, d.dx_dtype == ADAPM_TYPE_F32);
+  return plan_of(d.out_features, d.in_features, d.tokens, 64, true, d.dweight_dtype == ADAPM_TYPE_F32);
 }
 
 // ---- strips -----------------------------------------------------------------------------------------------------------

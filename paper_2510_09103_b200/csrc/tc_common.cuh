@@ -210,6 +210,15 @@ __device__ __forceinline__ void tma_load_box_pair(void* smem_dst, const void* tm
       : "memory");
 }
 
+// ... and at (x, y, z) of a 3-D tensor map.
+__device__ __forceinline__ void tma_load_box3_pair(void* smem_dst, const void* tmap, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          smem_u32(smem_dst)),
+      "l"(tmap), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
 // One box at (x, y, z) of a 3-D tensor map.
 __device__ __forceinline__ void tma_load_box3(void* smem_dst, const void* tmap, int x, int y, int z, uint64_t* bar) {
   asm volatile(

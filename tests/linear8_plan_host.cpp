@@ -20,7 +20,8 @@ static std::string wrong(const adapm_linear8& d, int which) {
   const int step = which == FORWARD ? 128 : 64;
   if ((int64_t)p.stages * step < k || (int64_t)(p.stages - 1) * step >= k) return "stages";
   if (p.parts > 1 && which == FORWARD) return "a forward product that is cut";
-  const int64_t decoded = which == FORWARD ? 0 : 2 * k * p.cols, parts = p.parts > 1 ? 4ll * p.parts * p.rows * p.cols : 0;
+  const bool f32 = which == INPUT_GRAD ? d.dx_dtype == ADAPM_TYPE_F32 : d.dweight_dtype == ADAPM_TYPE_F32;
+  const int64_t decoded = which == FORWARD ? 0 : (f32 ? 6 : 2) * k * p.cols, parts = p.parts > 1 ? 4ll * p.parts * p.rows * p.cols : 0;
   if (p.part_at % 256 || p.part_at < kHeadBytes + decoded || p.bytes < p.part_at + parts) return "scratch";
   std::map<std::pair<int, int>, std::vector<Cut>> tiles;
   Cut t;

@@ -260,9 +260,13 @@ def _run_weight_grad(dy, x8, xs, code, group, dtype=BF16, pad=0, before=None, st
 
 
 def _bound(size, want, k, dtype, exact):
-    """size: the sum of the products' magnitudes.  Decoded numbers whose scale is no power of two are rounded to bf16, after a product in fp32."""
-    longest = 256 if dtype == F32 else 16384
-    return size * (_tensor_sum(k, longest) + (0 if exact else 2.0**-8 * 1.01)) + want.abs() * HALF[dtype] * 1.01 + 1e-37
+    """size: the sum of the products' magnitudes.  Decoded numbers whose scale is no power of two are a product in fp32, rounded to bf16 for a gradient
+    in bf16, and as three bf16 numbers, which have its 24 bits, in three times as many terms for one in fp32."""
+    if dtype == F32:
+        made = _tensor_sum(k, 256) if exact else _tensor_sum(3 * k, 256) + 2.0**-24
+    else:
+        made = _tensor_sum(k, 16384) + (0 if exact else 2.0**-8 * 1.01)
+    return size * made + want.abs() * HALF[dtype] * 1.01 + 1e-37
 
 
 def _check_input_grad(dy, w8, ws, dtype, exact, pad=0):
@@ -308,3 +312,22 @@ def test_weight_grad(dtype, code, group, tokens, out, inn):
     before = torch.randn(out, inn, generator=g, device="cuda").to(dtype) if tokens % 2 else None
     for pow2 in (True, False):
         _check_weight_grad(dy, x8, _scales(g, tokens, n, pow2=pow2), code, group, dtype, pow2, pad, before)
+
+
+@pytest.mark.parametrize("tokens,out,inn", [(5, 512, 264), (300, 1376, 520), (1500, 2056, 1024)])
+def test_gradients_in_fp32_are_as_exact_as_fp32_for_any_scales(tokens, out, inn):
+    """One scale in the middle of K that is no power of two, and scales of every size: the error is that of a sum in fp32, in the norm too."""
+    g = _gen(out)
+    dy, _ = _rows(g, tokens, out, BF16)
+    w8, x8 = _codes(g, out, inn, full=True), _codes(g, tokens, inn, full=True)
+    ws, xs = _scales(g, out), _scales(g, tokens, -(-inn // 128))
+    ws[out // 2], xs[tokens // 2, -1] = 0.3, 0.7
+    for w_scales, x_scales in ((ws, xs), (_scales(g, out, pow2=False), _scales(g, *xs.shape, pow2=False))):
+        _check_input_grad(dy, w8, w_scales, F32, False)
+        _check_weight_grad(dy, x8, x_scales, "int8", 128, F32, False)
+        dx = _run_input_grad(dy, w8, w_scales, F32).double()
+        want = dy.double() @ R.decode(_as_numbers(w8, "int8"), w_scales, 0)
+        assert (dx - want).norm() <= 5e-7 * want.norm()
+        dw = _run_weight_grad(dy, x8, x_scales, "int8", 128, F32).double()
+        want = dy.double().T @ R.decode(_as_numbers(x8, "int8"), x_scales, 128)
+        assert (dw - want).norm() <= 5e-7 * want.norm()
