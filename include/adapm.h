@@ -486,9 +486,10 @@ size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which);
 /*
  *   forward: y[t, n] = fl(xs[t] ws[n] sum_k x8[t, k] w8[n, k]); the sum is of whole numbers, without rounding.
  *   input_grad: dx[t, k] = sum_n dy[t, n] ws[n] w8[n, k];  weight_grad: dweight[n, k] = sum_t dy[t, n] xs[t, group of k] x8[t, k].
- *     Sums in fp32.  code * scale enters the product of a gradient in bf16 rounded to bf16, which changes nothing where the scale is a
- *     power of two and is off by 2^-8 of it at most where not; that of a gradient in fp32 with the 24 bits of an fp32 product (as
- *     three bf16 numbers, at three times the product's cost, where some scale is no power of two).
+ *     Sums in fp32.  Where the scales are powers of two nothing is rounded on the way into the product.  Where not, code * scale is rounded to bf16
+ *     for a gradient in bf16 (off by 2^-8 of it at most, per term), but with at most 16 tokens (dx) or output features (dweight), whose
+ *     few terms do not average that out, carried with 16 bits; for a gradient in fp32 it is carried with 24 bits, at up to three times the
+ *     product's cost.
  * A scale that is NaN makes its row or column (of dweight: its 128 columns, of dx: all of it) NaN.  tokens = 0: nothing, or
  * dweight = 0 (unless accumulate).
  * The scratch of a gradient holds what the codes of its 8-bit operand stand for in bf16 (three times that for a gradient in fp32), and

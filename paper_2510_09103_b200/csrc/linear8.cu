@@ -77,6 +77,13 @@ __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint64_t a_desc, uint64_
 
 __device__ __forceinline__ void put4(void* p, const uint32_t* v) { *reinterpret_cast<uint4*>(p) = make_uint4(v[0], v[1], v[2], v[3]); }
 
+// What a bf16 number leaves of x (nothing where it is not finite).
+__device__ __forceinline__ float2 left_of_bf16(float2 x) {
+  const uint32_t w = pack_bf16x2_rn(x.x, x.y);
+  const float hi[2] = {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
+  return make_float2(fabsf(hi[0]) <= 3.402823466e38f ? x.x - hi[0] : 0.f, fabsf(hi[1]) <= 3.402823466e38f ? x.y - hi[1] : 0.f);
+}
+
 // x += 32 values of a row of which those below n (a multiple of 8) exist.
 __device__ __forceinline__ void add_row32(const void* base, int64_t at, float* x, int n, bool f32) {
 #pragma unroll
@@ -412,13 +419,6 @@ __global__ void __launch_bounds__(256) linear8_scales_kernel(const float* scales
     for (int i = (int)(gridDim.x + threadIdx.x); i < kScaleWords; i += 256) words[i] = 0;      // of no CTA
 }
 
-// What a bf16 number leaves of x (nothing where it is not finite).
-__device__ __forceinline__ float2 left_of_bf16(float2 x) {
-  const uint32_t w = pack_bf16x2_rn(x.x, x.y);
-  const float hi[2] = {__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
-  return make_float2(fabsf(hi[0]) <= 3.402823466e38f ? x.x - hi[0] : 0.f, fabsf(hi[1]) <= 3.402823466e38f ? x.y - hi[1] : 0.f);
-}
-
 struct PlanesArgs {
   const uint8_t* codes;
   const float* scales;
@@ -506,6 +506,11 @@ __global__ void __launch_bounds__(256) linear8_sum_kernel(const SumArgs a) {
 //   input grad    input features of w8 x tokens of dy          codes made bf16 numbers on their way: sixteen warps, four to a stage,
 //   weight grad   input features of x8 x output features of dy     write them into shared memory, times their scales
 // The result lies across: out[column][feature].
+// FOLD (up to 16 columns, or a gradient in fp32): code x scale rounded to bf16 would be a rounding per term that few terms do not average out,
+// or too coarse.  The scale is a number per index of K, so it may as well go into the other operand: the codes are bf16 numbers
+// without it, and dy x scale is carried as two bf16 numbers (three for fp32), next to one another as columns of one product, whose sums are
+// added at the end.  Where all scales of the CTA's part of K are powers of two, dy x scale is one bf16 number.  K is taken in segments that are
+// added up in registers, as above.
 
 struct StripArgs {
   CUtensorMap codes, other;
@@ -518,15 +523,14 @@ struct StripArgs {
   int32_t columns, features, k, scale_groups, f32, accumulate, e4m3;
 };
 
-// LONG: K in segments that the epilogue adds up in registers, as above: for gradients in fp32, at most 128 columns wide.
-template <int OP, bool LONG>
+template <int OP, bool FOLD>
 struct StripShape {
   static constexpr bool kGrad = OP != FORWARD;
   static constexpr int kThreads = kGrad ? 768 : 256;       // warp 0 loads, 1 issues the MMAs, 4 to 7 drain, 8 to 23 make numbers of codes
-  static constexpr int kAccs = LONG ? 2 : 1;
+  static constexpr int kAccs = FOLD ? 2 : 1;
 };
-// LONG: registers of the launch, and as the four warps that issue, the four that drain and the sixteen that decode divide them.
-constexpr int kStripRegs = 80, kStripIssue = 56, kStripDrain = 200, kStripDecode = 56;
+// FOLD: registers of the launch, and as the four warps that issue, the four that drain and the sixteen that decode divide them.
+constexpr int kStripRegs = 80, kStripIssue = 72, kStripDrain = 152, kStripDecode = 64;
 static_assert(4 * kStripIssue + 4 * kStripDrain + 16 * kStripDecode <= 24 * kStripRegs, "a block has the registers that it was launched with");
 
 struct __align__(8) StripShared {
@@ -541,26 +545,42 @@ __device__ __forceinline__ int4 load_shared4_at(uint32_t at) {
   return v;
 }
 
-// Eight codes of one row, times its scale, as bf16 numbers: 16 bytes; plane 1, 2: what the planes before it leave.
-template <bool E4M3, bool LONG>
-__device__ __forceinline__ void decode8(uint32_t c0, uint32_t c1, float s, int plane, uint32_t* w) {
+// Eight codes of one row, times its scale, as bf16 numbers: 16 bytes.
+template <bool E4M3>
+__device__ __forceinline__ void decode8(uint32_t c0, uint32_t c1, float s, uint32_t* w) {
   float x[8];
   unpack4<E4M3>(c0, x);
   unpack4<E4M3>(c1, x + 4);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float2 t = mul2(make_float2(x[2 * i], x[2 * i + 1]), make_float2(s, s));
-    if (LONG)
-      for (int p = 0; p < plane; ++p) t = left_of_bf16(t);
+    const float2 t = mul2(make_float2(x[2 * i], x[2 * i + 1]), make_float2(s, s));
     w[i] = pack_bf16x2_rn(t.x, t.y);
+  }
+}
+// ... without a scale, which rounds nothing.  int8: the lower seven bits become those of a bf16 number from 128 on, the upper one says whether 128
+// or 256 is taken off again.
+template <bool E4M3>
+__device__ __forceinline__ void decode8(uint32_t c0, uint32_t c1, uint32_t* w) {
+  if (E4M3) {
+    float x[8];
+    unpack4<E4M3>(c0, x);
+    unpack4<E4M3>(c1, x + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16x2_rn(x[2 * i], x[2 * i + 1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t two = __byte_perm(i < 2 ? c0 : c1, 0u, i & 1 ? 0x4342u : 0x4140u);          // in the lower halves of 16 bits each
+      asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(w[i]) : "r"((two & 0x007f007fu) | 0x43004300u), "r"((two & 0x00800080u) | 0xc300c300u));
+    }
   }
 }
 
 // A CTA puts its share of the features together, a thread four of them, for every few columns: eight loads of four sums on their way
 // at a time.
-template <int OP, bool LONG, int SPLIT>
+template <int OP, bool FOLD, int SPLIT>
 __device__ __forceinline__ void put_together(const StripArgs& a, const uint8_t* sums, int rank, int f0, int c0) {
-  constexpr int kShare = 128 / SPLIT, kFours = kShare / 4, kStep = StripShape<OP, LONG>::kThreads / kFours, kAtOnce = 8 / SPLIT;
+  constexpr int kShare = 128 / SPLIT, kFours = kShare / 4, kStep = StripShape<OP, FOLD>::kThreads / kFours, kAtOnce = 8 / SPLIT;
   const int mine = rank * kShare + 4 * ((int)threadIdx.x % kFours), f = f0 + mine, columns = min(a.plan.width, a.columns - c0);
   if (f >= a.features) return;
   float4 ws = make_float4(1.f, 1.f, 1.f, 1.f);
@@ -594,7 +614,7 @@ __device__ __forceinline__ void put_together(const StripArgs& a, const uint8_t* 
         for (int r = 1; r < SPLIT; ++r) {
           y[0] += __int_as_float(v[u][r].x); y[1] += __int_as_float(v[u][r].y); y[2] += __int_as_float(v[u][r].z); y[3] += __int_as_float(v[u][r].w);
         }
-        if (LONG && a.accumulate) {
+        if (a.f32 && a.accumulate) {
           const float4 o = *reinterpret_cast<const float4*>(static_cast<const float*>(a.out) + to);
           y[0] += o.x; y[1] += o.y; y[2] += o.z; y[3] += o.w;
         } else if (a.accumulate) {
@@ -603,15 +623,15 @@ __device__ __forceinline__ void put_together(const StripArgs& a, const uint8_t* 
           y[2] += __uint_as_float(o.y << 16); y[3] += __uint_as_float(o.y & 0xffff0000u);
         }
       }
-      if (LONG || (OP == FORWARD && a.f32)) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y[0], y[1], y[2], y[3]);
+      if (a.f32) *reinterpret_cast<float4*>(static_cast<float*>(a.out) + to) = make_float4(y[0], y[1], y[2], y[3]);
       else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + to) = make_uint2(pack_bf16x2_rn(y[0], y[1]), pack_bf16x2_rn(y[2], y[3]));
     }
   }
 }
 
-template <int OP, bool LONG>
-__global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_strip_kernel(const __grid_constant__ StripArgs a) {
-  using S = StripShape<OP, LONG>;
+template <int OP, bool FOLD>
+__global__ void __launch_bounds__(StripShape<OP, FOLD>::kThreads, 1) linear8_strip_kernel(const __grid_constant__ StripArgs a) {
+  using S = StripShape<OP, FOLD>;
   constexpr int kStep = S::kGrad ? 64 : 128;                       // K of a stage
   extern __shared__ uint8_t dyn_smem[];
   __shared__ StripShared sh;
@@ -619,15 +639,16 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
   const StripPlan& p = a.plan;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, split = p.split, rank = split > 1 ? (int)cluster_rank() : 0;
   const int tile = (int)blockIdx.x / split, c_tile = tile / p.f_tiles, f0 = (tile - c_tile * p.f_tiles) * 128, c0 = c_tile * p.width;
-  const int k0 = p.first(rank), count = p.first(rank + 1) - k0, bytes = strip_stage_bytes(p.width);
+  const int k0 = p.first(rank), count = p.first(rank + 1) - k0, bytes = p.stage_bytes;
   uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~(uintptr_t)1023);
   uint8_t* const raw = ring + p.ring * bytes;
   volatile int* const abort = &sh.abort;
   int32_t* const status = a.status + blockIdx.x;
-  const uint32_t acc_cols = p.width <= 32 ? 32 : p.width <= 64 ? 64 : p.width <= 128 ? 128 : 256, tmem_cols = S::kAccs * acc_cols;
+  const int widest = p.width * p.planes;
+  const uint32_t acc_cols = widest <= 32 ? 32 : widest <= 64 ? 64 : widest <= 128 ? 128 : 256, tmem_cols = S::kAccs * acc_cols;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < p.ring; ++i) { mbar_init(&sh.full[i], S::kGrad ? 1 + 4 : 1); mbar_init(&sh.empty[i], 1); }
+    for (int i = 0; i < p.ring; ++i) { mbar_init(&sh.full[i], (FOLD ? 0 : 1) + (S::kGrad ? 4 : 0)); mbar_init(&sh.empty[i], 1); }
     if (S::kGrad)
       for (int i = 0; i < p.raw; ++i) { mbar_init(&sh.raw_full[i], 1); mbar_init(&sh.raw_empty[i], 4); }
     for (int i = 0; i < S::kAccs; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 4); }
@@ -644,31 +665,30 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
   if (blockIdx.x == 0)
     for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no CTA
   int planes = 1;
-  if (LONG) {                          // whether all scales of this CTA's part of K are powers of two
+  if (FOLD) {                          // whether all scales of this CTA's part of K are powers of two
     int others = 0;
     const float* const scale = a.scale + (a.scale_groups > 1 ? f0 / 128 : 0);
     for (int k = 64 * k0 + (int)threadIdx.x; k < min(a.k, 64 * (k0 + count)); k += S::kThreads) others |= __float_as_int(scale[(int64_t)k * a.scale_groups]) & 0x7fffff;
-    planes = __syncthreads_or(others) ? kPlanesF32 : 1;
+    planes = __syncthreads_or(others) ? p.planes : 1;
   } else {
     __syncthreads();
   }
   tc_fence_after();
-  const int total = count * planes;
   const uint32_t tmem_base = sh.tmem_base;
   if (warp < 4) {
-    if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripIssue));
-    if (warp == 0) {
+    if (FOLD) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripIssue));
+    if (warp == 0 && !FOLD) {
       // ------------------------------------------------------------------ the operands (forward), the other operand (gradients)
       const bool leader = elect_one();
       int stage = 0;
       uint32_t phase = 0, issued = 0;
       bool ok = true;
-      for (int i = 0, at = 0; i < total; ++i, at = at + 1 == count ? 0 : at + 1) {
+      for (int i = 0; i < count; ++i) {
         if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
         if (leader) {
           uint8_t* const dst = ring + stage * bytes;
           uint64_t* const bar = &sh.full[stage];
-          const int k = (k0 + at) * kStep;
+          const int k = (k0 + i) * kStep;
           mbar_arrive_expect_tx(bar, (uint32_t)(S::kGrad ? bytes - 16384 : bytes));
           if (OP == FORWARD) tma_load_box(dst, &a.codes, k, f0, bar);
           if (OP == WEIGHT_GRAD) {
@@ -683,16 +703,23 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       }
       if (!ok) drain_ring<false>(sh.full, stage, phase, issued, p.ring, 0);
     } else if (S::kGrad && warp == 2) {
-      // ------------------------------------------------------------------ codes, as they lie
+      // ------------------------------------------------------------------ codes, and what scales go into, as they lie
       const bool leader = elect_one();
       int stage = 0;
       uint32_t phase = 0, issued = 0;
       bool ok = true;
-      for (int i = 0, at = 0; i < total; ++i, at = at + 1 == count ? 0 : at + 1) {
+      for (int i = 0; i < count; ++i) {
         if (!mbar_wait_warp(&sh.raw_empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) { ok = false; break; }
         if (leader) {
-          mbar_arrive_expect_tx(&sh.raw_full[stage], kStripRawBytes);
-          tma_load_box(raw + stage * kStripRawBytes, &a.codes, f0, (k0 + at) * kStep, &sh.raw_full[stage]);
+          uint8_t* const dst = raw + stage * p.raw_bytes;
+          uint64_t* const bar = &sh.raw_full[stage];
+          const int k = (k0 + i) * kStep;
+          mbar_arrive_expect_tx(bar, (uint32_t)p.raw_bytes);
+          tma_load_box(dst, &a.codes, f0, k, bar);
+          if (FOLD) {
+            if (OP == WEIGHT_GRAD) tma_load_box(dst + kStripRawBytes, &a.other, c0, k, bar);
+            else tma_load_box(dst + kStripRawBytes, &a.other, k, c0, bar);
+          }
         }
         __syncwarp();
         ++issued;
@@ -708,15 +735,15 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       constexpr bool kAmn = S::kGrad, kBmn = OP == WEIGHT_GRAD;
       constexpr uint32_t kAstep = kAmn ? 128u : 2u, kBstep = kBmn ? 128u : 2u;
       const uint32_t ring0 = uniform(smem_u32(ring)), d0 = uniform(tmem_base), dhi = desc_hi();
-      const uint32_t idesc = uniform(S::kGrad ? make_idesc(p.width, kAmn, kBmn, false, 128) : i8_idesc(p.width, 128));
-      const int each = LONG ? kSegLong : total;
+      const uint32_t idesc = uniform(S::kGrad ? make_idesc(p.width * planes, kAmn, kBmn, false, 128) : i8_idesc(p.width, 128));
+      const int each = FOLD ? kSegLong : count;
       uint32_t run = 0;
-      for (int at = 0; at < total && ok; at += each, ++run) {
-        const int acc = LONG ? (int)(run & 1) : 0;
-        if (LONG && !mbar_wait_warp(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
-        if (LONG) tc_fence_after();
+      for (int at = 0; at < count && ok; at += each, ++run) {
+        const int acc = FOLD ? (int)(run & 1) : 0;
+        if (FOLD && !mbar_wait_warp(&sh.tempty[acc], ((run >> 1) & 1u) ^ 1u, abort, status, ST_WAIT_TMEM_EMPTY, kWaitSpinDefault)) { ok = false; break; }
+        if (FOLD) tc_fence_after();
         const uint32_t d = d0 + (uint32_t)acc * acc_cols;
-        for (int i = 0; i < min(each, total - at); ++i) {
+        for (int i = 0; i < min(each, count - at); ++i) {
           if (!mbar_wait_warp(&sh.full[stage], phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) { ok = false; break; }
           tc_fence_after();
           const uint32_t slot = ring0 + (uint32_t)(stage * bytes), alo = desc_lo(slot, kAmn ? 8192u : 16u), blo = desc_lo(slot + 16384, kBmn ? 8192u : 16u);
@@ -737,46 +764,79 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       }
     }
   } else if (S::kGrad && warp >= 8) {
-    if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripDecode));
+    if (FOLD) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripDecode));
     // ------------------------------------------------------------------ codes to bf16 numbers: the teams take turns; a warp has
     // four of every sixteen rows of K, eight lanes to a row, 16 codes to a lane
     const int team = (warp - 8) >> 2, row0 = 4 * (warp & 3) + (lane >> 3), j = lane & 7, sub = row0 & 7;
     // the 128-byte swizzle; lanes 4 to 7 write their second chunk first, so that eight lanes meet no bank twice
     const int odd = j >> 2, from = row0 * 128 + 16 * j, to = odd * 8192 + row0 * 128;
     const int at0 = to + ((2 * (j & 3) + odd) ^ sub) * 16, at1 = to + ((2 * (j & 3) + 1 - odd) ^ sub) * 16;
-    // a lane asks for the scale of one of its row's four, a turn ahead
+    // scales, a turn ahead: one of its row's four to a lane, or (FOLD, where K runs along a row) those of its chunk of eight
+    constexpr bool kAlong = FOLD && OP == INPUT_GRAD;
+    constexpr int kScales = kAlong ? 8 : 1;
     const float* const scale = a.scale + (a.scale_groups > 1 ? f0 / 128 : 0);
-    auto scale_at = [&](int i) {
-      const int k = (k0 + (LONG ? i % count : i)) * 64 + 16 * j + row0;
-      return j < 4 && i < total && k < a.k ? __ldg(scale + (int64_t)k * a.scale_groups) : 0.f;
+    float next[kScales];
+    auto scales_of = [&](int i) {
+#pragma unroll
+      for (int e = 0; e < kScales; ++e) {
+        const int k = (k0 + i) * 64 + (kAlong ? 8 * j + e : 16 * j + row0);
+        next[e] = (kAlong || j < 4) && i < count && k < a.k ? __ldg(scale + (int64_t)k * a.scale_groups) : 0.f;
+      }
     };
     int stage = team, rs = team;           // (either ring has at least as many stages as there are teams)
     uint32_t phase = 0, raw_phase = 0;
-    float next = scale_at(team);
-    for (int i = team; i < total; i += kStripTeams) {
-      const int plane = LONG ? i / count : 0;
-      const float mine = next;
-      next = scale_at(i + kStripTeams);
+    scales_of(team);
+    for (int i = team; i < count; i += kStripTeams) {
+      float mine[kScales];
+#pragma unroll
+      for (int e = 0; e < kScales; ++e) mine[e] = next[e];
+      scales_of(i + kStripTeams);
       if (!mbar_wait_warp(&sh.raw_full[rs], raw_phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) break;
+      const uint8_t* const src = raw + rs * p.raw_bytes;
       uint4 q[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const uint4*>(raw + rs * kStripRawBytes + from + r * 2048);
+      for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const uint4*>(src + from + r * 2048);
       if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) break;
       uint8_t* const dst = ring + stage * bytes;
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const float s = __shfl_sync(0xffffffffu, mine, (lane & 24) | r);
         const uint32_t c0 = odd ? q[r].z : q[r].x, c1 = odd ? q[r].w : q[r].y, c2 = odd ? q[r].x : q[r].z, c3 = odd ? q[r].y : q[r].w;
         uint32_t u[4], v[4];
-        if (a.e4m3) {
-          decode8<true, LONG>(c0, c1, s, plane, u);
-          decode8<true, LONG>(c2, c3, s, plane, v);
+        if (FOLD) {
+          if (a.e4m3) { decode8<true>(c0, c1, u); decode8<true>(c2, c3, v); }
+          else { decode8<false>(c0, c1, u); decode8<false>(c2, c3, v); }
         } else {
-          decode8<false, LONG>(c0, c1, s, plane, u);
-          decode8<false, LONG>(c2, c3, s, plane, v);
+          const float s = __shfl_sync(0xffffffffu, mine[0], (lane & 24) | r);
+          if (a.e4m3) { decode8<true>(c0, c1, s, u); decode8<true>(c2, c3, s, v); }
+          else { decode8<false>(c0, c1, s, u); decode8<false>(c2, c3, s, v); }
         }
         put4(dst + at0 + r * 2048, u);
         put4(dst + at1 + r * 2048, v);
+      }
+      if (FOLD) {
+        // the other operand times the scales, a chunk of eight at a time, from where TMA has put it to the same place of each plane
+        const int o = row0 * 128 + ((j ^ sub) * 16);
+#pragma unroll 1
+        for (int r = 0; r < p.width / 16; ++r) {
+          const uint4 b = *reinterpret_cast<const uint4*>(src + kStripRawBytes + o + r * 2048);
+          const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+          const float row_scale = kAlong ? 0.f : __shfl_sync(0xffffffffu, mine[0], (lane & 24) | (r & 3));
+          float2 x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[e] = mul2(make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)),
+                        kAlong ? make_float2(mine[2 * e % kScales], mine[(2 * e + 1) % kScales]) : make_float2(row_scale, row_scale));
+          for (int n = 0; n < planes; ++n) {
+            uint32_t u[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = pack_bf16x2_rn(x[e].x, x[e].y);
+            put4(dst + 16384 + n * p.width * 128 + o + r * 2048, u);
+            if (n + 1 < planes) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = left_of_bf16(x[e]);
+            }
+          }
+        }
       }
       fence_async_smem();
       __syncwarp();
@@ -790,7 +850,7 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       if (rs >= p.raw) { rs -= p.raw; raw_phase ^= 1u; }
     }
   } else {
-    if (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStripDrain));
+    if (FOLD) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStripDrain));
     // ------------------------------------------------------------------ this CTA's sums [columns][128], over the ring once all that was
     // in it has been multiplied
     bool ok = true;
@@ -801,24 +861,27 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
       ok = __shfl_sync(0xffffffffu, ok, 0);
       tc_fence_after();
     };
-    if (LONG) {
-      float v[128];
+    if (FOLD) {
+      float v[kFoldWidth];
 #pragma unroll
-      for (int e = 0; e < 128; ++e) v[e] = 0.f;
-      const int n_seg = (total + kSegLong - 1) / kSegLong;
+      for (int e = 0; e < kFoldWidth; ++e) v[e] = 0.f;
+      const int n_seg = (count + kSegLong - 1) / kSegLong;
 #pragma unroll 1
       for (int s = 0; s < n_seg && ok; ++s) {
         const int acc = s & 1;
         wait_full(acc, (uint32_t)(s >> 1) & 1u);
         if (!ok) break;
+#pragma unroll 1
+        for (int n = planes - 1; n >= 0; --n) {                      // (the smallest first)
 #pragma unroll
-        for (int c = 0; c < 128; c += 16) {
-          if (c < p.width) {
-            float x[16];
-            tmem_ld16(lane_addr + (uint32_t)acc * acc_cols + (uint32_t)c, x);
-            tmem_ld_wait();
+          for (int c = 0; c < kFoldWidth; c += 16) {
+            if (c < p.width) {
+              float x[16];
+              tmem_ld16(lane_addr + (uint32_t)acc * acc_cols + (uint32_t)(n * p.width + c), x);
+              tmem_ld_wait();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) v[c + e] += x[e];
+              for (int e = 0; e < 16; ++e) v[c + e] += x[e];
+            }
           }
         }
         tc_fence_before();
@@ -826,7 +889,7 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
         if (lane == 0) mbar_arrive(&sh.tempty[acc]);
       }
 #pragma unroll
-      for (int c = 0; c < 128; ++c)
+      for (int c = 0; c < kFoldWidth; ++c)
         if (ok && c < p.width) sums[c * 128] = __float_as_int(v[c]);
     } else {
       wait_full(0, 0);
@@ -842,16 +905,16 @@ __global__ void __launch_bounds__(StripShape<OP, LONG>::kThreads, 1) linear8_str
     }
     tc_fence_before();
     __syncwarp();
-    if (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripRegs));
+    if (FOLD) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStripRegs));
   }
   __syncthreads();
   // (not before: the warps that drain have taken theirs and given them back by now, so that nobody waits for registers of a warp that waits here)
-  if (LONG && (warp < 4 || warp >= 8)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStripRegs));
+  if (FOLD && (warp < 4 || warp >= 8)) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStripRegs));
   if (split > 1) cluster_sync();
-  if (split == 1) put_together<OP, LONG, 1>(a, ring, rank, f0, c0);
-  else if (split == 2) put_together<OP, LONG, 2>(a, ring, rank, f0, c0);
-  else if (split == 4) put_together<OP, LONG, 4>(a, ring, rank, f0, c0);
-  else put_together<OP, LONG, 8>(a, ring, rank, f0, c0);
+  if (split == 1) put_together<OP, FOLD, 1>(a, ring, rank, f0, c0);
+  else if (split == 2) put_together<OP, FOLD, 2>(a, ring, rank, f0, c0);
+  else if (split == 4) put_together<OP, FOLD, 4>(a, ring, rank, f0, c0);
+  else put_together<OP, FOLD, 8>(a, ring, rank, f0, c0);
   __syncwarp();
   if (split > 1) cluster_sync();      // no CTA leaves while another may still read its sums
   if (warp == 1) {
@@ -1088,7 +1151,7 @@ Buffer floats_at(const float* p, int64_t n, int64_t align) { return Buffer{p, al
 
 template <int OP, bool LONG>
 cudaError_t launch_strips(const StripArgs& a, cudaStream_t s) {
-  const size_t smem = (size_t)a.plan.ring * strip_stage_bytes(a.plan.width) + (size_t)a.plan.raw * kStripRawBytes + 1024;
+  const size_t smem = (size_t)a.plan.ring * a.plan.stage_bytes + (size_t)a.plan.raw * a.plan.raw_bytes + 1024;
   return launch_clusters(true, (unsigned)a.plan.split, linear8_strip_kernel<OP, LONG>, (unsigned)a.plan.ctas, (unsigned)StripShape<OP, LONG>::kThreads, smem, s, a);
 }
 
@@ -1110,9 +1173,9 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
     t.scale = scales; t.scale_groups = weight && d.x_group ? (int32_t)((d.in_features + 127) / 128) : 1;
     t.out = out; t.out_ld = out_ld; t.status = (int32_t*)scratch;
     t.columns = (int32_t)(weight ? d.out_features : d.tokens); t.features = (int32_t)d.in_features;
-    t.accumulate = weight && d.accumulate != 0; t.e4m3 = weight && d.x_code == ADAPM_CODE_E4M3;
-    ADAPM_CUDA(out_dtype == ADAPM_TYPE_F32 ? (weight ? launch_strips<WEIGHT_GRAD, true>(t, s) : launch_strips<INPUT_GRAD, true>(t, s))
-                                           : (weight ? launch_strips<WEIGHT_GRAD, false>(t, s) : launch_strips<INPUT_GRAD, false>(t, s)));
+    t.f32 = out_dtype == ADAPM_TYPE_F32; t.accumulate = weight && d.accumulate != 0; t.e4m3 = weight && d.x_code == ADAPM_CODE_E4M3;
+    ADAPM_CUDA(strip.fold ? (weight ? launch_strips<WEIGHT_GRAD, true>(t, s) : launch_strips<INPUT_GRAD, true>(t, s))
+                          : (weight ? launch_strips<WEIGHT_GRAD, false>(t, s) : launch_strips<INPUT_GRAD, false>(t, s)));
     return ADAPM_OK;
   }
   Args a;

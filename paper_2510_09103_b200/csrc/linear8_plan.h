@@ -19,7 +19,7 @@ constexpr int kBand = 16;                        // row tiles that share the col
 constexpr int kMostWords = 2048;                 // status words, one per pair of CTAs or per CTA, at the head of the scratch
 constexpr int kScaleWords = 256;                 // behind them, of a gradient in fp32: whether the scales that a CTA saw are powers of two
 constexpr int kHeadBytes = 4 * (kMostWords + kScaleWords);
-constexpr int kPlanesF32 = 3;                    // bf16 numbers that code x scale is carried as into a gradient in fp32, where some scale is no power of two
+constexpr int kPlanesF32 = 3, kPlanesBf16 = 2;   // bf16 numbers that one times a scale is carried as, where some scale is no power of two
 constexpr int kPlannedPairs = 74;                // what the number of parts goes by: results do not depend on the device's own number
 constexpr int kShortStages = 256;                // longest K, in stages of 64, that one accumulator takes for a gradient in bf16
 
@@ -100,33 +100,41 @@ inline Plan plan_of(const adapm_linear8& d, int32_t which) {
 
 // ---- strips -----------------------------------------------------------------------------------------------------------
 // A tile is 128 features of the 8-bit operand x `width` columns of the other; the `split` CTAs of a cluster share its K.  The ring has `ring`
-// stages, that of a gradient's codes as they lie `raw`.
+// stages of `stage_bytes`, that of a gradient's operands as they lie `raw` of `raw_bytes`.  fold: a gradient's scales go into the other operand,
+// whose numbers then take up to `planes` columns of the product each.
 struct StripPlan {
-  int32_t width, c_tiles, f_tiles, stages, split, ring, raw, ctas;
+  int32_t width, c_tiles, f_tiles, stages, split, ring, stage_bytes, raw, raw_bytes, fold, planes, ctas;
   __host__ __device__ int first(int part) const { return (int)((int64_t)stages * part / split); }      // stage of a part of K
 };
 
 constexpr int kLineTokens = 2;                   // up to so many a forward product goes by rows of the weight, end to end
-constexpr int kStripWidth = 256, kStripSmem = 224 * 1024, kStripRing = 8;
+constexpr int kStripWidth = 256, kFoldWidth = 64, kFoldFew = 16, kStripSmem = 224 * 1024, kStripRing = 8;
 constexpr int kStripTeams = 4, kStripRawBytes = 64 * 128;        // gradients: stages that are decoded at the same time; bytes of a stage's codes
 
-__host__ __device__ __forceinline__ int strip_stage_bytes(int width) { return 16384 + 128 * width; }
+inline bool f32_gradient(const adapm_linear8& d, int32_t which) {
+  return which == INPUT_GRAD ? d.dx_dtype == ADAPM_TYPE_F32 : which == WEIGHT_GRAD && d.dweight_dtype == ADAPM_TYPE_F32;
+}
 
 inline StripPlan strip_plan_of(const adapm_linear8& d, int32_t which) {
   const int64_t features = which == FORWARD ? d.out_features : d.in_features, columns = which == WEIGHT_GRAD ? d.out_features : d.tokens;
   const int64_t k = which == FORWARD ? d.in_features : which == INPUT_GRAD ? d.out_features : d.tokens;
-  const bool f32_grad = which == INPUT_GRAD ? d.dx_dtype == ADAPM_TYPE_F32 : which == WEIGHT_GRAD && d.dweight_dtype == ADAPM_TYPE_F32;
-  const int widest = f32_grad ? kStripWidth / 2 : kStripWidth;          // (a thread keeps its row's sums)
+  const bool f32 = f32_gradient(d, which);
   StripPlan p;
+  // (one rounding per term is not averaged out over few columns; with 64 of them folded scales take longer: 64 x 14336 x 4096 51 us for 28, 16 x 14336 x 4096
+  // 34 for 28)
+  p.fold = which != FORWARD && (f32 || columns <= kFoldFew);
+  p.planes = !p.fold ? 1 : f32 ? kPlanesF32 : kPlanesBf16;
+  const int widest = p.fold ? kFoldWidth : kStripWidth;
   p.c_tiles = (int32_t)((columns + widest - 1) / widest);
   p.width = (int32_t)round_up((columns + p.c_tiles - 1) / std::max(1, p.c_tiles), which == WEIGHT_GRAD ? 64 : 16);
   p.f_tiles = (int32_t)((features + 127) / 128);
   const int step = which == FORWARD ? 128 : 64;
   p.stages = (int32_t)((k + step - 1) / step);
   const int64_t tiles = (int64_t)p.c_tiles * p.f_tiles;
-  const int bytes = strip_stage_bytes(p.width), kept = which == FORWARD ? 0 : kStripRing * kStripRawBytes;
-  p.ring = std::max(kStripTeams, std::min(kStripRing, (kStripSmem - kept) / bytes));
-  p.raw = which == FORWARD ? 0 : std::min(kStripRing, (kStripSmem - p.ring * bytes) / kStripRawBytes);
+  p.stage_bytes = 16384 + 128 * p.width * p.planes;
+  p.raw_bytes = which == FORWARD ? 0 : kStripRawBytes + (p.fold ? 128 * p.width : 0);
+  p.ring = std::max(kStripTeams, std::min(kStripRing, (kStripSmem - (p.fold ? kStripTeams : kStripRing) * p.raw_bytes) / p.stage_bytes));
+  p.raw = which == FORWARD ? 0 : std::min(kStripRing, (kStripSmem - p.ring * p.stage_bytes) / p.raw_bytes);
   p.split = 1;
   // (sixteen clusters of eight do not fit the device's groups of SMs at the same time: 1024 x 512 x 14336 in eighths 29 us, in quarters 20)
   while (p.split < (tiles <= 8 ? 8 : 4) && tiles * p.split <= kPlannedPairs && 4 * p.split <= p.stages) p.split *= 2;
@@ -138,18 +146,18 @@ inline StripPlan strip_plan_of(const adapm_linear8& d, int32_t which) {
 // a pair's 256 x 256 tiles, for a gradient with the launch that decodes its codes and the one that sums the parts of K.
 inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const StripPlan& s, const Plan& p) {
   if (s.ctas > kMostWords) return false;
-  const bool f32 = which == INPUT_GRAD ? d.dx_dtype == ADAPM_TYPE_F32 : which == WEIGHT_GRAD && d.dweight_dtype == ADAPM_TYPE_F32;
+  const bool f32 = f32_gradient(d, which);
   const int each = (s.stages + s.split - 1) / s.split;
-  if (which != FORWARD && !f32 && each > kShortStages) return false;
+  if (which != FORWARD && !s.fold && each > kShortStages) return false;
   const bool grad = which != FORWARD;
   int levels = 0;                                     // of the cluster
   while ((1 << levels) < s.split) ++levels;
   const double rounds = (double)((s.ctas + 2 * kPlannedPairs - 1) / (2 * kPlannedPairs));
-  const double stage = grad ? 0.36 + 0.0005 * s.width : 0.16 + 0.0006 * s.width, level = grad ? 0.4 + 0.006 * s.width : 0.3 + 0.0025 * s.width;
+  const double stage = s.fold ? 0.36 + 0.008 * s.width : grad ? 0.36 + 0.0005 * s.width : 0.16 + 0.0006 * s.width, level = grad ? 0.4 + 0.006 * s.width : 0.3 + 0.0025 * s.width;
   const double strips = 2.0 + rounds * ((f32 ? 4.3 : grad ? 2.3 : 3.2) + 0.012 * s.width + each * stage + levels * level);
   const double pair_rounds = (double)((p.items + kPlannedPairs - 1) / kPlannedPairs);
-  double pairs = 6.0 + pair_rounds * (1.0 + 0.31 * p.each * (0.2 + 0.8 / 256 * p.width));
-  if (grad) pairs += 2.0 + 5e-7 * p.stages * 64.0 * p.cols + (p.parts > 1 ? 2.5 + 5e-7 * p.rows * (double)p.cols * p.parts : 0);
+  double pairs = 6.0 + pair_rounds * (1.0 + 0.31 * p.each * (f32 ? kPlanesF32 : 1) * (0.2 + 0.8 / 256 * p.width));
+  if (grad) pairs += (f32 ? 3.5 + 1.2e-6 * p.stages * 64.0 * p.cols : 2.0 + 5e-7 * p.stages * 64.0 * p.cols) + (p.parts > 1 ? 2.5 + 5e-7 * p.rows * (double)p.cols * p.parts : 0);
   return strips < pairs;
 }
 

@@ -40,6 +40,8 @@ static std::string wrong(const adapm_linear8& d, int which) {
   if ((int64_t)tiles.size() != (int64_t)p.m_tiles * p.n_tiles || (int64_t)p.m_tiles * kTile < p.rows || (int64_t)p.n_tiles * p.width < p.cols) return "tiles left out";
   const StripPlan q = strip_plan_of(d, which);
   const int64_t features = which == FORWARD ? d.out_features : d.in_features, columns = which == WEIGHT_GRAD ? d.out_features : d.tokens;
+  if (q.fold && (which == FORWARD || q.width > 64 || q.planes * q.width > 256)) return "folded scales";
+  if (!q.fold && q.planes != 1) return "planes";
   if (q.width < 1 || q.width > 256 || q.width % (which == WEIGHT_GRAD ? 64 : 16)) return "a strip's width";
   if ((int64_t)q.c_tiles * q.width < columns || (int64_t)(q.c_tiles - 1) * q.width >= columns) return "strips' columns";
   if ((int64_t)q.f_tiles * 128 < features || (int64_t)(q.f_tiles - 1) * 128 >= features) return "strips' features";
@@ -49,9 +51,10 @@ static std::string wrong(const adapm_linear8& d, int which) {
   if (q.first(0) != 0 || q.first(q.split) != q.stages) return "a strip's K";
   for (int i = 0; i < q.split; ++i)
     if (q.first(i + 1) <= q.first(i)) return "a part without a stage";
-  const int64_t ring = (int64_t)q.ring * strip_stage_bytes(q.width);
+  if (q.stage_bytes != 16384 + 128 * q.width * q.planes || q.raw_bytes != (which == FORWARD ? 0 : 8192 + (q.fold ? 128 * q.width : 0))) return "bytes of a stage";
+  const int64_t ring = (int64_t)q.ring * q.stage_bytes;
   if (q.ring < kStripTeams || q.ring > kStripRing || (which != FORWARD && (q.raw < kStripTeams || q.raw > kStripRing))) return "a ring";
-  if (ring + (int64_t)q.raw * kStripRawBytes > kStripSmem || ring < 512 * q.width || kStripSmem + 1024 + 512 > 227 * 1024) return "shared memory";
+  if (ring + (int64_t)q.raw * q.raw_bytes > kStripSmem || ring < 512 * q.width || kStripSmem + 1024 + 512 > 227 * 1024) return "shared memory";
   for (const auto& of : tiles)
     if (of.second.back().k0 + of.second.back().count != p.stages || (int)of.second.size() != p.parts) return "K";
   return "";

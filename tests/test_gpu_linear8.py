@@ -331,3 +331,24 @@ def test_gradients_in_fp32_are_as_exact_as_fp32_for_any_scales(tokens, out, inn)
         dw = _run_weight_grad(dy, x8, x_scales, "int8", 128, F32).double()
         want = dy.double().T @ R.decode(_as_numbers(x8, "int8"), x_scales, 128)
         assert (dw - want).norm() <= 5e-7 * want.norm()
+
+
+@pytest.mark.parametrize("columns", [1, 3, 16])
+@pytest.mark.parametrize("k", [64, 200, 1500])
+def test_gradients_of_few_columns_carry_any_scale_with_16_bits(columns, k):
+    """What is left in a bf16 gradient of few tokens, or few output features, is its own rounding: two roundings of a term, the second of what
+    the first leaves."""
+    g = _gen(columns + k)
+    inn = 392
+    dy, _ = _rows(g, columns, 8 * k, BF16)
+    w8, ws = _codes(g, 8 * k, inn, full=True), _scales(g, 8 * k, pow2=False)
+    w = R.decode(_as_numbers(w8, "int8"), ws, 0)
+    want = dy.double() @ w
+    _close(_run_input_grad(dy, w8, ws), want, dy.double().abs() @ w.abs() * (_tensor_sum(2 * 8 * k, 256) + 2.0**-16) + want.abs() * HALF[BF16] * 1.01, "dx")
+    out = max(8, columns // 8 * 8)
+    dy, _ = _rows(g, k, out, BF16)
+    for code, group in (("int8", 128), ("e4m3", 0)):
+        x8, xs = _codes(g, k, inn, code, full=code == "int8"), _scales(g, k, -(-inn // 128) if group else 1, pow2=False)
+        x = R.decode(_as_numbers(x8, code), xs, group)
+        want = dy.double().T @ x
+        _close(_run_weight_grad(dy, x8, xs, code, group), want, dy.double().abs().T @ x.abs() * (_tensor_sum(2 * k, 256) + 2.0**-16) + want.abs() * HALF[BF16] * 1.01, "dweight")
