@@ -148,6 +148,7 @@ inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const Strip
   if (s.ctas > kMostWords) return false;
   const bool f32 = f32_gradient(d, which);
   const int each = (s.stages + s.split - 1) / s.split;
+  if (s.fold && !f32) return true;                    // (for what the call promises)
   if (which != FORWARD && !s.fold && each > kShortStages) return false;
   const bool grad = which != FORWARD;
   int levels = 0;                                     // of the cluster

@@ -42,6 +42,7 @@ static std::string wrong(const adapm_linear8& d, int which) {
   const int64_t features = which == FORWARD ? d.out_features : d.in_features, columns = which == WEIGHT_GRAD ? d.out_features : d.tokens;
   if (q.fold && (which == FORWARD || q.width > 64 || q.planes * q.width > 256)) return "folded scales";
   if (!q.fold && q.planes != 1) return "planes";
+  if (which != FORWARD && !f32 && columns <= 16 && (!q.fold || !strips_are_faster(d, which, q, p))) return "few columns without 16 bits of a scale";
   if (q.width < 1 || q.width > 256 || q.width % (which == WEIGHT_GRAD ? 64 : 16)) return "a strip's width";
   if ((int64_t)q.c_tiles * q.width < columns || (int64_t)(q.c_tiles - 1) * q.width >= columns) return "strips' columns";
   if ((int64_t)q.f_tiles * 128 < features || (int64_t)(q.f_tiles - 1) * 128 >= features) return "strips' features";
