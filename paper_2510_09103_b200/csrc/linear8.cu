@@ -161,7 +161,15 @@ __device__ __forceinline__ void segments(int stages, int most, int& n, int& each
   n = (stages + each - 1) / each;
 }
 
-// Pairs of CTAs (cta_group::2), 256 x 256 tiles.  Warp 0 loads A, warp 2 B, warp 1 issues the MMAs, the others drain the accumulators.
+// Pairs of CTAs (cta_group::2), tiles of 256 x 256 (192, 128 columns).  Warp 0 loads A, warp 2 B, warp 1 issues the MMAs, the others drain the
+// accumulators.
+// What bounds it: the tensor cores, and with them the power cap.  8192 x 14336 x 4096: forward 300 to 340 us = 2.8 to 3.2 P operations/s (the
+// library's 8-bit integer product alone 314 to 355), gradients with the decoding of their codes (16 to 30 us) 680 to 800 us = 1.2 to 1.4 PFLOP/s (the
+// library's bf16 products alone 620 to 940 and 670 to 760).  With short K the epilogue (forward 8192 x 14336 x 512 76 us, of them 36 for the result's
+// way to memory), with few tiles the rounds of them.
+// Not kept: codes made bf16 numbers by warps of this kernel on their way into shared memory, which the CTA of rank 1 has to tell the one of rank
+// 0: an arrival that releases at cluster scope takes 1000 to 1800 cycles, twice to three times what a stage does (8192 x 14336 x 4096 1230 us, by a
+// warp that does nothing else 1660, with a relaxed one, which does not order the codes, 980).
 // LONG: K in segments that the epilogue adds up in registers, because the tensor cores cut every partial sum off toward zero (a K step of 16 leaves
 // an accumulator up to 2^-23 of itself too small).  For gradients in fp32, and for sums above 16384 terms.
 template <int OP, bool LONG>
