@@ -302,3 +302,44 @@ def test_activations_kept_in_e4m3_by_the_norm_make_the_weight_gradient(tokens):
         want = R.decode(y8, scales, group)
         _close(back, want, want.abs() * 2.0**-23, "x")
         T._check_weight_grad(dy, y8.view(torch.uint8), scales, "e4m3", group, BF16, False)
+
+
+FIRST_CALL_IN_A_CAPTURE = """
+import torch, paper_2510_09103_b200 as A
+bf16, i8 = torch.bfloat16, torch.int8
+def buffers(tokens, out, inn):
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    x, w, dy = (torch.randn(*s, generator=g, device="cuda").to(bf16) for s in ((tokens, inn), (out, inn), (tokens, out)))
+    d = A.linear8_desc(tokens, out, inn)
+    return dict(d=d, x=x, w=w, dy=dy, x8=torch.zeros(tokens, inn, dtype=i8, device="cuda"), w8=torch.zeros(out, inn, dtype=i8, device="cuda"),
+                xs=torch.zeros(tokens, device="cuda"), ws=torch.zeros(out, device="cuda"), y=torch.zeros_like(dy), dx=torch.zeros_like(x), dw=torch.zeros_like(w),
+                s=[torch.zeros(A.adapm_linear8_scratch_bytes(d, i), dtype=torch.uint8, device="cuda") for i in range(3)])
+def run(b):
+    A.adapm_quant8(A.quant8_desc(*b["x"].shape), b["x"], b["x8"], b["xs"])
+    A.adapm_quant8(A.quant8_desc(*b["w"].shape), b["w"], b["w8"], b["ws"])
+    A.adapm_linear8_forward(b["d"], b["x8"], b["xs"], b["w8"], b["ws"], b["y"], b["s"][0])
+    A.adapm_linear8_input_grad(b["d"], b["dy"], b["w8"], b["ws"], b["dx"], b["s"][1])
+    A.adapm_linear8_weight_grad(b["d"], b["dy"], b["x8"], b["xs"], b["dw"], b["s"][2])
+sets = [buffers(1, 256, 512), buffers(40, 1376, 512), buffers(3000, 2048, 1024)]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    for b in sets: run(b)
+graph.replay()
+torch.cuda.synchronize()
+got = [[b[k].clone() for k in ("y", "dx", "dw")] for b in sets]
+for b in sets: run(b)
+torch.cuda.synchronize()
+for b, old in zip(sets, got):
+    for k, o in zip(("y", "dx", "dw"), old): assert torch.equal(b[k], o) and o.float().abs().sum() > 0
+print("same")
+"""
+
+
+def test_the_first_call_of_a_process_may_be_a_captured_one():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALL_IN_A_CAPTURE], cwd=root, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
