@@ -438,20 +438,37 @@ __global__ void __launch_bounds__(256) dequant8_odd_kernel(const DequantArgs a) 
   T* const to = static_cast<T*>(a.x) + row * a.x_ld + base + lane;
   const float* const scales = a.scales + (a.per_row ? row : row * a.groups + base / 128);
   const int left = (int)(a.cols - base < 512 ? a.cols - base : 512) - lane;
-  const bool whole = base + 512 <= a.cols;
-  uint32_t q[16];
   float s[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) s[g] = base + 128 * g < a.cols ? scales[a.per_row ? 0 : g] : 0.f;
+  uint32_t b[16];
+  auto decode = [&](int i, float* v) {
+    unpack4<E4M3>(b[4 * i] | (b[4 * i + 1] << 8) | (b[4 * i + 2] << 16) | (b[4 * i + 3] << 24), v);
 #pragma unroll
-  for (int e = 0; e < 16; ++e) q[e] = whole || 32 * e < left ? p[32 * e] : 0u;
+    for (int e = 0; e < 4; ++e) v[e] *= s[i];
+  };
+  // (a block that is whole asks nothing of each element: 16384 x 1601 28 -> 20 us; two or four blocks per warp, their codes on the way at the same time: 20 and 23)
+  if (left > 480) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) b[e] = p[32 * e];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float v[4];
+      decode(i, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) put(to + 32 * (4 * i + e), v[e]);
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 16; ++e) b[e] = 32 * e < left ? p[32 * e] : 0u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float v[4];
-    unpack4<E4M3>(q[4 * i] | (q[4 * i + 1] << 8) | (q[4 * i + 2] << 16) | (q[4 * i + 3] << 24), v);
+    decode(i, v);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (whole || 32 * (4 * i + e) < left) put(to + 32 * (4 * i + e), v[e] * s[i]);
+      if (32 * (4 * i + e) < left) put(to + 32 * (4 * i + e), v[e]);
   }
 }
 
