@@ -6,7 +6,7 @@
 //
 // Every element is read once and written once (rows with one scale above 65536 columns in bf16, 32768 in fp32, are read twice).  A row, or a group
 // of 128 columns, is held in registers between its maximum and its codes.  Bound by HBM: 14336 x 4096 with a scale per row 27 us = 6.5 TB/s, 8192 x
-// 14336 with one per 128 columns 57 to 61 (6.2 to 5.8; 72 % of the issue slots), back 54 (6.6); rows that start anywhere at 0.4 to 0.7 of that.
+// 14336 with one per 128 columns 57 to 61 (6.2 to 5.8; 72 % of the issue slots), back 54 (6.6); rows that start anywhere at 0.5 to 0.75 of that.
 #include <algorithm>
 
 #include "codes.cuh"
@@ -441,13 +441,13 @@ __global__ void __launch_bounds__(256) dequant8_odd_kernel(const DequantArgs a) 
   float s[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) s[g] = base + 128 * g < a.cols ? scales[a.per_row ? 0 : g] : 0.f;
-  uint32_t b[16];
+  uint32_t b[16] = {};
   auto decode = [&](int i, float* v) {
     unpack4<E4M3>(b[4 * i] | (b[4 * i + 1] << 8) | (b[4 * i + 2] << 16) | (b[4 * i + 3] << 24), v);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] *= s[i];
   };
-  // (a block that is whole asks nothing of each element: 16384 x 1601 28 -> 20 us; two or four blocks per warp, their codes on the way at the same time: 20 and 23)
+  // (a block that is whole asks nothing of each element: 16384 x 1601 28 -> 18 us; two or four blocks per warp, their codes on the way at the same time: 20 and 23)
   if (left > 480) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) b[e] = p[32 * e];
