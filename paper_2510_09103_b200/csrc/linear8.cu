@@ -25,16 +25,16 @@ using namespace tc;
 
 constexpr int kOperandBytes = 16384;             // of one CTA and stage: 128 rows or columns of an operand, 128 bytes of K (or the reverse)
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kBoxBytesOut = 2048;                // of a warp's box of results
 constexpr int kSegLong = 4, kSegShort = 64;      // stages of 64 K between two sums in registers: gradients in fp32, long ones in bf16
 
-template <int OP, bool LONG>
+// WIDE: boxes of results with rows of 128 bytes (see Outlet); only without LONG.
+template <int OP, bool LONG, bool WIDE>
 struct Shape {
   static constexpr bool kGrad = OP != FORWARD;
   static constexpr int kDrain = LONG ? 8 : 16;   // warps that drain, after four that issue
   static constexpr int kThreads = 32 * (4 + kDrain);
-  static constexpr int kStages = 6;
-  static constexpr int kSmem = kStages * kStageBytes + kDrain * kBoxBytesOut + 1024;
+  static constexpr int kStages = WIDE ? 5 : 6, kBox = WIDE ? 4096 : 2048;
+  static constexpr int kSmem = kStages * kStageBytes + kDrain * kBox + 1024;
 };
 // LONG: registers of the launch, and as the first four and the other eight warps divide them (the eight keep 128 sums each).
 constexpr int kLongRegs = 168, kLongIssue = 88, kLongDrain = 208;
@@ -51,9 +51,9 @@ struct Args {
   int32_t pairs, out_f32, accumulate, seg;
 };
 
-template <int OP, bool LONG>
+template <int OP, bool LONG, bool WIDE>
 struct __align__(8) Shared {
-  using S = Shape<OP, LONG>;
+  using S = Shape<OP, LONG, WIDE>;
   uint64_t full[S::kStages], empty[S::kStages], tfull[2], tempty[2];
   uint32_t tmem_base;
   int abort;
@@ -106,24 +106,30 @@ __device__ __forceinline__ void add_row32(const void* base, int64_t at, float* x
   }
 }
 
-// A warp's way out: 32 rows of 64 bytes (16 columns in fp32, 32 in bf16) are put into its box in shared memory, with the 64-byte
-// swizzle, and stored as a whole by TMA, which leaves out what the result does not have.  (Every thread storing 32 bytes of a row of its
+// A warp's way out: 32 rows of 64 bytes (16 columns in fp32, 32 in bf16), or (WIDE) of 128, are put into its box in shared memory, with the
+// swizzle of as many, and stored as a whole by TMA, which leaves out what the result does not have.  (Every thread storing 32 bytes of a row of its
 // own: weight gradient of 1 x 14336 x 4096 36 to 42 us, with a box 27.  Eight warps with boxes of 128 bytes for 128 columns each instead of
 // sixteen for 64: forward 8192 x 14336 x 512 92 us for 76.)
+// Wide boxes are for results in bf16 whose rows do not all start on 32 bytes: of a row of 64 bytes two sectors of three are then written in two
+// pieces (input gradient 10166 x 144 x 12408 110 us, wide 86; 12416 columns 68 and 71; forward 15697 x 7576 x 280 94 and 72).  Two warps that fill a
+// wide box together, which leaves the sixth stage: 87 and 78, and 8 % more where rows start on 32 bytes.
+template <bool WIDE>
 struct Outlet {
   const CUtensorMap* map;
   uint8_t* box;
   int lane;
-  // 32 columns from column `col` on of the rows from `row0` on, the lane's own in x; `part`: of K.
-  __device__ __forceinline__ void put32(const float* x, int col, int row0, int part, bool f32, int rows, int cols) {
-    uint8_t* const line = box + lane * 64;
-    const int swap = (lane >> 1) & 3;
+  // 32 columns from column `col` on of the rows from `row0` on, the lane's own in x; `part`: of K; `half`: whether they are the second 32 of 64.
+  __device__ __forceinline__ void put32(const float* x, int half, int col, int row0, int part, bool f32, int rows, int cols) {
+    uint8_t* const line = box + lane * (WIDE ? 128 : 64);
+    const int swap = WIDE ? lane & 7 : (lane >> 1) & 3, first = WIDE ? 4 * half : 0;      // (a wide box takes two turns)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      if (!f32 && h == 1) break;
-      if (lane == 0) bulk_wait_group_read<0>();
-      __syncwarp();
-      if (f32) {
+      if ((WIDE || !f32) && h == 1) break;
+      if (first == 0) {
+        if (lane == 0) bulk_wait_group_read<0>();
+        __syncwarp();
+      }
+      if (!WIDE && f32) {
 #pragma unroll
         for (int c = 0; c < 4; ++c)
           *reinterpret_cast<float4*>(line + ((c ^ swap) * 16)) = make_float4(x[16 * h + 4 * c], x[16 * h + 4 * c + 1], x[16 * h + 4 * c + 2], x[16 * h + 4 * c + 3]);
@@ -133,13 +139,15 @@ struct Outlet {
           uint32_t w[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2_rn(x[8 * c + 2 * e], x[8 * c + 2 * e + 1]);
-          put4(line + ((c ^ swap) * 16), w);
+          put4(line + (((first + c) ^ swap) * 16), w);
         }
       }
+      if (WIDE && half == 0) continue;
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
-        if (row0 < rows && col + 16 * h < cols) tma_store_box3(map, col + 16 * h, row0, part, box);
+        const int from = col + 16 * h - 8 * first;
+        if (row0 < rows && from < cols) tma_store_box3(map, from, row0, part, box);
         bulk_commit_group();
       }
     }
@@ -147,11 +155,12 @@ struct Outlet {
 };
 
 // What a gradient's item does with 32 columns of its sums.
-__device__ __forceinline__ void finish32(const Args& a, const Cut& t, Outlet& out, int row0, int col, float* x) {
+template <bool WIDE>
+__device__ __forceinline__ void finish32(const Args& a, const Cut& t, Outlet<WIDE>& out, int half, int row0, int col, float* x) {
   const int row = row0 + out.lane;
   if (a.accumulate && a.plan.parts == 1 && row < a.plan.rows) add_row32(a.out, (int64_t)row * a.out_ld + col, x, a.plan.cols - col, a.out_f32);
   __syncwarp();
-  out.put32(x, col, row0, t.part, a.plan.parts > 1 || a.out_f32, a.plan.rows, a.plan.cols);
+  out.put32(x, half, col, row0, t.part, a.plan.parts > 1 || a.out_f32, a.plan.rows, a.plan.cols);
 }
 
 // An item's K in segments of even length: how many, and the stages of each but the last.
@@ -172,11 +181,11 @@ __device__ __forceinline__ void segments(int stages, int most, int& n, int& each
 // warp that does nothing else 1660, with a relaxed one, which does not order the codes, 980).
 // LONG: K in segments that the epilogue adds up in registers, because the tensor cores cut every partial sum off toward zero (a K step of 16 leaves
 // an accumulator up to 2^-23 of itself too small).  For gradients in fp32, and for sums above 16384 terms.
-template <int OP, bool LONG>
-__global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(const __grid_constant__ Args a) {
-  using S = Shape<OP, LONG>;
+template <int OP, bool LONG, bool WIDE>
+__global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_kernel(const __grid_constant__ Args a) {
+  using S = Shape<OP, LONG, WIDE>;
   extern __shared__ uint8_t dyn_smem[];
-  __shared__ Shared<OP, LONG> sh;
+  __shared__ Shared<OP, LONG, WIDE> sh;
   let_next_kernel_start();
   const uint32_t rank = cluster_rank();
   uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(dyn_smem) + 1023) & ~(uintptr_t)1023);
@@ -303,7 +312,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
     // group of four warps, 64 (LONG: 128) of the columns
     const int q = 32 * (warp & 3) + lane, grp = (warp - 4) >> 2;
     const uint32_t lane_addr = (uint32_t)(32 * (warp & 3)) << 16;
-    Outlet out = {&a.o, ring + S::kStages * kStageBytes + (warp - 4) * kBoxBytesOut, lane};
+    Outlet<WIDE> out = {&a.o, ring + S::kStages * kStageBytes + (warp - 4) * S::kBox, lane};
     uint32_t run = 0;
     bool ok = true;
     auto wait_full = [&](int acc) {
@@ -352,7 +361,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
         if (!ok) break;
 #pragma unroll
         for (int c = 0; c < 128; c += 32)
-          if (c < mine) finish32(a, t, out, row - lane, col0 + c, v + c);
+          if (c < mine) finish32(a, t, out, c / 32 % 2, row - lane, col0 + c, v + c);
       } else {
         const int acc = (int)(run & 1);
         const float xs = OP == FORWARD && row < a.plan.rows ? a.a_scale[row] : 0.f;
@@ -384,9 +393,9 @@ __global__ void __launch_bounds__(Shape<OP, LONG>::kThreads, 1) linear8_kernel(c
                 v[4 * e + 3] = (float)__float_as_int(v[4 * e + 3]) * xs * ws[e].w;
               }
               if (c == 0) scales_of(col0 + 32);
-              out.put32(v, col0 + c, row - lane, 0, a.out_f32, a.plan.rows, a.plan.cols);
+              out.put32(v, c / 32, col0 + c, row - lane, 0, a.out_f32, a.plan.rows, a.plan.cols);
             } else {
-              finish32(a, t, out, row - lane, col0 + c, v);
+              finish32(a, t, out, c / 32, row - lane, col0 + c, v);
             }
           }
         } else {
@@ -1034,18 +1043,21 @@ bool encode_planes(CUtensorMap* out, const void* base, int64_t planes, int64_t r
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// `parts` results [rows, cols], one behind the other, in boxes of 32 rows of 64 bytes with the 64-byte swizzle.
-bool encode_result(CUtensorMap* out, void* base, int64_t parts, int64_t rows, int64_t cols, int64_t pitch, bool f32) {
+// `parts` results [rows, cols], one behind the other, in boxes of 32 rows of 64 bytes, or `wide` of 128, with the swizzle of as many.
+bool encode_result(CUtensorMap* out, void* base, int64_t parts, int64_t rows, int64_t cols, int64_t pitch, bool f32, bool wide) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t bytes = f32 ? 4 : 2, line = (cuuint64_t)pitch * bytes;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)parts};
   const cuuint64_t strides[2] = {line, parts > 1 ? (cuuint64_t)rows * line : line};
-  const cuuint32_t box[3] = {(cuuint32_t)(64 / bytes), 32, 1};
+  const cuuint32_t box[3] = {(cuuint32_t)((wide ? 128 : 64) / bytes), 32, 1};
   const cuuint32_t estr[3] = {1, 1, 1};
   return fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+            wide ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+// Whether some row of a result starts inside a sector of 32 bytes.
+bool off_sectors(const void* out, int64_t pitch, bool f32) { return !f32 && ((uintptr_t)out % 32 || pitch % 16); }
 
 // A row-major matrix of bytes in boxes of 128 columns x box_rows rows, with the 128-byte swizzle or as they lie.
 bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows, bool swizzle = true) {
@@ -1060,13 +1072,13 @@ bool encode_bytes(CUtensorMap* out, const void* base, uint64_t rows, uint64_t co
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int OP, bool LONG>
+template <int OP, bool LONG, bool WIDE>
 int allow(int* resident, int sms) {
-  using S = Shape<OP, LONG>;
-  ADAPM_CUDA(cudaFuncSetAttribute(linear8_kernel<OP, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
+  using S = Shape<OP, LONG, WIDE>;
+  ADAPM_CUDA(cudaFuncSetAttribute(linear8_kernel<OP, LONG, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem));
   if (LONG) {
     cudaFuncAttributes fa;                  // (with fewer registers at launch the split above would wait for ever)
-    ADAPM_CUDA(cudaFuncGetAttributes(&fa, linear8_kernel<OP, LONG>));
+    ADAPM_CUDA(cudaFuncGetAttributes(&fa, linear8_kernel<OP, LONG, WIDE>));
     if (fa.numRegs < kLongRegs) {
       set_error_text("linear8_kernel was built with fewer registers than it divides among its warps");
       return ADAPM_EUNSUPPORTED;
@@ -1079,7 +1091,7 @@ int allow(int* resident, int sms) {
   at.val.clusterDim.x = 2; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
   cfg.attrs = &at; cfg.numAttrs = 1;
   int n = 0;
-  ADAPM_CUDA(cudaOccupancyMaxActiveClusters(&n, linear8_kernel<OP, LONG>, &cfg));
+  ADAPM_CUDA(cudaOccupancyMaxActiveClusters(&n, linear8_kernel<OP, LONG, WIDE>, &cfg));
   *resident = std::min(*resident, n);
   return ADAPM_OK;
 }
@@ -1108,11 +1120,14 @@ int pairs_of(int device, int* pairs) {
     int sms = 0;
     ADAPM_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device));
     int n = std::min(sms / 2, (int)kMostWords);
-    int rc = allow<FORWARD, false>(&n, sms);
-    if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, false>(&n, sms);
-    if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, true>(&n, sms);
-    if (rc == ADAPM_OK) rc = allow<WEIGHT_GRAD, false>(&n, sms);
-    if (rc == ADAPM_OK) rc = allow<WEIGHT_GRAD, true>(&n, sms);
+    int rc = allow<FORWARD, false, false>(&n, sms);
+    if (rc == ADAPM_OK) rc = allow<FORWARD, false, true>(&n, sms);
+    if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, false, false>(&n, sms);
+    if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, false, true>(&n, sms);
+    if (rc == ADAPM_OK) rc = allow<INPUT_GRAD, true, false>(&n, sms);
+    if (rc == ADAPM_OK) rc = allow<WEIGHT_GRAD, false, false>(&n, sms);
+    if (rc == ADAPM_OK) rc = allow<WEIGHT_GRAD, false, true>(&n, sms);
+    if (rc == ADAPM_OK) rc = allow<WEIGHT_GRAD, true, false>(&n, sms);
     if (rc == ADAPM_OK) rc = allow_strips<FORWARD, false>();
     if (rc == ADAPM_OK) rc = allow_strips<INPUT_GRAD, false>();
     if (rc == ADAPM_OK) rc = allow_strips<INPUT_GRAD, true>();
@@ -1125,11 +1140,13 @@ int pairs_of(int device, int* pairs) {
   return ADAPM_OK;
 }
 
-template <int OP, bool LONG>
+template <int OP, bool LONG, bool WIDE>
 cudaError_t launch(const Args& a, cudaStream_t s) {
-  using S = Shape<OP, LONG>;
-  return launch_clusters(true, 2, linear8_kernel<OP, LONG>, 2 * (unsigned)a.pairs, S::kThreads, S::kSmem, s, a);
+  using S = Shape<OP, LONG, WIDE>;
+  return launch_clusters(true, 2, linear8_kernel<OP, LONG, WIDE>, 2 * (unsigned)a.pairs, S::kThreads, S::kSmem, s, a);
 }
+template <int OP>
+cudaError_t launch_short(const Args& a, bool wide, cudaStream_t s) { return wide ? launch<OP, false, true>(a, s) : launch<OP, false, false>(a, s); }
 
 struct Buffer { const void* p; int64_t align; Place at; };
 
@@ -1206,7 +1223,9 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
   a.pairs = std::min(pairs, plan.items);
   a.seg = a.out_f32 ? kSegLong : kSegShort;
   const bool is_long = a.out_f32 || plan.each > kShortStages;
-  if (!(plan.parts > 1 ? encode_result(&a.o, parts, plan.parts, plan.rows, plan.cols, plan.cols, true) : encode_result(&a.o, out, 1, plan.rows, plan.cols, out_ld, a.out_f32))) {
+  const bool wide = !is_long && plan.parts == 1 && off_sectors(out, out_ld, a.out_f32);
+  if (!(plan.parts > 1 ? encode_result(&a.o, parts, plan.parts, plan.rows, plan.cols, plan.cols, true, wide)
+                       : encode_result(&a.o, out, 1, plan.rows, plan.cols, out_ld, a.out_f32, wide))) {
     set_error_text("cuTensorMapEncodeTiled failed for a gradient of linear8");
     return ADAPM_ECUDA;
   }
@@ -1226,8 +1245,8 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
     const int rc = launch_dequant8(q, codes, scales, decoded, s);
     if (rc != ADAPM_OK) return rc;
   }
-  ADAPM_CUDA(weight ? (is_long ? launch<WEIGHT_GRAD, true>(a, s) : launch<WEIGHT_GRAD, false>(a, s))
-                    : (is_long ? launch<INPUT_GRAD, true>(a, s) : launch<INPUT_GRAD, false>(a, s)));
+  ADAPM_CUDA(weight ? (is_long ? launch<WEIGHT_GRAD, true, false>(a, s) : launch_short<WEIGHT_GRAD>(a, wide, s))
+                    : (is_long ? launch<INPUT_GRAD, true, false>(a, s) : launch_short<INPUT_GRAD>(a, wide, s)));
   if (plan.parts == 1) return ADAPM_OK;
   SumArgs u;
   u.part = parts; u.out = out; u.out_ld = out_ld; u.fours = plan.cols / 4; u.places = (int64_t)plan.rows * u.fours;
@@ -1292,8 +1311,9 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
   Args a;
   std::memset(&a, 0, sizeof(a));
   a.plan = plan;
+  const bool wide = off_sectors(y, d->y_ld, d->y_dtype == ADAPM_TYPE_F32);
   if (!encode_bytes(&a.a, x8, d->tokens, d->in_features, d->x8_ld, 128) || !encode_bytes(&a.b, w8, d->out_features, d->in_features, d->w8_ld, 128) ||
-      !encode_result(&a.o, y, 1, d->tokens, d->out_features, d->y_ld, d->y_dtype == ADAPM_TYPE_F32)) {
+      !encode_result(&a.o, y, 1, d->tokens, d->out_features, d->y_ld, d->y_dtype == ADAPM_TYPE_F32, wide)) {
     set_error_text("cuTensorMapEncodeTiled failed for linear8");
     return ADAPM_ECUDA;
   }
@@ -1301,7 +1321,7 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
   a.out = y; a.out_ld = d->y_ld; a.out_f32 = d->y_dtype == ADAPM_TYPE_F32;
   a.status = (int32_t*)scratch;
   a.pairs = std::min(pairs, plan.items);
-  ADAPM_CUDA((launch<FORWARD, false>(a, (cudaStream_t)stream)));
+  ADAPM_CUDA(launch_short<FORWARD>(a, wide, (cudaStream_t)stream));
   return ADAPM_OK;
 }
 
