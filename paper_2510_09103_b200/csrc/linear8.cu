@@ -111,7 +111,7 @@ __device__ __forceinline__ void add_row32(const void* base, int64_t at, float* x
 // own: weight gradient of 1 x 14336 x 4096 36 to 42 us, with a box 27.  Eight warps with boxes of 128 bytes for 128 columns each instead of
 // sixteen for 64: forward 8192 x 14336 x 512 92 us for 76.)
 // Wide boxes are for results in bf16 whose rows do not all start on 32 bytes: of a row of 64 bytes two sectors of three are then written in two
-// pieces (input gradient 10166 x 144 x 12408 110 us, wide 86; 12416 columns 68 and 71; forward 15697 x 7576 x 280 94 and 72).  Two warps that fill a
+// pieces (input gradient 10166 x 144 x 12408 112 us, wide 87; 12416 columns without 67; forward 15697 x 7576 x 280 95 and 72).  Two warps that fill a
 // wide box together, which leaves the sixth stage: 87 and 78, and 8 % more where rows start on 32 bytes.
 template <bool WIDE>
 struct Outlet {
@@ -365,11 +365,11 @@ __global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_ke
       } else {
         const int acc = (int)(run & 1);
         const float xs = OP == FORWARD && row < a.plan.rows ? a.a_scale[row] : 0.f;
-        // (the columns' scales are asked for 32 columns ahead: 2048 x 2736 x 1024 forward 13.3 -> 11.4 us)
-        float4 ws[8];
+        // (the columns' scales are asked for sixteen columns ahead: forward 2048 x 2736 x 1024 13.3 -> 10.3 us; 32 ahead, which does not fit the registers, 10.6)
+        float4 ws[4];
         auto scales_of = [&](int col) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) ws[e] = col + 4 * e < a.plan.cols ? __ldg(reinterpret_cast<const float4*>(a.b_scale + col + 4 * e)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int e = 0; e < 4; ++e) ws[e] = col + 4 * e < a.plan.cols ? __ldg(reinterpret_cast<const float4*>(a.b_scale + col + 4 * e)) : make_float4(0.f, 0.f, 0.f, 0.f);
         };
         if (OP == FORWARD) scales_of(col0);
         wait_full(acc);
@@ -386,13 +386,17 @@ __global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_ke
             if (c == 32) release(acc);
             if (OP == FORWARD) {
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                v[4 * e] = (float)__float_as_int(v[4 * e]) * xs * ws[e].x;
-                v[4 * e + 1] = (float)__float_as_int(v[4 * e + 1]) * xs * ws[e].y;
-                v[4 * e + 2] = (float)__float_as_int(v[4 * e + 2]) * xs * ws[e].z;
-                v[4 * e + 3] = (float)__float_as_int(v[4 * e + 3]) * xs * ws[e].w;
+              for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  float* const to = v + 16 * h + 4 * e;
+                  to[0] = (float)__float_as_int(to[0]) * xs * ws[e].x;
+                  to[1] = (float)__float_as_int(to[1]) * xs * ws[e].y;
+                  to[2] = (float)__float_as_int(to[2]) * xs * ws[e].z;
+                  to[3] = (float)__float_as_int(to[3]) * xs * ws[e].w;
+                }
+                if (c + 16 * h < 48) scales_of(col0 + c + 16 * h + 16);
               }
-              if (c == 0) scales_of(col0 + 32);
               out.put32(v, c / 32, col0 + c, row - lane, 0, a.out_f32, a.plan.rows, a.plan.cols);
             } else {
               finish32(a, t, out, c / 32, row - lane, col0 + c, v);
