@@ -444,8 +444,8 @@ struct PlanesArgs {
   const uint8_t* codes;
   const float* scales;
   int32_t* words;
-  uint16_t* out;                 // [planes][rows][cols]
-  int64_t codes_ld, rows, scan;  // scan: scales to look through, 0: the words say it
+  uint16_t* out;                 // [planes][rows][ld]
+  int64_t codes_ld, ld, rows, scan;  // scan: scales to look through, 0: the words say it
   int32_t cols, groups;          // cols: a multiple of eight; scales per row
 };
 
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(256) linear8_planes_kernel(const PlanesArgs a)
   others = __syncthreads_or(others);
   if (a.scan && blockIdx.x == 0) a.words[threadIdx.x] = others;
   const int planes = others ? kPlanesF32 : 1, eights = a.cols / 8;
-  const int64_t chunks = a.rows * eights, plane = a.rows * a.cols;
+  const int64_t chunks = a.rows * eights, plane = a.rows * a.ld;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < chunks; i += (int64_t)gridDim.x * 256) {
     const int64_t row = chunks <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)eights) : i / eights;
     const int c = 8 * (int)(i - row * eights);
@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(256) linear8_planes_kernel(const PlanesArgs a)
         w[e] = pack_bf16x2_rn(v[e].x, v[e].y);
         v[e] = left_of_bf16(v[e]);
       }
-      put4(a.out + p * plane + i * 8, w);
+      put4(a.out + p * plane + row * a.ld + c, w);
     }
   }
 }
@@ -1036,11 +1036,11 @@ __global__ void __launch_bounds__(kLineThreads) linear8_line_kernel(const LineAr
 // ---- host ----------------------------------------------------------------------------------------------------------
 
 // `planes` matrices of bf16 numbers [rows, cols], one behind the other, in boxes of 64 columns x 64 rows.
-bool encode_planes(CUtensorMap* out, const void* base, int64_t planes, int64_t rows, int64_t cols) {
+bool encode_planes(CUtensorMap* out, const void* base, int64_t planes, int64_t rows, int64_t cols, int64_t pitch) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (!fn) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes};
-  const cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)(rows * cols) * 2};
+  const cuuint64_t strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)(rows * pitch) * 2};
   const cuuint32_t box[3] = {64, 64, 1};
   const cuuint32_t estr[3] = {1, 1, 1};
   return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -1212,10 +1212,10 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
   a.plan = plan;
   void* const decoded = (char*)scratch + kHeadBytes;
   adapm_codes8 q;
-  q.rows = weight ? d.tokens : d.out_features; q.cols = d.in_features; q.x_ld = d.in_features; q.codes_ld = weight ? d.x8_ld : d.w8_ld;
+  q.rows = weight ? d.tokens : d.out_features; q.cols = d.in_features; q.x_ld = decoded_pitch(d.in_features); q.codes_ld = weight ? d.x8_ld : d.w8_ld;
   q.dtype = ADAPM_TYPE_BF16; q.code = weight ? d.x_code : ADAPM_CODE_INT8; q.group = weight ? d.x_group : 0; q.pow2 = 0;
   const int planes = out_dtype == ADAPM_TYPE_F32 ? kPlanesF32 : 1;
-  if (!encode_bf16_matrix(&a.a, dy, d.tokens, d.out_features, d.y_ld, weight ? 64 : 128) || !encode_planes(&a.b, decoded, planes, q.rows, q.cols)) {
+  if (!encode_bf16_matrix(&a.a, dy, d.tokens, d.out_features, d.y_ld, weight ? 64 : 128) || !encode_planes(&a.b, decoded, planes, q.rows, q.cols, q.x_ld)) {
     set_error_text("cuTensorMapEncodeTiled failed for a gradient of linear8");
     return ADAPM_ECUDA;
   }
@@ -1241,7 +1241,7 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
     PlanesArgs p;
     p.codes = static_cast<const uint8_t*>(codes); p.scales = scales; p.words = words; p.out = (uint16_t*)decoded;
     p.scan = n > kFewScales ? 0 : n;
-    p.codes_ld = q.codes_ld; p.rows = q.rows; p.cols = (int32_t)q.cols; p.groups = q.group ? (int32_t)((q.cols + 127) / 128) : 1;
+    p.codes_ld = q.codes_ld; p.ld = q.x_ld; p.rows = q.rows; p.cols = (int32_t)q.cols; p.groups = q.group ? (int32_t)((q.cols + 127) / 128) : 1;
     const int64_t chunks = q.rows * (q.cols / 8);
     const unsigned grid = (unsigned)std::min<int64_t>((chunks + 255) / 256, 148 * 16);
     ADAPM_CUDA(q.code == ADAPM_CODE_E4M3 ? launch_chained(true, linear8_planes_kernel<true>, grid, 256, 0, s, p) : launch_chained(true, linear8_planes_kernel<false>, grid, 256, 0, s, p));

@@ -23,6 +23,9 @@ constexpr int kPlanesF32 = 3, kPlanesBf16 = 2;   // bf16 numbers that one times 
 constexpr int kPlannedPairs = 74;                // what the number of parts goes by: results do not depend on the device's own number
 constexpr int kShortStages = 256;                // longest K, in stages of 64, that one accumulator takes for a gradient in bf16
 
+// Of the codes' bf16 numbers in the scratch: rows start on 128 bytes (2048 x 4104 x 4104 weight gradient 81 -> 66 us).
+inline int64_t decoded_pitch(int64_t cols) { return round_up(cols, 64); }
+
 struct Cut { int m0, n0, bn, k0, count, part; };
 
 // A result of `rows` x `cols`, K of `stages` stages, cut into `parts` parts of `each` stages (the last may be shorter).
@@ -70,7 +73,7 @@ inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool gra
       p.items = (int32_t)(tiles * parts);
     }
   }
-  p.part_at = kHeadBytes + (grad ? round_up(k * cols * 2 * (f32 ? kPlanesF32 : 1), 256) : 0);
+  p.part_at = kHeadBytes + (grad ? round_up(k * decoded_pitch(cols) * 2 * (f32 ? kPlanesF32 : 1), 256) : 0);
   p.bytes = p.part_at + (p.parts > 1 ? round_up((int64_t)p.parts * rows * cols * 4, 256) : 0);
   return p;
 }
@@ -115,6 +118,17 @@ inline bool f32_gradient(const adapm_linear8& d, int32_t which) {
   return which == INPUT_GRAD ? d.dx_dtype == ADAPM_TYPE_F32 : which == WEIGHT_GRAD && d.dweight_dtype == ADAPM_TYPE_F32;
 }
 
+// What strips were measured to take (us): a start and end, longer with their width, stages, and the sums' ways through a cluster.  (Within 6 % of the measured
+// times of 240 gradients.)
+inline double strips_take(const StripPlan& s, int32_t which) {
+  const double width = s.width, each = (s.stages + s.split - 1) / s.split, levels = s.split == 8 ? 3 : s.split == 4 ? 2 : s.split == 2 ? 1 : 0;
+  const double rounds = (double)((s.ctas + 2 * kPlannedPairs - 1) / (2 * kPlannedPairs));
+  if (which == FORWARD) return 2.0 + rounds * (3.2 + 0.012 * width + each * (0.16 + 0.0006 * width) + levels * (0.3 + 0.0025 * width));
+  const double cluster = s.split == 1 ? 0.0 : s.fold ? 1.0 : 0.9 + levels * (0.004 * width - 0.25);
+  if (s.fold) return 2.0 + rounds * (2.8 + 0.026 * width + each * (0.39 + 0.0076 * width) + cluster);
+  return 2.0 + rounds * (2.5 + 0.011 * width + each * (0.35 + 0.0005 * width) + cluster);
+}
+
 inline StripPlan strip_plan_of(const adapm_linear8& d, int32_t which) {
   const int64_t features = which == FORWARD ? d.out_features : d.in_features, columns = which == WEIGHT_GRAD ? d.out_features : d.tokens;
   const int64_t k = which == FORWARD ? d.in_features : which == INPUT_GRAD ? d.out_features : d.tokens;
@@ -124,26 +138,40 @@ inline StripPlan strip_plan_of(const adapm_linear8& d, int32_t which) {
   // 34 for 28)
   p.fold = which != FORWARD && (f32 || columns <= kFoldFew);
   p.planes = !p.fold ? 1 : f32 ? kPlanesF32 : kPlanesBf16;
-  const int widest = p.fold ? kFoldWidth : kStripWidth;
-  p.c_tiles = (int32_t)((columns + widest - 1) / widest);
-  p.width = (int32_t)round_up((columns + p.c_tiles - 1) / std::max(1, p.c_tiles), which == WEIGHT_GRAD ? 64 : 16);
   p.f_tiles = (int32_t)((features + 127) / 128);
-  const int step = which == FORWARD ? 128 : 64;
+  const int step = which == FORWARD ? 128 : 64, unit = which == WEIGHT_GRAD ? 64 : 16, widest = p.fold ? kFoldWidth : kStripWidth;
   p.stages = (int32_t)((k + step - 1) / step);
-  const int64_t tiles = (int64_t)p.c_tiles * p.f_tiles;
+  // How many strips, and how many CTAs to each: what takes least, as long as all run at the same time.  (Clusters have to fit the device's groups of
+  // SMs: 1024 x 512 x 14336 in sixteen clusters of eight 29 us, of four 20; 42 x 2176 x 2256 forward in 34 of four 10.8, in 17 6.4.)
+  const int64_t fewest = (columns + widest - 1) / widest;
+  int64_t split = 1;
+  int32_t width = 0, last = -1;
+  double best = -1;
+  for (int64_t n = fewest; n == fewest || (n * p.f_tiles <= 2 * kPlannedPairs && n < 2 * fewest + 8); ++n) {
+    p.width = (int32_t)round_up((columns + n - 1) / std::max<int64_t>(1, n), unit);
+    if (p.width == last) continue;
+    last = p.width;
+    const int64_t tiles = (columns + p.width - 1) / std::max(1, p.width) * p.f_tiles;
+    const int64_t most = std::min<int64_t>(p.stages, tiles <= 8 ? 8 : tiles <= 32 ? 4 : tiles <= kPlannedPairs ? 2 : 1);
+    for (p.split = 1; p.split == 1 || p.split <= most; p.split *= 2) {
+      p.ctas = (int32_t)std::min<int64_t>(tiles * p.split, INT32_MAX);
+      const double t = strips_take(p, which);
+      if (best >= 0 && t >= best) continue;
+      best = t; width = p.width; split = p.split;
+    }
+  }
+  p.width = width; p.split = (int32_t)split;
+  p.c_tiles = (int32_t)((columns + width - 1) / std::max(1, width));
+  p.ctas = (int32_t)std::min<int64_t>((int64_t)p.c_tiles * p.f_tiles * split, INT32_MAX);
   p.stage_bytes = 16384 + 128 * p.width * p.planes;
   p.raw_bytes = which == FORWARD ? 0 : kStripRawBytes + (p.fold ? 128 * p.width : 0);
   p.ring = std::max(kStripTeams, std::min(kStripRing, (kStripSmem - (p.fold ? kStripTeams : kStripRing) * p.raw_bytes) / p.stage_bytes));
   p.raw = which == FORWARD ? 0 : std::min(kStripRing, (kStripSmem - p.ring * p.stage_bytes) / p.raw_bytes);
-  p.split = 1;
-  // (sixteen clusters of eight do not fit the device's groups of SMs at the same time: 1024 x 512 x 14336 in eighths 29 us, in quarters 20)
-  while (p.split < (tiles <= 8 ? 8 : 4) && tiles * p.split <= kPlannedPairs && 4 * p.split <= p.stages) p.split *= 2;
-  p.ctas = (int32_t)std::min<int64_t>(tiles * p.split, INT32_MAX);
   return p;
 }
 
-// Whether a call goes by strips, by what both forms were measured to take (us): a strip's start and end, longer with its width, and its stages;
-// a pair's 256 x 256 tiles, for a gradient with the launch that decodes its codes and the one that sums the parts of K.
+// Whether a call goes by strips, by what both forms were measured to take (us): strips as above; a pair's 256 x 256 tiles, for a gradient with the launch that decodes its codes and the
+// one that sums the parts of K.
 inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const StripPlan& s, const Plan& p) {
   if (s.ctas > kMostWords) return false;
   const bool f32 = f32_gradient(d, which);
@@ -151,11 +179,7 @@ inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const Strip
   if (s.fold && !f32) return true;                    // (for what the call promises)
   if (which != FORWARD && !s.fold && each > kShortStages) return false;
   const bool grad = which != FORWARD;
-  int levels = 0;                                     // of the cluster
-  while ((1 << levels) < s.split) ++levels;
-  const double rounds = (double)((s.ctas + 2 * kPlannedPairs - 1) / (2 * kPlannedPairs));
-  const double stage = s.fold ? 0.36 + 0.008 * s.width : grad ? 0.36 + 0.0005 * s.width : 0.16 + 0.0006 * s.width, level = grad ? 0.4 + 0.006 * s.width : 0.3 + 0.0025 * s.width;
-  const double strips = 2.0 + rounds * ((f32 ? 4.3 : grad ? 2.3 : 3.2) + 0.012 * s.width + each * stage + levels * level);
+  const double strips = strips_take(s, which);
   const double pair_rounds = (double)((p.items + kPlannedPairs - 1) / kPlannedPairs);
   double pairs = 6.0 + pair_rounds * (1.0 + 0.31 * p.each * (f32 ? kPlanesF32 : 1) * (0.2 + 0.8 / 256 * p.width));
   if (grad) pairs += (f32 ? 3.5 + 1.2e-6 * p.stages * 64.0 * p.cols : 2.0 + 5e-7 * p.stages * 64.0 * p.cols) + (p.parts > 1 ? 2.5 + 5e-7 * p.rows * (double)p.cols * p.parts : 0);
