@@ -180,9 +180,12 @@ inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const Strip
   if (which != FORWARD && !s.fold && each > kShortStages) return false;
   const bool grad = which != FORWARD;
   const double strips = strips_take(s, which);
-  const double pair_rounds = (double)((p.items + kPlannedPairs - 1) / kPlannedPairs);
-  double pairs = 6.0 + pair_rounds * (1.0 + 0.31 * p.each * (f32 ? kPlanesF32 : 1) * (0.2 + 0.8 / 256 * p.width));
-  if (grad) pairs += (f32 ? 3.5 + 1.2e-6 * p.stages * 64.0 * p.cols : 2.0 + 5e-7 * p.stages * 64.0 * p.cols) + (p.parts > 1 ? 2.5 + 5e-7 * p.rows * (double)p.cols * p.parts : 0);
+  const double pair_rounds = (double)((p.items + kPlannedPairs - 1) / kPlannedPairs), wide = 0.2 + 0.8 / 256 * p.width, out = (double)p.rows * p.cols * p.parts / 1e6;
+  if (!grad) return strips < 6.0 + pair_rounds * (1.0 + 0.31 * p.each * wide);
+  const double decoded = 64e-6 * p.stages * p.cols, dy = 1e-6 * d.tokens * d.out_features;
+  double pairs;
+  if (f32) pairs = 8.0 + pair_rounds * (1.0 + 0.37 * kPlanesF32 * p.each * wide) + 0.14 * dy + 1.5 * decoded + (p.parts > 1 ? 3.5 + 1.7 * out : 0);
+  else pairs = 7.0 + pair_rounds * (1.5 + 0.39 * p.each * wide) + 0.1 * dy + 0.5 * decoded + (p.parts > 1 ? 4.5 + 0.25 * out : 0);
   return strips < pairs;
 }
 
