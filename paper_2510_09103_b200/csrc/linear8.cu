@@ -48,13 +48,13 @@ struct Args {
   int32_t* status;
   const int32_t* scale_words;    // a gradient in fp32: not all zero where B has three planes
   int64_t out_ld;
-  int32_t pairs, out_f32, accumulate, seg;
+  int32_t pairs, out_f32, accumulate, seg;      // accumulate: not where K has parts
 };
 
 template <int OP, bool LONG, bool WIDE>
 struct __align__(8) Shared {
   using S = Shape<OP, LONG, WIDE>;
-  uint64_t full[S::kStages], empty[S::kStages], tfull[2], tempty[2];
+  uint64_t full[S::kStages], empty[S::kStages], tfull[2], tempty[2], old_full[S::kDrain];
   uint32_t tmem_base;
   int abort;
 };
@@ -84,24 +84,17 @@ __device__ __forceinline__ float2 left_of_bf16(float2 x) {
   return make_float2(fabsf(hi[0]) <= 3.402823466e38f ? x.x - hi[0] : 0.f, fabsf(hi[1]) <= 3.402823466e38f ? x.y - hi[1] : 0.f);
 }
 
-// x += 32 values of a row of which those below n (a multiple of 8) exist.
-__device__ __forceinline__ void add_row32(const void* base, int64_t at, float* x, int n, bool f32) {
+// x += 32 bf16 numbers of a row of which those below n (a multiple of 8) exist.
+__device__ __forceinline__ void add_row32(const uint16_t* from, float* x, int n) {
 #pragma unroll
   for (int h = 0; h < 4; ++h) {
     if (8 * h >= n) continue;
-    if (f32) {
-      const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(base) + at + 8 * h);
-      const float4 u = *p, v = *(p + 1);
-      x[8 * h] += u.x; x[8 * h + 1] += u.y; x[8 * h + 2] += u.z; x[8 * h + 3] += u.w;
-      x[8 * h + 4] += v.x; x[8 * h + 5] += v.y; x[8 * h + 6] += v.z; x[8 * h + 7] += v.w;
-    } else {
-      const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(base) + at + 8 * h);
-      const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    const uint4 u = *reinterpret_cast<const uint4*>(from + 8 * h);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[8 * h + 2 * e] += __uint_as_float(w[e] << 16);
-        x[8 * h + 2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
-      }
+    for (int e = 0; e < 4; ++e) {
+      x[8 * h + 2 * e] += __uint_as_float(w[e] << 16);
+      x[8 * h + 2 * e + 1] += __uint_as_float(w[e] & 0xffff0000u);
     }
   }
 }
@@ -113,19 +106,22 @@ __device__ __forceinline__ void add_row32(const void* base, int64_t at, float* x
 // Wide boxes are for results in bf16 whose rows do not all start on 32 bytes: of a row of 64 bytes two sectors of three are then written in two
 // pieces (input gradient 10166 x 144 x 12408 112 us, wide 87; 12416 columns without 67; forward 15697 x 7576 x 280 95 and 72).  Two warps that fill a
 // wide box together, which leaves the sixth stage: 87 and 78, and 8 % more where rows start on 32 bytes.
-template <bool WIDE>
+// Results that are added to what is there: in fp32 by TMA; in bf16, where the sum is to be rounded once, the box holds what is there before its results
+// come (`old`).  (Every thread reading its row of it: weight gradient 512 x 14336 x 4096 111 us, 31 x 3576 x 4104 in fp32 48; now 74 and 29.)
+template <bool LONG, bool WIDE>
 struct Outlet {
   const CUtensorMap* map;
   uint8_t* box;
   int lane;
+  bool add;                      // LONG, fp32
   // 32 columns from column `col` on of the rows from `row0` on, the lane's own in x; `part`: of K; `half`: whether they are the second 32 of 64.
-  __device__ __forceinline__ void put32(const float* x, int half, int col, int row0, int part, bool f32, int rows, int cols) {
+  __device__ __forceinline__ void put32(float* x, int half, int col, int row0, int part, bool f32, int rows, int cols, bool old = false) {
     uint8_t* const line = box + lane * (WIDE ? 128 : 64);
     const int swap = WIDE ? lane & 7 : (lane >> 1) & 3, first = WIDE ? 4 * half : 0;      // (a wide box takes two turns)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       if ((WIDE || !f32) && h == 1) break;
-      if (first == 0) {
+      if (first == 0 && !(WIDE && old)) {
         if (lane == 0) bulk_wait_group_read<0>();
         __syncwarp();
       }
@@ -136,10 +132,20 @@ struct Outlet {
       } else {
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
+          uint8_t* const to = line + (((first + c) ^ swap) * 16);
+          if (WIDE && old) {
+            const uint4 o = *reinterpret_cast<const uint4*>(to);
+            const uint32_t v[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              x[8 * c + 2 * e] += __uint_as_float(v[e] << 16);
+              x[8 * c + 2 * e + 1] += __uint_as_float(v[e] & 0xffff0000u);
+            }
+          }
           uint32_t w[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2_rn(x[8 * c + 2 * e], x[8 * c + 2 * e + 1]);
-          put4(line + (((first + c) ^ swap) * 16), w);
+          put4(to, w);
         }
       }
       if (WIDE && half == 0) continue;
@@ -147,7 +153,10 @@ struct Outlet {
       __syncwarp();
       if (lane == 0) {
         const int from = col + 16 * h - 8 * first;
-        if (row0 < rows && from < cols) tma_store_box3(map, from, row0, part, box);
+        if (row0 < rows && from < cols) {
+          if (LONG && add) tma_add_box3(map, from, row0, part, box);
+          else tma_store_box3(map, from, row0, part, box);
+        }
         bulk_commit_group();
       }
     }
@@ -155,12 +164,12 @@ struct Outlet {
 };
 
 // What a gradient's item does with 32 columns of its sums.
-template <bool WIDE>
-__device__ __forceinline__ void finish32(const Args& a, const Cut& t, Outlet<WIDE>& out, int half, int row0, int col, float* x) {
+template <bool LONG, bool WIDE>
+__device__ __forceinline__ void finish32(const Args& a, const Cut& t, Outlet<LONG, WIDE>& out, int half, int row0, int col, float* x, bool old) {
   const int row = row0 + out.lane;
-  if (a.accumulate && a.plan.parts == 1 && row < a.plan.rows) add_row32(a.out, (int64_t)row * a.out_ld + col, x, a.plan.cols - col, a.out_f32);
+  if (LONG && a.accumulate && !a.out_f32 && row < a.plan.rows) add_row32(static_cast<const uint16_t*>(a.out) + (int64_t)row * a.out_ld + col, x, a.plan.cols - col);
   __syncwarp();
-  out.put32(x, half, col, row0, t.part, a.plan.parts > 1 || a.out_f32, a.plan.rows, a.plan.cols);
+  out.put32(x, half, col, row0, t.part, a.plan.parts > 1 || a.out_f32, a.plan.rows, a.plan.cols, old);
 }
 
 // An item's K in segments of even length: how many, and the stages of each but the last.
@@ -199,6 +208,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_ke
       mbar_init(&sh.empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) { mbar_init(&sh.tfull[i], 1); mbar_init(&sh.tempty[i], 2 * S::kDrain); }
+    for (int i = 0; i < S::kDrain; ++i) mbar_init(&sh.old_full[i], 1);
     sh.abort = 0;
     mbar_fence_init();
   }
@@ -312,7 +322,23 @@ __global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_ke
     // group of four warps, 64 (LONG: 128) of the columns
     const int q = 32 * (warp & 3) + lane, grp = (warp - 4) >> 2;
     const uint32_t lane_addr = (uint32_t)(32 * (warp & 3)) << 16;
-    Outlet<WIDE> out = {&a.o, ring + S::kStages * kStageBytes + (warp - 4) * S::kBox, lane};
+    Outlet<LONG, WIDE> out = {&a.o, ring + S::kStages * kStageBytes + (warp - 4) * S::kBox, lane, LONG && a.accumulate && a.out_f32};
+    // what is there already of this warp's box of an item: asked for as soon as the box is free of the item before
+    const bool old = OP == WEIGHT_GRAD && WIDE && a.accumulate;
+    uint64_t* const old_bar = &sh.old_full[warp - 4];
+    uint32_t old_phase = 0;
+    bool asked = false;
+    auto ask = [&](int i) {
+      Cut n;
+      asked = old && a.plan.item(i, n) && 64 * grp < n.bn;
+      if (asked && lane == 0) {
+        bulk_wait_group_read<0>();
+        mbar_arrive_expect_tx(old_bar, S::kBox);
+        tma_load_box3(out.box, &a.o, n.n0 + 64 * grp, n.m0 + (int)rank * 128 + 32 * (warp & 3), 0, old_bar);
+      }
+      __syncwarp();
+    };
+    if (WIDE) ask(pair);
     uint32_t run = 0;
     bool ok = true;
     auto wait_full = [&](int acc) {
@@ -361,7 +387,7 @@ __global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_ke
         if (!ok) break;
 #pragma unroll
         for (int c = 0; c < 128; c += 32)
-          if (c < mine) finish32(a, t, out, c / 32 % 2, row - lane, col0 + c, v + c);
+          if (c < mine) finish32(a, t, out, c / 32 % 2, row - lane, col0 + c, v + c, false);
       } else {
         const int acc = (int)(run & 1);
         const float xs = OP == FORWARD && row < a.plan.rows ? a.a_scale[row] : 0.f;
@@ -376,6 +402,12 @@ __global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_ke
         if (!ok) break;
         const uint32_t at = tmem_base + lane_addr + (uint32_t)(acc * kTile + grp * 64);
         if (64 * grp < t.bn) {                         // (tiles are multiples of 64 wide)
+          if (WIDE && old) {
+            ok = mbar_wait_warp(old_bar, old_phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault);
+            if (!ok) break;
+            old_phase ^= 1u;
+            asked = false;
+          }
 #pragma unroll
           for (int c = 0; c < 64; c += 32) {
             __syncwarp();
@@ -399,15 +431,18 @@ __global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_ke
               }
               out.put32(v, c / 32, col0 + c, row - lane, 0, a.out_f32, a.plan.rows, a.plan.cols);
             } else {
-              finish32(a, t, out, c / 32, row - lane, col0 + c, v);
+              finish32(a, t, out, c / 32, row - lane, col0 + c, v, old);
             }
           }
         } else {
           release(acc);
         }
+        if (WIDE) ask(i + a.pairs);
         ++run;
       }
     }
+    if (WIDE && asked)                                 // (a wait ran out: the box is not left before what was asked for has come)
+      for (uint32_t spin = 0; spin < kDrainSpins && !mbar_try_wait<WAIT_CTA>(old_bar, old_phase); ++spin) __nanosleep(64);
     if (lane == 0) bulk_wait_group<0>();
     __syncwarp();
   }
@@ -1223,11 +1258,12 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
   a.status = (int32_t*)scratch;
   float* const parts = (float*)((char*)scratch + plan.part_at);
   a.out_f32 = out_dtype == ADAPM_TYPE_F32;
-  a.accumulate = weight && d.accumulate != 0;
+  const bool accumulate = weight && d.accumulate != 0;
+  a.accumulate = accumulate && plan.parts == 1;
   a.pairs = std::min(pairs, plan.items);
   a.seg = a.out_f32 ? kSegLong : kSegShort;
   const bool is_long = a.out_f32 || plan.each > kShortStages;
-  const bool wide = !is_long && plan.parts == 1 && off_sectors(out, out_ld, a.out_f32);
+  const bool wide = !is_long && plan.parts == 1 && (a.accumulate || off_sectors(out, out_ld, a.out_f32));
   if (!(plan.parts > 1 ? encode_result(&a.o, parts, plan.parts, plan.rows, plan.cols, plan.cols, true, wide)
                        : encode_result(&a.o, out, 1, plan.rows, plan.cols, out_ld, a.out_f32, wide))) {
     set_error_text("cuTensorMapEncodeTiled failed for a gradient of linear8");
@@ -1254,7 +1290,7 @@ int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* 
   if (plan.parts == 1) return ADAPM_OK;
   SumArgs u;
   u.part = parts; u.out = out; u.out_ld = out_ld; u.fours = plan.cols / 4; u.places = (int64_t)plan.rows * u.fours;
-  u.part_elems = (int64_t)plan.rows * plan.cols; u.parts = plan.parts; u.f32 = a.out_f32; u.accumulate = a.accumulate;
+  u.part_elems = (int64_t)plan.rows * plan.cols; u.parts = plan.parts; u.f32 = a.out_f32; u.accumulate = accumulate;
   ADAPM_CUDA(launch_chained(true, linear8_sum_kernel, (unsigned)std::min<int64_t>((u.places + 255) / 256, 148 * 8), 256, 0, s, u));
   return ADAPM_OK;
 }

@@ -242,6 +242,12 @@ __device__ __forceinline__ void tma_store_box3(const void* tmap, int x, int y, i
                "r"(y), "r"(z), "r"(smem_u32(smem_src))
                : "memory");
 }
+// The same, added to what is there (in the L2, one addition per element).
+__device__ __forceinline__ void tma_add_box3(const void* tmap, int x, int y, int z, const void* smem_src) {
+  asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(tmap), "r"(x),
+               "r"(y), "r"(z), "r"(smem_u32(smem_src))
+               : "memory");
+}
 __device__ __forceinline__ void bulk_commit_group() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Until at most N of this thread's bulk groups are still reading their shared-memory source.
 template <int N>

@@ -343,3 +343,19 @@ def test_the_first_call_of_a_process_may_be_a_captured_one():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", FIRST_CALL_IN_A_CAPTURE], cwd=root, capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "same" in r.stdout, r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tokens,out,inn,pad", [(40, 3592, 4104, 0), (40, 3592, 4104, 8), (200, 4096, 4352, 0), (130, 200, 20000, 24)])
+def test_added_weight_gradient_of_many_tiles(dtype, tokens, out, inn, pad):
+    """Several tiles to every pair of CTAs, rows on and off sectors of 32 bytes, last tiles that end inside: what is there is read while the tile before is
+    still on its way out.  Elements that nothing is added to keep their value to the bit."""
+    g = _gen(tokens + out + inn + pad)
+    dy, _ = _rows(g, tokens, out, BF16, out, 0)
+    dy[:, 5] = 0
+    x8 = T._codes(g, tokens, inn)
+    xs = T._scales(g, tokens, pow2=True)
+    before = (torch.randn(out, inn, generator=g, device="cuda") * 30).to(dtype)
+    T._check_weight_grad(dy, x8, xs, "int8", 0, dtype, True, pad, before)
+    dw = T._run_weight_grad(dy, x8, xs, "int8", 0, dtype, pad, before)
+    assert torch.equal(dw[5], before[5])
