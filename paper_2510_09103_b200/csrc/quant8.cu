@@ -89,6 +89,7 @@ __device__ __forceinline__ void fetch16(Eight<T>* x, const T* row, int64_t base,
   const int step = VEC ? 1 : team, left = (int)min((int64_t)INT32_MAX, cols - c);
   x[0].clear();
   x[1].clear();
+  if (VEC && left <= 0) return;                      // (the other lanes wait for what these ask: 16384 x 1600 back 22 -> 10.5 us, 28312 x 4128 72 -> 53)
   if (!VEC && base + 16 * team <= cols) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e >> 3].set(e & 7, p[e * step]);
@@ -113,6 +114,7 @@ __device__ __forceinline__ void put_codes(uint8_t* row, int64_t base, int me, in
     return;
   }
   const int step = VEC ? 1 : team, left = (int)min((int64_t)INT32_MAX, cols - c);
+  if (VEC && left <= 0) return;
   if (!VEC && base + 16 * team <= cols) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) p[e * step] = (uint8_t)(q[e >> 2] >> (8 * (e & 3)));
@@ -217,17 +219,21 @@ struct QuantArgs {
 };
 
 // ---- a scale per 128 columns -----------------------------------------------------------------------------------
-constexpr int kRows = 4;          // rows per thread
+// Rows per thread: several in bf16 and back (8192 x 14336 58.4 -> 56.3 us, back 54.8 -> 53.5), one of fp32 (8192 x 4096 35.7 -> 26.3).
+constexpr int kRows = 4;
+template <typename T>
+constexpr int kRowsOf = sizeof(T) == 2 ? kRows : 1;
 
-// Which rows and columns a thread of eight that share a group works on: kRows rows below one another, so that one division finds
+// Which rows and columns a thread of eight that share a group works on: ROWS rows below one another, so that one division finds
 // them all.  (16 elements per thread rather than eight: half the shuffles and half the scales per element.)
 struct Spot { int64_t row; int64_t col; int64_t group; };
+template <int ROWS>
 __device__ __forceinline__ bool spot_of(Spot& s, int64_t groups, int64_t total) {
   const int64_t i = (int64_t)blockIdx.x * 32 + (threadIdx.x >> 3);
   if (i >= total) return false;
   const int64_t band = total <= UINT32_MAX ? (int64_t)((uint32_t)i / (uint32_t)groups) : i / groups;
   s.group = i - band * groups;
-  s.row = band * kRows;
+  s.row = band * ROWS;
   s.col = s.group * 128;
   return true;
 }
@@ -243,19 +249,20 @@ __device__ __forceinline__ bool block_of(int64_t& row, int64_t& base, int64_t co
 
 template <typename T>
 __global__ void __launch_bounds__(256) quant8_groups_kernel(const QuantArgs a) {
+  constexpr int ROWS = kRowsOf<T>;
   wait_for_previous_kernel();
   const int me = threadIdx.x & 7;
   Spot s = {0, 0, 0};
-  const bool live = spot_of(s, a.groups, a.total);
-  Eight<T> x[kRows][2];
+  const bool live = spot_of<ROWS>(s, a.groups, a.total);
+  Eight<T> x[ROWS][2];
 #pragma unroll
-  for (int u = 0; u < kRows; ++u) {
+  for (int u = 0; u < ROWS; ++u) {
     x[u][0].clear();
     x[u][1].clear();
     if (live && s.row + u < a.rows) fetch16<true>(x[u], static_cast<const T*>(a.x) + (s.row + u) * a.x_ld, s.col, me, 8, a.cols, a.wide);
   }
 #pragma unroll
-  for (int u = 0; u < kRows; ++u) {
+  for (int u = 0; u < ROWS; ++u) {
     uint32_t m = max(x[u][0].top_bits(), x[u][1].top_bits());
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -359,7 +366,7 @@ struct DequantArgs {
   const float* scales;
   void* x;
   int64_t x_ld, codes_ld, rows, cols, groups, total;      // groups of 128 columns, whatever a scale stands for
-  int32_t per_row, wide;                                  // one scale per row; rows of x start on 32 bytes
+  int32_t per_row, codes16, wide;                         // one scale per row; rows of codes start on 16 bytes, rows of x on 32
 };
 
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
@@ -382,10 +389,11 @@ __global__ void __launch_bounds__(256) dequant8_kernel(const DequantArgs a) {
   wait_for_previous_kernel();
   const int me = threadIdx.x & 7;
   Spot t;
-  if (!spot_of(t, a.groups, a.total)) return;
+  if (!spot_of<kRows>(t, a.groups, a.total)) return;
   uint4 q[kRows];
   float s[kRows];
   const int64_t c = t.col + 16 * me;
+  if (c >= a.cols) return;         // (a lane without columns would hold up the others below)
 #pragma unroll
   for (int u = 0; u < kRows; ++u) {
     q[u] = make_uint4(0, 0, 0, 0);
@@ -394,12 +402,21 @@ __global__ void __launch_bounds__(256) dequant8_kernel(const DequantArgs a) {
     if (row >= a.rows) continue;
     const uint8_t* const p = a.codes + row * a.codes_ld;
     s[u] = a.scales[a.per_row ? row : row * a.groups + t.group];
-    if (c + 16 <= a.cols) {
+    if (c + 16 <= a.cols && a.codes16) {
       q[u] = *reinterpret_cast<const uint4*>(p + c);
-    } else {
+      continue;
+    }
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (c + e < a.cols) (&q[u].x)[e >> 2] |= (uint32_t)p[c + e] << (8 * (e & 3));
+    for (int h = 0; h < 2; ++h) {
+      const int64_t at = c + 8 * h;
+      if (at + 8 <= a.cols) {
+        const uint2 w = *reinterpret_cast<const uint2*>(p + at);
+        (&q[u].x)[2 * h] = w.x; (&q[u].x)[2 * h + 1] = w.y;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (at + e < a.cols) (&q[u].x)[2 * h + (e >> 2)] |= (uint32_t)p[at + e] << (8 * (e & 3));
+      }
     }
   }
 #pragma unroll
@@ -412,17 +429,20 @@ __global__ void __launch_bounds__(256) dequant8_kernel(const DequantArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) v[e] *= s[u];
     T* const p = static_cast<T*>(a.x) + row * a.x_ld;
-    if (c + 16 <= a.cols) {
-      if (a.wide) {
-        put16(p + c, v);
-      } else {
-        put8(p + c, v);
-        put8(p + c + 8, v + 8);
-      }
-    } else {
+    if (c + 16 <= a.cols && a.wide) {
+      put16(p + c, v);
+      continue;
+    }
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (c + e < a.cols) put(p + c + e, v[e]);
+    for (int h = 0; h < 2; ++h) {
+      const int64_t at = c + 8 * h;
+      if (at + 8 <= a.cols) {
+        put8(p + at, v + 8 * h);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (at + e < a.cols) put(p + at + e, v[8 * h + e]);
+      }
     }
   }
 }
@@ -536,8 +556,9 @@ int launch_dequant8(const adapm_codes8& d, const void* codes, const float* scale
   a.x_ld = d.x_ld; a.codes_ld = d.codes_ld; a.rows = d.rows; a.cols = d.cols; a.groups = (d.cols + 127) / 128;
   a.total = (d.rows + kRows - 1) / kRows * a.groups;
   a.per_row = d.group == 0;
+  a.codes16 = rows_of_eights(d, x, codes, 16);
   a.wide = rows_of_32(d, x);
-  const bool f32 = d.dtype == ADAPM_TYPE_F32, e4m3 = d.code == ADAPM_CODE_E4M3, vec = rows_of_eights(d, x, codes, 16);
+  const bool f32 = d.dtype == ADAPM_TYPE_F32, e4m3 = d.code == ADAPM_CODE_E4M3, vec = rows_of_eights(d, x, codes, 8);
   const int64_t grid = vec ? (a.total + 31) / 32 : odd_grid(d);
   if (grid > INT32_MAX) return ADAPM_ERANGE;
 #define ADAPM_DEQUANT(KERNEL, T, E) launch_chained(true, KERNEL<T, E>, (unsigned)grid, 256, 0, s, a)
@@ -564,7 +585,9 @@ extern "C" int adapm_quant8(const adapm_codes8* d, const void* x, void* codes, f
   QuantArgs a;
   a.x = x; a.codes = static_cast<uint8_t*>(codes); a.scales = scales;
   a.x_ld = d->x_ld; a.codes_ld = d->codes_ld; a.rows = d->rows; a.cols = d->cols;
-  a.groups = (d->cols + 127) / 128; a.total = (d->rows + kRows - 1) / kRows * a.groups;
+  a.groups = (d->cols + 127) / 128;
+  const int64_t per = d->dtype == ADAPM_TYPE_F32 ? kRowsOf<float> : kRowsOf<uint16_t>;
+  a.total = (d->rows + per - 1) / per * a.groups;
   a.codes16 = rows_of_eights(*d, x, codes, 16);
   a.wide = rows_of_32(*d, x);
   a.mode = d->code == ADAPM_CODE_E4M3 ? E4M3_POW2 : d->pow2 ? INT8_POW2 : INT8_MAX_SCALE;
