@@ -490,8 +490,9 @@ size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which);
  *     for a gradient in bf16 (off by 2^-8 of it at most, per term), but with at most 16 tokens (dx) or output features (dweight), whose
  *     few terms do not average that out, carried with 16 bits; for a gradient in fp32 it is carried with 24 bits, at up to three times the
  *     product's cost.
- * A scale that is NaN makes its row or column (of dweight: its 128 columns, of dx: all of it) NaN.  tokens = 0: nothing, or
- * dweight = 0 (unless accumulate).
+ * A scale that is NaN makes its row or column (of dweight: its 128 columns, of dx: all of it) NaN.  An infinity in dy may come out as NaN, and code * scale
+ * above 3.38e38, bf16's largest number, counts as infinite.  tokens = 0: nothing, or dweight = 0 (unless accumulate).
+ * Pitches: rows that start on 128 bytes go fastest (input gradient 2037 x 7168 x 3264 92 us, with 7192 columns of dy 118).
  * The scratch of a gradient holds what the codes of its 8-bit operand stand for in bf16 (three times that for a gradient in fp32), and
  * parts of its sums: one buffer, the largest that any layer asks for, does for all layers of a program that runs on one stream.
  * Errors: ADAPM_EINVAL, ADAPM_EALIGN (16 bytes for matrices and for the ws of the forward product, pitches), ADAPM_ERANGE (pitches from 2^31 on
