@@ -102,12 +102,12 @@ __device__ __forceinline__ void add_row32(const uint16_t* from, float* x, int n)
 // A warp's way out: 32 rows of 64 bytes (16 columns in fp32, 32 in bf16), or (WIDE) of 128, are put into its box in shared memory, with the
 // swizzle of as many, and stored as a whole by TMA, which leaves out what the result does not have.  (Every thread storing 32 bytes of a row of its
 // own: weight gradient of 1 x 14336 x 4096 36 to 42 us, with a box 27.  Eight warps with boxes of 128 bytes for 128 columns each instead of
-// sixteen for 64: forward 8192 x 14336 x 512 92 us for 76.)
+// sixteen for 64: forward 8192 x 14336 x 512 92 us for 76.  Two boxes of 64 bytes to a warp: no faster.)
 // Wide boxes are for results in bf16 whose rows do not all start on 32 bytes: of a row of 64 bytes two sectors of three are then written in two
 // pieces (input gradient 10166 x 144 x 12408 112 us, wide 87; 12416 columns without 67; forward 15697 x 7576 x 280 95 and 72).  Two warps that fill a
 // wide box together, which leaves the sixth stage: 87 and 78, and 8 % more where rows start on 32 bytes.
 // Results that are added to what is there: in fp32 by TMA; in bf16, where the sum is to be rounded once, the box holds what is there before its results
-// come (`old`).  (Every thread reading its row of it: weight gradient 512 x 14336 x 4096 111 us, 31 x 3576 x 4104 in fp32 48; now 74 and 29.)
+// come (`old`), for which it is wide.  (Every thread reading its row of it: weight gradient 512 x 14336 x 4096 111 us, 31 x 3576 x 4104 in fp32 48; now 74 and 29.)
 template <bool LONG, bool WIDE>
 struct Outlet {
   const CUtensorMap* map;
@@ -183,8 +183,8 @@ __device__ __forceinline__ void segments(int stages, int most, int& n, int& each
 // accumulators.
 // What bounds it: the tensor cores, and with them the power cap.  8192 x 14336 x 4096: forward 300 to 340 us = 2.8 to 3.2 P operations/s (the
 // library's 8-bit integer product alone 314 to 355), gradients with the decoding of their codes (16 to 30 us) 680 to 800 us = 1.2 to 1.4 PFLOP/s (the
-// library's bf16 products alone 620 to 940 and 670 to 760).  With short K the epilogue (forward 8192 x 14336 x 512 76 us, of them 36 for the result's
-// way to memory), with few tiles the rounds of them.
+// library's bf16 products alone 620 to 940 and 670 to 760).  With short K the result's way to memory (forward 8192 x 14336 x 512 73 us; a fill of as
+// many bytes takes 63), with few tiles the rounds of them.
 // Not kept: codes made bf16 numbers by warps of this kernel on their way into shared memory, which the CTA of rank 1 has to tell the one of rank
 // 0: an arrival that releases at cluster scope takes 1000 to 1800 cycles, twice to three times what a stage does (8192 x 14336 x 4096 1230 us, by a
 // warp that does nothing else 1660, with a relaxed one, which does not order the codes, 980).

@@ -359,3 +359,24 @@ def test_added_weight_gradient_of_many_tiles(dtype, tokens, out, inn, pad):
     T._check_weight_grad(dy, x8, xs, "int8", 0, dtype, True, pad, before)
     dw = T._run_weight_grad(dy, x8, xs, "int8", 0, dtype, pad, before)
     assert torch.equal(dw[5], before[5])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tokens,out,inn", [(40, 3592, 4104), (40, 72, 200), (600, 520, 392), (3000, 520, 392)])
+def test_gradients_added_one_call_behind_the_other(dtype, tokens, out, inn):
+    """A call reads what the one before it has written, whether or not the host waits in between."""
+    g = _gen(tokens + out)
+    dy, _ = _rows(g, tokens, out, BF16, out, 0)
+    x8, xs = T._codes(g, tokens, inn), T._scales(g, tokens, pow2=True)
+    d = A.linear8_desc(tokens, out, inn, dweight_dtype=TYPE[dtype], accumulate=True, x8_ld=x8.stride(0))
+    scratch = torch.empty(A.adapm_linear8_scratch_bytes(d, A.LINEAR8_WEIGHT_GRAD), dtype=torch.uint8, device="cuda")
+    got = []
+    for wait in (True, False):
+        dw = torch.ones(out, inn, dtype=dtype, device="cuda")
+        for _ in range(5):
+            A.adapm_linear8_weight_grad(d, dy, x8, xs, dw, scratch)
+            if wait:
+                assert A.adapm_linear8_status(scratch) == 0
+        got.append(dw)
+    assert torch.equal(*got)
+    assert not torch.equal(got[0], torch.ones_like(got[0]))
