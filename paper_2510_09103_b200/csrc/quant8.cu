@@ -167,25 +167,26 @@ __device__ __forceinline__ uint32_t encode4(const float* x, const Scale& k) {
     // that is not half a step is at least 2^-24 / f away from it, and d (1 / s) is off by f 2^-26 at most, which is less.  A quotient
     // that is half a step wants 2 x / s to be a whole number: of bf16 elements, where s is the nearest number to an
     // 8-bit number over 127, only for powers of two, whose reciprocal is not rounded; of fp32 elements it has to be looked for.
+    // (What is left is doubled for that, which rounds nothing; half of s has no fp32 number where s is below 2^-125 and odd in its last place.)
     float left[4], worst = 0.f;
-    const float half = 0.5f * k.s;
 #pragma unroll
     for (int e = 0; e < 4; e += 2) {
       const float2 r = add2(make_float2(t[e], t[e + 1]), make_float2(-kMagic, -kMagic));
       const float2 d = fma2(r, make_float2(-k.s, -k.s), make_float2(x[e], x[e + 1]));
       if (F32) {
-        left[e] = d.x; left[e + 1] = d.y;
-        worst = fmaxf(worst, fmaxf(fabsf(d.x), fabsf(d.y)));
+        const float2 twice = add2(d, d);
+        left[e] = twice.x; left[e + 1] = twice.y;
+        worst = fmaxf(worst, fmaxf(fabsf(twice.x), fabsf(twice.y)));
       } else {
         const float2 q = fma2(d, make_float2(k.inv, k.inv), make_float2(t[e], t[e + 1]));
         t[e] = q.x; t[e + 1] = q.y;
       }
     }
-    if (F32 && worst >= half) {
+    if (F32 && worst >= k.s) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float d = fabsf(left[e]);
-        if (d > half || (d == half && (__float_as_uint(t[e]) & 1u))) t[e] += copysignf(1.f, left[e]);
+        if (d > k.s || (d == k.s && (__float_as_uint(t[e]) & 1u))) t[e] += copysignf(1.f, left[e]);
       }
     }
   }
