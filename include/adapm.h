@@ -491,7 +491,9 @@ size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which);
  *     few terms do not average that out, carried with 16 bits; for a gradient in fp32 it is carried with 24 bits, at up to three times the
  *     product's cost.
  * A scale that is NaN makes its row or column (of dweight: its 128 columns, of dx: all of it) NaN.  An infinity in dy may come out as NaN, and code * scale
- * above 3.38e38, bf16's largest number, counts as infinite.  tokens = 0: nothing, or dweight = 0 (unless accumulate).
+ * above 3.38e38, bf16's largest number, counts as infinite (where it is carried with 16 or 24 bits and the scale is no power of two, from half of that on).  What is
+ * carried with 16 or 24 bits has fewer where code * scale, or dy, or for scales of 2^-30 to 1 dy * scale, is below 2^-110.  tokens = 0: nothing, or dweight = 0
+ * (unless accumulate).
  * Pitches: rows that start on 128 bytes go fastest (input gradient 2037 x 7168 x 3264 92 us, with 7192 columns of dy 118).
  * The scratch of a gradient holds what the codes of its 8-bit operand stand for in bf16 (three times that for a gradient in fp32), and
  * parts of its sums: one buffer, the largest that any layer asks for, does for all layers of a program that runs on one stream.

@@ -11,6 +11,7 @@
 #include <cmath>
 #include <cstring>
 #include <mutex>
+#include <type_traits>
 
 #include "codes.cuh"
 #include "linear8_plan.h"
@@ -563,10 +564,11 @@ __global__ void __launch_bounds__(256) linear8_sum_kernel(const SumArgs a) {
 //   weight grad   input features of x8 x output features of dy     write them into shared memory, times their scales
 // The result lies across: out[column][feature].
 // FOLD (up to 16 columns, or a gradient in fp32): code x scale rounded to bf16 would be a rounding per term that few terms do not average out,
-// or too coarse.  The scale is a number per index of K, so it may as well go into the other operand: the codes are bf16 numbers
-// without it, and dy x scale is carried as two bf16 numbers (three for fp32), next to one another as columns of one product, whose sums are
-// added at the end.  Where all scales of the CTA's part of K are powers of two, dy x scale is one bf16 number.  K is taken in segments that are
-// added up in registers, as above.
+// or too coarse.  The scale is a number per index of K, so it may as well go into the other operand, as far as its size is not in the way: scale = 2^e m, 1/2 < m <= 1,
+// the codes are bf16 numbers times 2^e, which rounds nothing, and dy x m is carried as two bf16 numbers (three for fp32), next to one another as columns of
+// one product, whose sums are added at the end.  Where all scales of the CTA's part of K are powers of two, m is 1 and dy goes in as it is; where all lie between
+// 2^-30 and 1, 2^e stays with m (1 x 14336 x 4096 34 us; apart 41), which beyond would leave bf16's range where code x scale does not.  K is taken in segments
+// that are added up in registers, as above.
 
 struct StripArgs {
   CUtensorMap codes, other;
@@ -630,6 +632,25 @@ __device__ __forceinline__ void decode8(uint32_t c0, uint32_t c1, uint32_t* w) {
       asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(w[i]) : "r"((two & 0x007f007fu) | 0x43004300u), "r"((two & 0x00800080u) | 0xc300c300u));
     }
   }
+}
+
+// scale = power x m: the power of two as two bf16 numbers of a register, with the scale's sign, and m from above 1/2 to 1 (1 to 2 for scales above 2^127,
+// whose next power has no number).  A NaN is one in the power; an infinity, or zero, is a power.
+struct Split { uint32_t power; float m; };
+__device__ __forceinline__ Split split_scale(float s) {
+  const uint32_t bits = __float_as_uint(s), size = bits & 0x7fffffffu, fraction = size & 0x7fffffu;
+  const int e = (int)(size >> 23), up = min(254, e + (fraction ? 1 : 0));
+  const uint32_t power = size >= 0x7f800000u ? size >> 16 | (fraction ? 0x40u : 0u) : (uint32_t)up << 7;
+  Split r;
+  r.power = (power | (bits >> 16 & 0x8000u)) * 0x10001u;
+  // (the reciprocal of 2^127 is subnormal)
+  r.m = fraction == 0 || e == 255 ? 1.f : __uint_as_float(size) * __uint_as_float(up < 254 ? (uint32_t)(254 - up) << 23 : 0x400000u);
+  return r;
+}
+__device__ __forceinline__ uint32_t times_bf16x2(uint32_t x, uint32_t y) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+  return r;
 }
 
 // A CTA puts its share of the features together, a thread four of them, for every few columns: eight loads of four sums on their way
@@ -721,11 +742,17 @@ __global__ void __launch_bounds__(StripShape<OP, FOLD>::kThreads, 1) linear8_str
   if (blockIdx.x == 0)
     for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no CTA
   int planes = 1;
-  if (FOLD) {                          // whether all scales of this CTA's part of K are powers of two
-    int others = 0;
+  bool apart = FOLD;
+  if (FOLD) {                          // whether all scales of this CTA's part of K are powers of two, or between 2^-30 and 1
+    int others = 0, far = 0;
     const float* const scale = a.scale + (a.scale_groups > 1 ? f0 / 128 : 0);
-    for (int k = 64 * k0 + (int)threadIdx.x; k < min(a.k, 64 * (k0 + count)); k += S::kThreads) others |= __float_as_int(scale[(int64_t)k * a.scale_groups]) & 0x7fffff;
+    for (int k = 64 * k0 + (int)threadIdx.x; k < min(a.k, 64 * (k0 + count)); k += S::kThreads) {
+      const float s = scale[(int64_t)k * a.scale_groups];
+      others |= __float_as_int(s) & 0x7fffff;
+      far |= !(fabsf(s) >= 9.31322575e-10f && fabsf(s) <= 1.f);
+    }
     planes = __syncthreads_or(others) ? p.planes : 1;
+    if (planes > 1) apart = __syncthreads_or(far);
   } else {
     __syncthreads();
   }
@@ -827,84 +854,105 @@ __global__ void __launch_bounds__(StripShape<OP, FOLD>::kThreads, 1) linear8_str
     // the 128-byte swizzle; lanes 4 to 7 write their second chunk first, so that eight lanes meet no bank twice
     const int odd = j >> 2, from = row0 * 128 + 16 * j, to = odd * 8192 + row0 * 128;
     const int at0 = to + ((2 * (j & 3) + odd) ^ sub) * 16, at1 = to + ((2 * (j & 3) + 1 - odd) ^ sub) * 16;
-    // scales, a turn ahead: one of its row's four to a lane, or (FOLD, where K runs along a row) those of its chunk of eight
+    // scales, a turn ahead: one of its row's four to a lane, or (FOLD, where K runs along a row of dy) those of its chunk of eight, or both
     constexpr bool kAlong = FOLD && OP == INPUT_GRAD;
-    constexpr int kScales = kAlong ? 8 : 1;
+    constexpr int kChunk = kAlong ? 8 : 1;
     const float* const scale = a.scale + (a.scale_groups > 1 ? f0 / 128 : 0);
-    float next[kScales];
-    auto scales_of = [&](int i) {
-#pragma unroll
-      for (int e = 0; e < kScales; ++e) {
-        const int k = (k0 + i) * 64 + (kAlong ? 8 * j + e : 16 * j + row0);
-        next[e] = (kAlong || j < 4) && i < count && k < a.k ? __ldg(scale + (int64_t)k * a.scale_groups) : 0.f;
-      }
+    auto scale_at = [&](int i, int at) {
+      const int k = (k0 + i) * 64 + at;
+      return i < count && k < a.k ? __ldg(scale + (int64_t)k * a.scale_groups) : 0.f;
     };
-    int stage = team, rs = team;           // (either ring has at least as many stages as there are teams)
-    uint32_t phase = 0, raw_phase = 0;
-    scales_of(team);
-    for (int i = team; i < count; i += kStripTeams) {
-      float mine[kScales];
+    // (the form is chosen once: asked for in every stage, 1 x 14336 x 4096 takes 39.5 us for 34)
+    auto decode = [&](auto form) {
+      constexpr bool kApart = FOLD && decltype(form)::value;
+      float next = 0.f, next_of[kChunk] = {};
+      auto scales_of = [&](int i) {
+        if (kApart || !kAlong) next = j < 4 ? scale_at(i, 16 * j + row0) : 0.f;
+        if (kAlong && planes > 1) {
 #pragma unroll
-      for (int e = 0; e < kScales; ++e) mine[e] = next[e];
-      scales_of(i + kStripTeams);
-      if (!mbar_wait_warp(&sh.raw_full[rs], raw_phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) break;
-      const uint8_t* const src = raw + rs * p.raw_bytes;
-      uint4 q[4];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const uint4*>(src + from + r * 2048);
-      if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) break;
-      uint8_t* const dst = ring + stage * bytes;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const uint32_t c0 = odd ? q[r].z : q[r].x, c1 = odd ? q[r].w : q[r].y, c2 = odd ? q[r].x : q[r].z, c3 = odd ? q[r].y : q[r].w;
-        uint32_t u[4], v[4];
-        if (FOLD) {
-          if (a.e4m3) { decode8<true>(c0, c1, u); decode8<true>(c2, c3, v); }
-          else { decode8<false>(c0, c1, u); decode8<false>(c2, c3, v); }
-        } else {
-          const float s = __shfl_sync(0xffffffffu, mine[0], (lane & 24) | r);
-          if (a.e4m3) { decode8<true>(c0, c1, s, u); decode8<true>(c2, c3, s, v); }
-          else { decode8<false>(c0, c1, s, u); decode8<false>(c2, c3, s, v); }
+          for (int e = 0; e < kChunk; ++e) next_of[e] = scale_at(i, 8 * j + e);
         }
-        put4(dst + at0 + r * 2048, u);
-        put4(dst + at1 + r * 2048, v);
-      }
-      if (FOLD) {
-        // the other operand times the scales, a chunk of eight at a time, from where TMA has put it to the same place of each plane
-        const int o = row0 * 128 + ((j ^ sub) * 16);
+      };
+      int stage = team, rs = team;           // (either ring has at least as many stages as there are teams)
+      uint32_t phase = 0, raw_phase = 0;
+      scales_of(team);
+      for (int i = team; i < count; i += kStripTeams) {
+        const float mine = next;
+        const Split own = kApart ? split_scale(mine) : Split{0u, mine};
+        float m_of[kChunk];
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) m_of[e] = kApart && planes > 1 ? split_scale(next_of[e]).m : next_of[e];
+        scales_of(i + kStripTeams);
+        if (!mbar_wait_warp(&sh.raw_full[rs], raw_phase, abort, status, ST_WAIT_FULL, kWaitSpinDefault)) break;
+        const uint8_t* const src = raw + rs * p.raw_bytes;
+        uint4 q[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) q[r] = *reinterpret_cast<const uint4*>(src + from + r * 2048);
+        if (!mbar_wait_warp(&sh.empty[stage], phase ^ 1u, abort, status, ST_WAIT_EMPTY, kWaitSpinDefault)) break;
+        uint8_t* const dst = ring + stage * bytes;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const uint32_t c0 = odd ? q[r].z : q[r].x, c1 = odd ? q[r].w : q[r].y, c2 = odd ? q[r].x : q[r].z, c3 = odd ? q[r].y : q[r].w;
+          uint32_t u[4], v[4];
+          if (FOLD) {
+            if (a.e4m3) { decode8<true>(c0, c1, u); decode8<true>(c2, c3, v); }
+            else { decode8<false>(c0, c1, u); decode8<false>(c2, c3, v); }
+            if (kApart) {
+              const uint32_t power = __shfl_sync(0xffffffffu, own.power, (lane & 24) | r);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) { u[e] = times_bf16x2(u[e], power); v[e] = times_bf16x2(v[e], power); }
+            }
+          } else {
+            const float s = __shfl_sync(0xffffffffu, mine, (lane & 24) | r);
+            if (a.e4m3) { decode8<true>(c0, c1, s, u); decode8<true>(c2, c3, s, v); }
+            else { decode8<false>(c0, c1, s, u); decode8<false>(c2, c3, s, v); }
+          }
+          put4(dst + at0 + r * 2048, u);
+          put4(dst + at1 + r * 2048, v);
+        }
+        if (FOLD) {
+          // the other operand times m, a chunk of eight at a time, from where TMA has put it to the same place of each plane
+          const int o = row0 * 128 + ((j ^ sub) * 16);
 #pragma unroll 1
-        for (int r = 0; r < p.width / 16; ++r) {
-          const uint4 b = *reinterpret_cast<const uint4*>(src + kStripRawBytes + o + r * 2048);
-          const uint32_t w[4] = {b.x, b.y, b.z, b.w};
-          const float row_scale = kAlong ? 0.f : __shfl_sync(0xffffffffu, mine[0], (lane & 24) | (r & 3));
-          float2 x[4];
+          for (int r = 0; r < p.width / 16; ++r) {
+            const uint4 b = *reinterpret_cast<const uint4*>(src + kStripRawBytes + o + r * 2048);
+            const uint32_t w[4] = {b.x, b.y, b.z, b.w};
+            if (kApart && planes == 1) {
+              put4(dst + 16384 + o + r * 2048, w);
+              continue;
+            }
+            const float row_m = kAlong ? 0.f : __shfl_sync(0xffffffffu, own.m, (lane & 24) | (r & 3));
+            float2 x[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[e] = mul2(make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)),
-                        kAlong ? make_float2(mine[2 * e % kScales], mine[(2 * e + 1) % kScales]) : make_float2(row_scale, row_scale));
-          for (int n = 0; n < planes; ++n) {
-            uint32_t u[4];
+            for (int e = 0; e < 4; ++e)
+              x[e] = mul2(make_float2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u)),
+                          kAlong ? make_float2(m_of[2 * e % kChunk], m_of[(2 * e + 1) % kChunk]) : make_float2(row_m, row_m));
+            for (int n = 0; n < planes; ++n) {
+              uint32_t u[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) u[e] = pack_bf16x2_rn(x[e].x, x[e].y);
-            put4(dst + 16384 + n * p.width * 128 + o + r * 2048, u);
-            if (n + 1 < planes) {
+              for (int e = 0; e < 4; ++e) u[e] = pack_bf16x2_rn(x[e].x, x[e].y);
+              put4(dst + 16384 + n * p.width * 128 + o + r * 2048, u);
+              if (n + 1 < planes) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = left_of_bf16(x[e]);
+                for (int e = 0; e < 4; ++e) x[e] = left_of_bf16(x[e]);
+              }
             }
           }
         }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(&sh.raw_empty[rs]);
+          mbar_arrive(&sh.full[stage]);
+        }
+        stage += kStripTeams;
+        if (stage >= p.ring) { stage -= p.ring; phase ^= 1u; }
+        rs += kStripTeams;
+        if (rs >= p.raw) { rs -= p.raw; raw_phase ^= 1u; }
       }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(&sh.raw_empty[rs]);
-        mbar_arrive(&sh.full[stage]);
-      }
-      stage += kStripTeams;
-      if (stage >= p.ring) { stage -= p.ring; phase ^= 1u; }
-      rs += kStripTeams;
-      if (rs >= p.raw) { rs -= p.raw; raw_phase ^= 1u; }
-    }
+    };
+    if (apart) decode(std::true_type{});
+    else decode(std::false_type{});
   } else {
     if (FOLD) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kStripDrain));
     // ------------------------------------------------------------------ this CTA's sums [columns][128], over the ring once all that was
