@@ -495,8 +495,10 @@ size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which);
  * carried with 16 or 24 bits has fewer where code * scale, or dy, or for scales of 2^-30 to 1 dy * scale, is below 2^-110.  tokens = 0: nothing, or dweight = 0
  * (unless accumulate).
  * Pitches: rows that start on 128 bytes go fastest (input gradient 2037 x 7168 x 3264 92 us, with 7192 columns of dy 118).
- * The scratch of a gradient holds what the codes of its 8-bit operand stand for in bf16 (three times that for a gradient in fp32), and
- * parts of its sums: one buffer, the largest that any layer asks for, does for all layers of a program that runs on one stream.
+ * The scratch of a large gradient holds what the codes of its 8-bit operand stand for in bf16 (three times that for a gradient in fp32), and
+ * parts of its sums; other calls use 9216 bytes of theirs.  One buffer, the largest that any layer asks for, does for all layers of a program that runs on
+ * one stream, and one that was asked for with some number of tokens does for fewer.  A call that would ask for more than it is given cuts its sums into
+ * fewer parts, or takes a form without: it takes longer, and may round otherwise.
  * Errors: ADAPM_EINVAL, ADAPM_EALIGN (16 bytes for matrices and for the ws of the forward product, pitches), ADAPM_ERANGE (pitches from 2^31 on
  * among them), ADAPM_EUNSUPPORTED (features % 8; forward with x_code or x_group other than above), ADAPM_ENOWORKSPACE, ADAPM_ECUDA.
  */

@@ -1257,6 +1257,8 @@ int check_buffers(std::initializer_list<Buffer> in, const Buffer& out, void* scr
   return check_on_this_device({out.p, scratch, at[0].p, at[1].p, at[2].p, in.size() > 3 ? at[3].p : nullptr}, device);
 }
 
+int64_t room_of(size_t scratch_bytes) { return (int64_t)std::min<size_t>(scratch_bytes, (size_t)INT64_MAX); }
+
 Buffer bf16_or_f32(const void* p, int64_t rows, int64_t ld, int64_t cols, int32_t dtype) { return Buffer{p, 16, matrix_at(p, rows, ld, cols, type_bytes(dtype))}; }
 Buffer codes_at(const void* p, int64_t rows, int64_t ld, int64_t cols) { return Buffer{p, 16, matrix_at(p, rows, ld, cols, 1)}; }
 Buffer floats_at(const float* p, int64_t n, int64_t align) { return Buffer{p, align, vector_at(p, n, 4)}; }
@@ -1269,10 +1271,11 @@ cudaError_t launch_strips(const StripArgs& a, cudaStream_t s) {
 
 // A gradient: [rows, cols] = A [rows, K] (or its transpose) times codes [K, cols].
 int gradient(const adapm_linear8& d, int32_t which, const void* dy, const void* codes, const float* scales, void* out, int32_t out_dtype, int64_t out_ld,
-             void* scratch, const Plan& plan, int pairs, cudaStream_t s) {
+             void* scratch, const Form& form, int pairs, cudaStream_t s) {
   const bool weight = which == WEIGHT_GRAD;
-  const StripPlan strip = strip_plan_of(d, which);
-  if (strips_are_faster(d, which, strip, plan)) {
+  const StripPlan& strip = form.strip;
+  const Plan& plan = form.plan;
+  if (form.form == STRIPS) {
     StripArgs t;
     std::memset(&t, 0, sizeof(t));
     t.plan = strip;
@@ -1350,7 +1353,7 @@ using namespace adapm;
 
 extern "C" size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which) {
   if (!d || check_desc(*d, which) != ADAPM_OK) return 0;
-  return (size_t)plan_of(*d, which).bytes;
+  return (size_t)form_of(*d, which).bytes;
 }
 
 extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, const float* xs, const void* w8, const float* ws, void* y,
@@ -1358,15 +1361,16 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
   if (!d) return ADAPM_EINVAL;
   int rc = check_desc(*d, FORWARD);
   if (rc != ADAPM_OK || d->tokens == 0) return rc;
-  const Plan plan = plan_of(*d, FORWARD);
+  const Form form = form_of(*d, FORWARD, room_of(scratch_size));
+  const Plan& plan = form.plan;
   int device, pairs;
   rc = check_buffers({codes_at(x8, d->tokens, d->x8_ld, d->in_features), floats_at(xs, d->tokens, 4), codes_at(w8, d->out_features, d->w8_ld, d->in_features),
                       floats_at(ws, d->out_features, 16)},
-                     bf16_or_f32(y, d->tokens, d->y_ld, d->out_features, d->y_dtype), scratch, scratch_size, plan.bytes,
+                     bf16_or_f32(y, d->tokens, d->y_ld, d->out_features, d->y_dtype), scratch, scratch_size, form.bytes,
                      "adapm_linear8_forward: the output or the scratch overlaps another buffer", &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
   if (rc != ADAPM_OK) return rc;
-  if (d->tokens <= kLineTokens) {
+  if (form.form == LINES) {
     LineArgs l;
     l.x = static_cast<const uint8_t*>(x8); l.w = static_cast<const uint8_t*>(w8); l.xs = xs; l.ws = ws; l.y = y;
     l.status = (int32_t*)scratch; l.y_ld = d->y_ld; l.x_ld = (int32_t)d->x8_ld; l.w_ld = (int32_t)d->w8_ld;
@@ -1381,8 +1385,8 @@ extern "C" int adapm_linear8_forward(const adapm_linear8* d, const void* x8, con
                              : launch_chained(true, linear8_line_kernel<2>, grid, kLineThreads, 0, s, l));
     return ADAPM_OK;
   }
-  const StripPlan strip = strip_plan_of(*d, FORWARD);
-  if (strips_are_faster(*d, FORWARD, strip, plan)) {
+  if (form.form == STRIPS) {
+    const StripPlan& strip = form.strip;
     StripArgs t;
     std::memset(&t, 0, sizeof(t));
     t.plan = strip;
@@ -1418,15 +1422,15 @@ extern "C" int adapm_linear8_input_grad(const adapm_linear8* d, const void* dy, 
   if (!d) return ADAPM_EINVAL;
   int rc = check_desc(*d, INPUT_GRAD);
   if (rc != ADAPM_OK || d->tokens == 0) return rc;
-  const Plan plan = plan_of(*d, INPUT_GRAD);
+  const Form form = form_of(*d, INPUT_GRAD, room_of(scratch_size));
   int device, pairs;
   rc = check_buffers({bf16_or_f32(dy, d->tokens, d->y_ld, d->out_features, ADAPM_TYPE_BF16), codes_at(w8, d->out_features, d->w8_ld, d->in_features),
                       floats_at(ws, d->out_features, 4)},
-                     bf16_or_f32(dx, d->tokens, d->dx_ld, d->in_features, d->dx_dtype), scratch, scratch_size, plan.bytes,
+                     bf16_or_f32(dx, d->tokens, d->dx_ld, d->in_features, d->dx_dtype), scratch, scratch_size, form.bytes,
                      "adapm_linear8_input_grad: the output or the scratch overlaps another buffer", &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
   if (rc != ADAPM_OK) return rc;
-  return gradient(*d, INPUT_GRAD, dy, w8, ws, dx, d->dx_dtype, d->dx_ld, scratch, plan, pairs, (cudaStream_t)stream);
+  return gradient(*d, INPUT_GRAD, dy, w8, ws, dx, d->dx_dtype, d->dx_ld, scratch, form, pairs, (cudaStream_t)stream);
 }
 
 extern "C" int adapm_linear8_weight_grad(const adapm_linear8* d, const void* dy, const void* x8, const float* xs, void* dweight, void* scratch,
@@ -1446,15 +1450,15 @@ extern "C" int adapm_linear8_weight_grad(const adapm_linear8* d, const void* dy,
     ADAPM_CUDA(cudaMemset2DAsync(dweight, (size_t)(d->dweight_ld * gb), 0, (size_t)(d->in_features * gb), (size_t)d->out_features, s));
     return ADAPM_OK;
   }
-  const Plan plan = plan_of(*d, WEIGHT_GRAD);
+  const Form form = form_of(*d, WEIGHT_GRAD, room_of(scratch_size));
   const int64_t groups = d->x_group ? (d->in_features + 127) / 128 : 1;
   rc = check_buffers({bf16_or_f32(dy, d->tokens, d->y_ld, d->out_features, ADAPM_TYPE_BF16), codes_at(x8, d->tokens, d->x8_ld, d->in_features),
                       floats_at(xs, d->tokens * groups, 4)},
-                     bf16_or_f32(dweight, d->out_features, d->dweight_ld, d->in_features, d->dweight_dtype), scratch, scratch_size, plan.bytes,
+                     bf16_or_f32(dweight, d->out_features, d->dweight_ld, d->in_features, d->dweight_dtype), scratch, scratch_size, form.bytes,
                      "adapm_linear8_weight_grad: the output or the scratch overlaps another buffer", &device);
   if (rc == ADAPM_OK) rc = pairs_of(device, &pairs);
   if (rc != ADAPM_OK) return rc;
-  return gradient(*d, WEIGHT_GRAD, dy, x8, xs, dweight, d->dweight_dtype, d->dweight_ld, scratch, plan, pairs, s);
+  return gradient(*d, WEIGHT_GRAD, dy, x8, xs, dweight, d->dweight_dtype, d->dweight_ld, scratch, form, pairs, s);
 }
 
 extern "C" int adapm_linear8_status(const void* scratch, adapm_stream stream, int32_t* status) {

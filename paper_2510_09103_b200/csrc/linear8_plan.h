@@ -52,10 +52,14 @@ struct Plan {
 // How wide the tiles are, and into how many parts K is cut (summed by one more launch, where there are fewer tiles than pairs of CTAs): what takes
 // least.  In units of a stage of 256 columns (512 cycles): an item takes its stages, narrower ones not quite in
 // proportion, and four more, the sums a launch of about eight and the
-// parts' way to memory and back.  (2048 x 6400 x 1600: 56 tiles of 256 columns for 74 pairs, or 72 of 192.)
-inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool grad, bool f32) {
+// parts' way to memory and back.  (2048 x 6400 x 1600: 56 tiles of 256 columns for 74 pairs, or 72 of 192.)  K is cut no further than the parts fit
+// `room` bytes of scratch.
+constexpr int64_t kAnyRoom = INT64_MAX;
+inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool grad, bool f32, int64_t room = kAnyRoom) {
   Plan p;
   p.rows = (int32_t)rows; p.cols = (int32_t)cols;
+  p.part_at = kHeadBytes + (grad ? round_up(k * decoded_pitch(cols) * 2 * (f32 ? kPlanesF32 : 1), 256) : 0);
+  auto bytes_of = [&](int64_t parts) { return p.part_at + (parts > 1 ? round_up(parts * rows * cols * 4, 256) : 0); };
   p.m_tiles = (int32_t)((rows + kTile - 1) / kTile);
   p.stages = (int32_t)((k + stage_k - 1) / stage_k);
   double best = -1;
@@ -64,7 +68,7 @@ inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool gra
     const int most = grad && tiles < kPlannedPairs ? std::max(1, std::min(64, p.stages / 4)) : 1;
     for (int n = 1; n <= most; ++n) {
       const int each = (p.stages + n - 1) / n, parts = each ? (p.stages + each - 1) / each : 1;
-      if (parts != n) continue;
+      if (parts != n || (n > 1 && bytes_of(n) > room)) continue;
       const double rounds = (double)((tiles * parts + kPlannedPairs - 1) / kPlannedPairs);
       const double t = rounds * (each * (0.2 + 0.8 / 256 * width) + 4) + (parts > 1 ? 8 + 2.5 * (double)(rows * cols) * parts / 1e6 : 0);
       if (best >= 0 && t >= best) continue;
@@ -73,8 +77,7 @@ inline Plan plan_of(int64_t rows, int64_t cols, int64_t k, int stage_k, bool gra
       p.items = (int32_t)(tiles * parts);
     }
   }
-  p.part_at = kHeadBytes + (grad ? round_up(k * decoded_pitch(cols) * 2 * (f32 ? kPlanesF32 : 1), 256) : 0);
-  p.bytes = p.part_at + (p.parts > 1 ? round_up((int64_t)p.parts * rows * cols * 4, 256) : 0);
+  p.bytes = bytes_of(p.parts);
   return p;
 }
 
@@ -95,10 +98,10 @@ inline int check_desc(const adapm_linear8& d, int32_t which) {
   return ADAPM_OK;
 }
 
-inline Plan plan_of(const adapm_linear8& d, int32_t which) {
-  if (which == FORWARD) return plan_of(d.tokens, d.out_features, d.in_features, 128, false, false);
-  if (which == INPUT_GRAD) return plan_of(d.tokens, d.in_features, d.out_features, 64, true, d.dx_dtype == ADAPM_TYPE_F32);
-  return plan_of(d.out_features, d.in_features, d.tokens, 64, true, d.dweight_dtype == ADAPM_TYPE_F32);
+inline Plan plan_of(const adapm_linear8& d, int32_t which, int64_t room = kAnyRoom) {
+  if (which == FORWARD) return plan_of(d.tokens, d.out_features, d.in_features, 128, false, false, room);
+  if (which == INPUT_GRAD) return plan_of(d.tokens, d.in_features, d.out_features, 64, true, d.dx_dtype == ADAPM_TYPE_F32, room);
+  return plan_of(d.out_features, d.in_features, d.tokens, 64, true, d.dweight_dtype == ADAPM_TYPE_F32, room);
 }
 
 // ---- strips -----------------------------------------------------------------------------------------------------------
@@ -170,14 +173,17 @@ inline StripPlan strip_plan_of(const adapm_linear8& d, int32_t which) {
   return p;
 }
 
+// Whether strips can take a call: a status word for every CTA, and sums no longer than one accumulator takes.
+inline bool strips_can(int32_t which, const StripPlan& s) {
+  return s.ctas <= kMostWords && (which == FORWARD || s.fold || (s.stages + s.split - 1) / s.split <= kShortStages);
+}
+
 // Whether a call goes by strips, by what both forms were measured to take (us): strips as above; a pair's 256 x 256 tiles, for a gradient with the launch that decodes its codes and the
 // one that sums the parts of K.
 inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const StripPlan& s, const Plan& p) {
-  if (s.ctas > kMostWords) return false;
+  if (!strips_can(which, s)) return false;
   const bool f32 = f32_gradient(d, which);
-  const int each = (s.stages + s.split - 1) / s.split;
   if (s.fold && !f32) return true;                    // (for what the call promises)
-  if (which != FORWARD && !s.fold && each > kShortStages) return false;
   const bool grad = which != FORWARD;
   const double strips = strips_take(s, which);
   const double pair_rounds = (double)((p.items + kPlannedPairs - 1) / kPlannedPairs), wide = 0.2 + 0.8 / 256 * p.width, out = (double)p.rows * p.cols * p.parts / 1e6;
@@ -187,6 +193,38 @@ inline bool strips_are_faster(const adapm_linear8& d, int32_t which, const Strip
   if (f32) pairs = 8.0 + pair_rounds * (1.0 + 0.37 * kPlanesF32 * p.each * wide) + 0.14 * dy + 1.5 * decoded + (p.parts > 1 ? 3.5 + 1.7 * out : 0);
   else pairs = 7.0 + pair_rounds * (1.5 + 0.39 * p.each * wide) + 0.1 * dy + 0.5 * decoded + (p.parts > 1 ? 4.5 + 0.25 * out : 0);
   return strips < pairs;
+}
+
+// ---- the form of a call ------------------------------------------------------------------------------------------------
+enum : int32_t { LINES, STRIPS, PAIRS };
+struct Form {
+  int32_t form;
+  Plan plan;               // of pairs
+  StripPlan strip;
+  int64_t bytes;           // of the scratch: strips and lines touch nothing but the words at its head
+};
+
+inline Form form_within(const adapm_linear8& d, int32_t which, int64_t room) {
+  Form f = {};
+  f.form = PAIRS;
+  f.bytes = kHeadBytes;
+  if (d.tokens == 0) return f;
+  f.plan = plan_of(d, which, room);
+  if (which == FORWARD && d.tokens <= kLineTokens) {
+    f.form = LINES;
+    return f;
+  }
+  f.strip = strip_plan_of(d, which);
+  if (strips_are_faster(d, which, f.strip, f.plan) || (f.plan.bytes > room && strips_can(which, f.strip))) f.form = STRIPS;
+  else f.bytes = f.plan.bytes;
+  return f;
+}
+// What takes least, or, with `room` bytes of scratch that are too few for it, what does with them.  (What another call, with more tokens, asked for may be too few:
+// fewer tokens are fewer tiles, whose K is cut into more parts.  K is then cut into as many parts as fit, and where not even the numbers of the
+// codes do, which is where that call went by strips, this one does too.)
+inline Form form_of(const adapm_linear8& d, int32_t which, int64_t room = kAnyRoom) {
+  const Form f = form_within(d, which, kAnyRoom);
+  return f.bytes <= room ? f : form_within(d, which, room);
 }
 
 }  // namespace linear8

@@ -2,6 +2,7 @@
 pass by.  Helpers and derivations are those of that file."""
 import pytest
 
+import paper_2510_09103_b200 as A
 import test_gpu_linear8 as T
 from oracle import linear8_oracle as R
 from test_gpu_operators import BF16, F32, HALF, _close, _rows, _tensor_sum
@@ -110,3 +111,33 @@ def test_input_grad_of_scales_that_are_not_finite_or_zero(dtype, tokens, out, in
     dx = T._run_input_grad(dy, w8, bad, dtype)
     sign = dy[:, 3].double()[:, None] * T._as_numbers(w8, "int8")[3][None, :]
     assert dx[:, 0].isnan().all() and (dx[sign > 0] == float("inf")).all() and (dx[sign < 0] == float("-inf")).all()
+
+
+# ---- scratch that was asked for with another number of tokens ----------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tokens,more,out,inn", [(768, 8192, 2736, 1024), (598, 4096, 12904, 304), (2900, 3000, 2048, 1024), (1700, 2000, 4096, 200), (30, 40, 264, 136)])
+def test_gradients_in_the_scratch_of_more_tokens_and_in_the_least(dtype, tokens, more, out, inn):
+    """Parts of K that do not fit are not made, and where the numbers of the codes do not fit the call goes without: what comes out is the same
+    product."""
+    g = T._gen(13)
+    dy, _ = _rows(g, tokens, out, BF16)
+    ld = -(-inn // 16) * 16
+    w8, x8 = T._codes(g, out, inn), T._codes(g, tokens, inn)
+    ws, xs = T._scales(g, out), T._scales(g, tokens, -(-inn // 128))
+    form = dict(x_group=128, x8_ld=ld, w8_ld=ld, dx_dtype=T.TYPE[dtype], dweight_dtype=T.TYPE[dtype])
+    d, wide = A.linear8_desc(tokens, out, inn, **form), A.linear8_desc(more, out, inn, **form)
+    w, x = R.decode(T._as_numbers(w8, "int8"), ws, 0), R.decode(T._as_numbers(x8, "int8"), xs, 128)
+    dx, dw = torch.empty(tokens, inn, dtype=dtype, device="cuda"), torch.empty(out, inn, dtype=dtype, device="cuda")
+    cases = ((A.LINEAR8_INPUT_GRAD, A.adapm_linear8_input_grad, w8, ws, dx, dy.double(), w), (A.LINEAR8_WEIGHT_GRAD, A.adapm_linear8_weight_grad, x8, xs, dw, dy.double().T, x))
+    for which, call, codes, scales, result, left, right in cases:
+        want, size = left @ right, left.abs() @ right.abs()
+        for n in {A.adapm_linear8_scratch_bytes(d, which), A.adapm_linear8_scratch_bytes(wide, which), 9216}:
+            buf = torch.full((n + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+            try:
+                call(d, dy, codes, scales, result.fill_(5), buf[:n])
+            except A.AdapmError as e:
+                assert e.code == -5 and n == 9216 and out * tokens > 4e6, (which, n)      # (sums too long for a form without)
+                continue
+            assert A.adapm_linear8_status(buf) == 0 and (buf[n:] == 0xA5).all()
+            _close(result, want, T._bound(size, want, left.shape[1], dtype, True), "gradient")
