@@ -60,8 +60,9 @@ __device__ __forceinline__ void wait_for_previous_kernel() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
-// The same in two steps, for a kernel that sets up its shared and tensor memory in between: nothing in global memory, read or written, comes
-// before the second.
+// The same in two steps, for a kernel that sets up its shared memory in between: nothing in global memory, read or written, comes before the second.  Nor does
+// tensor memory: a kernel that holds some while it waits would wait for ever for one before it (not necessarily of this library) that has let it start
+// and is yet to allocate on the same SM.  (Allocated before the wait: 0.1 us faster.)
 __device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_what_is_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 #endif

@@ -213,12 +213,12 @@ __global__ void __launch_bounds__(Shape<OP, LONG, WIDE>::kThreads, 1) linear8_ke
     sh.abort = 0;
     mbar_fence_init();
   }
+  wait_for_what_is_before();
   if (warp == 1) {
     tmem_alloc<true>(&sh.tmem_base, 512);
     tmem_relinquish<true>();
   }
   tc_fence_before();
-  wait_for_what_is_before();
   if (rank == 0 && threadIdx.x == 0) *status = 0;      // (the cluster barrier orders it before what either CTA adds)
   if (blockIdx.x == 0)
     for (int i = a.pairs + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no pair
@@ -732,12 +732,12 @@ __global__ void __launch_bounds__(StripShape<OP, FOLD>::kThreads, 1) linear8_str
     sh.abort = 0;
     mbar_fence_init();
   }
+  wait_for_what_is_before();
   if (warp == 1) {
     tmem_alloc(&sh.tmem_base, tmem_cols);
     tmem_relinquish();
   }
   tc_fence_before();
-  wait_for_what_is_before();
   if (threadIdx.x == 0) *status = 0;
   if (blockIdx.x == 0)
     for (int i = (int)gridDim.x + (int)threadIdx.x; i < kMostWords; i += S::kThreads) a.status[i] = 0;      // words of no CTA
