@@ -484,7 +484,8 @@ enum { ADAPM_LINEAR8_FORWARD = 0, ADAPM_LINEAR8_INPUT_GRAD = 1, ADAPM_LINEAR8_WE
 size_t adapm_linear8_scratch_bytes(const adapm_linear8* d, int32_t which);
 
 /*
- *   forward: y[t, n] = fl(xs[t] ws[n] sum_k x8[t, k] w8[n, k]); the sum is of whole numbers, without rounding.
+ *   forward: y[t, n] = (xs[t] sum_k x8[t, k] w8[n, k]) ws[n]; the sum is of whole numbers, without rounding, and comes to fp32 (it may pass 2^24); each
+ *     product is rounded to fp32 (the first counts as infinite from 3.4e38 on), the result to y's type.
  *   input_grad: dx[t, k] = sum_n dy[t, n] ws[n] w8[n, k];  weight_grad: dweight[n, k] = sum_t dy[t, n] xs[t, group of k] x8[t, k].
  *     Sums in fp32.  Where the scales are powers of two nothing is rounded on the way into the product.  Where not, code * scale is rounded to bf16
  *     for a gradient in bf16 (off by 2^-8 of it at most, per term), but with at most 16 tokens (dx) or output features (dweight), whose
@@ -512,7 +513,7 @@ int adapm_linear8_weight_grad(const adapm_linear8* d, const void* dy, const void
 /*
  * Every wait inside the three calls above is bounded.  This call synchronises `stream` and returns ADAPM_EDEVICE and the
  * status word of the last call that used `scratch` if one of its waits ran out (the output is then not to be used);
- * 0: fine.
+ * 0: fine.  A call with tokens = 0 uses none and leaves what the one before has left; of a buffer that no call has used yet, nothing is said.
  */
 int adapm_linear8_status(const void* scratch, adapm_stream stream, int32_t* status);
 

@@ -107,7 +107,7 @@ class adapm_codes8(C.Structure):
 
 
 def quant8_desc(rows, cols, dtype=TYPE_BF16, code=CODE_INT8, group=0, pow2=False, x_ld=None, codes_ld=None) -> adapm_codes8:
-    """Pitches that are not given are `cols`."""
+    """Pitches that are not given are `cols`.  With pow2 the gradients of linear8 round nothing on their way into the product."""
     return adapm_codes8(rows, cols, cols if x_ld is None else x_ld, cols if codes_ld is None else codes_ld, dtype, code, group,
                         1 if pow2 else 0)
 
@@ -121,7 +121,8 @@ class adapm_linear8(C.Structure):
 
 def linear8_desc(tokens, out_features, in_features, x_code=CODE_INT8, x_group=0, y_dtype=TYPE_BF16, dx_dtype=TYPE_BF16,
                  dweight_dtype=TYPE_BF16, accumulate=False, x8_ld=None, w8_ld=None, y_ld=None, dx_ld=None, dweight_ld=None) -> adapm_linear8:
-    """Pitches that are not given are the matrix's own number of columns."""
+    """Pitches that are not given are the matrix's own number of columns.  Those of codes have to be multiples of 16: where in_features is none, rows of codes
+    lie further apart (adapm_quant8's codes_ld), and x8_ld and w8_ld say how far."""
     ld = lambda v, cols: cols if v is None else v  # noqa: E731
     return adapm_linear8(tokens, out_features, in_features, ld(x8_ld, in_features), ld(w8_ld, in_features), ld(y_ld, out_features),
                          ld(dx_ld, in_features), ld(dweight_ld, in_features), x_code, x_group, y_dtype, dx_dtype, dweight_dtype,

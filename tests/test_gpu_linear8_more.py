@@ -141,3 +141,18 @@ def test_gradients_in_the_scratch_of_more_tokens_and_in_the_least(dtype, tokens,
                 continue
             assert A.adapm_linear8_status(buf) == 0 and (buf[n:] == 0xA5).all()
             _close(result, want, T._bound(size, want, left.shape[1], dtype, True), "gradient")
+
+
+# ---- the forward product ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("tokens,out,inn", [(1, 264, 520), (2, 264, 520), (5, 200, 256), (300, 520, 384), (3000, 2056, 512)])
+def test_forward_of_scales_far_apart(dtype, tokens, out, inn):
+    """Large scales of tokens beside small ones of channels, and the reverse."""
+    g = T._gen(14)
+    x8, w8 = T._codes(g, tokens, inn, full=True), T._codes(g, out, inn, full=True)
+    for power in (96, -96):
+        xs, ws = T._scales(g, tokens, pow2=False) * 2.0**power, T._scales(g, out, pow2=False) * 2.0**-power
+        y = T._run_forward(x8, xs, w8, ws, dtype)
+        want = R.forward(T._as_numbers(x8, "int8"), xs, T._as_numbers(w8, "int8"), ws)
+        _close(y, want, want.abs() * (3.1 * 2.0**-24 + HALF[dtype] * 1.01) + 1e-37, "y")
