@@ -182,10 +182,11 @@ __device__ __forceinline__ void segments(int stages, int most, int& n, int& each
 
 // Pairs of CTAs (cta_group::2), tiles of 256 x 256 (192, 128 columns).  Warp 0 loads A, warp 2 B, warp 1 issues the MMAs, the others drain the
 // accumulators.
-// What bounds it: the tensor cores, and with them the power cap.  8192 x 14336 x 4096: forward 300 to 340 us = 2.8 to 3.2 P operations/s (the
-// library's 8-bit integer product alone 314 to 355), gradients with the decoding of their codes (16 to 30 us) 680 to 800 us = 1.2 to 1.4 PFLOP/s (the
-// library's bf16 products alone 620 to 940 and 670 to 760).  With short K the result's way to memory (forward 8192 x 14336 x 512 73 us; a fill of as
-// many bytes takes 63), with few tiles the rounds of them.
+// What bounds it: the tensor cores, and with them the power cap.  8192 x 14336 x 4096: forward 285 to 350 us = 2.7 to 3.4 P operations/s (the
+// library's 8-bit integer product alone 314 to 355), gradients with the decoding of their codes (16 to 30 us) 690 to 850 us = 1.1 to 1.4 PFLOP/s (the
+// library's bf16 products alone 620 to 940 and 670 to 760).  With short K a tile's way out: forward 8192 x 14336 x 512 70 to 80 us, in fp32 97 to 119, is 2.9 us for a round
+// of tiles whose products take 1.1.  That is not memory's doing, since dequant8_kernel writes the same 235 MB, and reads 117 besides, in 54 us; which part of the way is
+// to blame is open.  With few tiles the rounds of them, and a start and an end that nothing runs beside.
 // Not kept: codes made bf16 numbers by warps of this kernel on their way into shared memory, which the CTA of rank 1 has to tell the one of rank
 // 0: an arrival that releases at cluster scope takes 1000 to 1800 cycles, twice to three times what a stage does (8192 x 14336 x 4096 1230 us, by a
 // warp that does nothing else 1660, with a relaxed one, which does not order the codes, 980).
