@@ -6,7 +6,9 @@
 //
 // The scale of a gradient's codes stands beside an index of K, so it cannot wait for the end as in the forward product: code x scale is
 // made a bf16 number first (which rounds nothing where the scale is a power of two), by a launch of its own, and then multiplied
-// (kind::f16, sums in fp32).
+// (kind::f16, sums in fp32).  Where the scale is no power of two, that is a rounding per term, as large as the one of a bf16 result: the error's norm is 2.4e-3 of the
+// result's, 1.7e-3 without (input gradient 8192 x 14336 x 4096).  A second bf16 number for what it leaves would double the product (700 us and more), so that only results
+// that it would spoil have one: gradients of few columns, and in fp32.
 #include <algorithm>
 #include <cmath>
 #include <cstring>
